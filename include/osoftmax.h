@@ -1,6 +1,6 @@
 /*
- * osoftmax -- row-wise softmax with the online normalizer, and fused
- * softmax + top-k, for AMD Instinct MI355X (gfx950).
+ * osoftmax -- row-wise softmax with the online normalizer, fused softmax +
+ * top-k, sampling and expert routing, for AMD Instinct MI355X (gfx950).
  *
  * Method: M. Milakov and N. Gimelshein, "Online normalizer calculation for
  * softmax" (arXiv:1805.02867, 2018).
@@ -8,7 +8,8 @@
  * Conventions shared by every entry point:
  *  - Buffers are device pointers on the current HIP device, owned by the
  *    caller.  Batches are row-major N x V, rows contiguous (row r starts V
- *    elements after row r-1), each pointer aligned to its element size.
+ *    elements after row r-1, or ldx where an entry point has it), each pointer
+ *    aligned to its element size.
  *  - Element types (dtype): OSM_F32 = IEEE binary32, OSM_BF16 = bfloat16
  *    (16-bit patterns).  All arithmetic is binary32; bfloat16 inputs are
  *    widened exactly and bfloat16 outputs are rounded to nearest even.
@@ -268,6 +269,99 @@ OSM_API int proj_fwd(const void* h, const void* w, float* logits, int64_t N, int
  * bytes, S = vocabulary chunks) cannot be allocated. */
 OSM_API int proj_softmax_topk(const void* h, const void* w, float* vals, int32_t* idx,
                               int64_t N, int64_t H, int64_t V, int K, hipStream_t stream);
+
+/* What softmax_sample does with a batch.  Each setting is an array of N device
+ * values, one a row, or, where its pointer is NULL, one value for all rows.
+ *  temperature: logits are divided by it.  0, negative or NaN: the row's
+ *               largest element is taken (the lowest index of equal ones).
+ *  top_k      : the elements that are kept, in the order of Eq. 5.  0, negative
+ *               or at least V: all.
+ *  top_p      : of those, the shortest prefix in that order whose sum reaches
+ *               this part of their sum, at least one.  At least 1 or NaN: all.
+ *  min_p      : of those, the ones whose probability is at least this part of
+ *               the largest one.  0, negative or NaN: all; more than 1 is 1. */
+typedef struct osm_sample_params {
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    float temperature_all;
+    int32_t top_k_all;
+    float top_p_all;
+    float min_p_all;
+} osm_sample_params;
+
+/* Samples one element of each row from the softmax of its logits, with the
+ * row's random number given.  With w_j = e^{(x_j - max x) / temperature} and
+ * the filters of osm_sample_params applied in the order in which they stand
+ * there: idx[r] is the lowest kept index at which the running sum of w over the
+ * kept elements, in index order, exceeds u[r] times their sum, and vals[r] its
+ * probability among the kept elements (w / sum).  u below 0 or NaN counts as 0,
+ * above 1 as 1; elements of weight 0 are never taken.  Weights and sums are
+ * binary64, so the choice is that of the formula but for numbers u within about
+ * 1e-15 of a border; the same call gives the same result.
+ * A row holding NaN or +inf, or only -inf, gives idx -1 and a NaN value.
+ * x: row r starts at x + r * ldx elements, ldx >= V.  u: N binary32.  vals: N
+ * binary32.  idx: N int32.  params NULL: temperature 1, no filter.
+ * Errors: OSM_EINVAL for bad sizes, ldx < V, unknown dtype, null (with N > 0),
+ * misaligned or overlapping buffers (the memory between rows is part of x). */
+OSM_API int softmax_sample(const void* x, int64_t ldx, const float* u,
+                           const osm_sample_params* params, float* vals, int32_t* idx, int64_t N,
+                           int64_t V, int dtype, hipStream_t stream);
+
+/* Largest number of experts, and of groups of them, of route_fwd. */
+#define OSM_ROUTE_EMAX 1024
+#define OSM_ROUTE_GMAX 64
+
+/* Scores of a router. */
+enum osm_score { OSM_SCORE_SOFTMAX = 0, OSM_SCORE_SIGMOID = 1 };
+
+/* How route_fwd picks and weighs experts.
+ *  score     : s = softmax(x) over the row, or s = 1 / (1 + e^-x).
+ *  groups    : the E experts form this many groups of E / groups neighbours
+ *              (1: no groups).  The best top_groups of them are searched, a
+ *              group's score being the sum of its group_top (1 or 2) largest
+ *              s + bias; of equal groups the lower index is taken.
+ *  renorm    : nonzero: weights are divided by their sum.
+ *  scale     : factor of the weights. */
+typedef struct osm_route {
+    int score;
+    int groups;
+    int top_groups;
+    int group_top;
+    int renorm;
+    float scale;
+} osm_route;
+
+/* Routes each of N tokens to K of E experts.  With s the scores and c = s + bias
+ * (c = x without a bias: both scores increase with x), idx[r] are the K experts
+ * of the kept groups with the largest c, larger first, equal ones in increasing
+ * index order, and vals[r] = scale * s (divided by the K scores' sum with
+ * renorm).  The bias takes part in the choice only.  Scores and their sums with
+ * the bias are binary64.
+ * An expert whose logit or bias is -inf, or whose bias is NaN, is never chosen;
+ * where too few are left, the missing places get idx -1 and weight 0.  A row
+ * holding NaN or +inf gives idx -1 and NaN weights.
+ * x: N*E logits of dtype.  bias: E binary32 or NULL.  vals: N*K binary32.  idx:
+ * N*K int32.
+ * Errors: OSM_EINVAL for N < 0, E < 1, E > OSM_ROUTE_EMAX, K < 1, K > OSM_TOPK_KMAX,
+ * unknown dtype or score, groups < 1, above OSM_ROUTE_GMAX or not dividing E,
+ * top_groups outside [1, groups], K > top_groups * E / groups, group_top other
+ * than 1 and 2, null r or (with N > 0) buffers, misaligned or overlapping
+ * buffers. */
+OSM_API int route_fwd(const void* x, const float* bias, float* vals, int32_t* idx, int64_t N,
+                      int64_t E, int K, int dtype, const osm_route* r, hipStream_t stream);
+
+/* The gradient of route_fwd's weights with respect to the logits: dx = sum over
+ * the places i of dvals[i] * d vals[i] / dx, with the choice idx held fixed, for
+ * the same score, renorm and scale (the other members of r are not read).
+ * Places whose idx is outside [0, E) take no part; a row without any other gets
+ * zeros.  An index that occurs twice adds both.  Sums are binary64.
+ * x: N*E logits of dtype.  idx: N*K int32.  dvals: N*K binary32.  dx: N*E
+ * elements of dtype, every one written.
+ * Errors: as route_fwd, for the arguments it has. */
+OSM_API int route_bwd(const void* x, const int32_t* idx, const float* dvals, void* dx, int64_t N,
+                      int64_t E, int K, int dtype, const osm_route* r, hipStream_t stream);
 
 /* Reference streaming kernels, for measurement only (nothing of the method):
  * op 0 reads `bytes` bytes of x (y: a device buffer of at least 1 KB that

@@ -1,5 +1,5 @@
-"""Python binding of libosoftmax (online-normalizer softmax and fused softmax +
-top-k on MI355X).  Argument marshalling only: every step of the computation
+"""Python binding of libosoftmax (online-normalizer softmax, fused softmax +
+top-k, sampling and expert routing on MI355X).  Argument marshalling only: every step of the computation
 runs in the library's HIP kernels, reached through its C ABI
 (``include/osoftmax.h``).  PyTorch supplies device memory and the current
 stream.  There is no fallback: if the library is missing, every call raises.
@@ -22,6 +22,8 @@ OK, EINVAL, EUNSUPPORTED, EHIP, ENOMEM, ESCRATCH = 0, 1, 2, 3, 4, 5
 NOALLOC_SCRATCH_BYTES = 1 << 20
 TOPK_KMAX = 64
 PROJ_KMAX = 16
+ROUTE_EMAX, ROUTE_GMAX = 1024, 64
+SCORES = {"softmax": 0, "sigmoid": 1}
 TOPK_ONLINE_FUSED, TOPK_SAFE_FUSED, TOPK_SAFE_UNFUSED, TOPK_ONLINE_UNFUSED, TOPK_VALUES = range(5)
 TOPK_ALGOS = {"online_fused": TOPK_ONLINE_FUSED, "safe_fused": TOPK_SAFE_FUSED,
               "safe_unfused": TOPK_SAFE_UNFUSED, "online_unfused": TOPK_ONLINE_UNFUSED,
@@ -32,6 +34,20 @@ MODES = {"naive": NAIVE, "safe": SAFE, "online": ONLINE, "resident": RESIDENT}
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 _lib = None
+
+
+class SampleParams(ctypes.Structure):
+    """``osm_sample_params``."""
+    _fields_ = [("temperature", ctypes.c_void_p), ("top_k", ctypes.c_void_p),
+                ("top_p", ctypes.c_void_p), ("min_p", ctypes.c_void_p),
+                ("temperature_all", ctypes.c_float), ("top_k_all", ctypes.c_int32),
+                ("top_p_all", ctypes.c_float), ("min_p_all", ctypes.c_float)]
+
+
+class Route(ctypes.Structure):
+    """``osm_route``."""
+    _fields_ = [("score", ctypes.c_int), ("groups", ctypes.c_int), ("top_groups", ctypes.c_int),
+                ("group_top", ctypes.c_int), ("renorm", ctypes.c_int), ("scale", ctypes.c_float)]
 
 
 class OsmError(RuntimeError):
@@ -72,6 +88,12 @@ def lib() -> ctypes.CDLL:
     L.proj_fwd.restype = i32
     L.proj_softmax_topk.argtypes = [vp, vp, vp, vp, i64, i64, i64, i32, vp]
     L.proj_softmax_topk.restype = i32
+    L.softmax_sample.argtypes = [vp, i64, vp, vp, vp, vp, i64, i64, i32, vp]
+    L.softmax_sample.restype = i32
+    L.route_fwd.argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, vp, vp]
+    L.route_fwd.restype = i32
+    L.route_bwd.argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, vp, vp]
+    L.route_bwd.restype = i32
     L.osm_plan.argtypes = [i64, i64, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i64)]
     L.osm_plan.restype = i32
     L.osm_stream_release.argtypes = [vp]
@@ -337,3 +359,123 @@ def proj_softmax_topk(h: torch.Tensor, w: torch.Tensor, K: int, vals: torch.Tens
     if rc != OK:
         raise OsmError(rc, "proj_softmax_topk")
     return vals, idx
+
+
+def _on_current_device(x: torch.Tensor, name: str) -> None:
+    """The library launches on the current device and its stream."""
+    current = torch.cuda.current_device() if _device is None else _device()
+    if x.get_device() != current:
+        raise ValueError(f"{name} must be on the current device")
+
+
+def _rows(x: torch.Tensor):
+    """(N, V, elements from row to row) of a batch whose rows are contiguous."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError("x must be a CUDA (HIP) tensor")
+    if x.dtype not in _DTYPES:
+        raise ValueError(f"x must be float32 or bfloat16, got {x.dtype}")
+    if x.dim() == 1:
+        x = x.unsqueeze(0)
+    if x.dim() != 2:
+        raise ValueError("x must be 1-D or 2-D (N x V)")
+    N, V = x.shape
+    ld = x.stride(0) if N > 1 else V
+    if V > 1 and x.stride(1) != 1 or ld < V:
+        raise ValueError("the rows of x must be contiguous and must not overlap")
+    return N, V, ld
+
+
+def _vector(t, dtype, x: torch.Tensor, n: int, name: str) -> torch.Tensor:
+    if not isinstance(t, torch.Tensor) or not _holds(t, dtype, x, n):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {n} elements on x's "
+                         "device")
+    return t
+
+
+def _setting(v, dtype, x: torch.Tensor, N: int, name: str):
+    """(pointer, value for all rows) of a setting given as a tensor or a number."""
+    if isinstance(v, torch.Tensor):
+        return _vector(v, dtype, x, N, name).data_ptr(), 0
+    return None, int(v) if dtype is torch.int32 else float(v)
+
+
+def softmax_sample(x: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0,
+                   min_p=0.0, vals: torch.Tensor | None = None, idx: torch.Tensor | None = None,
+                   stream=None):
+    """(vals, idx) = one element sampled from each row's softmax, with its probability
+    among the elements that the filters keep (``softmax_sample``).
+
+    ``u``: N random numbers in [0, 1), float32.  ``temperature``, ``top_p`` and
+    ``min_p`` (float32) and ``top_k`` (int32) are numbers or tensors of N.  Rows may
+    be apart (``x[:, :V]`` of a padded batch)."""
+    N, V, ld = _rows(x)
+    _on_current_device(x, "x")
+    _vector(u, torch.float32, x, N, "u")
+    t, t_all = _setting(temperature, torch.float32, x, N, "temperature")
+    k, k_all = _setting(top_k, torch.int32, x, N, "top_k")
+    p, p_all = _setting(top_p, torch.float32, x, N, "top_p")
+    q, q_all = _setting(min_p, torch.float32, x, N, "min_p")
+    if vals is None:
+        vals = torch.empty(N, dtype=torch.float32, device=x.device)
+    if idx is None:
+        idx = torch.empty(N, dtype=torch.int32, device=x.device)
+    _vector(vals, torch.float32, x, N, "vals")
+    _vector(idx, torch.int32, x, N, "idx")
+    params = SampleParams(t, k, p, q, t_all, k_all, p_all, q_all)
+    rc = lib().softmax_sample(x.data_ptr(), ld, u.data_ptr(), ctypes.byref(params),
+                              vals.data_ptr(), idx.data_ptr(), N, V, _DTYPES[x.dtype],
+                              _stream(stream))
+    if rc != OK:
+        raise OsmError(rc, "softmax_sample")
+    return vals, idx
+
+
+def _score(score) -> int:
+    if isinstance(score, str):
+        if score not in SCORES:
+            raise ValueError(f"score must be one of {sorted(SCORES)}")
+        return SCORES[score]
+    return int(score)
+
+
+def route_fwd(x: torch.Tensor, K: int, bias: torch.Tensor | None = None, score="softmax",
+              groups: int = 1, top_groups: int = 1, group_top: int = 1, renorm: bool = True,
+              scale: float = 1.0, vals: torch.Tensor | None = None,
+              idx: torch.Tensor | None = None, stream=None):
+    """(vals, idx) = weights and indices of each row's K experts (``route_fwd``): N x K
+    float32 and int32, best first."""
+    N, E = _batch(x)
+    _on_current_device(x, "x")
+    if bias is not None:
+        _vector(bias, torch.float32, x, E, "bias")
+    vals, idx = _topk_outputs(x, N, K, vals, idx)
+    r = Route(_score(score), int(groups), int(top_groups), int(group_top), bool(renorm),
+              float(scale))
+    rc = lib().route_fwd(x.data_ptr(), None if bias is None else bias.data_ptr(),
+                         vals.data_ptr(), idx.data_ptr(), N, E, int(K), _DTYPES[x.dtype],
+                         ctypes.byref(r), _stream(stream))
+    if rc != OK:
+        raise OsmError(rc, "route_fwd")
+    return vals, idx
+
+
+def route_bwd(x: torch.Tensor, idx: torch.Tensor, dvals: torch.Tensor, score="softmax",
+              renorm: bool = True, scale: float = 1.0, dx: torch.Tensor | None = None,
+              stream=None) -> torch.Tensor:
+    """dx = gradient with respect to x of route_fwd's weights, whose own gradient is
+    ``dvals`` (N x K) at the experts ``idx`` (``route_bwd``)."""
+    N, E = _batch(x)
+    _on_current_device(x, "x")
+    K = idx.shape[-1]
+    _vector(idx, torch.int32, x, N * K, "idx")
+    _vector(dvals, torch.float32, x, N * K, "dvals")
+    if dx is None:
+        dx = torch.empty_like(x)
+    elif not _like(dx, x):
+        raise ValueError("dx must be a contiguous tensor like x")
+    r = Route(_score(score), 1, 1, 1, bool(renorm), float(scale))
+    rc = lib().route_bwd(x.data_ptr(), idx.data_ptr(), dvals.data_ptr(), dx.data_ptr(), N, E, K,
+                         _DTYPES[x.dtype], ctypes.byref(r), _stream(stream))
+    if rc != OK:
+        raise OsmError(rc, "route_bwd")
+    return dx

@@ -633,6 +633,103 @@ int run_proj_topk(const void* h, const void* w, float* vals, int32_t* idx, int64
     return hip_status(f);
 }
 
+// ------------------------------------------------------ sampling and routing
+struct Span {
+    const void* p;
+    size_t bytes;
+};
+
+// Whether any of the outputs overlaps an input or another output.
+template <size_t O, size_t I>
+bool any_overlap(const Span (&out)[O], const Span (&in)[I]) {
+    for (size_t i = 0; i < O; ++i) {
+        for (size_t j = 0; j < I; ++j)
+            if (in[j].p && overlaps(out[i].p, out[i].bytes, in[j].p, in[j].bytes)) return true;
+        for (size_t j = 0; j < i; ++j)
+            if (overlaps(out[i].p, out[i].bytes, out[j].p, out[j].bytes)) return true;
+    }
+    return false;
+}
+
+int run_sample(const void* x, int64_t ldx, const float* u, const osm_sample_params* params,
+               float* vals, int32_t* idx, int64_t N, int64_t V, int dtype, hipStream_t stream) {
+    size_t bytes = 0;
+    if (!check_shape(N, V, dtype, &bytes) || ldx < V || ldx > kMaxDim) return OSM_EINVAL;
+    if (N == 0) return OSM_OK;
+    const osm_sample_params plain = {nullptr, nullptr, nullptr, nullptr, 1.0f, 0, 1.0f, 0.0f};
+    const osm_sample_params& s = params ? *params : plain;
+    const size_t es = elem_size(dtype), nb = (size_t)N * 4;
+    if (!x || !u || !vals || !idx) return OSM_EINVAL;
+    if (!aligned(x, es) || !aligned(u, 4) || !aligned(vals, 4) || !aligned(idx, 4) ||
+        !aligned(s.temperature, 4) || !aligned(s.top_k, 4) || !aligned(s.top_p, 4) ||
+        !aligned(s.min_p, 4))
+        return OSM_EINVAL;
+    const Span out[] = {{vals, nb}, {idx, nb}};
+    const Span in[] = {{x, ((size_t)(N - 1) * (size_t)ldx + (size_t)V) * es},
+                       {u, nb},
+                       {s.temperature, nb},
+                       {s.top_k, nb},
+                       {s.top_p, nb},
+                       {s.min_p, nb}};
+    if (any_overlap(out, in)) return OSM_EINVAL;
+    if (!device_state(nullptr)) return OSM_EHIP;
+    const osm::SampleRows a{x,          u,          s.temperature,     s.top_k,     s.top_p,
+                            s.min_p,    s.temperature_all, s.top_k_all, s.top_p_all,
+                            s.min_p_all, vals,      idx,               N,           V,
+                            ldx};
+    return hip_status(osm::launch_sample(a, dtype, stream));
+}
+
+// Sizes and options of a router; the groups only where `choose`.
+bool check_route(int64_t N, int64_t E, int K, int dtype, const osm_route* r, bool choose) {
+    if (N < 0 || N > kMaxDim || E < 1 || E > OSM_ROUTE_EMAX || K < 1 || K > OSM_TOPK_KMAX || !r)
+        return false;
+    if (dtype != OSM_F32 && dtype != OSM_BF16) return false;
+    if (r->score != OSM_SCORE_SOFTMAX && r->score != OSM_SCORE_SIGMOID) return false;
+    if (!choose) return true;
+    if (r->groups < 1 || r->groups > OSM_ROUTE_GMAX || E % r->groups != 0) return false;
+    if (r->top_groups < 1 || r->top_groups > r->groups) return false;
+    return (r->group_top == 1 || r->group_top == 2) && K <= r->top_groups * (E / r->groups);
+}
+
+int run_route_fwd(const void* x, const float* bias, float* vals, int32_t* idx, int64_t N,
+                  int64_t E, int K, int dtype, const osm_route* r, hipStream_t stream) {
+    if (!check_route(N, E, K, dtype, r, true)) return OSM_EINVAL;
+    if (N == 0) return OSM_OK;
+    const size_t es = elem_size(dtype), kb = (size_t)N * K * 4;
+    if (!x || !vals || !idx) return OSM_EINVAL;
+    if (!aligned(x, es) || !aligned(bias, 4) || !aligned(vals, 4) || !aligned(idx, 4))
+        return OSM_EINVAL;
+    const Span out[] = {{vals, kb}, {idx, kb}};
+    const Span in[] = {{x, (size_t)N * (size_t)E * es}, {bias, (size_t)E * 4}};
+    if (any_overlap(out, in)) return OSM_EINVAL;
+    if (!device_state(nullptr)) return OSM_EHIP;
+    osm::RouteRows a{};
+    a.x = x, a.bias = bias, a.vals = vals, a.idx = idx, a.N = N, a.E = (int)E, a.K = K;
+    a.groups = r->groups, a.top_groups = r->top_groups, a.group_top = r->group_top;
+    a.sigmoid = r->score == OSM_SCORE_SIGMOID, a.renorm = r->renorm != 0, a.scale = r->scale;
+    return hip_status(osm::launch_route_fwd(a, dtype, stream));
+}
+
+int run_route_bwd(const void* x, const int32_t* idx, const float* dvals, void* dx, int64_t N,
+                  int64_t E, int K, int dtype, const osm_route* r, hipStream_t stream) {
+    if (!check_route(N, E, K, dtype, r, false)) return OSM_EINVAL;
+    if (N == 0) return OSM_OK;
+    const size_t es = elem_size(dtype), kb = (size_t)N * K * 4, eb = (size_t)N * (size_t)E * es;
+    if (!x || !idx || !dvals || !dx) return OSM_EINVAL;
+    if (!aligned(x, es) || !aligned(idx, 4) || !aligned(dvals, 4) || !aligned(dx, es))
+        return OSM_EINVAL;
+    const Span out[] = {{dx, eb}};
+    const Span in[] = {{x, eb}, {idx, kb}, {dvals, kb}};
+    if (any_overlap(out, in)) return OSM_EINVAL;
+    if (!device_state(nullptr)) return OSM_EHIP;
+    osm::RouteRows a{};
+    a.x = x, a.idx = const_cast<int32_t*>(idx), a.dvals = dvals, a.dx = dx;
+    a.N = N, a.E = (int)E, a.K = K;
+    a.sigmoid = r->score == OSM_SCORE_SIGMOID, a.renorm = r->renorm != 0, a.scale = r->scale;
+    return hip_status(osm::launch_route_bwd(a, dtype, stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -712,6 +809,22 @@ int proj_fwd(const void* h, const void* w, float* logits, int64_t N, int64_t H, 
 int proj_softmax_topk(const void* h, const void* w, float* vals, int32_t* idx, int64_t N,
                       int64_t H, int64_t V, int K, hipStream_t stream) {
     return run_proj_topk(h, w, vals, idx, N, H, V, K, stream);
+}
+
+int softmax_sample(const void* x, int64_t ldx, const float* u, const osm_sample_params* params,
+                   float* vals, int32_t* idx, int64_t N, int64_t V, int dtype,
+                   hipStream_t stream) {
+    return run_sample(x, ldx, u, params, vals, idx, N, V, dtype, stream);
+}
+
+int route_fwd(const void* x, const float* bias, float* vals, int32_t* idx, int64_t N, int64_t E,
+              int K, int dtype, const osm_route* r, hipStream_t stream) {
+    return run_route_fwd(x, bias, vals, idx, N, E, K, dtype, r, stream);
+}
+
+int route_bwd(const void* x, const int32_t* idx, const float* dvals, void* dx, int64_t N,
+              int64_t E, int K, int dtype, const osm_route* r, hipStream_t stream) {
+    return run_route_bwd(x, idx, dvals, dx, N, E, K, dtype, r, stream);
 }
 
 int osm_stream_release(hipStream_t stream) {

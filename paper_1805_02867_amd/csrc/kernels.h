@@ -98,4 +98,38 @@ inline hipError_t launch_topk(const TopkLaunch& a, int dtype, int var) {
     }
 }
 
+// Sampling: rows of V elements, row r at x + r * ld; a setting is an array of N
+// or, where that is null, one value for all rows.
+struct SampleRows {
+    const void* x;
+    const float* u;
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    float temperature_all;
+    int32_t top_k_all;
+    float top_p_all, min_p_all;
+    float* vals;
+    int32_t* idx;
+    int64_t N, V, ld;
+};
+hipError_t launch_sample(const SampleRows& a, int dtype, hipStream_t st);
+
+// Routing: rows of E scores, K experts of each (see osm_route).
+struct RouteRows {
+    const void* x;
+    const float* bias;    // E, or null
+    float* vals;          // forward: written
+    int32_t* idx;         // forward: written; backward: read
+    const float* dvals;   // backward
+    void* dx;             // backward: written
+    int64_t N;
+    int E, K, groups, top_groups, group_top;
+    bool sigmoid, renorm;
+    float scale;
+};
+hipError_t launch_route_fwd(const RouteRows& a, int dtype, hipStream_t st);
+hipError_t launch_route_bwd(const RouteRows& a, int dtype, hipStream_t st);
+
 }  // namespace osm

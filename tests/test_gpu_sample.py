@@ -1,0 +1,264 @@
+"""softmax_sample against a plain binary64 implementation: tokens equal, their
+probabilities within the rounding of binary32."""
+import numpy as np
+import pytest
+import torch
+
+import paper_1805_02867_amd as osm
+import pick_ref
+
+pytestmark = pytest.mark.gpu
+INF, NAN = float("inf"), float("nan")
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+LOWEST = {t: float(torch.finfo(d).min) for t, d in TYPES.items()}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need an MI355X; none is visible")
+    return torch.device("cuda:0")
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def logits(N, V, dtype, seed, dev, sigma=2.0):
+    g = torch.Generator().manual_seed(seed)
+    r = torch.randn(N, V, generator=g)
+    up = (r - 2.0).clamp(min=0.0)
+    return ((r + 0.5 * up * up) * sigma).to(TYPES[dtype]).to(dev)
+
+
+def uniform(N, seed, dev):
+    return torch.rand(N, generator=torch.Generator().manual_seed(seed)).to(dev)
+
+
+def on_device(kw, dev):
+    out = {}
+    for n, v in kw.items():
+        if np.ndim(v):
+            v = torch.tensor(v, dtype=torch.int32 if n == "top_k" else torch.float32).to(dev)
+        out[n] = v
+    return out
+
+
+def check(x, u, dev, **kw):
+    """One call against the reference; the settings are numbers or lists of N."""
+    vals, idx = osm.softmax_sample(x, u, **on_device(kw, dev))
+    torch.cuda.synchronize()
+    rv, ri = pick_ref.sample(host(x if x.dim() == 2 else x.unsqueeze(0)), host(u), **kw)
+    got = idx.cpu().numpy()
+    assert np.array_equal(got, ri), [(r, got[r], ri[r]) for r in np.flatnonzero(got != ri)[:5]]
+    pick_ref.close(host(vals), rv)
+    return vals, idx
+
+
+SETTINGS = {
+    "plain": {}, "hot": dict(temperature=1.7), "cold": dict(temperature=0.05),
+    "greedy": dict(temperature=0.0), "k1": dict(top_k=1), "k7": dict(top_k=7),
+    "k300": dict(top_k=300), "p": dict(top_p=0.9), "small_p": dict(top_p=0.01),
+    "large_p": dict(top_p=0.9999), "q": dict(min_p=0.05), "q1": dict(min_p=1.0),
+    "kp": dict(temperature=0.8, top_k=50, top_p=0.9),
+    "pq": dict(temperature=1.3, top_p=0.95, min_p=0.03),
+    "kpq": dict(top_k=900, top_p=0.7, min_p=0.001),
+}
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [1, 2, 3, 63, 64, 65, 257, 1000, 2049, 4099, 8193, 16411, 50257])
+def test_settings(V, dtype, dev):
+    N = 7
+    x = logits(N, V, dtype, V, dev)
+    for i, kw in enumerate(SETTINGS.values()):
+        check(x, uniform(N, 31 * V + i, dev), dev, **kw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("N,V", [(1, 128256), (3, 131073), (70, 32000), (600, 1000), (2, 1000003)])
+def test_a_setting_a_row(N, V, dtype, dev):
+    rng = np.random.default_rng(V + N)
+    x = logits(N, V, dtype, N, dev)
+    kind = rng.integers(0, 6, N)
+    kw = dict(temperature=np.where(kind == 0, 0.0, rng.uniform(0.5, 1.5, N)).tolist(),
+              top_k=np.where(kind % 3 == 2, rng.integers(1, 2000, N), 0).tolist(),
+              top_p=np.where(kind >= 3, rng.uniform(0.3, 0.999, N), 1.0).tolist(),
+              min_p=np.where(kind >= 4, rng.uniform(0.0, 0.1, N), 0.0).tolist())
+    check(x, uniform(N, 5, dev), dev, **kw)
+    check(x, uniform(N, 6, dev), dev, top_p=0.95)
+    check(x, uniform(N, 7, dev), dev)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [8, 1000, 20000])
+def test_ties(V, dtype, dev):
+    """Cuts inside runs of equal logits: the lower indices stay.  Equal weights make the
+    part of a top-p fall exactly on an element."""
+    n = 64
+    u = torch.linspace(0, 1 - 2.0 ** -24, n).to(dev)
+    same = torch.full((n, V), 1.25, dtype=TYPES[dtype], device=dev)
+    g = torch.Generator().manual_seed(V)
+    few = torch.randint(0, 4, (n, V), generator=g).to(TYPES[dtype]).to(dev)
+    zeros = torch.where(torch.rand(n, V, generator=g) < 0.5, 0.0, -0.0).to(TYPES[dtype]).to(dev)
+    for x in (same, few, zeros):
+        check(x, u, dev)
+        check(x, u, dev, top_k=V // 2 + 1)
+        check(x, u, dev, top_k=3, top_p=0.5)
+        check(x, u, dev, top_p=0.5)
+        check(x, u, dev, top_p=0.3, top_k=V - 1)
+        check(x, u, dev, min_p=1.0)
+        check(x, u, dev, temperature=0.0)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [5, 300, 9000, 40000])
+def test_masks(V, dtype, dev):
+    """Masks of -inf and of the type's lowest value; rows with one element left, with
+    none, and with what a row must not hold."""
+    x = logits(12, V, dtype, V, dev)
+    g = torch.Generator().manual_seed(V)
+    masked = (torch.rand(12, V, generator=g) < 0.9).to(dev)
+    masked[:, V // 2] = False
+    x[:4] = x[:4].masked_fill(masked[:4], -INF)
+    x[4:6] = x[4:6].masked_fill(masked[4:6], LOWEST[dtype])
+    x[6] = -INF
+    x[7] = -INF
+    x[7, V - 1] = -3.0
+    x[8] = LOWEST[dtype]
+    x[9, V // 3] = NAN
+    x[10, V - 1] = INF
+    x[11] = LOWEST[dtype]
+    x[11, 0] = -INF
+    u = uniform(12, 9, dev)
+    for kw in SETTINGS.values():
+        vals, idx = check(x, u, dev, **kw)
+        assert idx[[6, 9, 10]].tolist() == [-1, -1, -1] and vals[[6, 9, 10]].isnan().all()
+        assert idx[7].item() == V - 1 and vals[7].item() == 1.0
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_ends_of_the_settings(dtype, dev):
+    N, V = 9, 700
+    x = logits(N, V, dtype, 1, dev)
+    x[0, :300] = -INF
+    u = [0.0, 2.0 ** -24, 0.5, 1 - 2.0 ** -24, 1.0, 7.0, -3.0, NAN, 0.25]
+    ut = torch.tensor(u, device=dev)
+    for kw in (dict(temperature=-1.0), dict(temperature=NAN), dict(temperature=INF),
+               dict(temperature=1e-30), dict(temperature=1e-42), dict(temperature=1e30),
+               dict(top_k=-5), dict(top_k=V), dict(top_k=V + 9), dict(top_k=V - 1),
+               dict(top_k=2 ** 31 - 1), dict(top_p=0.0), dict(top_p=-1.0), dict(top_p=2.0),
+               dict(top_p=NAN), dict(top_p=1e-30), dict(top_p=1 - 2.0 ** -24),
+               dict(min_p=-1.0), dict(min_p=NAN), dict(min_p=2.0), dict(min_p=1e-30),
+               dict(top_k=5, top_p=1e-9, min_p=1.0)):
+        check(x, ut, dev, **kw)
+        check(x[1:2], ut[4:5], dev, **{n: [v] for n, v in kw.items()})
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_far_values(dtype, dev):
+    """Magnitudes from the smallest to the largest of the type, and rows shifted far."""
+    g = torch.Generator().manual_seed(2)
+    e = torch.rand(6, 5000, generator=g) * 76 - 38
+    x = (torch.sign(torch.randn(6, 5000, generator=g)) * 10.0 ** e).to(TYPES[dtype])
+    x[4:] = x[4:] * 1e-38
+    x = x.to(dev)
+    shifted = logits(6, 5000, dtype, 3, dev) + torch.tensor([1e3, -1e3, 1e4, -1e4, 88.0, -88.0],
+                                                            device=dev).unsqueeze(1)
+    for t in (x, shifted.to(TYPES[dtype])):
+        for kw in (dict(), dict(top_k=1700), dict(top_p=0.8), dict(temperature=1e30, top_p=0.8),
+                   dict(temperature=1e38, top_k=2500, top_p=0.5)):
+            check(t, uniform(6, 4, dev), dev, **kw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V,ld,first", [(1000, 1003, 1), (50257, 50304, 0), (4097, 5000, 3),
+                                        (1, 64, 5), (33, 33, 1)])
+def test_rows_apart_and_unaligned(V, ld, first, dtype, dev):
+    N = 11
+    buf = torch.full((N * ld + first,), NAN, dtype=TYPES[dtype], device=dev)
+    x = buf[first:].view(N, ld)[:, :V]
+    x.copy_(logits(N, V, dtype, V, dev))
+    for kw in (dict(), dict(top_k=40, top_p=0.9), dict(top_p=0.97, temperature=1.5)):
+        check(x, uniform(N, V, dev), dev, **kw)
+    check(x[::2], uniform(6, V, dev), dev, top_p=0.9)     # every other row
+    check(x[3], uniform(1, V, dev), dev, top_k=9)         # one row, 1-D
+    assert buf.view(-1)[:first].isnan().all()
+
+
+def test_outputs_are_written_in_place_and_nothing_else(dev):
+    x, u = logits(5, 300, "f32", 1, dev), uniform(5, 1, dev)
+    vals = torch.full((9,), -7.0, device=dev)
+    idx = torch.full((9,), -7, dtype=torch.int32, device=dev)
+    v, i = osm.softmax_sample(x, u, vals=vals[2:7], idx=idx[2:7])
+    assert v.data_ptr() == vals[2:7].data_ptr() and i.data_ptr() == idx[2:7].data_ptr()
+    rv, ri = pick_ref.sample(host(x), host(u))
+    assert np.array_equal(idx[2:7].cpu().numpy(), ri)
+    assert (vals[[0, 1, 7, 8]] == -7).all() and (idx[[0, 1, 7, 8]] == -7).all()
+    v, i = osm.softmax_sample(x[:0], u[:0])
+    assert v.shape == (0,) and i.shape == (0,)
+
+
+def test_refusals(dev):
+    x, u = logits(4, 64, "f32", 1, dev), uniform(4, 1, dev)
+    bad = [dict(u=u[:3]), dict(u=u.double()), dict(u=u.cpu()), dict(x=x.half()),
+           dict(x=x.t()), dict(x=x[:, ::2]), dict(x=x[0].expand(4, 64)), dict(x=x.view(2, 2, 64)),
+           dict(temperature=u[:2]), dict(temperature=u.double()),
+           dict(top_k=torch.ones(4, device=dev)), dict(top_p=u.cpu()),
+           dict(min_p=u.new_zeros(8)[::2]), dict(vals=u.double()), dict(idx=u)]
+    for b in bad:
+        kw = dict(x=x, u=u) | b
+        with pytest.raises(ValueError):
+            osm.softmax_sample(kw.pop("x"), kw.pop("u"), **kw)
+    with pytest.raises(osm.OsmError):
+        osm.softmax_sample(x, u, vals=u)                  # overlaps an input
+
+
+@pytest.mark.parametrize("N,V", [(3, 128256), (40, 5000)])
+def test_streams_and_captured_replays(N, V, dev):
+    """Two streams at once, and captured calls replayed with eager calls between."""
+    kw = dict(temperature=0.9, top_k=400, top_p=0.9)
+    xs = [logits(N, V, "bf16", s, dev) for s in range(2)]
+    us = [uniform(N, s, dev) for s in range(2)]
+    want = [pick_ref.sample(host(x), host(u), **kw) for x, u in zip(xs, us)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for s, x, u in zip(streams, xs, us):                  # warm
+        with torch.cuda.stream(s):
+            osm.softmax_sample(x, u, **kw)
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for s, x, u in zip(streams, xs, us):
+            with torch.cuda.stream(s):
+                got.append(osm.softmax_sample(x, u, **kw))
+    torch.cuda.synchronize()
+    for n, (v, i) in enumerate(got):
+        assert np.array_equal(i.cpu().numpy(), want[n % 2][1])
+    graphs, outs = [], []
+    for s, x, u in zip(streams, xs, us):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append(osm.softmax_sample(x, u, **kw))
+        graphs.append(g)
+    for rep in range(4):
+        for v, i in outs:
+            i.fill_(-5)
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):                 # both graphs at once
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for (v, i), (rv, ri) in zip(outs, want):
+            assert np.array_equal(i.cpu().numpy(), ri), f"replay {rep}"
+            pick_ref.close(host(v), rv)
+        check(xs[0], us[0], dev, **kw)                    # eager between replays
+
+
+def test_same_bits_every_time(dev):
+    x, u = logits(20, 60000, "f32", 8, dev), uniform(20, 8, dev)
+    for kw in (dict(), dict(top_p=0.9), dict(top_k=3000, top_p=0.9, min_p=1e-4)):
+        first = osm.softmax_sample(x, u, **kw)
+        for _ in range(5):
+            again = osm.softmax_sample(x, u, **kw)
+            assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
