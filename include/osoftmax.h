@@ -299,7 +299,7 @@ typedef struct osm_sample_params {
  * probability among the kept elements (w / sum).  u below 0 or NaN counts as 0,
  * above 1 as 1; elements of weight 0 are never taken.  Weights and sums are
  * binary64, so the choice is that of the formula but for numbers u within about
- * 1e-15 of a border; the same call gives the same result.
+ * 1e-13 of a border; the same call gives the same result.
  * A row holding NaN or +inf, or only -inf, gives idx -1 and a NaN value.
  * x: row r starts at x + r * ldx elements, ldx >= V.  u: N binary32.  vals: N
  * binary32.  idx: N int32.  params NULL: temperature 1, no filter.
@@ -308,6 +308,23 @@ typedef struct osm_sample_params {
 OSM_API int softmax_sample(const void* x, int64_t ldx, const float* u,
                            const osm_sample_params* params, float* vals, int32_t* idx, int64_t N,
                            int64_t V, int dtype, hipStream_t stream);
+
+/* softmax_sample with the caller's workspace instead of the library's scratch: nothing
+ * is allocated, and calls share nothing but what the caller lets them share.  For
+ * HIP graph capture: graphs captured with workspaces of their own may be replayed
+ * at the same time.  workspace: osm_sample_workspace(N, V, dtype) bytes, aligned
+ * to 256, of any contents; NULL where that is 0.
+ * Errors: as softmax_sample, OSM_EINVAL for a misaligned or overlapping workspace,
+ * OSM_ESCRATCH for one that is too small. */
+OSM_API int softmax_sample_ws(const void* x, int64_t ldx, const float* u,
+                              const osm_sample_params* params, float* vals, int32_t* idx,
+                              int64_t N, int64_t V, int dtype, void* workspace,
+                              size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of workspace that softmax_sample_ws needs for this shape on the current device
+ * (0 for rows that one workgroup takes), for any ldx and alignment.
+ * Errors: OSM_EINVAL for bad sizes or dtype or NULL bytes. */
+OSM_API int osm_sample_workspace(int64_t N, int64_t V, int dtype, size_t* bytes);
 
 /* Largest number of experts, and of groups of them, of route_fwd. */
 #define OSM_ROUTE_EMAX 1024

@@ -90,6 +90,11 @@ def lib() -> ctypes.CDLL:
     L.proj_softmax_topk.restype = i32
     L.softmax_sample.argtypes = [vp, i64, vp, vp, vp, vp, i64, i64, i32, vp]
     L.softmax_sample.restype = i32
+    L.softmax_sample_ws.argtypes = [vp, i64, vp, vp, vp, vp, i64, i64, i32, vp, ctypes.c_size_t,
+                                    vp]
+    L.softmax_sample_ws.restype = i32
+    L.osm_sample_workspace.argtypes = [i64, i64, i32, ctypes.POINTER(ctypes.c_size_t)]
+    L.osm_sample_workspace.restype = i32
     L.route_fwd.argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, vp, vp]
     L.route_fwd.restype = i32
     L.route_bwd.argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, vp, vp]
@@ -401,13 +406,16 @@ def _setting(v, dtype, x: torch.Tensor, N: int, name: str):
 
 def softmax_sample(x: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0,
                    min_p=0.0, vals: torch.Tensor | None = None, idx: torch.Tensor | None = None,
-                   stream=None):
+                   workspace: torch.Tensor | None = None, stream=None):
     """(vals, idx) = one element sampled from each row's softmax, with its probability
     among the elements that the filters keep (``softmax_sample``).
 
     ``u``: N random numbers in [0, 1), float32.  ``temperature``, ``top_p`` and
     ``min_p`` (float32) and ``top_k`` (int32) are numbers or tensors of N.  Rows may
-    be apart (``x[:, :V]`` of a padded batch)."""
+    be apart (``x[:, :V]`` of a padded batch).  ``workspace``: uint8, at least
+    ``sample_workspace(N, V, dtype)`` bytes, used instead of the library's scratch
+    (``softmax_sample_ws``); while the current stream is being captured into a graph,
+    one is taken from the graph's own memory."""
     N, V, ld = _rows(x)
     _on_current_device(x, "x")
     _vector(u, torch.float32, x, N, "u")
@@ -422,12 +430,31 @@ def softmax_sample(x: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, t
     _vector(vals, torch.float32, x, N, "vals")
     _vector(idx, torch.int32, x, N, "idx")
     params = SampleParams(t, k, p, q, t_all, k_all, p_all, q_all)
-    rc = lib().softmax_sample(x.data_ptr(), ld, u.data_ptr(), ctypes.byref(params),
-                              vals.data_ptr(), idx.data_ptr(), N, V, _DTYPES[x.dtype],
-                              _stream(stream))
+    if workspace is None and torch.cuda.is_current_stream_capturing():
+        workspace = torch.empty(sample_workspace(N, V, x.dtype), dtype=torch.uint8,
+                                device=x.device)
+    if workspace is None:
+        rc = lib().softmax_sample(x.data_ptr(), ld, u.data_ptr(), ctypes.byref(params),
+                                  vals.data_ptr(), idx.data_ptr(), N, V, _DTYPES[x.dtype],
+                                  _stream(stream))
+    else:
+        _vector(workspace, torch.uint8, x, workspace.numel(), "workspace")
+        rc = lib().softmax_sample_ws(x.data_ptr(), ld, u.data_ptr(), ctypes.byref(params),
+                                     vals.data_ptr(), idx.data_ptr(), N, V, _DTYPES[x.dtype],
+                                     workspace.data_ptr(), workspace.numel(), _stream(stream))
     if rc != OK:
         raise OsmError(rc, "softmax_sample")
     return vals, idx
+
+
+def sample_workspace(N: int, V: int, dtype=torch.float32) -> int:
+    """Bytes of workspace of softmax_sample for this shape (``osm_sample_workspace``)."""
+    n = ctypes.c_size_t()
+    dt = _DTYPES[dtype] if isinstance(dtype, torch.dtype) else int(dtype)
+    rc = lib().osm_sample_workspace(int(N), int(V), dt, ctypes.byref(n))
+    if rc != OK:
+        raise OsmError(rc, "osm_sample_workspace")
+    return n.value
 
 
 def _score(score) -> int:

@@ -651,8 +651,16 @@ bool any_overlap(const Span (&out)[O], const Span (&in)[I]) {
     return false;
 }
 
+// Scratch of a split plan: the chunks' sums, then the row counters.
+size_t sample_counters_at(const osm::SamplePlan& p) {
+    return (osm::sample_scratch_bytes(p) + 255) / 256 * 256;
+}
+
+// own: the workspace is the caller's (and may be null where none is needed), else the
+// stream's scratch is used.
 int run_sample(const void* x, int64_t ldx, const float* u, const osm_sample_params* params,
-               float* vals, int32_t* idx, int64_t N, int64_t V, int dtype, hipStream_t stream) {
+               float* vals, int32_t* idx, int64_t N, int64_t V, int dtype, bool own,
+               void* workspace, size_t workspace_bytes, hipStream_t stream) {
     size_t bytes = 0;
     if (!check_shape(N, V, dtype, &bytes) || ldx < V || ldx > kMaxDim) return OSM_EINVAL;
     if (N == 0) return OSM_OK;
@@ -672,12 +680,45 @@ int run_sample(const void* x, int64_t ldx, const float* u, const osm_sample_para
                        {s.top_p, nb},
                        {s.min_p, nb}};
     if (any_overlap(out, in)) return OSM_EINVAL;
-    if (!device_state(nullptr)) return OSM_EHIP;
+    if (own && workspace) {
+        if (!aligned(workspace, 256)) return OSM_EINVAL;
+        const Span ws[] = {{workspace, workspace_bytes}};
+        const Span all[] = {in[0], in[1], in[2], in[3], in[4], in[5], out[0], out[1]};
+        if (any_overlap(ws, all)) return OSM_EINVAL;
+    }
+    DeviceState* ds = device_state(nullptr);
+    if (!ds) return OSM_EHIP;
     const osm::SampleRows a{x,          u,          s.temperature,     s.top_k,     s.top_p,
                             s.min_p,    s.temperature_all, s.top_k_all, s.top_p_all,
                             s.min_p_all, vals,      idx,               N,           V,
                             ldx};
-    return hip_status(osm::launch_sample(a, dtype, stream));
+    const osm::SamplePlan p = osm::sample_plan(N, V, ldx, aligned(x, 16), dtype, ds->cus);
+    if (p.S <= 1) return hip_status(osm::launch_sample(a, p, dtype, nullptr, nullptr, stream));
+    const size_t at = sample_counters_at(p);
+    if (own) {
+        if (!workspace || workspace_bytes < at + (size_t)p.rows * 4) return OSM_ESCRATCH;
+        uint32_t* ctr = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + at);
+        hipLaunchKernelGGL(zero_u32, dim3((unsigned)((p.rows + 255) / 256)), dim3(256), 0, stream,
+                           ctr, p.rows);
+        if (hipGetLastError() != hipSuccess) return OSM_EHIP;
+        return hip_status(osm::launch_sample(a, p, dtype, workspace, ctr, stream));
+    }
+    void* scratch = nullptr;
+    bool temp = false, ctemp = false;
+    uint32_t* ctr = nullptr;
+    std::unique_lock<std::mutex> lk(ds->mu, std::defer_lock);  // held until the launches are in
+    int st = acquire_scratch(ds, lk, stream, at, &scratch, &temp);
+    if (st != OSM_OK) return st;
+    st = acquire_counters(ds, lk, stream, (size_t)p.rows, &ctr, &ctemp);
+    if (st != OSM_OK) {
+        if (temp) (void)hipFreeAsync(scratch, stream);
+        return st;
+    }
+    const hipError_t e = osm::launch_sample(a, p, dtype, scratch, ctr, stream);
+    const hipError_t f = temp ? hipFreeAsync(scratch, stream) : hipSuccess;
+    const hipError_t g = ctemp ? hipFreeAsync(ctr, stream) : hipSuccess;
+    if (e != hipSuccess) return OSM_EHIP;
+    return hip_status(f != hipSuccess ? f : g);
 }
 
 // Sizes and options of a router; the groups only where `choose`.
@@ -814,7 +855,24 @@ int proj_softmax_topk(const void* h, const void* w, float* vals, int32_t* idx, i
 int softmax_sample(const void* x, int64_t ldx, const float* u, const osm_sample_params* params,
                    float* vals, int32_t* idx, int64_t N, int64_t V, int dtype,
                    hipStream_t stream) {
-    return run_sample(x, ldx, u, params, vals, idx, N, V, dtype, stream);
+    return run_sample(x, ldx, u, params, vals, idx, N, V, dtype, false, nullptr, 0, stream);
+}
+
+int softmax_sample_ws(const void* x, int64_t ldx, const float* u, const osm_sample_params* params,
+                      float* vals, int32_t* idx, int64_t N, int64_t V, int dtype, void* workspace,
+                      size_t workspace_bytes, hipStream_t stream) {
+    return run_sample(x, ldx, u, params, vals, idx, N, V, dtype, true, workspace, workspace_bytes,
+                      stream);
+}
+
+int osm_sample_workspace(int64_t N, int64_t V, int dtype, size_t* bytes) {
+    size_t batch = 0;
+    if (!check_shape(N, V, dtype, &batch) || !bytes) return OSM_EINVAL;
+    DeviceState* ds = device_state(nullptr);
+    // (rows that are not aligned may take one path less, never a larger split)
+    const osm::SamplePlan p = osm::sample_plan(N, V, V, false, dtype, ds ? ds->cus : 256);
+    *bytes = p.S <= 1 ? 0 : sample_counters_at(p) + (size_t)p.rows * 4;
+    return OSM_OK;
 }
 
 int route_fwd(const void* x, const float* bias, float* vals, int32_t* idx, int64_t N, int64_t E,

@@ -114,7 +114,26 @@ struct SampleRows {
     int32_t* idx;
     int64_t N, V, ld;
 };
-hipError_t launch_sample(const SampleRows& a, int dtype, hipStream_t st);
+// How a batch is sampled.  S = 1: a wavefront a row (R = 0), a workgroup that holds R
+// vectors a lane, or one that streams the row (R < 0).  S > 1: S chunks a row,
+// `rows` rows a launch; scratch of sample_scratch_bytes, and `rows` zeroed counters,
+// which are left zeroed.
+struct SamplePlan {
+    int R, S;
+    int64_t chunk, rows;
+};
+struct SampleSplit {
+    int S;
+    int64_t chunk, row0;
+    uint64_t* parts;
+    uint64_t* mass;
+    uint32_t* counts;
+    uint32_t* ctr;
+};
+SamplePlan sample_plan(int64_t N, int64_t V, int64_t ld, bool aligned, int dtype, int cus);
+size_t sample_scratch_bytes(const SamplePlan& p);
+hipError_t launch_sample(const SampleRows& a, const SamplePlan& p, int dtype, void* scratch,
+                         uint32_t* ctr, hipStream_t st);
 
 // Routing: rows of E scores, K experts of each (see osm_route).
 struct RouteRows {

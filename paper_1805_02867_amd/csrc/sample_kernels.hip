@@ -1,326 +1,119 @@
-// Sampling a token of each row: temperature, top-k, top-p and min-p, with the
-// random number given.
-//
-// With m the row's maximum, the weights are w_j = 2^{(x_j - m) log2(e) / T}.  Each
-// filter keeps a prefix of the order "x descending, index ascending", so all
-// of them together are one cut in that order, held as the 64-bit key
-// (ordered x) << 32 | ~index of the last kept element:
-//   top-k  the k-th element;
-//   top-p  the first element at which the sum of weights, in that order and over
-//          what top-k kept, reaches p times the whole;
-//   min-p  the last element with w_j >= min_p (a test on the weight).
-// Nothing is sorted: a cut is found by histograms over the keys, each round
-// over the bin in which the count (top-k) or the mass (top-p) passes its target.
-// Masses in the histograms are weights in fixed point, whose sums do not depend
-// on the order of the atomic additions.
-//
-// The token is the first kept one, in index order, at which the running sum
-// passes u times the sum of the kept weights.
-//
-// Weights and sums are binary64: in binary32 the sums of 10^5 weights are off by
-// more than the distance between the borders they put on [0, 1), and the token
-// would depend on the order of the additions.
-#include "wide.hpp"
-#include "kernels.h"
+// Kernels of softmax_sample (sample.hpp): rows held whole by a wavefront or a workgroup,
+// rows split into chunks, and rows streamed from memory.
+#include "sample.hpp"
 
 namespace osm {
 
-constexpr int SM_BLOCK = 512;
-constexpr int SM_WAVES = SM_BLOCK / 64;
-constexpr int SM_LOG_BINS = 10;
-constexpr int SM_BINS = 1 << SM_LOG_BINS;
-static_assert(SM_BINS == 2 * SM_BLOCK, "two bins a thread");
+constexpr int SM_W = 8;  // wavefronts of a workgroup that has a row, or a chunk, to itself
+constexpr int SM_BLOCK = 64 * SM_W;
 
-struct SampleSmem {
-    union {
-        uint64_t bins[SM_BINS];
-        double seg[SM_BINS];
-    };
-    uint64_t wave64[SM_WAVES];
-    double waved[SM_WAVES];
-    uint32_t wave32[SM_WAVES];
-    int flag[SM_WAVES];
-    int found;
-    uint64_t above, here;
-    double base;
-};
-
-// What a row asks for.
-struct Rule {
-    bool greedy;
-    double c;       // log2(e) / T
-    int64_t k;      // elements that top-k keeps (0: all)
-    double p, q, u;
-};
-
-__device__ __forceinline__ Rule row_rule(const SampleRows& a, int64_t row) {
-    const float T = a.temperature ? a.temperature[row] : a.temperature_all;
-    const int32_t k = a.top_k ? a.top_k[row] : a.top_k_all;
-    const float p = a.top_p ? a.top_p[row] : a.top_p_all;
-    const float q = a.min_p ? a.min_p[row] : a.min_p_all;
-    const float u = a.u[row];
-    Rule r;
-    r.greedy = !(T > 0.0f);
-    r.c = kLog2eD / (double)T;
-    r.k = k > 0 && k < a.V ? k : 0;
-    r.p = p < 1.0f ? (double)p : 1.0;  // (NaN: off)
-    r.q = q > 0.0f ? __builtin_fmin((double)q, 1.0) : 0.0;
-    r.u = u > 0.0f ? __builtin_fmin((double)u, 1.0) : 0.0;
-    return r;
+__device__ __forceinline__ void no_token(float* val, int32_t* idx) {
+    *val = __builtin_nanf("");
+    *idx = -1;
 }
 
-// w of x; 0 at -inf, whatever c.
-__device__ __forceinline__ double weight(float x, double m, double c) {
-    return exp2_wide(((double)x - m) * c);
-}
-
-// A weight in fixed point, to nearest.
-__device__ __forceinline__ uint64_t fixed(double w, double scale) {
-    return (uint64_t)__builtin_fma(w, scale, 0.5);
-}
-
-template <typename T>
-struct RowSource {
-    const T* x;
-    int64_t n;
-    __device__ __forceinline__ float value(int64_t i) const { return load1(x + i); }
-};
-
-// The bin in which the running sum over sm.bins reaches `target`, with the sum
-// before it: results in sm.found, sm.above (which starts at `above`) and sm.here.
-// p >= 0: the target is the part p of the bins' sum, at least 1, and is returned.
-__device__ __forceinline__ uint64_t find_bin(SampleSmem& sm, uint64_t above, uint64_t target,
-                                             double p) {
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    const uint64_t a = sm.bins[2 * tid], b = sm.bins[2 * tid + 1];
-    const uint64_t incl = wave_scan(a + b);
-    if (lane == 63) sm.wave64[wv] = incl;
-    __syncthreads();
-    uint64_t before = above, total = above;
+// A row held by the team: loaded once.
+template <typename T, int W, int R>
+__device__ __forceinline__ void held_row(SampleSmem<W>& sm, const T* x, int32_t V, const Rule& r,
+                                         float* val, int32_t* idx) {
+    constexpr int THREADS = 64 * W, PER = SampleShape<W>::PER;
+    const int tid = threadIdx.x % THREADS;
+    Held<T, W, R> h;
+    h.load(x, V);
+    const float m = team_maximum(sm, h.maximum());
+    if (!(m < __builtin_inff()) || m == -__builtin_inff()) {
+        if (tid == 0) no_token(val, idx);
+        return;
+    }
+    if (r.greedy) {
+        uint32_t at = ~0u;
 #pragma unroll
-    for (int w = 0; w < SM_WAVES; ++w) {
-        if (w < wv) before += sm.wave64[w];
-        total += sm.wave64[w];
-    }
-    if (p >= 0.0) {
-        const double want = __builtin_ceil(p * (double)total);
-        target = want >= 1.0 ? (uint64_t)want : 1;
-        target = target < total ? target : total;
-    }
-    before += incl - a - b;
-    if (before < target && target <= before + a) {
-        sm.found = 2 * tid;
-        sm.above = before;
-        sm.here = a;
-    } else if (before + a < target && target <= before + a + b) {
-        sm.found = 2 * tid + 1;
-        sm.above = before + a;
-        sm.here = b;
-    }
-    __syncthreads();
-    return target;
-}
-
-__device__ __forceinline__ int bin_shift(uint32_t range) {
-    const int bits = 32 - __builtin_clz(range | 1u);
-    return bits > SM_LOG_BINS ? bits - SM_LOG_BINS : 0;
-}
-
-// The cut behind which `target` elements (MASS: the part p of the weights) of
-// those at or above `cut` lie.
-template <bool MASS, typename Src>
-__device__ __forceinline__ uint64_t find_cut(SampleSmem& sm, const Src src, uint32_t lo,
-                                             uint32_t hi, uint64_t cut, uint64_t target, double p,
-                                             double m, double c, double scale) {
-    const int tid = threadIdx.x;
-    uint64_t above = 0;
-    bool first = MASS;
-    for (;;) {  // rounds over values
-        const int shift = bin_shift(hi - lo);
-        sm.bins[tid] = 0;
-        sm.bins[tid + SM_BLOCK] = 0;
-        __syncthreads();
-        for (int64_t i = tid; i < src.n; i += SM_BLOCK) {
-            const float x = src.value(i);
-            const uint32_t k = order_key(x);
-            if (k < lo || k > hi || ((uint64_t)k << 32 | (uint32_t)~(uint32_t)i) < cut) continue;
-            const uint64_t w = MASS ? fixed(weight(x, m, c), scale) : 1;
-            atomicAdd((unsigned long long*)&sm.bins[(hi - k) >> shift], (unsigned long long)w);
-        }
-        __syncthreads();
-        target = find_bin(sm, above, target, first ? p : -1.0);
-        first = false;
-        above = sm.above;
-        hi -= (uint32_t)sm.found << shift;
-        if (shift == 0) break;
-        const uint32_t width = (1u << shift) - 1;
-        lo = hi - lo > width ? hi - width : lo;
-        __syncthreads();
-    }
-    // the value is hi; how many of the elements that hold it are kept
-    const uint64_t w = MASS ? fixed(weight(order_value(hi), m, c), scale) : 1;
-    const uint64_t ties = sm.here / w, need = (target - above + w - 1) / w;
-    __syncthreads();
-    uint64_t last = (uint64_t)hi << 32;
-    if (need < ties) {
-        uint32_t ilo = 0, ihi = (uint32_t)(src.n - 1);
-        above = 0;
-        for (;;) {  // rounds over the indices of the ties
-            const int shift = bin_shift(ihi - ilo);
-            sm.bins[tid] = 0;
-            sm.bins[tid + SM_BLOCK] = 0;
-            __syncthreads();
-            for (int64_t i = (int64_t)ilo + tid; i <= (int64_t)ihi; i += SM_BLOCK) {
-                const uint32_t k = order_key(src.value(i));
-                if (k != hi || ((uint64_t)k << 32 | (uint32_t)~(uint32_t)i) < cut) continue;
-                atomicAdd((unsigned long long*)&sm.bins[((uint32_t)i - ilo) >> shift], 1ull);
+        for (int rr = 0; rr < R; ++rr)
+#pragma unroll
+            for (int e = 0; e < h.E; ++e) {
+                const uint32_t i = h.index(rr, e);
+                at = h.at(rr, e) == m && i < at ? i : at;
             }
-            __syncthreads();
-            find_bin(sm, above, need, -1.0);
-            above = sm.above;
-            ilo += (uint32_t)sm.found << shift;
-            __syncthreads();
-            if (shift == 0) break;
-            const uint32_t width = (1u << shift) - 1;
-            ihi = ihi - ilo > width ? ilo + width : ihi;
-        }
-        last |= (uint32_t)~ilo;
-    }
-    return last > cut ? last : cut;
-}
-
-// One row by the workgroup.
-template <typename Src>
-__device__ __forceinline__ void sample_row(SampleSmem& sm, const Src src, const Rule r,
-                                           float* val, int32_t* idx) {
-    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-    // the maximum with its lowest index, and whether a NaN or +inf is there
-    uint64_t best = 0;
-    int bad = 0;
-    for (int64_t i = tid; i < src.n; i += SM_BLOCK) {
-        const float x = src.value(i);
-        bad |= !(x < __builtin_inff());
-        const uint64_t k = (uint64_t)order_key(x) << 32 | (uint32_t)~(uint32_t)i;
-        best = k > best ? k : best;
-    }
-    best = group_max<64>(best);
-    bad = __any(bad);
-    if (lane == 0) {
-        sm.wave64[wv] = best;
-        sm.flag[wv] = bad;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < SM_WAVES; ++w) {
-        best = sm.wave64[w] > best ? sm.wave64[w] : best;
-        bad |= sm.flag[w];
-    }
-    __syncthreads();
-    const float mx = order_value((uint32_t)(best >> 32));
-    if (bad || mx == -__builtin_inff() || r.greedy) {
+        at = team_minimum(sm, at);
         if (tid == 0) {
-            const bool none = bad || mx == -__builtin_inff();
-            *idx = none ? -1 : (int32_t)~(uint32_t)best;
-            *val = none ? __builtin_nanf("") : 1.0f;
+            *idx = (int32_t)at;
+            *val = 1.0f;
         }
         return;
     }
-    const double m = mx;
-    const uint32_t top = (uint32_t)(best >> 32), bottom = order_key(-__builtin_inff());
-    uint64_t cut = 0;
-    if (r.k) cut = find_cut<false>(sm, src, bottom, top, cut, (uint64_t)r.k, 0.0, m, r.c, 0.0);
-    if (r.p < 1.0) {
-        // the largest weight is 2^s with n 2^s <= 2^62
-        const int s = 62 - (64 - __builtin_clzll((uint64_t)src.n));
-        cut = find_cut<true>(sm, src, bottom, top, cut, 0, r.p > 0.0 ? r.p : 0.0, m, r.c,
-                             __builtin_ldexp(1.0, s));
+    const RowSource<T> src{x, V};
+    if ((r.k || r.p < 1.0) && cold((double)m * r.c)) {
+        sample_row(sm, src, r, val, idx);
+        return;
     }
-
-    // the token: sums of up to SM_BINS segments of the range, then the segment
-    // that the target falls into as the next range
-    int64_t a = 0, b = src.n;
-    double target = 0.0, total = 0.0;
-    bool first = true;
-    do {
-        int64_t L = (b - a + SM_BINS - 1) / SM_BINS;
-        L = (L + 63) / 64 * 64;
-        for (int s = wv; s < SM_BINS; s += SM_WAVES) {
-            double sum = 0.0;
-            const int64_t e = a + (s + 1) * L < b ? a + (s + 1) * L : b;
-            for (int64_t i = a + s * L + lane; i < e; i += 64) {
-                const float x = src.value(i);
-                const double w = weight(x, m, r.c);
-                const uint64_t k = (uint64_t)order_key(x) << 32 | (uint32_t)~(uint32_t)i;
-                sum += k >= cut && w >= r.q ? w : 0.0;
-            }
-            sum = group_sum<64>(sum);
-            if (lane == 0) sm.seg[s] = sum;
-        }
-        if (tid == 0) sm.found = SM_BINS;
-        __syncthreads();
-        const double s0 = sm.seg[2 * tid], s1 = sm.seg[2 * tid + 1];
-        const double incl = wave_scan(s0 + s1);
-        if (lane == 63) sm.waved[wv] = incl;
-        __syncthreads();
-        double before = 0.0, all = 0.0;
+    const Anchor an = anchor(m, r.c);
+    Cut cut = no_cut();
+    if (r.k || r.p < 1.0) {
 #pragma unroll
-        for (int w = 0; w < SM_WAVES; ++w) {
-            if (w < wv) before += sm.waved[w];
-            all += sm.waved[w];
+        for (int j = 0; j < PER; ++j) {
+            sm.mass[tid + j * THREADS] = 0;
+            sm.counts[tid + j * THREADS] = 0;
         }
-        if (first) {
-            total = all;
-            target = r.u * all;
-            first = false;
+        team_sync<W>();
+        bool tail = false;
+        if (!r.k) add_histogram<true, false>(sm, h, an);
+        else if (!(r.p < 1.0)) tail = add_histogram<false, true>(sm, h, an);
+        else tail = add_histogram<true, true>(sm, h, an);
+        tail = team_minimum(sm, tail ? 0u : 1u) == 0;
+        team_sync<W>();
+#pragma unroll
+        for (int j = 0; j < PER; ++j)
+            sm.sums[tid + j * THREADS] = (double)sm.mass[tid + j * THREADS] * 0x1p-48;
+        team_sync<W>();
+        const Filtered f = filter_row(sm, r, an, tail, (uint32_t)V - 1, false,
+                                      [&](const Range& g) {
+#pragma unroll
+                                          for (int rr = 0; rr < R; ++rr)
+#pragma unroll
+                                              for (int e = 0; e < h.E; ++e)
+                                                  append(sm, g, an, h.at(rr, e), h.index(rr, e));
+                                      });
+        if (!f.ok) {
+            sample_row(sm, src, r, val, idx);
+            return;
         }
-        const double prev = __shfl_up(incl, 1);
-        before += lane ? prev : 0.0;
-        // (a last positive segment stands in where rounding leaves the target unreached)
-        const bool in0 = s0 > 0.0 && before + s0 > target;
-        const bool in1 = s1 > 0.0 && before + s0 + s1 > target;
-        if (in0 || in1) atomicMin(&sm.found, in0 ? 2 * tid : 2 * tid + 1);
+        cut = f.cut;
+    }
+    locate<false>(sm, h,
+                  [&](float v, uint32_t i) {
+                      const double w = an.weight(v);
+                      return cut.keeps(v, i) && w >= r.q ? w : 0.0;
+                  },
+                  r.u, 0.0, 0, val, idx);
+}
+
+// Short rows, a wavefront each.
+constexpr int SM_SHORT = 1024;  // elements
+template <typename T>
+__global__ __launch_bounds__(256) void sample_short(const SampleRows a) {
+    constexpr int R = SM_SHORT / 64 / Vec<T>::N;
+    __shared__ SampleSmem<1> sm[4];
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    for (int64_t row = (int64_t)blockIdx.x * 4 + wv; row < a.N; row += (int64_t)gridDim.x * 4) {
+        held_row<T, 1, R>(sm[wv], static_cast<const T*>(a.x) + row * a.ld, (int32_t)a.V,
+                          row_rule(a, row), a.vals + row, a.idx + row);
+        wave_sync();
+    }
+}
+
+template <typename T, int R>
+__global__ __launch_bounds__(SM_BLOCK) void sample_rows(const SampleRows a) {
+    __shared__ SampleSmem<SM_W> sm;
+    for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
+        held_row<T, SM_W, R>(sm, static_cast<const T*>(a.x) + row * a.ld, (int32_t)a.V,
+                             row_rule(a, row), a.vals + row, a.idx + row);
         __syncthreads();
-        int at = sm.found;
-        __syncthreads();
-        if (at == SM_BINS) {
-            if (tid == 0) sm.found = -1;
-            __syncthreads();
-            if (s1 > 0.0) atomicMax(&sm.found, 2 * tid + 1);
-            else if (s0 > 0.0) atomicMax(&sm.found, 2 * tid);
-            __syncthreads();
-            at = sm.found;
-            target = __builtin_inf();
-        }
-        if (tid == at / 2) sm.base = at & 1 ? before + s0 : before;
-        __syncthreads();
-        target -= sm.base;
-        a += at * L;
-        b = a + L < b ? a + L : b;
-        __syncthreads();
-    } while (b - a > 64);
-    if (wv == 0) {
-        const int64_t i = a + lane;
-        double w = 0.0;
-        if (i < b) {
-            const float x = src.value(i);
-            const uint64_t k = (uint64_t)order_key(x) << 32 | (uint32_t)~(uint32_t)i;
-            w = weight(x, m, r.c);
-            w = k >= cut && w >= r.q ? w : 0.0;
-        }
-        const double incl = wave_scan(w);
-        const uint64_t some = __ballot(w > 0.0);
-        const uint64_t past = __ballot(w > 0.0 && incl > target);
-        const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
-        if (lane == at) {
-            *idx = (int32_t)i;
-            *val = (float)(w / total);
-        }
     }
 }
 
 template <typename T>
-__global__ __launch_bounds__(SM_BLOCK) void sample_rows(const SampleRows a) {
-    __shared__ SampleSmem sm;
+__global__ __launch_bounds__(SM_BLOCK) void sample_streamed(const SampleRows a) {
+    __shared__ SampleSmem<SM_W> sm;
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
         const RowSource<T> src{static_cast<const T*>(a.x) + row * a.ld, a.V};
         sample_row(sm, src, row_rule(a, row), a.vals + row, a.idx + row);
@@ -328,14 +121,365 @@ __global__ __launch_bounds__(SM_BLOCK) void sample_rows(const SampleRows a) {
     }
 }
 
-hipError_t launch_sample(const SampleRows& a, int dtype, hipStream_t st) {
+// ------------------------------------------------------------------ split rows
+// What a chunk leaves for the workgroup that completes the row, at the device's
+// coherence point: its maximum, the index of that (greedy rows) or whether elements
+// of some weight lie below its histogram, and the sum of its weights relative to
+// its own anchor (rows without a filter) or its histograms.
+struct ChunkSum {
+    float m;
+    uint32_t at;
+    double z;
+};
+
+__device__ __forceinline__ void put(uint64_t* p, uint64_t v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void put(uint32_t* p, uint32_t v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t get(const uint64_t* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint32_t get(const uint32_t* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The row's end, by the workgroup that put its last chunk.
+template <typename T, int R>
+__device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows& a,
+                                          const SampleSplit& s, const T* x, const Rule& r,
+                                          const uint64_t* parts, const uint64_t* mass,
+                                          const uint32_t* counts, float* val, int32_t* idx) {
+    constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
+    constexpr int SUB = SampleShape<SM_W>::SUB, E = Vec<T>::N;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, S = s.S;
+    const RowSource<T> src{x, a.V};
+    // every wavefront: chunk `lane`
+    float mc = -__builtin_inff();
+    uint32_t at = 0;
+    double z = 0.0;
+    if (lane < S) {
+        const uint64_t p0 = get(parts + 2 * lane);
+        z = __builtin_bit_cast(double, get(parts + 2 * lane + 1));
+        mc = __uint_as_float((uint32_t)p0);
+        at = (uint32_t)(p0 >> 32);
+    }
+    const float m = wave_maximum(mc);
+    if (!(m < __builtin_inff()) || m == -__builtin_inff()) {
+        if (tid == 0) no_token(val, idx);
+        return;
+    }
+    if (r.greedy) {
+        const int c = __builtin_ctzll(__ballot(mc == m));
+        if (tid == c) {
+            *idx = (int32_t)at;
+            *val = 1.0f;
+        }
+        return;
+    }
+    // a chunk far below the row's maximum has no weight at all
+    const bool none = mc == -__builtin_inff() || ((double)mc - (double)m) * r.c < -1100.0;
+    const bool filtered = r.k || r.p < 1.0 || r.q > 0.0;
+    // (the histograms leave out what is below 2^-64 of the largest weight; only a u at
+    // the very ends of [0, 1] can fall there)
+    const bool ends = r.u < 0x1p-30 || r.u > 1.0 - 0x1p-30;
+    if (filtered && (__ballot(!none && cold((double)mc * r.c)) != 0 || ends)) {
+        sample_row(sm, src, r, val, idx);
+        return;
+    }
+    const Anchor an = anchor(m, r.c);
+    // bins of the row's histogram that its own starts below, and its weights' factor
+    const int down = none || !filtered ? 0 : (int)(an.a - anchor(mc, r.c).a) * SUB;
+    const double part = none ? 0.0 : exp2_wide(((double)mc - (double)m) * r.c);
+    Cut cut = no_cut();
+    double kept = 0.0;  // of chunk `lane`
+    if (!filtered) {
+        kept = z * part;
+    } else {
+        // the row's histograms
+        bool tail = r.k && __ballot(lane < S && !none && at != 0) != 0;
+        double sum[PER];
+        uint32_t num[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            sum[j] = 0.0;
+            num[j] = 0;
+        }
+        for (int c = 0; c < S; ++c) {
+            const int off = __builtin_amdgcn_readlane(down, c);
+            const double part_c = __shfl(part, c);
+            if (part_c == 0.0) continue;
+            uint64_t w[PER];
+            uint32_t n[PER];
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const int b = tid + j * SM_BLOCK;
+                w[j] = b >= off ? get(mass + (int64_t)c * BINS + b - off) : 0;
+                if (r.k) n[j] = get(counts + (int64_t)c * BINS + b);
+            }
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const int b = tid + j * SM_BLOCK;
+                sum[j] += (double)w[j] * 0x1p-48 * part_c;
+                if (r.k) tail |= n[j] != 0 && b + off >= BINS - 1;
+            }
+            if (r.k) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const int b = tid + j * SM_BLOCK;
+                    num[j] += b >= off ? get(counts + (int64_t)c * BINS + b - off) : 0;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int b = tid + j * SM_BLOCK;
+            sm.sums[b] = b < BINS - 1 ? sum[j] : 0.0;
+            sm.counts[b] = b < BINS - 1 ? num[j] : 0;
+        }
+        tail = team_minimum(sm, tail ? 0u : 1u) == 0;
+        __syncthreads();
+        const Filtered f = filter_row(
+            sm, r, an, tail, (uint32_t)a.V - 1, true, [&](const Range& g) {
+                const int h = (int)(((uintptr_t)x & 15) / sizeof(T));
+                const int64_t vecs = (a.V + h + E - 1) / E;
+                for (int64_t v0 = 0; v0 < vecs; v0 += 4 * SM_BLOCK) {
+                    u32x4 q[4];
+                    int64_t i0[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        i0[j] = (v0 + j * SM_BLOCK + tid) * E - h;
+                        if (i0[j] >= 0 && i0[j] + E <= a.V)
+                            q[j] = *reinterpret_cast<const u32x4*>(x + i0[j]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const bool whole = i0[j] >= 0 && i0[j] + E <= a.V;
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            const int64_t i = i0[j] + e;
+                            const float v = whole ? elem(q[j], e, (T*)nullptr)
+                                            : i >= 0 && i < a.V ? load1(x + i)
+                                                                : -__builtin_inff();
+                            append(sm, g, an, v, (uint32_t)i);
+                        }
+                    }
+                }
+            });
+        if (!f.ok) {
+            sample_row(sm, src, r, val, idx);
+            return;
+        }
+        cut = f.cut;
+        // the kept weights of each chunk: of the bins kept whole, and of the list
+        const int n = f.sure < BINS - 1 ? sm.n : 0;
+        if (tid < 64) sm.chunk[tid] = 0;
+        __syncthreads();
+        for (int j = tid; j < n; j += SM_BLOCK) {
+            const float v = sm.lx[j];
+            const uint32_t i = sm.li[j];
+            const double w = an.weight(v);
+            if (an.bin<SM_W>(v) >= f.sure && cut.keeps(v, i) && w >= r.q)
+                add_bin(sm.chunk[i / (uint32_t)s.chunk], fixed48(w));
+        }
+        __syncthreads();
+        kept = (double)sm.chunk[lane] * 0x1p-48;
+        for (int c = wv; c < S; c += SM_W) {
+            const int off = __builtin_amdgcn_readlane(down, c);
+            const double part_c = __shfl(part, c);
+            uint64_t units = 0;
+            if (part_c > 0.0)
+                for (int b = lane; b + off < f.sure; b += 64)
+                    units += get(mass + (int64_t)c * BINS + b);
+            units = wave_total(units);
+            if (lane == 0) sm.whole[c] = (double)units * 0x1p-48 * part_c;
+        }
+        __syncthreads();
+        kept += lane < S ? sm.whole[lane] : 0.0;
+    }
+    // the chunk that the token is in (every wavefront: the same numbers)
+    const double incl = wave_scan(kept);
+    const double total = __shfl(incl, 63), target = r.u * total;
+    const uint64_t some = __ballot(kept > 0.0), past = __ballot(kept > 0.0 && incl > target);
+    const int c = past ? __builtin_ctzll(past) : some ? 63 - __builtin_clzll(some) : 0;
+    const double rem = past ? target - (c ? __shfl(incl, c - 1) : 0.0) : __builtin_inf();
+    const int64_t i0 = (int64_t)c * s.chunk;
+    Held<T, SM_W, R> h;
+    h.load(x + i0, (int32_t)(a.V - i0 < s.chunk ? a.V - i0 : s.chunk));
+    __syncthreads();
+    const bool found = locate<true>(sm, h,
+                                    [&](float v, uint32_t i) {
+                                        const double w = an.weight(v);
+                                        return cut.keeps(v, (uint32_t)i0 + i) && w >= r.q ? w
+                                                                                            : 0.0;
+                                    },
+                                    rem, total, (uint32_t)i0, val, idx);
+    if (!found) {
+        __syncthreads();
+        sample_row(sm, src, r, val, idx);
+    }
+}
+
+// Workgroup: chunk blockIdx % S of row row0 + blockIdx / S.
+template <typename T, int R>
+__global__ __launch_bounds__(SM_BLOCK) void sample_split(const SampleRows a, const SampleSplit s) {
+    constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
+    __shared__ SampleSmem<SM_W> sm;
+    const int tid = threadIdx.x;
+    const int rel = (int)(blockIdx.x / (unsigned)s.S), c = (int)(blockIdx.x % (unsigned)s.S);
+    const int64_t row = s.row0 + rel;
+    const T* x = static_cast<const T*>(a.x) + row * a.ld;
+    const Rule r = row_rule(a, row);
+    uint64_t* parts = s.parts + (int64_t)rel * s.S * 2;
+    uint64_t* mass = s.mass + (int64_t)rel * s.S * BINS;
+    uint32_t* counts = s.counts + (int64_t)rel * s.S * BINS;
+    {
+        const int64_t i0 = (int64_t)c * s.chunk;
+        Held<T, SM_W, R> h;
+        h.load(x + i0, (int32_t)(a.V - i0 < s.chunk ? a.V - i0 : s.chunk));
+        ChunkSum p{team_maximum(sm, h.maximum()), 0, 0.0};
+        const bool live = p.m < __builtin_inff() && p.m > -__builtin_inff();
+        if (r.greedy) {
+            uint32_t at = ~0u;
+#pragma unroll
+            for (int rr = 0; rr < R; ++rr)
+#pragma unroll
+                for (int e = 0; e < h.E; ++e) {
+                    const uint32_t i = h.index(rr, e);
+                    at = h.at(rr, e) == p.m && i < at ? i : at;
+                }
+            p.at = team_minimum(sm, at) + (uint32_t)i0;
+        } else if (live) {
+            const Anchor an = anchor(p.m, r.c);
+            if (!(r.k || r.p < 1.0 || r.q > 0.0)) {
+                double z = 0.0;
+#pragma unroll
+                for (int rr = 0; rr < R; ++rr)
+#pragma unroll
+                    for (int e = 0; e < h.E; ++e) z += an.weight(h.at(rr, e));
+                p.z = team_sum(sm, z);
+            } else if (!cold((double)p.m * r.c)) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    sm.mass[tid + j * SM_BLOCK] = 0;
+                    sm.counts[tid + j * SM_BLOCK] = 0;
+                }
+                __syncthreads();
+                bool tail = false;
+                if (!r.k) add_histogram<true, false>(sm, h, an);
+                else tail = add_histogram<true, true>(sm, h, an);
+                p.at = team_minimum(sm, tail ? 0u : 1u) == 0;
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const int b = tid + j * SM_BLOCK;
+                    put(mass + (int64_t)c * BINS + b, sm.mass[b]);
+                    if (r.k) put(counts + (int64_t)c * BINS + b, sm.counts[b]);
+                }
+            }
+        }
+        if (tid == 0) {
+            put(parts + 2 * c, (uint64_t)p.at << 32 | __float_as_uint(p.m));
+            put(parts + 2 * c + 1, __builtin_bit_cast(uint64_t, p.z));
+        }
+    }
+    // every store of the chunk has completed before the row's count moves
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0)
+        sm.found = (int)__hip_atomic_fetch_add(s.ctr + rel, 1u, __ATOMIC_RELAXED,
+                                               __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    const int done = sm.found;
+    __syncthreads();
+    if (done != s.S - 1) return;
+    if (tid == 0) __hip_atomic_store(s.ctr + rel, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    split_end<T, R>(sm, a, s, x, r, parts, mass, counts, a.vals + row, a.idx + row);
+}
+
+// ------------------------------------------------------------------------ plan
+namespace {
+constexpr int kSplitMax = 64;            // chunks of a row: a lane each
+constexpr int64_t kSplitChunks = 4096;   // of one launch, which bounds the scratch
+
+template <typename T>
+constexpr int64_t held_elems(int R) {
+    return (int64_t)SM_BLOCK * R * Vec<T>::N;
+}
+}  // namespace
+
+SamplePlan sample_plan(int64_t N, int64_t V, int64_t ld, bool aligned, int dtype, int cus) {
+    const int E = dtype == 1 ? 8 : 4;
+    const int64_t room = V + (aligned && ld % E == 0 ? 0 : E - 1);
+    const int64_t one = (int64_t)SM_BLOCK * E;  // a vector a lane
+    if (room <= SM_SHORT) return {0, 1, V, 1};
+    if (room <= 2 * one) return {2, 1, V, 1};
+    // chunks of whole vectors, at most eight a lane; with few rows more of them, of at
+    // least two vectors a lane
+    const int64_t least = (V + 8 * one - E - 1) / (8 * one - E);
+    int64_t S = 2 * (int64_t)cus / (N > 0 ? N : 1);
+    const int64_t most = V / (2 * one);
+    S = S < 16 ? S : 16;
+    S = S < most ? S : most;
+    S = S > least ? S : least;
+    if (S > kSplitMax) return {-1, 1, V, 1};
+    if (S <= 1) return {8, 1, V, 1};
+    int64_t chunk = (V + S - 1) / S;
+    chunk = (chunk + E - 1) / E * E;
+    S = (V + chunk - 1) / chunk;
+    const int R = chunk + E <= 2 * one ? 2 : chunk + E <= 4 * one ? 4 : 8;
+    int64_t rows = kSplitChunks / S;
+    rows = rows < N ? rows : N;
+    return {R, (int)S, chunk, rows > 0 ? rows : 1};
+}
+
+size_t sample_scratch_bytes(const SamplePlan& p) {
+    if (p.S <= 1) return 0;
+    constexpr size_t BINS = SampleShape<SM_W>::BINS;
+    return (size_t)p.rows * (size_t)p.S * (16 + 12 * BINS);
+}
+
+template <typename T>
+static hipError_t launch_sample_t(const SampleRows& a, const SamplePlan& p, void* scratch,
+                                  uint32_t* ctr, hipStream_t st) {
     // (a launch takes fewer than 2^32 threads: further rows by the same workgroups)
-    const unsigned blocks = (unsigned)(a.N < (1 << 22) ? a.N : 1 << 22);
-    if (dtype == 1)
-        hipLaunchKernelGGL(sample_rows<bf16_t>, dim3(blocks), dim3(SM_BLOCK), 0, st, a);
-    else
-        hipLaunchKernelGGL(sample_rows<float>, dim3(blocks), dim3(SM_BLOCK), 0, st, a);
-    return hipGetLastError();
+    const auto blocks = [](int64_t n) { return dim3((unsigned)(n < (1 << 22) ? n : 1 << 22)); };
+    if (p.S <= 1) {
+        if (p.R == 0)
+            hipLaunchKernelGGL(sample_short<T>, blocks((a.N + 3) / 4), dim3(256), 0, st, a);
+        else if (p.R == 2)
+            hipLaunchKernelGGL((sample_rows<T, 2>), blocks(a.N), dim3(SM_BLOCK), 0, st, a);
+        else if (p.R > 0)
+            hipLaunchKernelGGL((sample_rows<T, 8>), blocks(a.N), dim3(SM_BLOCK), 0, st, a);
+        else
+            hipLaunchKernelGGL(sample_streamed<T>, blocks(a.N), dim3(SM_BLOCK), 0, st, a);
+        return hipGetLastError();
+    }
+    constexpr int64_t BINS = SampleShape<SM_W>::BINS;
+    SampleSplit s;
+    s.S = p.S;
+    s.chunk = p.chunk;
+    s.parts = static_cast<uint64_t*>(scratch);
+    s.mass = s.parts + p.rows * p.S * 2;
+    s.counts = reinterpret_cast<uint32_t*>(s.mass + p.rows * p.S * BINS);
+    s.ctr = ctr;
+    for (s.row0 = 0; s.row0 < a.N; s.row0 += p.rows) {
+        const int64_t n = a.N - s.row0 < p.rows ? a.N - s.row0 : p.rows;
+        const dim3 grid((unsigned)(n * p.S)), block(SM_BLOCK);
+        if (p.R == 2) hipLaunchKernelGGL((sample_split<T, 2>), grid, block, 0, st, a, s);
+        else if (p.R == 4) hipLaunchKernelGGL((sample_split<T, 4>), grid, block, 0, st, a, s);
+        else hipLaunchKernelGGL((sample_split<T, 8>), grid, block, 0, st, a, s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+
+hipError_t launch_sample(const SampleRows& a, const SamplePlan& p, int dtype, void* scratch,
+                         uint32_t* ctr, hipStream_t st) {
+    return dtype == 1 ? launch_sample_t<bf16_t>(a, p, scratch, ctr, st)
+                      : launch_sample_t<float>(a, p, scratch, ctr, st);
 }
 
 }  // namespace osm

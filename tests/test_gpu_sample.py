@@ -255,6 +255,33 @@ def test_streams_and_captured_replays(N, V, dev):
         check(xs[0], us[0], dev, **kw)                    # eager between replays
 
 
+@pytest.mark.parametrize("N,V", [(3, 128256), (70, 32000)])
+def test_workspaces(N, V, dev):
+    """Two calls at once in workspaces of their own, of any contents; a small one is refused."""
+    kw = dict(top_p=0.9, temperature=1.1)
+    n = osm.sample_workspace(N, V, torch.bfloat16)
+    assert n > 0
+    ws = [torch.full((n,), 255, dtype=torch.uint8, device=dev) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    xs = [logits(N, V, "bf16", s, dev) for s in range(2)]
+    us = [uniform(N, s, dev) for s in range(2)]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for s, w, x, u in zip(streams, ws, xs, us):
+            with torch.cuda.stream(s):
+                got.append(osm.softmax_sample(x, u, workspace=w, **kw))
+    torch.cuda.synchronize()
+    for j in range(2):
+        want = pick_ref.sample(host(xs[j]), host(us[j]), **kw)
+        for v, i in got[j::2]:
+            assert np.array_equal(i.cpu().numpy(), want[1])
+            pick_ref.close(host(v), want[0])
+    for bad in (ws[0][:n - 1], ws[0][:0], ws[0][1:]):
+        with pytest.raises(osm.OsmError):
+            osm.softmax_sample(xs[0], us[0], workspace=bad, **kw)
+
+
 def test_same_bits_every_time(dev):
     x, u = logits(20, 60000, "f32", 8, dev), uniform(20, 8, dev)
     for kw in (dict(), dict(top_p=0.9), dict(top_k=3000, top_p=0.9, min_p=1e-4)):

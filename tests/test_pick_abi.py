@@ -34,6 +34,24 @@ def test_sample_refuses(bad):
     assert _sample(**bad) == osm.EINVAL
 
 
+@pytest.mark.parametrize("ws,n", [(D_ + 16, 1 << 24), (X, 1 << 24), (V_ - 256, 1 << 20)])
+def test_sample_refuses_a_bad_workspace(ws, n):
+    assert osm.lib().softmax_sample_ws(X, 10, U, None, V_, I_, 4, 10, 0, ws, n, None) == osm.EINVAL
+
+
+def test_workspace_sizes():
+    n = ctypes.c_size_t()
+    size = osm.lib().osm_sample_workspace
+    assert size(4, 0, 0, ctypes.byref(n)) == osm.EINVAL
+    assert size(4, 10, 7, ctypes.byref(n)) == osm.EINVAL
+    assert size(-1, 10, 0, ctypes.byref(n)) == osm.EINVAL
+    assert size(4, 10, 0, None) == osm.EINVAL
+    assert osm.sample_workspace(0, 128256) >= 0 and osm.sample_workspace(1000, 1000) == 0
+    for V, rows in ((32000, (1, 64)), (128256, (1, 64, 4000)), (1000000, (1, 4000))):
+        for N in rows:   # a launch's rows at a time: 4096 chunks of 12 KB and a row's few
+            assert 0 < osm.sample_workspace(N, V) <= 4096 * (12 * 1024 + 16) + 256 + 4 * 4096
+
+
 def test_empty_batches_are_noops():
     assert _sample(N=0, x=0, u=0, vals=0, idx=0) == osm.OK
     assert _fwd(N=0, x=0, vals=0, idx=0) == osm.OK
