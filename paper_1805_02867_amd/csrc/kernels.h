@@ -124,7 +124,7 @@ struct SamplePlan {
 };
 struct SampleSplit {
     int S;
-    int64_t chunk, row0;
+    int64_t chunk, row0, rows;  // the launch's rows
     uint64_t* parts;
     uint64_t* mass;
     uint32_t* counts;

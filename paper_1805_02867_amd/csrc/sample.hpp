@@ -131,7 +131,7 @@ __device__ __forceinline__ uint64_t find_bin(SampleSmem<W>& sm, uint64_t above, 
     const uint64_t incl = wave_scan(sum);
     uint64_t before = above, total = above;
     if constexpr (W == 1) {
-        total += __shfl(incl, 63);
+        total += lane_value(incl, 63);
     } else {
         if (lane == 63) sm.wave64[wv] = incl;
         __syncthreads();
@@ -339,8 +339,7 @@ __device__ __forceinline__ void sample_row(SampleSmem<W>& sm, const RowSource<T>
             sum += s[j];
         }
         const double incl = wave_scan(sum);
-        const double prev = __shfl_up(incl, 1);
-        double before = lane ? prev : 0.0, all = __shfl(incl, 63);
+        double before = lane_before(incl), all = lane_value(incl, 63);
         if constexpr (W > 1) {
             if (lane == 63) sm.waved[wv] = incl;
             __syncthreads();
@@ -516,32 +515,31 @@ __device__ __forceinline__ double team_sum(SampleSmem<W>& sm, double v) {
     return v;
 }
 
-// Weights relative to the maximum m of a row or a chunk, which is exactly 1; and the
-// bins of a histogram, which are counted down from a power of two just above: 2^s,
-// s = x c - a with a = ceil(m c), has the same bin in every chunk but for a shift
-// by the difference of their a.  (The product is exact in the fma; m c has to be
-// small enough for its ceiling to be one.)
+// Weights 2^t relative to the maximum m of a row or a chunk, which is exactly 1, and
+// their bins in a histogram, 1/SUB of a power of two a bin.  Bins are counted down from
+// a power of two, 2^0 standing for the value a / c just above m, so that the bins
+// of another chunk are the same ones but for a shift by the difference of their a.
+// (m c has to be small enough for its ceiling to be one.)
 struct Anchor {
-    double m, c, a;
-    __device__ __forceinline__ double t(float x) const { return ((double)x - m) * c; }
-    __device__ __forceinline__ double weight(float x) const { return exp2_wide(t(x)); }
-    // 1/SUB of a power of two a bin: s + 1.5 2^52 / SUB has round(s SUB) in its low bits
-    template <int W>
-    __device__ __forceinline__ static int bin_of(double s) {
-        constexpr double M = 0x1.8p52 / SampleShape<W>::SUB;
-        const int b = -(int)(uint32_t)__builtin_bit_cast(uint64_t, __builtin_fmax(s, -1100.0) + M);
-        return b > 0 ? b : 0;
+    double m, c, a, shift;  // shift: of the maximum, in (-1, 0]
+    // (weights vanish below 2^-1075; the bound also takes the place of -inf and NaN)
+    __device__ __forceinline__ double t(float x) const {
+        return __builtin_fmax(((double)x - m) * c, -1100.0);
     }
+    __device__ __forceinline__ double weight(float x) const { return exp2_bounded(t(x)); }
+    // the low bits of s + 1.5 2^52 / SUB are round(s SUB)
     template <int W>
-    __device__ __forceinline__ int bin(float x) const {
-        return bin_of<W>(__builtin_fma((double)x, c, -a));
+    __device__ __forceinline__ int bin(double t) const {
+        constexpr double M = 0x1.8p52 / SampleShape<W>::SUB;
+        return -(int)(uint32_t)__builtin_bit_cast(uint64_t, t + shift + M);
     }
 };
 
 constexpr double kAnchorMax = 0x1p30;
 __device__ __forceinline__ bool cold(double mc) { return !(__builtin_fabs(mc) <= kAnchorMax); }
 __device__ __forceinline__ Anchor anchor(float m, double c) {
-    return Anchor{(double)m, c, __builtin_ceil((double)m * c)};
+    const double mc = (double)m * c, a = __builtin_ceil(mc);
+    return Anchor{(double)m, c, a, mc - a};
 }
 
 // Adds the held elements to the histogram sm.mass of weights (MASS) and to that of
@@ -555,13 +553,13 @@ __device__ __forceinline__ bool add_histogram(SampleSmem<W>& sm, const Held<T, W
     for (int r = 0; r < R; ++r) {
 #pragma unroll
         for (int e = 0; e < h.E; ++e) {
-            const float x = h.at(r, e);
-            const int b = an.bin<W>(x);
+            const double t = an.t(h.at(r, e));
+            const int b = an.bin<W>(t);
             if (b < SampleShape<W>::BINS - 1) {
-                if constexpr (MASS) add_bin(sm.mass[b], fixed48(an.weight(x)));
+                if constexpr (MASS) add_bin(sm.mass[b], fixed48(exp2_bounded(t)));
                 if constexpr (COUNT) atomicAdd(&sm.counts[b], 1u);
             } else if constexpr (COUNT) {
-                tail |= an.t(x) > -1080.0;  // (2^-1075 and below is 0; -inf never counts)
+                tail |= t > -1080.0;
             }
         }
     }
@@ -586,13 +584,16 @@ struct Range {
     }
 };
 
+// Whether x may be in the range.
+__device__ __forceinline__ bool near(const Range& g, float x) { return x >= g.x0 && x <= g.x1; }
+
 // Appends x to the list if its bin is in the range; all lanes call.
 template <int W>
 __device__ __forceinline__ void append(SampleSmem<W>& sm, const Range& g, const Anchor& an,
                                        float x, uint32_t i) {
-    bool in = x >= g.x0 && x <= g.x1;
+    bool in = near(g, x);
     if (__ballot(in) == 0) return;
-    const int b = an.bin<W>(x);
+    const int b = an.bin<W>(an.t(x));
     in = in && b >= g.lo && b <= g.hi;
     const uint64_t who = __ballot(in);
     if (who == 0) return;
@@ -633,11 +634,9 @@ __device__ __forceinline__ Cut list_cut(SampleSmem<W>& sm, int n, Cut cut, uint6
         const uint64_t w = !in ? 0 : MASS ? units(x) : 1;
         uint64_t incl = 0;
         for (int l = 0; l < n; ++l) {
-            const float xl = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l));
-            const uint32_t il = __builtin_amdgcn_readlane(i, l);
-            const uint64_t wl =
-                (uint64_t)__builtin_amdgcn_readlane((uint32_t)(w >> 32), l) << 32 |
-                (uint32_t)__builtin_amdgcn_readlane((uint32_t)w, l);
+            const float xl = lane_value(x, l);
+            const uint32_t il = lane_value(i, l);
+            const uint64_t wl = lane_value(w, l);
             incl += xl > x || (xl == x && il <= i) ? wl : 0;
         }
         if (in && incl >= target && incl - w < target) {
@@ -666,14 +665,18 @@ __device__ __forceinline__ uint64_t wave_total(uint64_t v) {
 template <int W>
 __device__ __forceinline__ uint64_t list_sum(SampleSmem<W>& sm, int n, Cut cut,
                                              const Anchor& an) {
-    const int tid = threadIdx.x % (64 * W);
-    if (tid == 0) sm.here = 0;
-    team_sync<W>();
-    for (int j = tid; j < n; j += 64 * W)
-        if (cut.keeps(sm.lx[j], sm.li[j])) add_bin(sm.here, fixed48(an.weight(sm.lx[j])));
-    team_sync<W>();
-    const uint64_t s = sm.here;
-    team_sync<W>();
+    uint64_t s = 0;
+    for (int j = threadIdx.x % (64 * W); j < n; j += 64 * W)
+        if (cut.keeps(sm.lx[j], sm.li[j])) s += fixed48(an.weight(sm.lx[j]));
+    s = wave_total(s);
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 63) == 0) sm.wave64[threadIdx.x >> 6] = s;
+        __syncthreads();
+        s = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) s += sm.wave64[w];
+        __syncthreads();
+    }
     return s;
 }
 
@@ -691,8 +694,7 @@ __device__ __forceinline__ int find_mass(SampleSmem<W>& sm, int limit, double ex
         sum += v[j];
     }
     const double incl = wave_scan(sum);
-    const double prev = __shfl_up(incl, 1);
-    double before = lane ? prev : 0.0, total = __shfl(incl, 63);
+    double before = lane_before(incl), total = lane_value(incl, 63);
     if (tid == 0) sm.found = BINS;
     if constexpr (W > 1) {
         if (lane == 63) sm.waved[wv] = incl;
@@ -847,8 +849,7 @@ __device__ __forceinline__ Filtered filter_row(SampleSmem<W>& sm, const Rule& r,
     }
     if (r.q > 0.0 && sums) {
         // min-p: w >= q, somewhere in the bins around that
-        const double s = __builtin_fma(an.m, an.c, -an.a) + (double)__builtin_log2f((float)r.q);
-        const int b = Anchor::bin_of<W>(s);
+        const int b = an.bin<W>((double)__builtin_log2f((float)r.q));
         const int lo = b > 1 ? b - 1 : 0, hi = b + 1;
         if (lo < f.sure) f.sure = lo;
         if (hi < f.last) f.last = hi;
@@ -883,7 +884,7 @@ __device__ __forceinline__ bool locate(SampleSmem<W>& sm, const Held<T, W, R>& h
     const double seg = lane < R * W ? sm.seg[lane] : 0.0;
     const double incl = wave_scan(seg);
     if constexpr (!PART) {
-        total = __shfl(incl, 63);
+        total = lane_value(incl, 63);
         target *= total;
     }
     const uint64_t some = __ballot(seg > 0.0);
@@ -892,7 +893,7 @@ __device__ __forceinline__ bool locate(SampleSmem<W>& sm, const Held<T, W, R>& h
     const uint64_t past = __ballot(seg > 0.0 && incl > target);
     const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
     if (at % W == wv) {
-        target = past ? target - (at ? __shfl(incl, at - 1) : 0.0) : __builtin_inf();
+        target = past ? target - (at ? lane_value(incl, at - 1) : 0.0) : __builtin_inf();
         const int ra = at / W;
         double v = s[0];
         u32x4 q = h.q[0];
@@ -902,11 +903,11 @@ __device__ __forceinline__ bool locate(SampleSmem<W>& sm, const Held<T, W, R>& h
             q = ra == r ? h.q[r] : q;
         }
         const double run = wave_scan(v);
-        const double prev = __shfl_up(run, 1);
+        const double prev = lane_before(run);
         const uint64_t mine = __ballot(v > 0.0), over = __ballot(v > 0.0 && run > target);
         const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(mine);
         if (lane == l) {
-            const double rest = over ? target - (lane ? prev : 0.0) : __builtin_inf();
+            const double rest = over ? target - prev : __builtin_inf();
             const uint32_t i0 = h.index(0, 0) + (uint32_t)(ra * 64 * W * h.E);
             double sum = 0.0, w1 = 0.0;
             uint32_t i1 = 0;

@@ -68,10 +68,16 @@ __device__ __forceinline__ void held_row(SampleSmem<W>& sm, const T* x, int32_t 
         const Filtered f = filter_row(sm, r, an, tail, (uint32_t)V - 1, false,
                                       [&](const Range& g) {
 #pragma unroll
-                                          for (int rr = 0; rr < R; ++rr)
+                                          for (int rr = 0; rr < R; ++rr) {
+                                              bool any = false;
+#pragma unroll
+                                              for (int e = 0; e < h.E; ++e)
+                                                  any |= near(g, h.at(rr, e));
+                                              if (__ballot(any) == 0) continue;
 #pragma unroll
                                               for (int e = 0; e < h.E; ++e)
                                                   append(sm, g, an, h.at(rr, e), h.index(rr, e));
+                                          }
                                       });
         if (!f.ok) {
             sample_row(sm, src, r, val, idx);
@@ -206,30 +212,36 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
             sum[j] = 0.0;
             num[j] = 0;
         }
-        for (int c = 0; c < S; ++c) {
-            const int off = __builtin_amdgcn_readlane(down, c);
-            const double part_c = __shfl(part, c);
-            if (part_c == 0.0) continue;
-            uint64_t w[PER];
-            uint32_t n[PER];
+        constexpr int AT_ONCE = 4;  // chunks whose loads are in flight
+        for (int c0 = 0; c0 < S; c0 += AT_ONCE) {
+            uint64_t w[AT_ONCE][PER];
+            uint32_t n[AT_ONCE][PER];
+            int off[AT_ONCE];
+            double part_c[AT_ONCE];
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const int b = tid + j * SM_BLOCK;
-                w[j] = b >= off ? get(mass + (int64_t)c * BINS + b - off) : 0;
-                if (r.k) n[j] = get(counts + (int64_t)c * BINS + b);
-            }
-#pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const int b = tid + j * SM_BLOCK;
-                sum[j] += (double)w[j] * 0x1p-48 * part_c;
-                if (r.k) tail |= n[j] != 0 && b + off >= BINS - 1;
-            }
-            if (r.k) {
+            for (int k = 0; k < AT_ONCE; ++k) {
+                const int c = c0 + k < S ? c0 + k : S - 1;
+                off[k] = __builtin_amdgcn_readlane(down, c);
+                part_c[k] = c0 + k < S ? lane_value(part, c) : 0.0;
 #pragma unroll
                 for (int j = 0; j < PER; ++j) {
-                    const int b = tid + j * SM_BLOCK;
-                    num[j] += b >= off ? get(counts + (int64_t)c * BINS + b - off) : 0;
+                    const int b = tid + j * SM_BLOCK - off[k];
+                    const bool in = b >= 0 && part_c[k] > 0.0;
+                    w[k][j] = in ? get(mass + (int64_t)c * BINS + b) : 0;
+                    n[k][j] = in && r.k ? get(counts + (int64_t)c * BINS + b) : 0;
                 }
+            }
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    sum[j] += (double)w[k][j] * 0x1p-48 * part_c[k];
+                    num[j] += n[k][j];
+                }
+                // what a shift moves out of the window
+                if (r.k && part_c[k] > 0.0)
+                    for (int b = BINS - 1 - off[k] + tid; b < BINS; b += SM_BLOCK)
+                        tail |= b >= 0 && get(counts + (int64_t)(c0 + k) * BINS + b) != 0;
             }
         }
 #pragma unroll
@@ -256,14 +268,20 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const bool whole = i0[j] >= 0 && i0[j] + E <= a.V;
+                        float v[E];
+                        bool any = false;
 #pragma unroll
                         for (int e = 0; e < E; ++e) {
                             const int64_t i = i0[j] + e;
-                            const float v = whole ? elem(q[j], e, (T*)nullptr)
-                                            : i >= 0 && i < a.V ? load1(x + i)
-                                                                : -__builtin_inff();
-                            append(sm, g, an, v, (uint32_t)i);
+                            v[e] = whole                ? elem(q[j], e, (T*)nullptr)
+                                   : i >= 0 && i < a.V ? load1(x + i)
+                                                       : -__builtin_inff();
+                            any |= near(g, v[e]);
                         }
+                        if (__ballot(any) == 0) continue;
+#pragma unroll
+                        for (int e = 0; e < E; ++e)
+                            append(sm, g, an, v[e], (uint32_t)(i0[j] + e));
                     }
                 }
             });
@@ -280,14 +298,14 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
             const float v = sm.lx[j];
             const uint32_t i = sm.li[j];
             const double w = an.weight(v);
-            if (an.bin<SM_W>(v) >= f.sure && cut.keeps(v, i) && w >= r.q)
+            if (an.bin<SM_W>(an.t(v)) >= f.sure && cut.keeps(v, i) && w >= r.q)
                 add_bin(sm.chunk[i / (uint32_t)s.chunk], fixed48(w));
         }
         __syncthreads();
         kept = (double)sm.chunk[lane] * 0x1p-48;
         for (int c = wv; c < S; c += SM_W) {
             const int off = __builtin_amdgcn_readlane(down, c);
-            const double part_c = __shfl(part, c);
+            const double part_c = lane_value(part, c);
             uint64_t units = 0;
             if (part_c > 0.0)
                 for (int b = lane; b + off < f.sure; b += 64)
@@ -300,10 +318,10 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
     }
     // the chunk that the token is in (every wavefront: the same numbers)
     const double incl = wave_scan(kept);
-    const double total = __shfl(incl, 63), target = r.u * total;
+    const double total = lane_value(incl, 63), target = r.u * total;
     const uint64_t some = __ballot(kept > 0.0), past = __ballot(kept > 0.0 && incl > target);
     const int c = past ? __builtin_ctzll(past) : some ? 63 - __builtin_clzll(some) : 0;
-    const double rem = past ? target - (c ? __shfl(incl, c - 1) : 0.0) : __builtin_inf();
+    const double rem = past ? target - (c ? lane_value(incl, c - 1) : 0.0) : __builtin_inf();
     const int64_t i0 = (int64_t)c * s.chunk;
     Held<T, SM_W, R> h;
     h.load(x + i0, (int32_t)(a.V - i0 < s.chunk ? a.V - i0 : s.chunk));
@@ -321,19 +339,27 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
     }
 }
 
-// Workgroup: chunk blockIdx % S of row row0 + blockIdx / S.
+// A chunk of a row a workgroup.  Workgroups go to the eight dies in turn, and the one
+// that ends a row is as a rule the last of its chunks to start: with a row's chunks
+// side by side, every row would end on the same one or two dies (512 x 128256
+// bfloat16, four chunks a row: 376 us, of which 300 with a fifth of the chip busy).
+// So a row's chunks are eight apart, all on one die, whose L2 then also has their
+// sums; fewer than eight rows spread theirs over all dies.
 template <typename T, int R>
 __global__ __launch_bounds__(SM_BLOCK) void sample_split(const SampleRows a, const SampleSplit s) {
     constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
     __shared__ SampleSmem<SM_W> sm;
     const int tid = threadIdx.x;
-    const int rel = (int)(blockIdx.x / (unsigned)s.S), c = (int)(blockIdx.x % (unsigned)s.S);
+    const unsigned S = (unsigned)s.S, b = blockIdx.x, dies = s.rows < 8 ? 1 : 8;
+    const int64_t rel = (int64_t)(b / (dies * S) * dies + b % dies);
+    const int c = (int)(b / dies % S);
+    if (rel >= s.rows) return;
     const int64_t row = s.row0 + rel;
     const T* x = static_cast<const T*>(a.x) + row * a.ld;
     const Rule r = row_rule(a, row);
-    uint64_t* parts = s.parts + (int64_t)rel * s.S * 2;
-    uint64_t* mass = s.mass + (int64_t)rel * s.S * BINS;
-    uint32_t* counts = s.counts + (int64_t)rel * s.S * BINS;
+    uint64_t* parts = s.parts + rel * s.S * 2;
+    uint64_t* mass = s.mass + rel * s.S * BINS;
+    uint32_t* counts = s.counts + rel * s.S * BINS;
     {
         const int64_t i0 = (int64_t)c * s.chunk;
         Held<T, SM_W, R> h;
@@ -466,7 +492,8 @@ static hipError_t launch_sample_t(const SampleRows& a, const SamplePlan& p, void
     s.ctr = ctr;
     for (s.row0 = 0; s.row0 < a.N; s.row0 += p.rows) {
         const int64_t n = a.N - s.row0 < p.rows ? a.N - s.row0 : p.rows;
-        const dim3 grid((unsigned)(n * p.S)), block(SM_BLOCK);
+        s.rows = n;
+        const dim3 grid((unsigned)((n < 8 ? n : (n + 7) / 8 * 8) * p.S)), block(SM_BLOCK);
         if (p.R == 2) hipLaunchKernelGGL((sample_split<T, 2>), grid, block, 0, st, a, s);
         else if (p.R == 4) hipLaunchKernelGGL((sample_split<T, 4>), grid, block, 0, st, a, s);
         else hipLaunchKernelGGL((sample_split<T, 8>), grid, block, 0, st, a, s);

@@ -11,26 +11,28 @@ namespace osm {
 
 constexpr double kLog2eD = 1.4426950408889634074;
 
-// 2^t for t <= 1023, to 3e-16: n + f = t with |f| <= 1/2, 2^f = 1 + f g(f) with g
-// the polynomial through (2^f - 1) / f at the eleven Chebyshev nodes of
-// [-1/2, 1/2] (truncation 2e-17), so that 2^0 is 1 exactly.  Below 2^-1074, at
+// 2^t for t <= 1023, to 7e-16: n + f = t with |f| <= 1/2, 2^f = 1 + f g(f) with g
+// the polynomial through (2^f - 1) / f at the ten Chebyshev nodes of [-1/2, 1/2]
+// (truncation 6e-16), so that 2^0 is 1 exactly.  Below 2^-1074, at
 // -inf and at NaN: 0.
-__device__ __forceinline__ double exp2_wide(double t) {
-    t = __builtin_fmax(t, -1100.0);
+__device__ __forceinline__ double exp2_bounded(double t) {  // -2^30 < t
     const double n = __builtin_rint(t);
     const double f = t - n;
-    double g = 0x1.e9d3fe3952179p-32;
-    g = __builtin_fma(g, f, 0x1.e6063f7217bc6p-28);
-    g = __builtin_fma(g, f, 0x1.b524fae627834p-24);
-    g = __builtin_fma(g, f, 0x1.62bfd47773353p-20);
-    g = __builtin_fma(g, f, 0x1.ffcbfc670dcd4p-17);
-    g = __builtin_fma(g, f, 0x1.430913096fd9fp-13);
-    g = __builtin_fma(g, f, 0x1.5d87fe78a5276p-10);
-    g = __builtin_fma(g, f, 0x1.3b2ab6fba1ddap-7);
-    g = __builtin_fma(g, f, 0x1.c6b08d704a0c2p-5);
-    g = __builtin_fma(g, f, 0x1.ebfbdff82c598p-3);
-    g = __builtin_fma(g, f, 0x1.62e42fefa39efp-1);
+    double g = 0x1.e5e9f548e5725p-28;
+    g = __builtin_fma(g, f, 0x1.b6571de2f2351p-24);
+    g = __builtin_fma(g, f, 0x1.62bfe46117445p-20);
+    g = __builtin_fma(g, f, 0x1.ffcb76789860fp-17);
+    g = __builtin_fma(g, f, 0x1.4309130378460p-13);
+    g = __builtin_fma(g, f, 0x1.5d87fe908f88ap-10);
+    g = __builtin_fma(g, f, 0x1.3b2ab6fba385fp-7);
+    g = __builtin_fma(g, f, 0x1.c6b08d7044119p-5);
+    g = __builtin_fma(g, f, 0x1.ebfbdff82c590p-3);
+    g = __builtin_fma(g, f, 0x1.62e42fefa39f7p-1);
     return __builtin_ldexp(__builtin_fma(g, f, 1.0), (int)n);
+}
+
+__device__ __forceinline__ double exp2_wide(double t) {
+    return exp2_bounded(__builtin_fmax(t, -1100.0));
 }
 
 // Butterfly operands (md.hpp) of a 64-bit value.
@@ -79,16 +81,49 @@ __device__ __forceinline__ uint32_t group_max(uint32_t v) {
     }
 }
 
-// Inclusive prefix sum over the wavefront's lanes.
+// Inclusive prefix sum over the wavefront's lanes, in cross-lane VALU moves: within rows
+// of 16 lanes by shifts of 1, 2, 4 and 8, then the last lane of row 0 (2) is added
+// to row 1 (3), and that of the lower half to the upper one.  Lanes a move does not
+// reach add 0.  All lanes must be active.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp_or_zero(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp_or_zero(uint64_t v) {
+    return (uint64_t)dpp_or_zero<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 |
+           dpp_or_zero<CTRL, ROWS>((uint32_t)v);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_or_zero(double v) {
+    return __builtin_bit_cast(double, dpp_or_zero<CTRL, ROWS>(__builtin_bit_cast(uint64_t, v)));
+}
 template <typename V>
 __device__ __forceinline__ V wave_scan(V v) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const V o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
+    v += dpp_or_zero<0x111, 0xF>(v);  // row_shr:1
+    v += dpp_or_zero<0x112, 0xF>(v);
+    v += dpp_or_zero<0x114, 0xF>(v);
+    v += dpp_or_zero<0x118, 0xF>(v);
+    v += dpp_or_zero<0x142, 0xA>(v);  // row_bcast:15 into rows 1 and 3
+    v += dpp_or_zero<0x143, 0xC>(v);  // row_bcast:31 into rows 2 and 3
     return v;
+}
+// The value of the lane before (0 in lane 0), and of one lane.
+template <typename V>
+__device__ __forceinline__ V lane_before(V v) {
+    return dpp_or_zero<0x138, 0xF>(v);  // wave_shr:1
+}
+__device__ __forceinline__ uint32_t lane_value(uint32_t v, int lane) {
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+__device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
+    return (uint64_t)lane_value((uint32_t)(v >> 32), lane) << 32 | lane_value((uint32_t)v, lane);
+}
+__device__ __forceinline__ double lane_value(double v, int lane) {
+    return __builtin_bit_cast(double, lane_value(__builtin_bit_cast(uint64_t, v), lane));
+}
+__device__ __forceinline__ float lane_value(float v, int lane) {
+    return __uint_as_float(lane_value(__float_as_uint(v), lane));
 }
 
 // Order of values as unsigned integers; -0.0 ranks as +0.0.
