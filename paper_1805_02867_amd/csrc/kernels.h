@@ -124,7 +124,8 @@ struct SamplePlan {
 };
 struct SampleSplit {
     int S;
-    int64_t chunk, row0, rows;  // the launch's rows
+    int64_t chunk, row0, rows;  // the launch's rows, their chunks
+    int group;                  // interleaved in groups of so many
     uint64_t* parts;
     uint64_t* mass;
     uint32_t* counts;

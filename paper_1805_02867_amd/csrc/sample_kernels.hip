@@ -339,20 +339,21 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
     }
 }
 
-// A chunk of a row a workgroup.  Workgroups go to the eight dies in turn, and the one
-// that ends a row is as a rule the last of its chunks to start: with a row's chunks
-// side by side, every row would end on the same one or two dies (512 x 128256
-// bfloat16, four chunks a row: 376 us, of which 300 with a fifth of the chip busy).
-// So a row's chunks are eight apart, all on one die, whose L2 then also has their
-// sums; fewer than eight rows spread theirs over all dies.
+// A chunk of a row a workgroup.  Workgroups go to the eight dies in turn, and there to
+// groups of CUs in turn, each waiting for room where its turn is; and the one that
+// ends a row is as a rule the last of its chunks to start.  With a row's chunks side by
+// side every row ends at the same few places, for which the next ones then wait (512 x
+// 128256 bfloat16, four chunks a row: a fifth of the chip busy).  So the chunks of 32
+// rows are interleaved: rows end at 32 places in turn, and a row's chunks are on one
+// die, whose L2 has their sums.  Fewer than eight rows spread theirs over all dies.
 template <typename T, int R>
 __global__ __launch_bounds__(SM_BLOCK) void sample_split(const SampleRows a, const SampleSplit s) {
     constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
     __shared__ SampleSmem<SM_W> sm;
     const int tid = threadIdx.x;
-    const unsigned S = (unsigned)s.S, b = blockIdx.x, dies = s.rows < 8 ? 1 : 8;
-    const int64_t rel = (int64_t)(b / (dies * S) * dies + b % dies);
-    const int c = (int)(b / dies % S);
+    const unsigned S = (unsigned)s.S, b = blockIdx.x, group = (unsigned)s.group;
+    const int64_t rel = (int64_t)(b / (group * S) * group + b % group);
+    const int c = (int)(b / group % S);
     if (rel >= s.rows) return;
     const int64_t row = s.row0 + rel;
     const T* x = static_cast<const T*>(a.x) + row * a.ld;
@@ -493,7 +494,8 @@ static hipError_t launch_sample_t(const SampleRows& a, const SamplePlan& p, void
     for (s.row0 = 0; s.row0 < a.N; s.row0 += p.rows) {
         const int64_t n = a.N - s.row0 < p.rows ? a.N - s.row0 : p.rows;
         s.rows = n;
-        const dim3 grid((unsigned)((n < 8 ? n : (n + 7) / 8 * 8) * p.S)), block(SM_BLOCK);
+        s.group = n < 8 ? 1 : n < 32 ? 8 : 32;
+        const dim3 grid((unsigned)((n + s.group - 1) / s.group * s.group * p.S)), block(SM_BLOCK);
         if (p.R == 2) hipLaunchKernelGGL((sample_split<T, 2>), grid, block, 0, st, a, s);
         else if (p.R == 4) hipLaunchKernelGGL((sample_split<T, 4>), grid, block, 0, st, a, s);
         else hipLaunchKernelGGL((sample_split<T, 8>), grid, block, 0, st, a, s);
