@@ -336,9 +336,10 @@ enum osm_score { OSM_SCORE_SOFTMAX = 0, OSM_SCORE_SIGMOID = 1 };
 /* How route_fwd picks and weighs experts.
  *  score     : s = softmax(x) over the row, or s = 1 / (1 + e^-x).
  *  groups    : the E experts form this many groups of E / groups neighbours
- *              (1: no groups).  The best top_groups of them are searched, a
- *              group's score being the sum of its group_top (1 or 2) largest
- *              s + bias; of equal groups the lower index is taken.
+ *              (1: no groups).  The best top_groups of them are searched: by
+ *              their largest c (see route_fwd; group_top 1), or by the sum of
+ *              their two largest s + bias (group_top 2; of one, if no other can
+ *              be chosen).  Of equal groups the lower index is taken.
  *  renorm    : nonzero: weights are divided by their sum.
  *  scale     : factor of the weights. */
 typedef struct osm_route {

@@ -2,15 +2,21 @@
 //
 // Forward, a row of E logits x: scores s = softmax(x) or 1 / (1 + e^-x); experts
 // are ranked by c = s + bias, or by x itself without a bias (both scores
-// increase with x); with groups, each group of E / G experts is ranked by the
-// sum of its group_top best, and only the best top_groups are searched; the K
-// largest c, ties to the lower index, give the experts, and their s the weights
-// (renormalised to sum 1 if asked, times scale).  Renormalised weights are
-// taken from the chosen logits alone, relative to the largest, so they do not
-// underflow together.
+// increase with x); with groups, each group of E / G experts is ranked by its best
+// c, or the sum of its two best (of s without a bias), and only the best top_groups
+// are searched; the K largest c, ties to the lower index, give the experts, and
+// their s the weights (renormalised to sum 1 if asked, times scale).  Renormalised
+// weights are taken from the chosen logits alone, relative to the largest, so they do
+// not underflow together.
 //
-// Scores are binary64: a bias brings experts close together, and a choice must
-// not depend on the order of a sum.
+// The choice is that of binary64 scores: a bias brings experts close together, and a
+// choice must not depend on the order of a sum.  It is made on binary32 c first; where two of the K + 1 best, or two groups on the two
+// sides of the line, are closer than their errors, the row is done again in
+// binary64 (3 of 1000 rows of 256 sigmoid scores, 8 taken).  Where x itself ranks the
+// experts the first choice is exact.
+//
+// A row is taken by LANES lanes, R experts a lane, and the K are drawn one by one: each
+// lane has its best at hand, and only the one that is drawn looks for its next.
 //
 // Backward, with g the gradient of the K weights and p = weights / scale:
 //   softmax, renormalised:  dx_i = scale p_i (g_i - sum_j g_j p_j) at the chosen
@@ -25,242 +31,539 @@ namespace osm {
 
 constexpr int RT_BLOCK = 256;
 constexpr int RT_WAVES = RT_BLOCK / 64;
-constexpr int RT_EMAX = 1024;
-constexpr int RT_GMAX = 64;
 
-__device__ __forceinline__ double sigmoid_wide(double x) {
-    const double e = exp2_wide(-__builtin_fabs(x) * kLog2eD);
-    return (x >= 0.0 ? 1.0 : e) / (1.0 + e);
+// 1 / d for 1 <= d <= 2: the hardware's estimate and two Newton steps (each squares
+// the error 2^-26 or less).
+__device__ __forceinline__ double reciprocal(double d) {
+    double r = __builtin_amdgcn_rcp(d);
+    r = __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
+    return __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
 }
 
-// Experts that cannot be chosen rank here, below every score (even -1e308).
-constexpr uint64_t kNoRank = 0;
+// e^-|x|
+__device__ __forceinline__ double exp_minus_abs(double x) {
+    return exp2_wide(-__builtin_fabs(x) * kLog2eD);
+}
 
-// A wavefront per row; lane l holds experts l, l + 64, ...
-template <typename T, int R>
-__global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
-    __shared__ uint64_t ranks[RT_WAVES][RT_EMAX];
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int E = a.E, K = a.K;
-    const double inf = __builtin_inf();
-    uint64_t* const rk = ranks[wv];
-    for (int64_t row = (int64_t)blockIdx.x * RT_WAVES + wv; row < a.N;
-         row += (int64_t)gridDim.x * RT_WAVES) {
-        const T* xr = static_cast<const T*>(a.x) + row * E;
-        float x[R];
-        float mx = -__builtin_inff();
-        bool bad = false;
+__device__ __forceinline__ double sigmoid_wide(double x) {
+    const double e = exp_minus_abs(x), r = reciprocal(1.0 + e);
+    return x >= 0.0 ? r : e * r;
+}
+
+// Largest distance of a binary32 c = s + bias from the exact one, |bias| <= bmax.  s is at
+// most 1: the hardware's 2^t and reciprocal are off by 2^-23 of their value each, the
+// rounding of t adds |t| s 2^-23 < 2^-23 (a sigmoid a quarter of both: in all under
+// 2^-21); the sum of a softmax adds as much as its terms and 2^-24 for each of at most
+// 22 additions (under 2^-19).  The sum with the bias rounds c.
+__device__ __forceinline__ float score_error(bool sigmoid, float bmax) {
+    return (sigmoid ? 0x1p-20f : 0x1p-18f) + 0x1p-23f * (1.0f + bmax);
+}
+
+// The row team of a lane: LANES lanes, `lane` within it.  Lane l's j-th expert is
+// (j / VEC * LANES + l) * VEC + j % VEC: VEC neighbours are loaded together.
+template <int LANES, int VEC>
+__device__ __forceinline__ int expert(int lane, int j) {
+    return (j / VEC * LANES + lane) * VEC + j % VEC;
+}
+
+template <typename T, int LANES, int R, int VEC>
+__device__ __forceinline__ void load_experts(const T* xr, int E, bool live, int lane,
+                                             float (&x)[R]) {
+    if constexpr (VEC == 1) {
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const int e = j * 64 + lane;
-            x[j] = e < E ? load1(xr + e) : -__builtin_inff();
-            bad |= !(x[j] < __builtin_inff());
-            mx = fmaxf(mx, x[j]);
+            const int e = j * LANES + lane;
+            x[j] = live && e < E ? load1(xr + e) : -__builtin_inff();
         }
-        mx = group_max<64>(mx);
-        bad = __any(bad);
-        if (bad || mx == -__builtin_inff()) {
-            if (lane < K) {
-                a.idx[row * K + lane] = -1;
-                a.vals[row * K + lane] = bad ? __builtin_nanf("") : 0.0f;
+    } else {
+#pragma unroll
+        for (int j = 0; j < R; j += 4) {
+            const int e = expert<LANES, VEC>(lane, j);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) x[j + v] = -__builtin_inff();
+            if (!live || e >= E) continue;
+            if constexpr (sizeof(T) == 4) {
+                const f32x4 q = *reinterpret_cast<const f32x4*>(xr + e);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) x[j + v] = q[v];
+            } else {
+                const uint2 q = *reinterpret_cast<const uint2*>(xr + e);
+                x[j] = bf16_lo(q.x);
+                x[j + 1] = bf16_hi(q.x);
+                x[j + 2] = bf16_lo(q.y);
+                x[j + 3] = bf16_hi(q.y);
             }
-            continue;
-        }
-        // scores
-        double s[R], sum = 0.0;
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            s[j] = a.sigmoid ? sigmoid_wide((double)x[j])
-                             : exp2_wide(((double)x[j] - (double)mx) * kLog2eD);
-            sum += s[j];
-        }
-        if (!a.sigmoid) {
-            sum = group_sum<64>(sum);
-#pragma unroll
-            for (int j = 0; j < R; ++j) s[j] /= sum;
-        }
-        // ranks
-        uint64_t r[R];
-        double b[R];
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int e = j * 64 + lane;
-            b[j] = a.bias && e < E ? (double)a.bias[e] : 0.0;
-            const bool may = x[j] > -__builtin_inff() && b[j] > -inf;  // (NaN bias: no)
-            r[j] = !may ? kNoRank : order_key(a.bias ? s[j] + b[j] : (double)x[j]);
-        }
-        if (a.groups > 1) {
-            // the score of group `lane`, from its best one or two experts
-            const int gs = E / a.groups;
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                const int e = j * 64 + lane;
-                if (e < E) rk[e] = r[j] == kNoRank ? kNoRank : order_key(s[j] + b[j]);
-            }
-            wave_sync();
-            uint64_t best = 0, second = 0;
-            if (lane < a.groups) {
-                for (int i = 0; i < gs; ++i) {
-                    const uint64_t k = rk[lane * gs + i];
-                    second = k > best ? best : k > second ? k : second;
-                    best = k > best ? k : best;
-                }
-            }
-            uint64_t g = best;
-            if (a.group_top == 2 && second != kNoRank)
-                g = order_key(order_value64(best) + order_value64(second));
-            int ahead = 0;
-            for (int o = 0; o < a.groups; ++o) {
-                const uint64_t k = __shfl(g, o);
-                ahead += k > g || (k == g && o < lane);
-            }
-            const uint64_t keep = __ballot(lane < a.groups && ahead < a.top_groups);
-            wave_sync();
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                const int e = j * 64 + lane;
-                if (e >= E || !(keep >> (e / gs) & 1)) r[j] = kNoRank;
-            }
-        }
-        // K times the largest rank, ties to the lower index
-        int mine = -1;
-        float mx_in = 0.0f;
-        for (int i = 0; i < K; ++i) {
-            uint64_t best = 0;
-            int at = 0;
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                at = r[j] > best ? j : at;
-                best = r[j] > best ? r[j] : best;
-            }
-            const uint64_t top = group_max<64>(best);
-            if (top == kNoRank) break;
-            // the lowest index of that rank
-            uint32_t e = best == top ? (uint32_t)(at * 64 + lane) : ~0u;
-            e = ~group_max<64>(~e);
-#pragma unroll
-            for (int j = 0; j < R; ++j)
-                if (e == (uint32_t)(j * 64 + lane)) r[j] = kNoRank;
-            mine = lane == i ? (int)e : mine;
-        }
-        // weights: lane i has the i-th expert
-        double w = 0.0;
-        if (mine >= 0) {
-            mx_in = load1(xr + mine);
-            w = a.sigmoid ? sigmoid_wide((double)mx_in)
-                          : exp2_wide(((double)mx_in - (double)mx) * kLog2eD) / sum;
-        }
-        if (a.renorm) {
-            // relative to the largest chosen one: e^x, or e^min(x, 0) / (1 + e^-|x|)
-            const double z = mine < 0   ? -inf
-                             : a.sigmoid ? __builtin_fmin((double)mx_in, 0.0)
-                                         : (double)mx_in;
-            const double zm = (double)group_max<64>((float)z);
-            w = exp2_wide((z - zm) * kLog2eD);
-            if (a.sigmoid) w /= 1.0 + exp2_wide(-__builtin_fabs((double)mx_in) * kLog2eD);
-            w = mine < 0 ? 0.0 : w;
-            const double all = group_sum<64>(w);
-            w = all > 0.0 ? w / all : 0.0;
-        }
-        if (lane < K) {
-            a.idx[row * K + lane] = mine;
-            a.vals[row * K + lane] = (float)(w * (double)a.scale);
         }
     }
 }
 
-template <typename T, int R>
-__global__ __launch_bounds__(RT_BLOCK) void route_bwd_rows(const RouteRows a) {
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int E = a.E, K = a.K;
-    const double inf = __builtin_inf();
-    for (int64_t row = (int64_t)blockIdx.x * RT_WAVES + wv; row < a.N;
-         row += (int64_t)gridDim.x * RT_WAVES) {
-        const T* xr = static_cast<const T*>(a.x) + row * E;
-        T* dr = static_cast<T*>(a.dx) + row * E;
-        const int e0 = lane < K ? a.idx[row * K + lane] : -1;
-        const bool in = e0 >= 0 && e0 < E;
-        const double g = in ? (double)a.dvals[row * K + lane] * (double)a.scale : 0.0;
-        const double xc = in ? (double)load1(xr + e0) : -inf;
-        double d[R];
+template <int LANES>
+__device__ __forceinline__ float team_maximum(float v) {  // (NaN where there is one)
+    float a, b;
+#define OSM_STEP(S)                                              \
+    if constexpr (LANES > (1 << S)) {                            \
+        bfly_operands<S>(v, a, b);                               \
+        v = __builtin_elementwise_maximum(a, b);                 \
+    }
+    OSM_STEP(0) OSM_STEP(1) OSM_STEP(2) OSM_STEP(3) OSM_STEP(4) OSM_STEP(5)
+#undef OSM_STEP
+    return v;
+}
+
+// The largest of a lane's c, the first of equal ones.
+template <int R>
+__device__ __forceinline__ void lane_best(const float (&c)[R], float& best, int& at) {
+    best = c[0];
+    at = 0;
 #pragma unroll
-        for (int j = 0; j < R; ++j) d[j] = 0.0;
-        // the gradient of the chosen logits, by place
-        double own = 0.0, dot = 0.0, mx = 0.0, rsum = 0.0;
-        const bool dense = !a.sigmoid && !a.renorm && __any(in);
-        float x[R];
-        if (dense) {
-            float m = -__builtin_inff();
+    for (int j = 1; j < R; ++j) {
+        const bool more = c[j] > best;
+        best = more ? c[j] : best;
+        at = more ? j : at;
+    }
+}
+
+template <int LANES>
+__device__ __forceinline__ float team_min(float v) {
+    return -group_max<LANES>(-v);
+}
+
+// A row's experts in binary64, by the whole wavefront: the K best one after the other,
+// each the first in the order (c, index) behind the one before.  rk: E ranks, the
+// order of c (0 for an expert that cannot be chosen).
+template <typename T>
+__device__ __forceinline__ void exact_row(const RouteRows& a, const T* xr, float mx, uint64_t* rk,
+                                          int* ch) {
+    const int lane = threadIdx.x & 63;
+    const int E = a.E, G = a.groups;
+    double sum = 0.0;
+    for (int e = lane; e < E; e += 64) {
+        const double x = (double)load1(xr + e);
+        const double s = a.sigmoid ? sigmoid_wide(x) : exp2_wide((x - (double)mx) * kLog2eD);
+        rk[e] = __builtin_bit_cast(uint64_t, s);
+        sum += s;
+    }
+    const double rsum = a.sigmoid ? 1.0 : 1.0 / group_sum<64>(sum);
+    for (int e = lane; e < E; e += 64) {
+        const float b = a.bias ? a.bias[e] : 0.0f;
+        const bool may = load1(xr + e) > -__builtin_inff() && b > -__builtin_inff();
+        const double s = __builtin_bit_cast(double, rk[e]) * rsum;
+        rk[e] = may ? order_key(s + (double)b) : 0;
+    }
+    wave_sync();
+    if (G > 1) {
+        const int gs = E / G;
+        int per = 64;
+        while (per * G > 64) per >>= 1;
+        const int g = lane / per;
+        uint64_t best = 0, second = 0;
+        if (g < G) {
+            for (int i = lane % per; i < gs; i += per) {
+                const uint64_t k = rk[g * gs + i];
+                second = k > best ? best : k > second ? k : second;
+                best = k > best ? k : best;
+            }
+        }
+        for (int d = 1; d < per; d *= 2) {
+            const uint64_t k = __shfl_xor(best, d), k2 = __shfl_xor(second, d);
+            const uint64_t lo = k > best ? best : k, hi2 = k2 > second ? k2 : second;
+            best = k > best ? k : best;
+            second = lo > hi2 ? lo : hi2;
+        }
+        if (a.group_top == 2 && second != 0)
+            best = order_key(order_value64(best) + order_value64(second));
+        int ahead = 0;
+        for (int o = 0; o < G; ++o) {
+            const uint64_t k = lane_value(best, o * per);
+            ahead += k > best || (k == best && o < g);
+        }
+        if (g < G && ahead >= a.top_groups)
+            for (int i = lane % per; i < gs; i += per) rk[g * gs + i] = 0;
+        wave_sync();
+    }
+    if (!a.bias) {  // the experts of the kept groups by x again
+        for (int e = lane; e < E; e += 64)
+            rk[e] = rk[e] != 0 ? (uint64_t)order_key(load1(xr + e)) << 32 : 0;
+        wave_sync();
+    }
+    for (int i = 0; i < a.K; ++i) {
+        uint64_t best = 0;
+        int at = 0;
+        for (int e = lane; e < E; e += 64) {
+            const uint64_t k = rk[e];
+            at = k > best ? e : at;
+            best = k > best ? k : best;
+        }
+        const uint64_t top = group_max<64>(best);
+        const uint32_t e = ~group_max<64>(best == top ? ~(uint32_t)at : 0u);
+        if (lane == 0) {
+            ch[i] = top != 0 ? (int)e : -1;
+            rk[e] = 0;
+        }
+        wave_sync();
+    }
+}
+
+template <typename T, int LANES, int R, int VEC>
+__global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
+    constexpr int ROWS = 64 / LANES;  // of a wavefront
+    const float ninf = -__builtin_inff();
+    __shared__ uint64_t ranks[RT_WAVES][64 * R];
+    __shared__ float best_of[RT_WAVES][64];
+    __shared__ int chosen[RT_WAVES][64 + ROWS];  // K + 1 a row
+    const int lane = threadIdx.x % LANES, wv = threadIdx.x >> 6, team = (threadIdx.x & 63) / LANES;
+    const int E = a.E, K = a.K, G = a.groups;
+    float* const hc = reinterpret_cast<float*>(ranks[wv]) + team * LANES * R;
+    float* const go = best_of[wv] + team * LANES;
+    int* const ch = chosen[wv] + team * (LANES + 1);
+    const bool sums = G > 1 && a.group_top == 2;
+    const bool scores = a.bias || sums;        // c, or a group's, is not x itself
+    const bool total = !a.sigmoid && (scores || !a.renorm);
+    const int draws = a.bias && K < E ? K + 1 : K;
+    // what does not depend on the row: the bias, and the groups
+    float b[R], bmax = 0.0f;
+    int ge[R];
+    const int gs = E / G;
+    int per = LANES;  // lanes that look at a group
+    while (per * G > LANES) per >>= 1;
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+        const int e = expert<LANES, VEC>(lane, j);
+        b[j] = a.bias && e < E ? a.bias[e] : 0.0f;
+        ge[j] = G > 1 ? (e < E ? e : 0) / gs * per + team * LANES : 0;
+        const float m = __builtin_fabsf(b[j]);
+        bmax = m < __builtin_inff() ? fmaxf(bmax, m) : bmax;
+    }
+    const float error = score_error(a.sigmoid, group_max<LANES>(bmax));
+    for (int64_t row0 = ((int64_t)blockIdx.x * RT_WAVES + wv) * ROWS; row0 < a.N;
+         row0 += (int64_t)gridDim.x * RT_WAVES * ROWS) {
+        const int64_t row = row0 + team;
+        const bool live = row < a.N;
+        const T* xr = static_cast<const T*>(a.x) + (live ? row : 0) * E;
+        float x[R], c[R];
+        load_experts<T, LANES, R, VEC>(xr, E, live, lane, x);
+        float mx = x[0];
+#pragma unroll
+        for (int j = 1; j < R; ++j) mx = __builtin_elementwise_maximum(mx, x[j]);
+        mx = team_maximum<LANES>(mx);
+        const bool bad = !(mx < __builtin_inff());
+        const bool some = !bad && mx > ninf;
+        double rsum = 1.0;  // of the exact scores
+        if (total && !a.renorm) {
             double sum = 0.0;
 #pragma unroll
-            for (int j = 0; j < R; ++j) {
-                const int e = j * 64 + lane;
-                x[j] = e < E ? load1(xr + e) : -__builtin_inff();
-                m = fmaxf(m, x[j]);
+            for (int j = 0; j < R; ++j) sum += exp2_wide(((double)x[j] - (double)mx) * kLog2eD);
+            rsum = 1.0 / group_sum<LANES>(sum);
+        }
+        if (scores) {
+            float rs = (float)rsum;
+            if (a.sigmoid) {
+#pragma unroll
+                for (int j = 0; j < R; ++j)
+                    c[j] = __builtin_amdgcn_rcpf(1.0f + exp2_hw(-x[j] * kLog2e));
+            } else {
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < R; ++j) {
+                    c[j] = exp2_hw((x[j] - mx) * kLog2e);
+                    sum += c[j];
+                }
+                if (a.renorm) rs = 1.0f / group_sum<LANES>(sum);
             }
-            mx = (double)group_max<64>(m);
+#pragma unroll
+            for (int j = 0; j < R; ++j) c[j] = __builtin_fmaf(c[j], rs, b[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < R; ++j) c[j] = x[j];
+        }
+#pragma unroll
+        for (int j = 0; j < R; ++j)  // (a NaN bias: no)
+            c[j] = some && x[j] > ninf && b[j] > ninf ? c[j] : ninf;
+        bool close = false;  // a line that binary32 does not decide
+        if (G > 1) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) hc[expert<LANES, VEC>(lane, j)] = c[j];
+            wave_sync();
+            const int g = lane / per;
+            float best = ninf, second = ninf;
+            if (g < G) {
+                for (int i = lane % per; i < gs; i += per) {
+                    const float v = hc[g * gs + i];
+                    second = __builtin_amdgcn_fmed3f(v, best, second);
+                    best = fmaxf(best, v);
+                }
+            }
+            for (int d = 1; d < per; d *= 2) {
+                const float v = __shfl_xor(best, d), v2 = __shfl_xor(second, d);
+                second = fmaxf(fminf(best, v), fmaxf(second, v2));
+                best = fmaxf(best, v);
+            }
+            if (sums && second > ninf) best += second;
+            if (g < G && lane % per == 0) go[g] = best;
+            wave_sync();
+            int ahead = 0;
+            for (int o = 0; o < G; ++o) {
+                const float v = go[o];
+                ahead += v > best || (v == best && o < g);
+            }
+            const bool stays = g < G && ahead < a.top_groups;
+            const uint64_t keep = __ballot(stays);
+            if (scores) {
+                const float low = team_min<LANES>(stays ? best : __builtin_inff());
+                const float high = group_max<LANES>(g < G && !stays ? best : ninf);
+                close = high > ninf && low < __builtin_inff() &&
+                        !(low - high > 4.0f * error);
+            }
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+                if (!(keep >> ge[j] & 1)) c[j] = ninf;
+            if (sums && !a.bias) {  // the experts of the kept groups by x again
+#pragma unroll
+                for (int j = 0; j < R; ++j) c[j] = c[j] > ninf ? x[j] : ninf;
+            }
+        }
+        ch[lane] = -1;
+        if (lane == 0) ch[LANES] = -1;
+        wave_sync();
+        float best, before = 0.0f;
+        int at;
+        lane_best(c, best, at);
+        for (int i = 0; i < draws; ++i) {
+            const float top = group_max<LANES>(best);
+            if (a.bias) {  // closer than the errors of both, equal ones among them
+                close = close || (i > 0 && top > ninf &&
+                                  !(before - top > 2.0f * error));
+                before = top;
+            }
+            bool win = best == top && best > ninf;
+            const uint64_t who = __ballot(win);
+            if (who == 0) break;
+            const uint64_t mine = LANES == 64 ? who
+                                              : who >> (team * LANES) & ((1ull << (LANES & 63)) - 1);
+            const int e = expert<LANES, VEC>(lane, at);
+            if (__any((mine & (mine - 1)) != 0)) {
+                const uint32_t first = ~group_max<LANES>(win ? ~(uint32_t)e : 0u);
+                win = win && (uint32_t)e == first;
+            }
+            if (win) {
+                ch[i] = e;
+#pragma unroll
+                for (int j = 0; j < R; ++j)
+                    if (j == at) c[j] = ninf;
+                lane_best(c, best, at);
+            }
+        }
+        if (scores) {
+            uint64_t again = __ballot(close && some && live);
+            while (again) {  // (uniform: a row of the wavefront at a time)
+                const int t = __builtin_ctzll(again) / LANES;
+                again = LANES == 64 ? 0 : again & ~(((1ull << (LANES & 63)) - 1) << (t * LANES));
+                wave_sync();
+                exact_row(a, static_cast<const T*>(a.x) + (row0 + t) * E,
+                          lane_value(mx, t * LANES), ranks[wv], chosen[wv] + t * (LANES + 1));
+            }
+        }
+        wave_sync();
+        // weights: lane i has the i-th expert
+        const int pick = lane < K ? ch[lane] : -1;
+        wave_sync();
+        const double xp = pick >= 0 ? (double)load1(xr + pick) : -__builtin_inf();
+        double w = 0.0;
+        if (a.renorm) {
+            // relative to the largest chosen one: e^x, or e^min(x, 0) / (1 + e^-|x|)
+            const double z = a.sigmoid ? __builtin_fmin(xp, 0.0) : xp;
+            const double zm = (double)team_maximum<LANES>((float)z);
+            w = exp2_wide((z - zm) * kLog2eD);
+            if (a.sigmoid) w *= reciprocal(1.0 + exp_minus_abs(xp));
+            w = pick >= 0 ? w : 0.0;
+            const double all = group_sum<LANES>(w);
+            w = all > 0.0 ? w / all : 0.0;
+        } else if (pick >= 0) {
+            w = a.sigmoid ? sigmoid_wide(xp) : exp2_wide((xp - (double)mx) * kLog2eD) * rsum;
+        }
+        if (live && lane < K) {
+            a.idx[row * K + lane] = pick;
+            a.vals[row * K + lane] = bad ? __builtin_nanf("") : (float)(w * (double)a.scale);
+        }
+    }
+}
+
+// The gradient.  A row by LANES lanes, R experts a lane; lane i also has place i.
+template <typename T, int LANES, int R, int VEC>
+__global__ __launch_bounds__(RT_BLOCK) void route_bwd_rows(const RouteRows a) {
+    constexpr int ROWS = 64 / LANES;
+    __shared__ double owns[RT_WAVES][64];
+    __shared__ int places[RT_WAVES][64];
+    __shared__ __align__(16) int place_of[RT_WAVES][64 * R];
+    const int lane = threadIdx.x % LANES, wv = threadIdx.x >> 6, team = (threadIdx.x & 63) / LANES;
+    const int E = a.E, K = a.K;
+    double* const so = owns[wv] + team * LANES;
+    int* const sp = places[wv] + team * LANES;
+    int* const po = place_of[wv] + team * LANES * R;
+    const bool dense = !a.sigmoid && !a.renorm;
+    for (int64_t row0 = ((int64_t)blockIdx.x * RT_WAVES + wv) * ROWS; row0 < a.N;
+         row0 += (int64_t)gridDim.x * RT_WAVES * ROWS) {
+        const int64_t row = row0 + team;
+        const bool live = row < a.N;
+        const T* xr = static_cast<const T*>(a.x) + (live ? row : 0) * E;
+        float x[R];
+        if (dense) load_experts<T, LANES, R, VEC>(xr, E, live, lane, x);
+        const int e0 = live && lane < K ? a.idx[row * K + lane] : -1;
+        const bool in = e0 >= 0 && e0 < E;
+        const double g = in ? (double)a.dvals[row * K + lane] * (double)a.scale : 0.0;
+        const double xc = in ? (double)load1(xr + e0) : -__builtin_inf();
+        double d[R], own;
+        if (dense) {
+            float m = x[0];
+#pragma unroll
+            for (int j = 1; j < R; ++j) m = __builtin_elementwise_maximum(m, x[j]);
+            const double mx = (double)team_maximum<LANES>(m);
+            double sum = 0.0;
 #pragma unroll
             for (int j = 0; j < R; ++j) {
                 d[j] = exp2_wide(((double)x[j] - mx) * kLog2eD);
                 sum += d[j];
             }
-            rsum = 1.0 / group_sum<64>(sum);
-            own = exp2_wide((xc - mx) * kLog2eD) * rsum;
-            dot = group_sum<64>(in ? g * own : 0.0);
-            own = g * own;
+            const double rsum = 1.0 / group_sum<LANES>(sum);
+            own = g * (exp2_wide((xc - mx) * kLog2eD) * rsum);
+            // (a row without any place, whatever it holds, has no gradient)
+            const uint64_t who = __ballot(in);
+            const bool any = (LANES == 64 ? who : who >> (team * LANES) & ((1ull << (LANES & 63)) - 1)) != 0;
+            const double dot = group_sum<LANES>(in ? own : 0.0) * rsum;
 #pragma unroll
-            for (int j = 0; j < R; ++j) d[j] = -d[j] * rsum * dot;
-        } else if (a.renorm) {
-            const double z = !in ? -inf : a.sigmoid ? __builtin_fmin(xc, 0.0) : xc;
-            const double zm = (double)group_max<64>((float)z);
-            const double e = exp2_wide(-__builtin_fabs(xc) * kLog2eD);
-            double p = exp2_wide((z - zm) * kLog2eD);
-            if (a.sigmoid) p /= 1.0 + e;
-            p = in ? p : 0.0;
-            const double all = group_sum<64>(p);
-            p = all > 0.0 ? p / all : 0.0;
-            dot = group_sum<64>(p * g);
-            own = p * (g - dot);
-            if (a.sigmoid) own *= (xc >= 0.0 ? e : 1.0) / (1.0 + e);
-        } else if (a.sigmoid) {
-            const double e = exp2_wide(-__builtin_fabs(xc) * kLog2eD);
-            own = g * e / ((1.0 + e) * (1.0 + e));
+            for (int j = 0; j < R; ++j) d[j] = any ? -d[j] * dot : 0.0;
+        } else {
+#pragma unroll
+            for (int j = 0; j < R; ++j) d[j] = 0.0;
+            const double e = exp_minus_abs(xc), f = reciprocal(1.0 + e);
+            if (a.renorm) {
+                const double z = a.sigmoid ? __builtin_fmin(xc, 0.0) : xc;
+                const double zm = (double)team_maximum<LANES>(in ? (float)z : -__builtin_inff());
+                double p = exp2_wide((z - zm) * kLog2eD);
+                if (a.sigmoid) p *= f;
+                p = in ? p : 0.0;
+                const double all = group_sum<LANES>(p);
+                p = all > 0.0 ? p / all : 0.0;
+                own = p * (g - group_sum<LANES>(p * g));
+                if (a.sigmoid) own *= (xc >= 0.0 ? e : 1.0) * f;
+            } else {
+                own = g * e * f * f;
+            }
         }
-        // places to experts
-        for (int i = 0; i < K; ++i) {
-            const int e = __shfl(in ? e0 : -1, i);
-            const double v = __shfl(own, i);
+        // places to experts: each expert finds the place that it has, if any
+        so[lane] = own;
+        if constexpr (VEC == 1) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) po[expert<LANES, VEC>(lane, j)] = -1;
+        } else {
+#pragma unroll
+            for (int j = 0; j < R; j += 4)
+                *reinterpret_cast<int4*>(po + expert<LANES, VEC>(lane, j)) = int4{-1, -1, -1, -1};
+        }
+        wave_sync();
+        if (in) po[e0] = lane;
+        wave_sync();
+        if (__any(in && po[e0] != lane)) {  // an expert twice: all places, in their order
+            sp[lane] = in ? e0 : -1;
+            wave_sync();
+            for (int i = 0; i < K; ++i) {
+                const int e = sp[i];
+                const double v = so[i];
+#pragma unroll
+                for (int j = 0; j < R; ++j)
+                    if (e == expert<LANES, VEC>(lane, j)) d[j] += v;
+            }
+        } else {
+            int p[R];
+            if constexpr (VEC == 1) {
+#pragma unroll
+                for (int j = 0; j < R; ++j) p[j] = po[expert<LANES, VEC>(lane, j)];
+            } else {
+#pragma unroll
+                for (int j = 0; j < R; j += 4) {
+                    const int4 q = *reinterpret_cast<const int4*>(po + expert<LANES, VEC>(lane, j));
+                    p[j] = q.x, p[j + 1] = q.y, p[j + 2] = q.z, p[j + 3] = q.w;
+                }
+            }
 #pragma unroll
             for (int j = 0; j < R; ++j)
-                if (e == j * 64 + lane) d[j] += v;
+                if (p[j] >= 0) d[j] += so[p[j]];
         }
+        wave_sync();
+        if (!live) continue;
+        T* dr = static_cast<T*>(a.dx) + row * E;
+        if constexpr (VEC == 1) {
 #pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int e = j * 64 + lane;
-            if (e < E) store1(dr + e, (float)d[j]);
+            for (int j = 0; j < R; ++j)
+                if (j * LANES + lane < E) store1(dr + j * LANES + lane, (float)d[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < R; j += 4) {
+                const int e = expert<LANES, VEC>(lane, j);
+                if (e >= E) continue;
+                if constexpr (sizeof(T) == 4)
+                    *reinterpret_cast<f32x4*>(dr + e) =
+                        f32x4{(float)d[j], (float)d[j + 1], (float)d[j + 2], (float)d[j + 3]};
+                else
+                    *reinterpret_cast<uint2*>(dr + e) =
+                        uint2{pack_bf16x2((float)d[j], (float)d[j + 1]),
+                              pack_bf16x2((float)d[j + 2], (float)d[j + 3])};
+            }
         }
     }
 }
 
-template <typename T, bool BWD>
-hipError_t launch_route_t(const RouteRows& a, hipStream_t st) {
-    const int64_t want = (a.N + RT_WAVES - 1) / RT_WAVES;
+// Lanes of a row: enough for its K places and its groups, and for its experts at
+// `each` a lane or few more.
+static int route_lanes(const RouteRows& a, int each) {
+    int lanes = 8;
+    while (lanes < 64 && (lanes < a.K || lanes < a.groups || lanes * each < a.E)) lanes *= 2;
+    return lanes;
+}
+
+template <typename T, bool BWD, int LANES, int VEC>
+hipError_t launch_route_l(const RouteRows& a, hipStream_t st) {
+    const int64_t want = (a.N + RT_WAVES * (64 / LANES) - 1) / (RT_WAVES * (64 / LANES));
     const unsigned blocks = (unsigned)(want < (1 << 20) ? want : 1 << 20);
-    const int r = (a.E + 63) / 64;
-#define OSM_ROUTE(R)                                                                            \
-    do {                                                                                        \
-        if constexpr (BWD)                                                                      \
-            hipLaunchKernelGGL((route_bwd_rows<T, R>), dim3(blocks), dim3(RT_BLOCK), 0, st, a); \
-        else                                                                                    \
-            hipLaunchKernelGGL((route_rows<T, R>), dim3(blocks), dim3(RT_BLOCK), 0, st, a);     \
+    const int r = (a.E + LANES - 1) / LANES;
+#define OSM_ROUTE(R)                                                                           \
+    do {                                                                                       \
+        if constexpr (R % VEC == 0 && (LANES == 64 || R <= 8)) {                               \
+            if constexpr (BWD)                                                                 \
+                hipLaunchKernelGGL((route_bwd_rows<T, LANES, R, VEC>), dim3(blocks),           \
+                                   dim3(RT_BLOCK), 0, st, a);                                  \
+            else                                                                               \
+                hipLaunchKernelGGL((route_rows<T, LANES, R, VEC>), dim3(blocks),               \
+                                   dim3(RT_BLOCK), 0, st, a);                                  \
+        }                                                                                      \
     } while (0)
-    if (r <= 1) OSM_ROUTE(1);
-    else if (r <= 2) OSM_ROUTE(2);
+    if (r <= 1 && VEC == 1) OSM_ROUTE(1);
+    else if (r <= 2 && VEC == 1) OSM_ROUTE(2);
     else if (r <= 4) OSM_ROUTE(4);
     else if (r <= 8) OSM_ROUTE(8);
     else OSM_ROUTE(16);
 #undef OSM_ROUTE
     return hipGetLastError();
+}
+
+template <typename T, bool BWD>
+hipError_t launch_route_t(const RouteRows& a, hipStream_t st) {
+    // four neighbours at a time where every row allows it
+    const uintptr_t at = (uintptr_t)a.x | (BWD ? (uintptr_t)a.dx : 0);
+    const bool vec = a.E % 4 == 0 && at % (4 * sizeof(T)) == 0 && a.E >= 32;
+    const int lanes = route_lanes(a, BWD ? 4 : 8);
+#define OSM_LANES(L)                                                \
+    case L:                                                         \
+        return vec ? launch_route_l<T, BWD, L, 4>(a, st)            \
+                   : launch_route_l<T, BWD, L, 1>(a, st);
+    switch (lanes) {
+        OSM_LANES(8)
+        OSM_LANES(16)
+        OSM_LANES(32)
+        default:
+        OSM_LANES(64)
+    }
+#undef OSM_LANES
 }
 
 hipError_t launch_route_fwd(const RouteRows& a, int dtype, hipStream_t st) {

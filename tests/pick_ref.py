@@ -99,7 +99,7 @@ def route(X, K, bias=None, score="softmax", groups=1, top_groups=1, group_top=1,
             may = may & (b > -np.inf)
             c = s + b
         if groups > 1:
-            gc = s if bias is None else c
+            gc = s if bias is None and group_top == 2 else c
             key = np.full(groups, -np.inf)
             for g in range(groups):
                 inside = gc[g * gs:(g + 1) * gs][may[g * gs:(g + 1) * gs]]

@@ -118,6 +118,25 @@ def test_a_bias_decides_between_close_scores(dev):
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("E,K,groups", [(8, 3, 2), (40, 6, 4), (256, 8, 8), (1000, 20, 10)])
+def test_near_ties_everywhere(E, K, groups, score, dev):
+    """Scores that differ by less than a binary32 sum with the bias can show: at every
+    place, at the last one, and between the groups at the line; beside ordinary rows."""
+    g = torch.Generator().manual_seed(E)
+    n = 48
+    x = torch.randn(n, E, generator=g)
+    x[::3] = 0.5 + 2.0 ** -22 * torch.randint(0, 9, (n // 3, E), generator=g)
+    x[1::3] = x[1::3].round()
+    x = x.to(dev)
+    for b in (torch.full((E,), 3.0), torch.zeros(E), 0.1 * torch.randn(E, generator=g),
+              1e6 * torch.randint(-1, 2, (E,), generator=g)):
+        b = b.to(dev)
+        for top in (1, 2):
+            check_fwd(x, K, b, score=score, groups=groups, top_groups=groups - 1, group_top=top)
+    check_fwd(x, K, score=score, groups=groups, top_groups=groups - 1, group_top=2)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("E,groups", [(24, 1), (24, 4), (200, 8), (600, 1)])
 def test_masks(E, groups, dtype, score, dev):
