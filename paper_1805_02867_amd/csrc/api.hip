@@ -744,8 +744,10 @@ int run_route_fwd(const void* x, const float* bias, float* vals, int32_t* idx, i
     const Span out[] = {{vals, kb}, {idx, kb}};
     const Span in[] = {{x, (size_t)N * (size_t)E * es}, {bias, (size_t)E * 4}};
     if (any_overlap(out, in)) return OSM_EINVAL;
-    if (!device_state(nullptr)) return OSM_EHIP;
+    const DeviceState* ds = device_state(nullptr);
+    if (!ds) return OSM_EHIP;
     osm::RouteRows a{};
+    a.cus = ds->cus;
     a.x = x, a.bias = bias, a.vals = vals, a.idx = idx, a.N = N, a.E = (int)E, a.K = K;
     a.groups = r->groups, a.top_groups = r->top_groups, a.group_top = r->group_top;
     a.sigmoid = r->score == OSM_SCORE_SIGMOID, a.renorm = r->renorm != 0, a.scale = r->scale;
@@ -763,8 +765,10 @@ int run_route_bwd(const void* x, const int32_t* idx, const float* dvals, void* d
     const Span out[] = {{dx, eb}};
     const Span in[] = {{x, eb}, {idx, kb}, {dvals, kb}};
     if (any_overlap(out, in)) return OSM_EINVAL;
-    if (!device_state(nullptr)) return OSM_EHIP;
+    const DeviceState* ds = device_state(nullptr);
+    if (!ds) return OSM_EHIP;
     osm::RouteRows a{};
+    a.cus = ds->cus;
     a.x = x, a.idx = const_cast<int32_t*>(idx), a.dvals = dvals, a.dx = dx;
     a.N = N, a.E = (int)E, a.K = K;
     a.sigmoid = r->score == OSM_SCORE_SIGMOID, a.renorm = r->renorm != 0, a.scale = r->scale;

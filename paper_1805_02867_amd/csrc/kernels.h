@@ -148,6 +148,7 @@ struct RouteRows {
     int E, K, groups, top_groups, group_top;
     bool sigmoid, renorm;
     float scale;
+    int cus;
 };
 hipError_t launch_route_fwd(const RouteRows& a, int dtype, hipStream_t st);
 hipError_t launch_route_bwd(const RouteRows& a, int dtype, hipStream_t st);

@@ -10,13 +10,16 @@
 // not underflow together.
 //
 // The choice is that of binary64 scores: a bias brings experts close together, and a
-// choice must not depend on the order of a sum.  It is made on binary32 c first; where two of the K + 1 best, or two groups on the two
-// sides of the line, are closer than their errors, the row is done again in
-// binary64 (3 of 1000 rows of 256 sigmoid scores, 8 taken).  Where x itself ranks the
-// experts the first choice is exact.
+// choice must not depend on the order of a sum.  It is made on binary32 c first.  Of
+// those drawn, the ones that are closer than their errors are ranked again in binary64;
+// experts are drawn past the K-th until the next one is clearly behind it.  A row whose
+// groups are that close on the two sides of the line, or that has more such experts
+// than lanes, is done again in binary64 as a whole.  (256 sigmoid scores, 8 taken:
+// 3 of 1000 rows have a close pair.)  Where x itself ranks the experts the first choice
+// is exact.
 //
-// A row is taken by LANES lanes, R experts a lane, and the K are drawn one by one: each
-// lane has its best at hand, and only the one that is drawn looks for its next.
+// A row is taken by LANES lanes, R experts a lane.  Each lane sorts its own, and the K
+// are drawn one by one, the largest head first: a 32-bit maximum over the lanes a draw.
 //
 // Backward, with g the gradient of the K weights and p = weights / scale:
 //   softmax, renormalised:  dx_i = scale p_i (g_i - sum_j g_j p_j) at the chosen
@@ -29,10 +32,25 @@
 
 namespace osm {
 
+#ifndef OSM_ROUTE_BLOCKS
+#define OSM_ROUTE_BLOCKS 4
+#endif
+#ifndef OSM_RW
+#define OSM_RW 4
+#endif
+#ifndef OSM_RWB
+#define OSM_RWB 4
+#endif
+#ifndef OSM_ROUTE_EACH
+#define OSM_ROUTE_EACH 8
+#endif
+#ifndef OSM_ROUTE_EACH_BWD
+#define OSM_ROUTE_EACH_BWD 4
+#endif
 constexpr int RT_BLOCK = 256;
 constexpr int RT_WAVES = RT_BLOCK / 64;
 
-// 1 / d for 1 <= d <= 2: the hardware's estimate and two Newton steps (each squares
+// 1 / d for 1/2 <= d <= 64: the hardware's estimate and two Newton steps (each squares
 // the error 2^-26 or less).
 __device__ __forceinline__ double reciprocal(double d) {
     double r = __builtin_amdgcn_rcp(d);
@@ -110,16 +128,26 @@ __device__ __forceinline__ float team_maximum(float v) {  // (NaN where there is
     return v;
 }
 
-// The largest of a lane's c, the first of equal ones.
+// Sorts a lane's keys, which differ, largest first: Batcher's odd-even merge network.
 template <int R>
-__device__ __forceinline__ void lane_best(const float (&c)[R], float& best, int& at) {
-    best = c[0];
-    at = 0;
+__device__ __forceinline__ void sort_lane(uint64_t (&k)[R]) {
 #pragma unroll
-    for (int j = 1; j < R; ++j) {
-        const bool more = c[j] > best;
-        best = more ? c[j] : best;
-        at = more ? j : at;
+    for (int p = 1; p < R; p *= 2) {
+#pragma unroll
+        for (int q = p; q >= 1; q /= 2) {
+#pragma unroll
+            for (int j = q % p; j + q < R; j += 2 * q) {
+#pragma unroll
+                for (int i = 0; i < q; ++i) {
+                    if (i + j + q < R && (i + j) / (2 * p) == (i + j + q) / (2 * p)) {
+                        const uint64_t a = k[i + j], b = k[i + j + q];
+                        const bool swap = b > a;
+                        k[i + j] = swap ? b : a;
+                        k[i + j + q] = swap ? a : b;
+                    }
+                }
+            }
+        }
     }
 }
 
@@ -204,37 +232,26 @@ __device__ __forceinline__ void exact_row(const RouteRows& a, const T* xr, float
     }
 }
 
-template <typename T, int LANES, int R, int VEC>
+// SCORES: with a bias, or groups ranked by the sum of their two best; without them x is
+// what ranks the experts.
+template <typename T, int LANES, int R, int VEC, bool SCORES>
 __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
     constexpr int ROWS = 64 / LANES;  // of a wavefront
     const float ninf = -__builtin_inff();
-    __shared__ uint64_t ranks[RT_WAVES][64 * R];
+    __shared__ uint64_t ranks[RT_WAVES][SCORES ? 64 * R : 32 * R];
     __shared__ float best_of[RT_WAVES][64];
-    __shared__ int chosen[RT_WAVES][64 + ROWS];  // K + 1 a row
+    __shared__ int chosen[RT_WAVES][64];
     const int lane = threadIdx.x % LANES, wv = threadIdx.x >> 6, team = (threadIdx.x & 63) / LANES;
     const int E = a.E, K = a.K, G = a.groups;
     float* const hc = reinterpret_cast<float*>(ranks[wv]) + team * LANES * R;
     float* const go = best_of[wv] + team * LANES;
-    int* const ch = chosen[wv] + team * (LANES + 1);
-    const bool sums = G > 1 && a.group_top == 2;
-    const bool scores = a.bias || sums;        // c, or a group's, is not x itself
-    const bool total = !a.sigmoid && (scores || !a.renorm);
-    const int draws = a.bias && K < E ? K + 1 : K;
-    // what does not depend on the row: the bias, and the groups
-    float b[R], bmax = 0.0f;
-    int ge[R];
-    const int gs = E / G;
+    int* const ch = chosen[wv] + team * LANES;
+    const bool sums = SCORES && G > 1 && a.group_top == 2;
+    const bool biased = SCORES && a.bias;
+    const int gs = G > 1 ? E / G : E;
+    const float rgs = 1.0f / (float)gs;
     int per = LANES;  // lanes that look at a group
     while (per * G > LANES) per >>= 1;
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-        const int e = expert<LANES, VEC>(lane, j);
-        b[j] = a.bias && e < E ? a.bias[e] : 0.0f;
-        ge[j] = G > 1 ? (e < E ? e : 0) / gs * per + team * LANES : 0;
-        const float m = __builtin_fabsf(b[j]);
-        bmax = m < __builtin_inff() ? fmaxf(bmax, m) : bmax;
-    }
-    const float error = score_error(a.sigmoid, group_max<LANES>(bmax));
     for (int64_t row0 = ((int64_t)blockIdx.x * RT_WAVES + wv) * ROWS; row0 < a.N;
          row0 += (int64_t)gridDim.x * RT_WAVES * ROWS) {
         const int64_t row = row0 + team;
@@ -249,14 +266,15 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
         const bool bad = !(mx < __builtin_inff());
         const bool some = !bad && mx > ninf;
         double rsum = 1.0;  // of the exact scores
-        if (total && !a.renorm) {
+        if (!a.sigmoid && !a.renorm) {
             double sum = 0.0;
 #pragma unroll
             for (int j = 0; j < R; ++j) sum += exp2_wide(((double)x[j] - (double)mx) * kLog2eD);
             rsum = 1.0 / group_sum<LANES>(sum);
         }
-        if (scores) {
-            float rs = (float)rsum;
+        float error = 0.0f;
+        if constexpr (SCORES) {
+            float rs = 1.0f, bmax = 0.0f;
             if (a.sigmoid) {
 #pragma unroll
                 for (int j = 0; j < R; ++j)
@@ -268,18 +286,29 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
                     c[j] = exp2_hw((x[j] - mx) * kLog2e);
                     sum += c[j];
                 }
-                if (a.renorm) rs = 1.0f / group_sum<LANES>(sum);
+                rs = 1.0f / group_sum<LANES>(sum);
+            }
+            float b[R];
+            if (biased) {
+                load_experts<float, LANES, R, VEC>(a.bias, E, true, lane, b);
+            } else {
+#pragma unroll
+                for (int j = 0; j < R; ++j) b[j] = 0.0f;
             }
 #pragma unroll
-            for (int j = 0; j < R; ++j) c[j] = __builtin_fmaf(c[j], rs, b[j]);
+            for (int j = 0; j < R; ++j) {
+                const float m = __builtin_fabsf(b[j]);
+                bmax = m < __builtin_inff() ? fmaxf(bmax, m) : bmax;
+                // (a NaN bias: no)
+                const bool may = some && x[j] > ninf && b[j] > ninf;
+                c[j] = may ? __builtin_fmaf(c[j], rs, b[j]) : ninf;
+            }
+            error = score_error(a.sigmoid, biased ? group_max<LANES>(bmax) : 0.0f);
         } else {
 #pragma unroll
-            for (int j = 0; j < R; ++j) c[j] = x[j];
+            for (int j = 0; j < R; ++j) c[j] = some ? x[j] : ninf;
         }
-#pragma unroll
-        for (int j = 0; j < R; ++j)  // (a NaN bias: no)
-            c[j] = some && x[j] > ninf && b[j] > ninf ? c[j] : ninf;
-        bool close = false;  // a line that binary32 does not decide
+        bool again = false;  // a line that binary32 does not decide
         if (G > 1) {
 #pragma unroll
             for (int j = 0; j < R; ++j) hc[expert<LANES, VEC>(lane, j)] = c[j];
@@ -308,65 +337,119 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
             }
             const bool stays = g < G && ahead < a.top_groups;
             const uint64_t keep = __ballot(stays);
-            if (scores) {
+            if constexpr (SCORES) {
                 const float low = team_min<LANES>(stays ? best : __builtin_inff());
                 const float high = group_max<LANES>(g < G && !stays ? best : ninf);
-                close = high > ninf && low < __builtin_inff() &&
-                        !(low - high > 4.0f * error);
+                again = high > ninf && low < __builtin_inff() && !(low - high > 4.0f * error);
             }
 #pragma unroll
-            for (int j = 0; j < R; ++j)
-                if (!(keep >> ge[j] & 1)) c[j] = ninf;
-            if (sums && !a.bias) {  // the experts of the kept groups by x again
+            for (int j = 0; j < R; ++j) {
+                // (the quotient of numbers up to 1024 by a reciprocal: half a unit is far
+                // more than its error)
+                const int e = expert<LANES, VEC>(lane, j);
+                const int ge = (int)(((float)(e < E ? e : 0) + 0.5f) * rgs);
+                if (!(keep >> (ge * per + team * LANES) & 1)) c[j] = ninf;
+            }
+            if (sums && !biased) {  // the experts of the kept groups by x again
 #pragma unroll
                 for (int j = 0; j < R; ++j) c[j] = c[j] > ninf ? x[j] : ninf;
             }
         }
         ch[lane] = -1;
-        if (lane == 0) ch[LANES] = -1;
         wave_sync();
-        float best, before = 0.0f;
-        int at;
-        lane_best(c, best, at);
-        for (int i = 0; i < draws; ++i) {
-            const float top = group_max<LANES>(best);
-            if (a.bias) {  // closer than the errors of both, equal ones among them
-                close = close || (i > 0 && top > ninf &&
-                                  !(before - top > 2.0f * error));
-                before = top;
-            }
-            bool win = best == top && best > ninf;
-            const uint64_t who = __ballot(win);
-            if (who == 0) break;
-            const uint64_t mine = LANES == 64 ? who
-                                              : who >> (team * LANES) & ((1ull << (LANES & 63)) - 1);
-            const int e = expert<LANES, VEC>(lane, at);
-            if (__any((mine & (mine - 1)) != 0)) {
-                const uint32_t first = ~group_max<LANES>(win ? ~(uint32_t)e : 0u);
-                win = win && (uint32_t)e == first;
-            }
-            if (win) {
-                ch[i] = e;
+        // keys: the order of c, then the lower index; 0 for what cannot be chosen
+        uint64_t k[R];
 #pragma unroll
-                for (int j = 0; j < R; ++j)
-                    if (j == at) c[j] = ninf;
-                lane_best(c, best, at);
+        for (int j = 0; j < R; ++j)
+            k[j] = c[j] > ninf ? (uint64_t)order_key(c[j]) << 32 |
+                                     (uint32_t)~(uint32_t)expert<LANES, VEC>(lane, j)
+                               : 0;
+        sort_lane(k);
+        float before = __builtin_inff();
+        bool close = false, open = true;  // open: the next one may still matter
+        int drawn = 0;
+        for (int i = 0;; ++i) {
+            if (!biased && i == K) break;
+            const uint32_t hi = (uint32_t)(k[0] >> 32), top = group_max<LANES>(hi);
+            open = open && top != 0;
+            if (biased) {
+                // past the K-th, those that are too close to the one before to be behind it
+                const float v = order_value(top);
+                const bool near = !(before - v > 2.0f * error);  // (equal ones among them)
+                open = open && (i < K || near);
+                close = close || (open && i > 0 && near);
+                before = v;
+                if (i == LANES) {  // (no lane for another)
+                    again = again || open;
+                    break;
+                }
+            }
+            const int teams = __popcll(__ballot(open)) / LANES;
+            if (teams == 0) break;
+            bool win = open && hi == top;
+            if (__popcll(__ballot(win)) != teams) {
+                const uint32_t lo = group_max<LANES>(win ? (uint32_t)k[0] : 0u);
+                win = win && (uint32_t)k[0] == lo;
+            }
+            drawn += open;
+            if (win) {
+                ch[i] = (int)~(uint32_t)k[0];
+#pragma unroll
+                for (int j = 0; j + 1 < R; ++j) k[j] = k[j + 1];
+                k[R - 1] = 0;
             }
         }
-        if (scores) {
-            uint64_t again = __ballot(close && some && live);
-            while (again) {  // (uniform: a row of the wavefront at a time)
-                const int t = __builtin_ctzll(again) / LANES;
-                again = LANES == 64 ? 0 : again & ~(((1ull << (LANES & 63)) - 1) << (t * LANES));
+        wave_sync();
+        int pick = ch[lane];
+        if constexpr (SCORES) {
+            if (__ballot(close && live) != 0) {
+                // the drawn ones by their exact c, and by the index where that is equal
+                double rs = 1.0;
+                if (!a.sigmoid) {
+                    double sum = 0.0;
+#pragma unroll
+                    for (int j = 0; j < R; ++j)
+                        sum += exp2_wide(((double)x[j] - (double)mx) * kLog2eD);
+                    rs = 1.0 / group_sum<LANES>(sum);
+                }
+                uint64_t mine = 0;
+                if (pick >= 0) {
+                    const double xp = (double)load1(xr + pick);
+                    const double s = a.sigmoid ? sigmoid_wide(xp)
+                                               : exp2_wide((xp - (double)mx) * kLog2eD) * rs;
+                    mine = order_key(s + (double)a.bias[pick]);
+                }
+                uint64_t* const rk = ranks[wv] + team * LANES;
+                rk[lane] = mine;
                 wave_sync();
-                exact_row(a, static_cast<const T*>(a.x) + (row0 + t) * E,
-                          lane_value(mx, t * LANES), ranks[wv], chosen[wv] + t * (LANES + 1));
+                int ahead = 0;
+                const int most = (int)group_max<64>((uint32_t)drawn);
+                for (int i = 0; i < most; ++i) {
+                    const uint64_t o = rk[i];
+                    ahead += o > mine || (o == mine && ch[i] < pick);
+                }
+                wave_sync();
+                if (pick >= 0) ch[ahead] = pick;
+                wave_sync();
+                pick = ch[lane];
+            }
+            uint64_t rows = __ballot(again && some && live);
+            if (rows) {
+                while (rows) {  // (uniform: a row of the wavefront at a time)
+                    const int r = __builtin_ctzll(rows) / LANES;
+                    rows = LANES == 64 ? 0
+                                       : rows & ~(((1ull << (LANES & 63)) - 1) << (r * LANES));
+                    wave_sync();
+                    exact_row(a, static_cast<const T*>(a.x) + (row0 + r) * E,
+                              lane_value(mx, r * LANES), ranks[wv], chosen[wv] + r * LANES);
+                }
+                wave_sync();
+                pick = ch[lane];
             }
         }
         wave_sync();
         // weights: lane i has the i-th expert
-        const int pick = lane < K ? ch[lane] : -1;
-        wave_sync();
+        if (lane >= K) pick = -1;
         const double xp = pick >= 0 ? (double)load1(xr + pick) : -__builtin_inf();
         double w = 0.0;
         if (a.renorm) {
@@ -376,8 +459,8 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
             w = exp2_wide((z - zm) * kLog2eD);
             if (a.sigmoid) w *= reciprocal(1.0 + exp_minus_abs(xp));
             w = pick >= 0 ? w : 0.0;
-            const double all = group_sum<LANES>(w);
-            w = all > 0.0 ? w / all : 0.0;
+            const double all = group_sum<LANES>(w);  // at least 1/2, if any
+            w = all > 0.0 ? w * reciprocal(all) : 0.0;
         } else if (pick >= 0) {
             w = a.sigmoid ? sigmoid_wide(xp) : exp2_wide((xp - (double)mx) * kLog2eD) * rsum;
         }
@@ -390,7 +473,7 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
 
 // The gradient.  A row by LANES lanes, R experts a lane; lane i also has place i.
 template <typename T, int LANES, int R, int VEC>
-__global__ __launch_bounds__(RT_BLOCK) void route_bwd_rows(const RouteRows a) {
+__global__ __launch_bounds__(RT_BLOCK, OSM_RWB) void route_bwd_rows(const RouteRows a) {
     constexpr int ROWS = 64 / LANES;
     __shared__ double owns[RT_WAVES][64];
     __shared__ int places[RT_WAVES][64];
@@ -515,53 +598,55 @@ __global__ __launch_bounds__(RT_BLOCK) void route_bwd_rows(const RouteRows a) {
 
 // Lanes of a row: enough for its K places and its groups, and for its experts at
 // `each` a lane or few more.
-static int route_lanes(const RouteRows& a, int each) {
+static int route_lanes(const RouteRows& a, int each) {  // (each <= 8: launch_route_l)
     int lanes = 8;
     while (lanes < 64 && (lanes < a.K || lanes < a.groups || lanes * each < a.E)) lanes *= 2;
     return lanes;
 }
 
+template <typename T, bool BWD, int LANES, int R, int VEC>
+hipError_t launch_route_r(const RouteRows& a, unsigned blocks, hipStream_t st) {
+    if constexpr (BWD)
+        hipLaunchKernelGGL((route_bwd_rows<T, LANES, R, VEC>), dim3(blocks), dim3(RT_BLOCK), 0, st,
+                           a);
+    else if (a.bias || (a.groups > 1 && a.group_top == 2))
+        hipLaunchKernelGGL((route_rows<T, LANES, R, VEC, true>), dim3(blocks), dim3(RT_BLOCK), 0,
+                           st, a);
+    else
+        hipLaunchKernelGGL((route_rows<T, LANES, R, VEC, false>), dim3(blocks), dim3(RT_BLOCK), 0,
+                           st, a);
+    return hipGetLastError();
+}
+
 template <typename T, bool BWD, int LANES, int VEC>
 hipError_t launch_route_l(const RouteRows& a, hipStream_t st) {
     const int64_t want = (a.N + RT_WAVES * (64 / LANES) - 1) / (RT_WAVES * (64 / LANES));
-    const unsigned blocks = (unsigned)(want < (1 << 20) ? want : 1 << 20);
+    const int64_t most = (int64_t)a.cus * OSM_ROUTE_BLOCKS;
+    const unsigned blocks = (unsigned)(want < most ? want : most);
     const int r = (a.E + LANES - 1) / LANES;
-#define OSM_ROUTE(R)                                                                           \
-    do {                                                                                       \
-        if constexpr (R % VEC == 0 && (LANES == 64 || R <= 8)) {                               \
-            if constexpr (BWD)                                                                 \
-                hipLaunchKernelGGL((route_bwd_rows<T, LANES, R, VEC>), dim3(blocks),           \
-                                   dim3(RT_BLOCK), 0, st, a);                                  \
-            else                                                                               \
-                hipLaunchKernelGGL((route_rows<T, LANES, R, VEC>), dim3(blocks),               \
-                                   dim3(RT_BLOCK), 0, st, a);                                  \
-        }                                                                                      \
-    } while (0)
-    if (r <= 1 && VEC == 1) OSM_ROUTE(1);
-    else if (r <= 2 && VEC == 1) OSM_ROUTE(2);
-    else if (r <= 4) OSM_ROUTE(4);
-    else if (r <= 8) OSM_ROUTE(8);
-    else OSM_ROUTE(16);
-#undef OSM_ROUTE
-    return hipGetLastError();
+    if constexpr (VEC == 1) {
+        if (r <= 1) return launch_route_r<T, BWD, LANES, 1, VEC>(a, blocks, st);
+        if (r <= 2) return launch_route_r<T, BWD, LANES, 2, VEC>(a, blocks, st);
+    }
+    if (r <= 4) return launch_route_r<T, BWD, LANES, 4, VEC>(a, blocks, st);
+    if constexpr (LANES < 64) return launch_route_r<T, BWD, LANES, 8, VEC>(a, blocks, st);
+    if (r <= 8) return launch_route_r<T, BWD, LANES, 8, VEC>(a, blocks, st);
+    return launch_route_r<T, BWD, LANES, 16, VEC>(a, blocks, st);
 }
 
 template <typename T, bool BWD>
 hipError_t launch_route_t(const RouteRows& a, hipStream_t st) {
-    // four neighbours at a time where every row allows it
+    // four neighbours at a time where every row (and the bias) allows it
     const uintptr_t at = (uintptr_t)a.x | (BWD ? (uintptr_t)a.dx : 0);
-    const bool vec = a.E % 4 == 0 && at % (4 * sizeof(T)) == 0 && a.E >= 32;
-    const int lanes = route_lanes(a, BWD ? 4 : 8);
-#define OSM_LANES(L)                                                \
-    case L:                                                         \
-        return vec ? launch_route_l<T, BWD, L, 4>(a, st)            \
-                   : launch_route_l<T, BWD, L, 1>(a, st);
-    switch (lanes) {
-        OSM_LANES(8)
-        OSM_LANES(16)
-        OSM_LANES(32)
-        default:
-        OSM_LANES(64)
+    const bool vec = a.E % 4 == 0 && at % (4 * sizeof(T)) == 0 && (uintptr_t)a.bias % 16 == 0 &&
+                     a.E >= 32;
+#define OSM_LANES(L) \
+    return vec ? launch_route_l<T, BWD, L, 4>(a, st) : launch_route_l<T, BWD, L, 1>(a, st)
+    switch (route_lanes(a, BWD ? OSM_ROUTE_EACH_BWD : OSM_ROUTE_EACH)) {
+        case 8: OSM_LANES(8);
+        case 16: OSM_LANES(16);
+        case 32: OSM_LANES(32);
+        default: OSM_LANES(64);
     }
 #undef OSM_LANES
 }
