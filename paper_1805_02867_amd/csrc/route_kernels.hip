@@ -35,12 +35,6 @@ namespace osm {
 #ifndef OSM_ROUTE_BLOCKS
 #define OSM_ROUTE_BLOCKS 4
 #endif
-#ifndef OSM_RW
-#define OSM_RW 4
-#endif
-#ifndef OSM_RWB
-#define OSM_RWB 4
-#endif
 #ifndef OSM_ROUTE_EACH
 #define OSM_ROUTE_EACH 8
 #endif
@@ -151,6 +145,10 @@ __device__ __forceinline__ void sort_lane(uint64_t (&k)[R]) {
     }
 }
 
+// Place of a number in LDS where rows of 32 are walked side by side: a free one after each
+// 32 puts them into different banks.
+constexpr __device__ __forceinline__ int padded(int i) { return i + i / 32; }
+
 template <int LANES>
 __device__ __forceinline__ float team_min(float v) {
     return -group_max<LANES>(-v);
@@ -238,12 +236,12 @@ template <typename T, int LANES, int R, int VEC, bool SCORES>
 __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
     constexpr int ROWS = 64 / LANES;  // of a wavefront
     const float ninf = -__builtin_inff();
-    __shared__ uint64_t ranks[RT_WAVES][SCORES ? 64 * R : 32 * R];
+    __shared__ uint64_t ranks[RT_WAVES][SCORES ? 64 * R : (ROWS * padded(LANES * R) + 1) / 2];
     __shared__ float best_of[RT_WAVES][64];
     __shared__ int chosen[RT_WAVES][64];
     const int lane = threadIdx.x % LANES, wv = threadIdx.x >> 6, team = (threadIdx.x & 63) / LANES;
     const int E = a.E, K = a.K, G = a.groups;
-    float* const hc = reinterpret_cast<float*>(ranks[wv]) + team * LANES * R;
+    float* const hc = reinterpret_cast<float*>(ranks[wv]) + team * padded(LANES * R);
     float* const go = best_of[wv] + team * LANES;
     int* const ch = chosen[wv] + team * LANES;
     const bool sums = SCORES && G > 1 && a.group_top == 2;
@@ -269,7 +267,10 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
         if (!a.sigmoid && !a.renorm) {
             double sum = 0.0;
 #pragma unroll
-            for (int j = 0; j < R; ++j) sum += exp2_wide(((double)x[j] - (double)mx) * kLog2eD);
+            for (int j = 0; j < R; ++j) {
+                sum += exp2_wide(((double)x[j] - (double)mx) * kLog2eD);
+                pair_end(j);
+            }
             rsum = 1.0 / group_sum<LANES>(sum);
         }
         float error = 0.0f;
@@ -311,13 +312,13 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
         bool again = false;  // a line that binary32 does not decide
         if (G > 1) {
 #pragma unroll
-            for (int j = 0; j < R; ++j) hc[expert<LANES, VEC>(lane, j)] = c[j];
+            for (int j = 0; j < R; ++j) hc[padded(expert<LANES, VEC>(lane, j))] = c[j];
             wave_sync();
             const int g = lane / per;
             float best = ninf, second = ninf;
             if (g < G) {
                 for (int i = lane % per; i < gs; i += per) {
-                    const float v = hc[g * gs + i];
+                    const float v = hc[padded(g * gs + i)];
                     second = __builtin_amdgcn_fmed3f(v, best, second);
                     best = fmaxf(best, v);
                 }
@@ -408,8 +409,10 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
                 if (!a.sigmoid) {
                     double sum = 0.0;
 #pragma unroll
-                    for (int j = 0; j < R; ++j)
+                    for (int j = 0; j < R; ++j) {
                         sum += exp2_wide(((double)x[j] - (double)mx) * kLog2eD);
+                        pair_end(j);
+                    }
                     rs = 1.0 / group_sum<LANES>(sum);
                 }
                 uint64_t mine = 0;
@@ -473,7 +476,7 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
 
 // The gradient.  A row by LANES lanes, R experts a lane; lane i also has place i.
 template <typename T, int LANES, int R, int VEC>
-__global__ __launch_bounds__(RT_BLOCK, OSM_RWB) void route_bwd_rows(const RouteRows a) {
+__global__ __launch_bounds__(RT_BLOCK) void route_bwd_rows(const RouteRows a) {
     constexpr int ROWS = 64 / LANES;
     __shared__ double owns[RT_WAVES][64];
     __shared__ int places[RT_WAVES][64];
@@ -506,6 +509,7 @@ __global__ __launch_bounds__(RT_BLOCK, OSM_RWB) void route_bwd_rows(const RouteR
             for (int j = 0; j < R; ++j) {
                 d[j] = exp2_wide(((double)x[j] - mx) * kLog2eD);
                 sum += d[j];
+                pair_end(j);
             }
             const double rsum = 1.0 / group_sum<LANES>(sum);
             own = g * (exp2_wide((xc - mx) * kLog2eD) * rsum);

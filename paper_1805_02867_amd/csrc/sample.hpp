@@ -561,6 +561,7 @@ __device__ __forceinline__ bool add_histogram(SampleSmem<W>& sm, const Held<T, W
             } else if constexpr (COUNT) {
                 tail |= t > -1080.0;
             }
+            pair_end(e);
         }
     }
     return tail;
@@ -875,7 +876,10 @@ __device__ __forceinline__ bool locate(SampleSmem<W>& sm, const Held<T, W, R>& h
     for (int r = 0; r < R; ++r) {
         s[r] = 0.0;
 #pragma unroll
-        for (int e = 0; e < h.E; ++e) s[r] += wt(h.at(r, e), h.index(r, e));
+        for (int e = 0; e < h.E; ++e) {
+            s[r] += wt(h.at(r, e), h.index(r, e));
+            pair_end(e);
+        }
         const double all = group_sum<64>(s[r]);
         if (lane == 0) sm.seg[r * W + wv] = all;
     }

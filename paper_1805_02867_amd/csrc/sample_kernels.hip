@@ -384,7 +384,10 @@ __global__ __launch_bounds__(SM_BLOCK) void sample_split(const SampleRows a, con
 #pragma unroll
                 for (int rr = 0; rr < R; ++rr)
 #pragma unroll
-                    for (int e = 0; e < h.E; ++e) z += an.weight(h.at(rr, e));
+                    for (int e = 0; e < h.E; ++e) {
+                        z += an.weight(h.at(rr, e));
+                        pair_end(e);
+                    }
                 p.z = team_sum(sm, z);
             } else if (!cold((double)p.m * r.c)) {
 #pragma unroll
