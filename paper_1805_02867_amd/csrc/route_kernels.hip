@@ -269,7 +269,6 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
 #pragma unroll
             for (int j = 0; j < R; ++j) {
                 sum += exp2_wide(((double)x[j] - (double)mx) * kLog2eD);
-                pair_end(j);
             }
             rsum = 1.0 / group_sum<LANES>(sum);
         }
@@ -411,8 +410,7 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
 #pragma unroll
                     for (int j = 0; j < R; ++j) {
                         sum += exp2_wide(((double)x[j] - (double)mx) * kLog2eD);
-                        pair_end(j);
-                    }
+                            }
                     rs = 1.0 / group_sum<LANES>(sum);
                 }
                 uint64_t mine = 0;
@@ -509,7 +507,6 @@ __global__ __launch_bounds__(RT_BLOCK) void route_bwd_rows(const RouteRows a) {
             for (int j = 0; j < R; ++j) {
                 d[j] = exp2_wide(((double)x[j] - mx) * kLog2eD);
                 sum += d[j];
-                pair_end(j);
             }
             const double rsum = 1.0 / group_sum<LANES>(sum);
             own = g * (exp2_wide((xc - mx) * kLog2eD) * rsum);

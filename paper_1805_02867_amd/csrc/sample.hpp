@@ -446,9 +446,28 @@ struct Held {
             }
         }
     }
-    __device__ __forceinline__ float at(int r, int e) const { return elem(q[r], e, (T*)nullptr); }
-    __device__ __forceinline__ uint32_t index(int r, int e) const {
-        return (uint32_t)(first + r * 64 * W * E + e);
+    // f(vector, index of its first element) for each, in a loop over registers that turn:
+    // unrolled, the code of a pass over the row leaves the instruction cache, which
+    // bounded it (the moves are one instruction in ten)
+    template <typename F>
+    __device__ __forceinline__ void each(const F& f) {
+        constexpr int STEP = R % 2 == 0 && E == 4 ? 2 : 1;
+#pragma unroll 1
+        for (int r = 0; r < R; r += STEP) {
+            u32x4 head[STEP];
+#pragma unroll
+            for (int s = 0; s < STEP; ++s) {
+                head[s] = q[s];
+                f(q[s], first + (r + s) * 64 * W * E);
+            }
+#pragma unroll
+            for (int j = 0; j + STEP < R; ++j) q[j] = q[j + STEP];
+#pragma unroll
+            for (int s = 0; s < STEP; ++s) q[R - STEP + s] = head[s];
+        }
+    }
+    __device__ __forceinline__ static float at(const u32x4& v, int e) {
+        return elem(v, e, (T*)nullptr);
     }
     // (NaN where there is one)
     __device__ __forceinline__ float maximum() const {
@@ -457,7 +476,7 @@ struct Held {
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int e = 0; e < E; e += 2)
-                m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(at(r, e), at(r, e + 1)), m);
+                m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(at(q[r], e), at(q[r], e + 1)), m);
         return m;
     }
 };
@@ -522,11 +541,12 @@ __device__ __forceinline__ double team_sum(SampleSmem<W>& sm, double v) {
 // (m c has to be small enough for its ceiling to be one.)
 struct Anchor {
     double m, c, a, shift;  // shift: of the maximum, in (-1, 0]
+    Exp2 exp2;
     // (weights vanish below 2^-1075; the bound also takes the place of -inf and NaN)
     __device__ __forceinline__ double t(float x) const {
         return __builtin_fmax(((double)x - m) * c, -1100.0);
     }
-    __device__ __forceinline__ double weight(float x) const { return exp2_bounded(t(x)); }
+    __device__ __forceinline__ double weight(float x) const { return exp2(t(x)); }
     // the low bits of s + 1.5 2^52 / SUB are round(s SUB)
     template <int W>
     __device__ __forceinline__ int bin(double t) const {
@@ -539,32 +559,54 @@ constexpr double kAnchorMax = 0x1p30;
 __device__ __forceinline__ bool cold(double mc) { return !(__builtin_fabs(mc) <= kAnchorMax); }
 __device__ __forceinline__ Anchor anchor(float m, double c) {
     const double mc = (double)m * c, a = __builtin_ceil(mc);
-    return Anchor{(double)m, c, a, mc - a};
+    return Anchor{(double)m, c, a, mc - a, Exp2::make()};
 }
 
 // Adds the held elements to the histogram sm.mass of weights (MASS) and to that of
 // their numbers sm.counts (COUNT).  The last bin stands for everything below the
 // window and stays empty; returns whether an element there has a weight at all.
 template <bool MASS, bool COUNT, typename T, int W, int R>
-__device__ __forceinline__ bool add_histogram(SampleSmem<W>& sm, const Held<T, W, R>& h,
+__device__ __forceinline__ bool add_histogram(SampleSmem<W>& sm, Held<T, W, R>& h,
                                               const Anchor& an) {
     bool tail = false;
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
+    h.each([&](const u32x4& v, int32_t) {
 #pragma unroll
         for (int e = 0; e < h.E; ++e) {
-            const double t = an.t(h.at(r, e));
+            const double t = an.t(h.at(v, e));
             const int b = an.bin<W>(t);
+            const uint64_t w = MASS ? fixed48(an.exp2(t)) : 0;
             if (b < SampleShape<W>::BINS - 1) {
-                if constexpr (MASS) add_bin(sm.mass[b], fixed48(exp2_bounded(t)));
+                if constexpr (MASS) add_bin(sm.mass[b], w);
                 if constexpr (COUNT) atomicAdd(&sm.counts[b], 1u);
-            } else if constexpr (COUNT) {
-                tail |= t > -1080.0;
             }
-            pair_end(e);
+            if constexpr (COUNT) tail |= b >= SampleShape<W>::BINS - 1 && t > -1080.0;
         }
-    }
+    });
     return tail;
+}
+
+// The sum of the held elements' weights.
+template <typename T, int W, int R>
+__device__ __forceinline__ double sum_weights(SampleSmem<W>& sm, Held<T, W, R>& h,
+                                              const Anchor& an) {
+    double z = 0.0;
+    h.each([&](const u32x4& v, int32_t) {
+#pragma unroll
+        for (int e = 0; e < h.E; ++e) z += an.weight(h.at(v, e));
+    });
+    return team_sum(sm, z);
+}
+
+// The lowest index of a held element equal to m.
+template <typename T, int W, int R>
+__device__ __forceinline__ uint32_t index_of(SampleSmem<W>& sm, Held<T, W, R>& h, float m) {
+    uint32_t at = ~0u;
+    h.each([&](const u32x4& v, int32_t i) {
+#pragma unroll
+        for (int e = 0; e < h.E; ++e)
+            at = h.at(v, e) == m && (uint32_t)(i + e) < at ? (uint32_t)(i + e) : at;
+    });
+    return team_minimum(sm, at);
 }
 
 // Values that a range of bins can hold, and a bit more.
@@ -793,71 +835,80 @@ __device__ __forceinline__ Filtered filter_row(SampleSmem<W>& sm, const Rule& r,
     const int tid = threadIdx.x % (64 * W);
     Filtered f{no_cut(), BINS - 1, BINS - 1, true};
     int held0 = 0, held1 = -1, n = 0;  // bins whose elements are in the list
-    const auto fill = [&](int lo, int hi) {
-        if (tid == 0) sm.n = 0;
-        team_sync<W>();
-        gather(Range::of<W>(lo, hi, an));
-        team_sync<W>();
-        n = sm.n;
-        held0 = lo;
-        held1 = hi;
-        f.ok = f.ok && n <= CAP;
-        team_sync<W>();
-    };
     double extra = 0.0;
     int limit = BINS - 1;
-    if (r.k) {
-        uint64_t above, here;
-        const int b = find_count(sm, r.k, &above, &here);
-        if (b < BINS) {
-            // (with the elements above it, if they all fit)
-            const int lo = above + here <= (uint64_t)CAP ? 0 : b;
-            fill(lo, b);
-            if (!f.ok || (uint64_t)n != (lo ? here : above + here)) {
-                f.ok = false;
+    // one after the other: top-k, top-p, min-p; each wants the elements of some bins
+#pragma unroll 1
+    for (int step = 0; step < 3; ++step) {
+        int lo = 0, hi = -1;
+        uint64_t above = 0, here = 0;
+        double need = 0.0;
+        if (step == 0) {
+            if (!r.k) continue;
+            const int b = find_count(sm, r.k, &above, &here);
+            if (b == BINS) {
+                if (!tail) continue;  // fewer elements than k have any weight
+                f.ok = false;         // the k-th is below the window
                 return f;
             }
-            f.cut = list_cut<false>(sm, n, f.cut, (uint64_t)r.k - (lo ? above : 0), an,
-                                    last_index);
-            f.sure = lo;
-            f.last = b;
+            // (with the elements above it, if they all fit)
+            lo = above + here <= (uint64_t)CAP ? 0 : b;
+            hi = b;
+            if (lo == 0) {
+                here += above;
+                above = 0;
+            }
+        } else if (step == 1) {
+            if (!(r.p < 1.0)) continue;
+            double all;
+            const int b = find_mass(sm, limit, extra, r.p, &all, &need);
+            if (b < BINS) lo = hi = b;
+            else if (limit == BINS - 1) continue;  // (a rounding: nothing to cut off)
+        } else {
+            if (!sums) break;
+            if (r.q > 0.0) {  // w >= q, somewhere in the bins around that
+                const int b = an.bin<W>((double)__builtin_log2f((float)r.q));
+                f.sure = b - 1 < f.sure ? (b > 1 ? b - 1 : 0) : f.sure;
+                f.last = b + 1 < f.last ? b + 1 : f.last;
+                f.sure = f.sure < f.last ? f.sure : f.last;
+            }
+            if (f.sure == BINS - 1 || (held0 <= f.sure && f.last <= held1)) break;
+            lo = f.sure;
+            hi = f.last;
+        }
+        if (lo <= hi) {
+            if (tid == 0) sm.n = 0;
+            team_sync<W>();
+            gather(Range::of<W>(lo, hi, an));
+            team_sync<W>();
+            n = sm.n;
+            held0 = lo;
+            held1 = hi;
+            // (a rounding can take an element out of its bin)
+            if (n > CAP || (step == 0 && (uint64_t)n != here)) f.ok = false;
+            team_sync<W>();
+            if (!f.ok) return f;
+        }
+        if (step == 0) {
+            f.cut = list_cut<false>(sm, n, f.cut, (uint64_t)r.k - above, an, last_index);
             limit = lo;
             if (r.p < 1.0) extra = (double)list_sum(sm, n, f.cut, an) * 0x1p-48;
-        } else if (tail) {
-            f.ok = false;  // the k-th element is below the window, among others of some weight
-            return f;
-        }
-    }
-    if (r.p < 1.0) {
-        double all, need;
-        const int b = find_mass(sm, limit, extra, r.p, &all, &need);
-        if (b < BINS || limit < BINS - 1) {
-            if (b < BINS) {
-                fill(b, b);
-                if (!f.ok) return f;
-                f.sure = f.last = b;
-            }
+        } else if (step == 1) {
             const uint64_t total = list_sum(sm, n, f.cut, an);
             const double want = __builtin_ceil(need * 0x1p48);
             uint64_t target = want >= 1.0 ? (uint64_t)want : 1;
             target = target < total ? target : total;
-            if (target == 0) {  // (a rounding took the bin's elements out of it)
+            if (target == 0) {
                 f.ok = false;
                 return f;
             }
             f.cut = list_cut<true>(sm, n, f.cut, target, an, last_index);
         }
+        if (step < 2 && lo <= hi) {
+            f.sure = lo;
+            f.last = hi;
+        }
     }
-    if (r.q > 0.0 && sums) {
-        // min-p: w >= q, somewhere in the bins around that
-        const int b = an.bin<W>((double)__builtin_log2f((float)r.q));
-        const int lo = b > 1 ? b - 1 : 0, hi = b + 1;
-        if (lo < f.sure) f.sure = lo;
-        if (hi < f.last) f.last = hi;
-        if (f.sure > f.last) f.sure = f.last;
-    }
-    if (sums && f.sure <= f.last && f.sure < BINS - 1 && !(held0 <= f.sure && f.last <= held1))
-        fill(f.sure, f.last);
     return f;
 }
 
@@ -866,25 +917,22 @@ __device__ __forceinline__ Filtered filter_row(SampleSmem<W>& sm, const Rule& r,
 // the target u * sum (PART: rem, of a row whose sum is `total`).  base: added to
 // the index.  False if no element has a weight.
 template <bool PART, typename T, int W, int R, typename Wt>
-__device__ __forceinline__ bool locate(SampleSmem<W>& sm, const Held<T, W, R>& h, const Wt& wt,
+__device__ __forceinline__ bool locate(SampleSmem<W>& sm, Held<T, W, R>& h, const Wt& wt,
                                        double target, double total, uint32_t base, float* val,
                                        int32_t* idx) {
     static_assert(R * W <= 64, "a lane a segment");
     const int lane = threadIdx.x & 63, wv = (threadIdx.x % (64 * W)) >> 6;
-    double s[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        s[r] = 0.0;
-#pragma unroll
-        for (int e = 0; e < h.E; ++e) {
-            s[r] += wt(h.at(r, e), h.index(r, e));
-            pair_end(e);
-        }
-        const double all = group_sum<64>(s[r]);
-        if (lane == 0) sm.seg[r * W + wv] = all;
-    }
-    team_sync<W>();
     // segments of 64 vectors, in index order
+    int at = wv;
+    h.each([&](const u32x4& v, int32_t i) {
+        double s = 0.0;
+#pragma unroll
+        for (int e = 0; e < h.E; ++e) s += wt(h.at(v, e), (uint32_t)(i + e));
+        s = group_sum<64>(s);
+        if (lane == 0) sm.seg[at] = s;
+        at += W;
+    });
+    team_sync<W>();
     const double seg = lane < R * W ? sm.seg[lane] : 0.0;
     const double incl = wave_scan(seg);
     if constexpr (!PART) {
@@ -895,16 +943,19 @@ __device__ __forceinline__ bool locate(SampleSmem<W>& sm, const Held<T, W, R>& h
     if (some == 0) return false;
     // (the last of any weight stands in where a rounding leaves the target unreached)
     const uint64_t past = __ballot(seg > 0.0 && incl > target);
-    const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
+    at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
     if (at % W == wv) {
         target = past ? target - (at ? lane_value(incl, at - 1) : 0.0) : __builtin_inf();
         const int ra = at / W;
-        double v = s[0];
         u32x4 q = h.q[0];
 #pragma unroll
-        for (int r = 1; r < R; ++r) {
-            v = ra == r ? s[r] : v;
-            q = ra == r ? h.q[r] : q;
+        for (int r = 1; r < R; ++r) q = ra == r ? h.q[r] : q;
+        const uint32_t i0 = (uint32_t)(h.first + ra * 64 * W * h.E);
+        double w[h.E], v = 0.0;
+#pragma unroll
+        for (int e = 0; e < h.E; ++e) {
+            w[e] = wt(h.at(q, e), i0 + e);
+            v += w[e];
         }
         const double run = wave_scan(v);
         const double prev = lane_before(run);
@@ -912,17 +963,15 @@ __device__ __forceinline__ bool locate(SampleSmem<W>& sm, const Held<T, W, R>& h
         const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(mine);
         if (lane == l) {
             const double rest = over ? target - prev : __builtin_inf();
-            const uint32_t i0 = h.index(0, 0) + (uint32_t)(ra * 64 * W * h.E);
             double sum = 0.0, w1 = 0.0;
             uint32_t i1 = 0;
             bool done = false;
 #pragma unroll
             for (int e = 0; e < h.E; ++e) {
-                const double w = wt(elem(q, e, (T*)nullptr), i0 + e);
-                sum += w;
-                if (w > 0.0 && !done) {
+                sum += w[e];
+                if (w[e] > 0.0 && !done) {
                     i1 = i0 + e;
-                    w1 = w;
+                    w1 = w[e];
                     done = sum > rest;
                 }
             }

@@ -6,6 +6,9 @@ namespace osm {
 
 constexpr int SM_W = 8;  // wavefronts of a workgroup that has a row, or a chunk, to itself
 constexpr int SM_BLOCK = 64 * SM_W;
+#ifndef OSM_SPW
+#define OSM_SPW 4
+#endif
 
 __device__ __forceinline__ void no_token(float* val, int32_t* idx) {
     *val = __builtin_nanf("");
@@ -26,15 +29,7 @@ __device__ __forceinline__ void held_row(SampleSmem<W>& sm, const T* x, int32_t 
         return;
     }
     if (r.greedy) {
-        uint32_t at = ~0u;
-#pragma unroll
-        for (int rr = 0; rr < R; ++rr)
-#pragma unroll
-            for (int e = 0; e < h.E; ++e) {
-                const uint32_t i = h.index(rr, e);
-                at = h.at(rr, e) == m && i < at ? i : at;
-            }
-        at = team_minimum(sm, at);
+        const uint32_t at = index_of(sm, h, m);
         if (tid == 0) {
             *idx = (int32_t)at;
             *val = 1.0f;
@@ -67,17 +62,16 @@ __device__ __forceinline__ void held_row(SampleSmem<W>& sm, const T* x, int32_t 
         team_sync<W>();
         const Filtered f = filter_row(sm, r, an, tail, (uint32_t)V - 1, false,
                                       [&](const Range& g) {
-#pragma unroll
-                                          for (int rr = 0; rr < R; ++rr) {
+                                          h.each([&](const u32x4& v, int32_t i) {
                                               bool any = false;
 #pragma unroll
                                               for (int e = 0; e < h.E; ++e)
-                                                  any |= near(g, h.at(rr, e));
-                                              if (__ballot(any) == 0) continue;
+                                                  any |= near(g, h.at(v, e));
+                                              if (__ballot(any) == 0) return;
 #pragma unroll
                                               for (int e = 0; e < h.E; ++e)
-                                                  append(sm, g, an, h.at(rr, e), h.index(rr, e));
-                                          }
+                                                  append(sm, g, an, h.at(v, e), (uint32_t)(i + e));
+                                          });
                                       });
         if (!f.ok) {
             sample_row(sm, src, r, val, idx);
@@ -108,7 +102,7 @@ __global__ __launch_bounds__(256) void sample_short(const SampleRows a) {
 }
 
 template <typename T, int R>
-__global__ __launch_bounds__(SM_BLOCK) void sample_rows(const SampleRows a) {
+__global__ __launch_bounds__(SM_BLOCK, 4) void sample_rows(const SampleRows a) {
     __shared__ SampleSmem<SM_W> sm;
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
         held_row<T, SM_W, R>(sm, static_cast<const T*>(a.x) + row * a.ld, (int32_t)a.V,
@@ -347,7 +341,7 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
 // rows are interleaved: rows end at 32 places in turn, and a row's chunks are on one
 // die, whose L2 has their sums.  Fewer than eight rows spread theirs over all dies.
 template <typename T, int R>
-__global__ __launch_bounds__(SM_BLOCK) void sample_split(const SampleRows a, const SampleSplit s) {
+__global__ __launch_bounds__(SM_BLOCK, OSM_SPW) void sample_split(const SampleRows a, const SampleSplit s) {
     constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
     __shared__ SampleSmem<SM_W> sm;
     const int tid = threadIdx.x;
@@ -368,27 +362,11 @@ __global__ __launch_bounds__(SM_BLOCK) void sample_split(const SampleRows a, con
         ChunkSum p{team_maximum(sm, h.maximum()), 0, 0.0};
         const bool live = p.m < __builtin_inff() && p.m > -__builtin_inff();
         if (r.greedy) {
-            uint32_t at = ~0u;
-#pragma unroll
-            for (int rr = 0; rr < R; ++rr)
-#pragma unroll
-                for (int e = 0; e < h.E; ++e) {
-                    const uint32_t i = h.index(rr, e);
-                    at = h.at(rr, e) == p.m && i < at ? i : at;
-                }
-            p.at = team_minimum(sm, at) + (uint32_t)i0;
+            p.at = index_of(sm, h, p.m) + (uint32_t)i0;
         } else if (live) {
             const Anchor an = anchor(p.m, r.c);
             if (!(r.k || r.p < 1.0 || r.q > 0.0)) {
-                double z = 0.0;
-#pragma unroll
-                for (int rr = 0; rr < R; ++rr)
-#pragma unroll
-                    for (int e = 0; e < h.E; ++e) {
-                        z += an.weight(h.at(rr, e));
-                        pair_end(e);
-                    }
-                p.z = team_sum(sm, z);
+                p.z = sum_weights(sm, h, an);
             } else if (!cold((double)p.m * r.c)) {
 #pragma unroll
                 for (int j = 0; j < PER; ++j) {

@@ -19,34 +19,39 @@ __device__ __forceinline__ double scalar(double c) {
     return c;
 }
 
-// 2^t for t <= 1023, to 7e-16: n + f = t with |f| <= 1/2, 2^f = 1 + f g(f) with g
+// 2^t for -2^30 < t <= 1023, to 7e-16: n + f = t with |f| <= 1/2, 2^f = 1 + f g(f) with g
 // the polynomial through (2^f - 1) / f at the ten Chebyshev nodes of [-1/2, 1/2]
-// (truncation 6e-16), so that 2^0 is 1 exactly.  Below 2^-1074, at
-// -inf and at NaN: 0.
-__device__ __forceinline__ double exp2_bounded(double t) {  // -2^30 < t
-    const double n = __builtin_rint(t);
-    const double f = t - n;
-    double g = 0x1.e5e9f548e5725p-28;
-    g = __builtin_fma(g, f, scalar(0x1.b6571de2f2351p-24));
-    g = __builtin_fma(g, f, scalar(0x1.62bfe46117445p-20));
-    g = __builtin_fma(g, f, scalar(0x1.ffcb76789860fp-17));
-    g = __builtin_fma(g, f, scalar(0x1.4309130378460p-13));
-    g = __builtin_fma(g, f, scalar(0x1.5d87fe908f88ap-10));
-    g = __builtin_fma(g, f, scalar(0x1.3b2ab6fba385fp-7));
-    g = __builtin_fma(g, f, scalar(0x1.c6b08d7044119p-5));
-    g = __builtin_fma(g, f, scalar(0x1.ebfbdff82c590p-3));
-    g = __builtin_fma(g, f, scalar(0x1.62e42fefa39f7p-1));
-    return __builtin_ldexp(__builtin_fma(g, f, 1.0), (int)n);
-}
+// (truncation 6e-16), so that 2^0 is 1 exactly.  Below 2^-1074: 0.  Made once and
+// handed to a loop, so that its constants stay where they are.
+struct Exp2 {
+    double k[10];
+    __device__ __forceinline__ static Exp2 make() {
+        return Exp2{{scalar(0x1.e5e9f548e5725p-28),
+                     scalar(0x1.b6571de2f2351p-24),
+                     scalar(0x1.62bfe46117445p-20),
+                     scalar(0x1.ffcb76789860fp-17),
+                     scalar(0x1.4309130378460p-13),
+                     scalar(0x1.5d87fe908f88ap-10),
+                     scalar(0x1.3b2ab6fba385fp-7),
+                     scalar(0x1.c6b08d7044119p-5),
+                     scalar(0x1.ebfbdff82c590p-3),
+                     scalar(0x1.62e42fefa39f7p-1)}};
+    }
+    __device__ __forceinline__ double operator()(double t) const {
+        const double n = __builtin_rint(t);
+        const double f = t - n;
+        double g = k[0];
+#pragma unroll
+        for (int i = 1; i < 10; ++i) g = __builtin_fma(g, f, k[i]);
+        return __builtin_ldexp(__builtin_fma(g, f, 1.0), (int)n);
+    }
+};
 
+__device__ __forceinline__ double exp2_bounded(double t) { return Exp2::make()(t); }
+
+// The same for any t <= 1023; 0 at -inf and at NaN.
 __device__ __forceinline__ double exp2_wide(double t) {
     return exp2_bounded(__builtin_fmax(t, -1100.0));
-}
-
-// Ends a pair of a loop's terms for the scheduler: unrolled loops of binary64 exponentials
-// that it may interleave take twice the registers for no time.
-__device__ __forceinline__ void pair_end(int j) {
-    if (j & 1) __builtin_amdgcn_sched_barrier(0);
 }
 
 // Butterfly operands (md.hpp) of a 64-bit value.
