@@ -60,8 +60,6 @@ struct SampleSmem {
         uint64_t bins[BINS];    // own histograms
         double seg[BINS];
     };
-    float lx[SampleShape<W>::CAP];     // the cut's bin: values and indices
-    uint32_t li[SampleShape<W>::CAP];
     uint64_t wave64[W];
     double waved[W];
     float wavef[W];
@@ -71,6 +69,12 @@ struct SampleSmem {
     int found, n;
     uint64_t above, here;
     double base;
+};
+
+template <int W>
+struct ListSmem : SampleSmem<W> {
+    float lx[SampleShape<W>::CAP];  // the cut's bin: values and indices
+    uint32_t li[SampleShape<W>::CAP];
 };
 
 // What a row asks for.
@@ -632,7 +636,7 @@ __device__ __forceinline__ bool near(const Range& g, float x) { return x >= g.x0
 
 // Appends x to the list if its bin is in the range; all lanes call.
 template <int W>
-__device__ __forceinline__ void append(SampleSmem<W>& sm, const Range& g, const Anchor& an,
+__device__ __forceinline__ void append(ListSmem<W>& sm, const Range& g, const Anchor& an,
                                        float x, uint32_t i) {
     bool in = near(g, x);
     if (__ballot(in) == 0) return;
@@ -653,7 +657,7 @@ __device__ __forceinline__ void append(SampleSmem<W>& sm, const Range& g, const 
 // The cut behind the first `target` units (MASS: of weight, else elements) of the list's
 // kept elements, 1 <= target <= their sum.
 template <bool MASS, int W>
-__device__ __forceinline__ Cut list_cut(SampleSmem<W>& sm, int n, Cut cut, uint64_t target,
+__device__ __forceinline__ Cut list_cut(ListSmem<W>& sm, int n, Cut cut, uint64_t target,
                                         const Anchor& an, uint32_t last) {
     const auto units = [an](float x) { return fixed48(an.weight(x)); };
     if (n > 64) {
@@ -706,7 +710,7 @@ __device__ __forceinline__ uint64_t wave_total(uint64_t v) {
 
 // Sum of the list's kept weights, in units.
 template <int W>
-__device__ __forceinline__ uint64_t list_sum(SampleSmem<W>& sm, int n, Cut cut,
+__device__ __forceinline__ uint64_t list_sum(ListSmem<W>& sm, int n, Cut cut,
                                              const Anchor& an) {
     uint64_t s = 0;
     for (int j = threadIdx.x % (64 * W); j < n; j += 64 * W)
@@ -828,7 +832,7 @@ struct Filtered {
 // sums: whether the caller wants the list to hold every element whose bin is neither
 // kept nor dropped whole.
 template <int W, typename Gather>
-__device__ __forceinline__ Filtered filter_row(SampleSmem<W>& sm, const Rule& r, const Anchor& an,
+__device__ __forceinline__ Filtered filter_row(ListSmem<W>& sm, const Rule& r, const Anchor& an,
                                                bool tail, uint32_t last_index, bool sums,
                                                const Gather& gather) {
     constexpr int BINS = SampleShape<W>::BINS, CAP = SampleShape<W>::CAP;

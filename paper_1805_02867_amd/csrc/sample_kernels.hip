@@ -1,6 +1,8 @@
 // Kernels of softmax_sample (sample.hpp): rows held whole by a wavefront or a workgroup,
 // rows split into chunks, and rows streamed from memory.
-#include "sample.hpp"
+#include <type_traits>
+
+#include "sample_values.hpp"
 
 namespace osm {
 
@@ -15,12 +17,25 @@ __device__ __forceinline__ void no_token(float* val, int32_t* idx) {
     *idx = -1;
 }
 
+__device__ __forceinline__ SampleSmem<SM_W>& smem_of(ValueSmem& sm) { return sm.s; }
+template <int W>
+__device__ __forceinline__ SampleSmem<W>& smem_of(ListSmem<W>& sm) {
+    return sm;
+}
+
 // A row held by the team: loaded once.
+// (bfloat16 rows of a workgroup by their values, others by the bins of their weights)
+template <typename T, int W>
+using RowSmem = std::conditional_t<W == SM_W && std::is_same_v<T, bf16_t>, ValueSmem, ListSmem<W>>;
+
 template <typename T, int W, int R>
-__device__ __forceinline__ void held_row(SampleSmem<W>& sm, const T* x, int32_t V, const Rule& r,
+__device__ __forceinline__ void held_row(RowSmem<T, W>& rm, const T* x, int32_t V, const Rule& r,
                                          float* val, int32_t* idx) {
+    constexpr bool VALUES = std::is_same_v<RowSmem<T, W>, ValueSmem>;
+    SampleSmem<W>& sm = smem_of(rm);
     constexpr int THREADS = 64 * W, PER = SampleShape<W>::PER;
     const int tid = threadIdx.x % THREADS;
+    [[maybe_unused]] const int lane = tid & 63;
     Held<T, W, R> h;
     h.load(x, V);
     const float m = team_maximum(sm, h.maximum());
@@ -37,13 +52,35 @@ __device__ __forceinline__ void held_row(SampleSmem<W>& sm, const T* x, int32_t 
         return;
     }
     const RowSource<T> src{x, V};
-    if ((r.k || r.p < 1.0) && cold((double)m * r.c)) {
-        sample_row(sm, src, r, val, idx);
-        return;
-    }
     const Anchor an = anchor(m, r.c);
     Cut cut = no_cut();
-    if (r.k || r.p < 1.0) {
+    if constexpr (VALUES) {
+        if (r.k || r.p < 1.0) {
+            clear_values(rm);
+            __syncthreads();
+            add_values(rm, h, an);
+            __syncthreads();
+            const ClassSum cl = {lane == 0 ? rm.mid : 0, lane == 0 ? rm.tail : 0,
+                                 lane == 0 ? rm.mid_n : 0, lane == 0 ? rm.tail_n : 0};
+            const bool ok = values_end(
+                rm, r, an, 1, V, cl, lane == 0 ? 1.0 : 0.0, h,
+                [&](int, int p, uint32_t(&n)[VB_PER]) {
+#pragma unroll
+                    for (int j = 0; j < VB_PER; ++j)
+                        n[j] = rm.values[p < VB_SIDE ? VB_SIDE - 1 - p - j : p + j];
+                },
+                [](int) {}, val, idx);
+            if (!ok) {
+                __syncthreads();
+                sample_row(sm, src, r, val, idx);
+            }
+            return;
+        }
+    } else if (r.k || r.p < 1.0) {
+        if (cold((double)m * r.c)) {
+            sample_row(sm, src, r, val, idx);
+            return;
+        }
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             sm.mass[tid + j * THREADS] = 0;
@@ -60,7 +97,7 @@ __device__ __forceinline__ void held_row(SampleSmem<W>& sm, const T* x, int32_t 
         for (int j = 0; j < PER; ++j)
             sm.sums[tid + j * THREADS] = (double)sm.mass[tid + j * THREADS] * 0x1p-48;
         team_sync<W>();
-        const Filtered f = filter_row(sm, r, an, tail, (uint32_t)V - 1, false,
+        const Filtered f = filter_row(rm, r, an, tail, (uint32_t)V - 1, false,
                                       [&](const Range& g) {
                                           h.each([&](const u32x4& v, int32_t i) {
                                               bool any = false;
@@ -70,7 +107,7 @@ __device__ __forceinline__ void held_row(SampleSmem<W>& sm, const T* x, int32_t 
                                               if (__ballot(any) == 0) return;
 #pragma unroll
                                               for (int e = 0; e < h.E; ++e)
-                                                  append(sm, g, an, h.at(v, e), (uint32_t)(i + e));
+                                                  append(rm, g, an, h.at(v, e), (uint32_t)(i + e));
                                           });
                                       });
         if (!f.ok) {
@@ -92,7 +129,7 @@ constexpr int SM_SHORT = 1024;  // elements
 template <typename T>
 __global__ __launch_bounds__(256) void sample_short(const SampleRows a) {
     constexpr int R = SM_SHORT / 64 / Vec<T>::N;
-    __shared__ SampleSmem<1> sm[4];
+    __shared__ ListSmem<1> sm[4];
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int64_t row = (int64_t)blockIdx.x * 4 + wv; row < a.N; row += (int64_t)gridDim.x * 4) {
         held_row<T, 1, R>(sm[wv], static_cast<const T*>(a.x) + row * a.ld, (int32_t)a.V,
@@ -102,8 +139,8 @@ __global__ __launch_bounds__(256) void sample_short(const SampleRows a) {
 }
 
 template <typename T, int R>
-__global__ __launch_bounds__(SM_BLOCK, 4) void sample_rows(const SampleRows a) {
-    __shared__ SampleSmem<SM_W> sm;
+__global__ __launch_bounds__(SM_BLOCK) void sample_rows(const SampleRows a) {
+    __shared__ RowSmem<T, SM_W> sm;
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
         held_row<T, SM_W, R>(sm, static_cast<const T*>(a.x) + row * a.ld, (int32_t)a.V,
                              row_rule(a, row), a.vals + row, a.idx + row);
@@ -126,6 +163,8 @@ __global__ __launch_bounds__(SM_BLOCK) void sample_streamed(const SampleRows a) 
 // coherence point: its maximum, the index of that (greedy rows) or whether elements
 // of some weight lie below its histogram, and the sum of its weights relative to
 // its own anchor (rows without a filter) or its histograms.
+constexpr int SAMPLE_PART = 6;  // 64-bit words of a chunk: its sum, and its classes
+static_assert(VB_BINS * 2 == SampleShape<SM_W>::BINS * 8, "counts take the place of masses");
 struct ChunkSum {
     float m;
     uint32_t at;
@@ -147,21 +186,23 @@ __device__ __forceinline__ uint32_t get(const uint32_t* p) {
 
 // The row's end, by the workgroup that put its last chunk.
 template <typename T, int R>
-__device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows& a,
+__device__ __forceinline__ void split_end(RowSmem<T, SM_W>& rm, const SampleRows& a,
                                           const SampleSplit& s, const T* x, const Rule& r,
                                           const uint64_t* parts, const uint64_t* mass,
                                           const uint32_t* counts, float* val, int32_t* idx) {
     constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
     constexpr int SUB = SampleShape<SM_W>::SUB, E = Vec<T>::N;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, S = s.S;
+    constexpr bool VALUES = std::is_same_v<T, bf16_t>;
+    SampleSmem<SM_W>& sm = smem_of(rm);
     const RowSource<T> src{x, a.V};
     // every wavefront: chunk `lane`
     float mc = -__builtin_inff();
     uint32_t at = 0;
     double z = 0.0;
     if (lane < S) {
-        const uint64_t p0 = get(parts + 2 * lane);
-        z = __builtin_bit_cast(double, get(parts + 2 * lane + 1));
+        const uint64_t p0 = get(parts + SAMPLE_PART * lane);
+        z = __builtin_bit_cast(double, get(parts + SAMPLE_PART * lane + 1));
         mc = __uint_as_float((uint32_t)p0);
         at = (uint32_t)(p0 >> 32);
     }
@@ -181,6 +222,43 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
     // a chunk far below the row's maximum has no weight at all
     const bool none = mc == -__builtin_inff() || ((double)mc - (double)m) * r.c < -1100.0;
     const bool filtered = r.k || r.p < 1.0 || r.q > 0.0;
+    const double part = none ? 0.0 : exp2_wide(((double)mc - (double)m) * r.c);
+    if constexpr (VALUES) {
+        if (filtered) {
+            ClassSum cl = {0, 0, 0, 0};
+            if (lane < S) {
+                const uint64_t n = get(parts + SAMPLE_PART * lane + 4);
+                cl = {get(parts + SAMPLE_PART * lane + 2), get(parts + SAMPLE_PART * lane + 3),
+                      (uint32_t)n, (uint32_t)(n >> 32)};
+            }
+            Held<T, SM_W, R> h;
+            const bool ok =
+                __ballot(!none && value_base(mc) != value_base(m)) == 0 &&
+                values_end(
+                    rm, r, anchor(m, r.c), S, s.chunk, cl, part, h,
+                    [&](int c, int p, uint32_t(&n)[VB_PER]) {
+                        // 16 bits a bin, eight bins in two words; positive ones from the last
+                        const int b = p < VB_SIDE ? VB_SIDE - VB_PER - p : p;
+                        const uint64_t* at = mass + (int64_t)c * BINS + b / 4;
+                        const uint64_t q0 = get(at), q1 = get(at + 1);
+#pragma unroll
+                        for (int j = 0; j < VB_PER; ++j) {
+                            const int i = p < VB_SIDE ? VB_PER - 1 - j : j;
+                            n[j] = (uint32_t)((i < 4 ? q0 : q1) >> (i % 4 * 16)) & 0xFFFFu;
+                        }
+                    },
+                    [&](int c) {
+                        const int64_t i0 = (int64_t)c * s.chunk;
+                        h.load(x + i0, (int32_t)(a.V - i0 < s.chunk ? a.V - i0 : s.chunk));
+                    },
+                    val, idx);
+            if (!ok) {
+                __syncthreads();
+                sample_row(sm, src, r, val, idx);
+            }
+            return;
+        }
+    }
     // (the histograms leave out what is below 2^-64 of the largest weight; only a u at
     // the very ends of [0, 1] can fall there)
     const bool ends = r.u < 0x1p-30 || r.u > 1.0 - 0x1p-30;
@@ -191,12 +269,11 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
     const Anchor an = anchor(m, r.c);
     // bins of the row's histogram that its own starts below, and its weights' factor
     const int down = none || !filtered ? 0 : (int)(an.a - anchor(mc, r.c).a) * SUB;
-    const double part = none ? 0.0 : exp2_wide(((double)mc - (double)m) * r.c);
     Cut cut = no_cut();
     double kept = 0.0;  // of chunk `lane`
     if (!filtered) {
         kept = z * part;
-    } else {
+    } else if constexpr (!VALUES) {
         // the row's histograms
         bool tail = r.k && __ballot(lane < S && !none && at != 0) != 0;
         double sum[PER];
@@ -247,7 +324,7 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
         tail = team_minimum(sm, tail ? 0u : 1u) == 0;
         __syncthreads();
         const Filtered f = filter_row(
-            sm, r, an, tail, (uint32_t)a.V - 1, true, [&](const Range& g) {
+            rm, r, an, tail, (uint32_t)a.V - 1, true, [&](const Range& g) {
                 const int h = (int)(((uintptr_t)x & 15) / sizeof(T));
                 const int64_t vecs = (a.V + h + E - 1) / E;
                 for (int64_t v0 = 0; v0 < vecs; v0 += 4 * SM_BLOCK) {
@@ -275,7 +352,7 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
                         if (__ballot(any) == 0) continue;
 #pragma unroll
                         for (int e = 0; e < E; ++e)
-                            append(sm, g, an, v[e], (uint32_t)(i0[j] + e));
+                            append(rm, g, an, v[e], (uint32_t)(i0[j] + e));
                     }
                 }
             });
@@ -289,8 +366,8 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
         if (tid < 64) sm.chunk[tid] = 0;
         __syncthreads();
         for (int j = tid; j < n; j += SM_BLOCK) {
-            const float v = sm.lx[j];
-            const uint32_t i = sm.li[j];
+            const float v = rm.lx[j];
+            const uint32_t i = rm.li[j];
             const double w = an.weight(v);
             if (an.bin<SM_W>(an.t(v)) >= f.sure && cut.keeps(v, i) && w >= r.q)
                 add_bin(sm.chunk[i / (uint32_t)s.chunk], fixed48(w));
@@ -343,7 +420,8 @@ __device__ __forceinline__ void split_end(SampleSmem<SM_W>& sm, const SampleRows
 template <typename T, int R>
 __global__ __launch_bounds__(SM_BLOCK, OSM_SPW) void sample_split(const SampleRows a, const SampleSplit s) {
     constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
-    __shared__ SampleSmem<SM_W> sm;
+    __shared__ RowSmem<T, SM_W> rm;
+    SampleSmem<SM_W>& sm = smem_of(rm);
     const int tid = threadIdx.x;
     const unsigned S = (unsigned)s.S, b = blockIdx.x, group = (unsigned)s.group;
     const int64_t rel = (int64_t)(b / (group * S) * group + b % group);
@@ -352,7 +430,7 @@ __global__ __launch_bounds__(SM_BLOCK, OSM_SPW) void sample_split(const SampleRo
     const int64_t row = s.row0 + rel;
     const T* x = static_cast<const T*>(a.x) + row * a.ld;
     const Rule r = row_rule(a, row);
-    uint64_t* parts = s.parts + rel * s.S * 2;
+    uint64_t* parts = s.parts + rel * s.S * SAMPLE_PART;
     uint64_t* mass = s.mass + rel * s.S * BINS;
     uint32_t* counts = s.counts + rel * s.S * BINS;
     {
@@ -367,6 +445,23 @@ __global__ __launch_bounds__(SM_BLOCK, OSM_SPW) void sample_split(const SampleRo
             const Anchor an = anchor(p.m, r.c);
             if (!(r.k || r.p < 1.0 || r.q > 0.0)) {
                 p.z = sum_weights(sm, h, an);
+            } else if constexpr (std::is_same_v<T, bf16_t>) {
+                clear_values(rm);
+                __syncthreads();
+                add_values(rm, h, an);
+                __syncthreads();
+                // 16 bits a bin: a chunk has at most 2^15 elements
+                const uint32_t* v = rm.values + VB_PER * tid;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    put(mass + (int64_t)c * BINS + 2 * tid + j,
+                        (uint64_t)(v[4 * j + 2] | v[4 * j + 3] << 16) << 32 |
+                            (v[4 * j] | v[4 * j + 1] << 16));
+                if (tid == 0) {
+                    put(parts + SAMPLE_PART * c + 2, rm.mid);
+                    put(parts + SAMPLE_PART * c + 3, rm.tail);
+                    put(parts + SAMPLE_PART * c + 4, (uint64_t)rm.tail_n << 32 | rm.mid_n);
+                }
             } else if (!cold((double)p.m * r.c)) {
 #pragma unroll
                 for (int j = 0; j < PER; ++j) {
@@ -388,8 +483,8 @@ __global__ __launch_bounds__(SM_BLOCK, OSM_SPW) void sample_split(const SampleRo
             }
         }
         if (tid == 0) {
-            put(parts + 2 * c, (uint64_t)p.at << 32 | __float_as_uint(p.m));
-            put(parts + 2 * c + 1, __builtin_bit_cast(uint64_t, p.z));
+            put(parts + SAMPLE_PART * c, (uint64_t)p.at << 32 | __float_as_uint(p.m));
+            put(parts + SAMPLE_PART * c + 1, __builtin_bit_cast(uint64_t, p.z));
         }
     }
     // every store of the chunk has completed before the row's count moves
@@ -403,7 +498,7 @@ __global__ __launch_bounds__(SM_BLOCK, OSM_SPW) void sample_split(const SampleRo
     __syncthreads();
     if (done != s.S - 1) return;
     if (tid == 0) __hip_atomic_store(s.ctr + rel, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    split_end<T, R>(sm, a, s, x, r, parts, mass, counts, a.vals + row, a.idx + row);
+    split_end<T, R>(rm, a, s, x, r, parts, mass, counts, a.vals + row, a.idx + row);
 }
 
 // ------------------------------------------------------------------------ plan
@@ -445,7 +540,7 @@ SamplePlan sample_plan(int64_t N, int64_t V, int64_t ld, bool aligned, int dtype
 size_t sample_scratch_bytes(const SamplePlan& p) {
     if (p.S <= 1) return 0;
     constexpr size_t BINS = SampleShape<SM_W>::BINS;
-    return (size_t)p.rows * (size_t)p.S * (16 + 12 * BINS);
+    return (size_t)p.rows * (size_t)p.S * (8 * SAMPLE_PART + 12 * BINS);
 }
 
 template <typename T>
@@ -469,7 +564,7 @@ static hipError_t launch_sample_t(const SampleRows& a, const SamplePlan& p, void
     s.S = p.S;
     s.chunk = p.chunk;
     s.parts = static_cast<uint64_t*>(scratch);
-    s.mass = s.parts + p.rows * p.S * 2;
+    s.mass = s.parts + p.rows * p.S * SAMPLE_PART;
     s.counts = reinterpret_cast<uint32_t*>(s.mass + p.rows * p.S * BINS);
     s.ctr = ctr;
     for (s.row0 = 0; s.row0 < a.N; s.row0 += p.rows) {
