@@ -470,6 +470,13 @@ struct Held {
             for (int s = 0; s < STEP; ++s) q[R - STEP + s] = head[s];
         }
     }
+    // the registers turn by one vector
+    __device__ __forceinline__ void turn() {
+        const u32x4 head = q[0];
+#pragma unroll
+        for (int j = 0; j + 1 < R; ++j) q[j] = q[j + 1];
+        q[R - 1] = head;
+    }
     __device__ __forceinline__ static float at(const u32x4& v, int e) {
         return elem(v, e, (T*)nullptr);
     }
@@ -926,62 +933,69 @@ __device__ __forceinline__ bool locate(SampleSmem<W>& sm, Held<T, W, R>& h, cons
                                        int32_t* idx) {
     static_assert(R * W <= 64, "a lane a segment");
     const int lane = threadIdx.x & 63, wv = (threadIdx.x % (64 * W)) >> 6;
-    // segments of 64 vectors, in index order
-    int at = wv;
-    h.each([&](const u32x4& v, int32_t i) {
-        double s = 0.0;
-#pragma unroll
-        for (int e = 0; e < h.E; ++e) s += wt(h.at(v, e), (uint32_t)(i + e));
-        s = group_sum<64>(s);
-        if (lane == 0) sm.seg[at] = s;
-        at += W;
-    });
-    team_sync<W>();
-    const double seg = lane < R * W ? sm.seg[lane] : 0.0;
-    const double incl = wave_scan(seg);
-    if constexpr (!PART) {
-        total = lane_value(incl, 63);
-        target *= total;
-    }
-    const uint64_t some = __ballot(seg > 0.0);
-    if (some == 0) return false;
-    // (the last of any weight stands in where a rounding leaves the target unreached)
-    const uint64_t past = __ballot(seg > 0.0 && incl > target);
-    at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
-    if (at % W == wv) {
-        target = past ? target - (at ? lane_value(incl, at - 1) : 0.0) : __builtin_inf();
-        const int ra = at / W;
-        u32x4 q = h.q[0];
-#pragma unroll
-        for (int r = 1; r < R; ++r) q = ra == r ? h.q[r] : q;
-        const uint32_t i0 = (uint32_t)(h.first + ra * 64 * W * h.E);
-        double w[h.E], v = 0.0;
+    // segments of 64 vectors, in index order: their sums, then (the last turn) the weights
+    // in the one that the target falls into, by the wavefront that has it
+    u32x4 q = h.q[0];
+    uint32_t i0 = (uint32_t)h.first;
+    double w[h.E], v, found_sum = 0.0;
+    bool reached = false;
+    int turn = 0;
+#pragma unroll 1
+    for (;; ++turn) {
+        v = 0.0;
 #pragma unroll
         for (int e = 0; e < h.E; ++e) {
             w[e] = wt(h.at(q, e), i0 + e);
             v += w[e];
         }
-        const double run = wave_scan(v);
-        const double prev = lane_before(run);
-        const uint64_t mine = __ballot(v > 0.0), over = __ballot(v > 0.0 && run > target);
-        const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(mine);
-        if (lane == l) {
-            const double rest = over ? target - prev : __builtin_inf();
-            double sum = 0.0, w1 = 0.0;
-            uint32_t i1 = 0;
-            bool done = false;
-#pragma unroll
-            for (int e = 0; e < h.E; ++e) {
-                sum += w[e];
-                if (w[e] > 0.0 && !done) {
-                    i1 = i0 + e;
-                    w1 = w[e];
-                    done = sum > rest;
-                }
-            }
-            *idx = (int32_t)(base + i1);
-            *val = (float)(w1 / total);
+        if (turn == R) break;
+        const double s = group_sum<64>(v);
+        if (lane == 0) sm.seg[turn * W + wv] = s;
+        h.turn();
+        q = h.q[0];
+        i0 += 64 * W * h.E;
+        if (turn + 1 < R) continue;
+        team_sync<W>();
+        const double seg = lane < R * W ? sm.seg[lane] : 0.0;
+        const double incl = wave_scan(seg);
+        if constexpr (!PART) {
+            total = lane_value(incl, 63);
+            target *= total;
         }
+        const uint64_t some = __ballot(seg > 0.0);
+        if (some == 0) return false;
+        // (the last of any weight stands in where a rounding leaves the target unreached)
+        const uint64_t past = __ballot(seg > 0.0 && incl > target);
+        const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
+        if (at % W != wv) return true;
+        reached = past != 0;
+        found_sum = at ? lane_value(incl, at - 1) : 0.0;
+        for (int r = 0; r < at / W; ++r) h.turn();
+        q = h.q[0];
+        for (int r = at / W; r < R; ++r) h.turn();
+        i0 = (uint32_t)(h.first + at / W * 64 * W * h.E);
+    }
+    target = reached ? target - found_sum : __builtin_inf();
+    const double run = wave_scan(v);
+    const double prev = lane_before(run);
+    const uint64_t mine = __ballot(v > 0.0), over = __ballot(v > 0.0 && run > target);
+    const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(mine);
+    if (lane == l) {
+        const double rest = over ? target - prev : __builtin_inf();
+        double sum = 0.0, w1 = 0.0;
+        uint32_t i1 = 0;
+        bool done = false;
+#pragma unroll
+        for (int e = 0; e < h.E; ++e) {
+            sum += w[e];
+            if (w[e] > 0.0 && !done) {
+                i1 = i0 + e;
+                w1 = w[e];
+                done = sum > rest;
+            }
+        }
+        *idx = (int32_t)(base + i1);
+        *val = (float)(w1 / total);
     }
     return true;
 }

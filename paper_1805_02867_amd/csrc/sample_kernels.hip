@@ -23,13 +23,13 @@ __device__ __forceinline__ SampleSmem<W>& smem_of(ListSmem<W>& sm) {
     return sm;
 }
 
-// A row held by the team: loaded once.
+// A row held by the team: loaded once.  False: it has to be done the slow way.
 // (bfloat16 rows of a workgroup by their values, others by the bins of their weights)
 template <typename T, int W>
 using RowSmem = std::conditional_t<W == SM_W && std::is_same_v<T, bf16_t>, ValueSmem, ListSmem<W>>;
 
 template <typename T, int W, int R>
-__device__ __forceinline__ void held_row(RowSmem<T, W>& rm, const T* x, int32_t V, const Rule& r,
+__device__ __forceinline__ bool held_row(RowSmem<T, W>& rm, const T* x, int32_t V, const Rule& r,
                                          float* val, int32_t* idx) {
     constexpr bool VALUES = std::is_same_v<RowSmem<T, W>, ValueSmem>;
     SampleSmem<W>& sm = smem_of(rm);
@@ -41,7 +41,7 @@ __device__ __forceinline__ void held_row(RowSmem<T, W>& rm, const T* x, int32_t 
     const float m = team_maximum(sm, h.maximum());
     if (!(m < __builtin_inff()) || m == -__builtin_inff()) {
         if (tid == 0) no_token(val, idx);
-        return;
+        return true;
     }
     if (r.greedy) {
         const uint32_t at = index_of(sm, h, m);
@@ -49,9 +49,8 @@ __device__ __forceinline__ void held_row(RowSmem<T, W>& rm, const T* x, int32_t 
             *idx = (int32_t)at;
             *val = 1.0f;
         }
-        return;
+        return true;
     }
-    const RowSource<T> src{x, V};
     const Anchor an = anchor(m, r.c);
     Cut cut = no_cut();
     if constexpr (VALUES) {
@@ -62,7 +61,7 @@ __device__ __forceinline__ void held_row(RowSmem<T, W>& rm, const T* x, int32_t 
             __syncthreads();
             const ClassSum cl = {lane == 0 ? rm.mid : 0, lane == 0 ? rm.tail : 0,
                                  lane == 0 ? rm.mid_n : 0, lane == 0 ? rm.tail_n : 0};
-            const bool ok = values_end(
+            return values_end(
                 rm, r, an, 1, V, cl, lane == 0 ? 1.0 : 0.0, h,
                 [&](int, int p, uint32_t(&n)[VB_PER]) {
 #pragma unroll
@@ -70,17 +69,9 @@ __device__ __forceinline__ void held_row(RowSmem<T, W>& rm, const T* x, int32_t 
                         n[j] = rm.values[p < VB_SIDE ? VB_SIDE - 1 - p - j : p + j];
                 },
                 [](int) {}, val, idx);
-            if (!ok) {
-                __syncthreads();
-                sample_row(sm, src, r, val, idx);
-            }
-            return;
         }
     } else if (r.k || r.p < 1.0) {
-        if (cold((double)m * r.c)) {
-            sample_row(sm, src, r, val, idx);
-            return;
-        }
+        if (cold((double)m * r.c)) return false;
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             sm.mass[tid + j * THREADS] = 0;
@@ -110,13 +101,10 @@ __device__ __forceinline__ void held_row(RowSmem<T, W>& rm, const T* x, int32_t 
                                                   append(rm, g, an, h.at(v, e), (uint32_t)(i + e));
                                           });
                                       });
-        if (!f.ok) {
-            sample_row(sm, src, r, val, idx);
-            return;
-        }
+        if (!f.ok) return false;
         cut = f.cut;
     }
-    locate<false>(sm, h,
+    return locate<false>(sm, h,
                   [&](float v, uint32_t i) {
                       const double w = an.weight(v);
                       return cut.keeps(v, i) && w >= r.q ? w : 0.0;
@@ -132,18 +120,26 @@ __global__ __launch_bounds__(256) void sample_short(const SampleRows a) {
     __shared__ ListSmem<1> sm[4];
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     for (int64_t row = (int64_t)blockIdx.x * 4 + wv; row < a.N; row += (int64_t)gridDim.x * 4) {
-        held_row<T, 1, R>(sm[wv], static_cast<const T*>(a.x) + row * a.ld, (int32_t)a.V,
-                          row_rule(a, row), a.vals + row, a.idx + row);
+        const T* x = static_cast<const T*>(a.x) + row * a.ld;
+        const Rule r = row_rule(a, row);
+        if (!held_row<T, 1, R>(sm[wv], x, (int32_t)a.V, r, a.vals + row, a.idx + row)) {
+            wave_sync();
+            sample_row(smem_of(sm[wv]), RowSource<T>{x, a.V}, r, a.vals + row, a.idx + row);
+        }
         wave_sync();
     }
 }
 
 template <typename T, int R>
-__global__ __launch_bounds__(SM_BLOCK) void sample_rows(const SampleRows a) {
+__global__ __launch_bounds__(SM_BLOCK, 4) void sample_rows(const SampleRows a) {
     __shared__ RowSmem<T, SM_W> sm;
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
-        held_row<T, SM_W, R>(sm, static_cast<const T*>(a.x) + row * a.ld, (int32_t)a.V,
-                             row_rule(a, row), a.vals + row, a.idx + row);
+        const T* x = static_cast<const T*>(a.x) + row * a.ld;
+        const Rule r = row_rule(a, row);
+        if (!held_row<T, SM_W, R>(sm, x, (int32_t)a.V, r, a.vals + row, a.idx + row)) {
+            __syncthreads();
+            sample_row(smem_of(sm), RowSource<T>{x, a.V}, r, a.vals + row, a.idx + row);
+        }
         __syncthreads();
     }
 }
@@ -184,9 +180,10 @@ __device__ __forceinline__ uint32_t get(const uint32_t* p) {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// The row's end, by the workgroup that put its last chunk.
+// The row's end, by the workgroup that put its last chunk.  False: the row has to be done
+// the slow way.
 template <typename T, int R>
-__device__ __forceinline__ void split_end(RowSmem<T, SM_W>& rm, const SampleRows& a,
+__device__ __forceinline__ bool split_end(RowSmem<T, SM_W>& rm, const SampleRows& a,
                                           const SampleSplit& s, const T* x, const Rule& r,
                                           const uint64_t* parts, const uint64_t* mass,
                                           const uint32_t* counts, float* val, int32_t* idx) {
@@ -195,7 +192,6 @@ __device__ __forceinline__ void split_end(RowSmem<T, SM_W>& rm, const SampleRows
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, S = s.S;
     constexpr bool VALUES = std::is_same_v<T, bf16_t>;
     SampleSmem<SM_W>& sm = smem_of(rm);
-    const RowSource<T> src{x, a.V};
     // every wavefront: chunk `lane`
     float mc = -__builtin_inff();
     uint32_t at = 0;
@@ -209,7 +205,7 @@ __device__ __forceinline__ void split_end(RowSmem<T, SM_W>& rm, const SampleRows
     const float m = wave_maximum(mc);
     if (!(m < __builtin_inff()) || m == -__builtin_inff()) {
         if (tid == 0) no_token(val, idx);
-        return;
+        return true;
     }
     if (r.greedy) {
         const int c = __builtin_ctzll(__ballot(mc == m));
@@ -217,7 +213,7 @@ __device__ __forceinline__ void split_end(RowSmem<T, SM_W>& rm, const SampleRows
             *idx = (int32_t)at;
             *val = 1.0f;
         }
-        return;
+        return true;
     }
     // a chunk far below the row's maximum has no weight at all
     const bool none = mc == -__builtin_inff() || ((double)mc - (double)m) * r.c < -1100.0;
@@ -232,8 +228,7 @@ __device__ __forceinline__ void split_end(RowSmem<T, SM_W>& rm, const SampleRows
                       (uint32_t)n, (uint32_t)(n >> 32)};
             }
             Held<T, SM_W, R> h;
-            const bool ok =
-                __ballot(!none && value_base(mc) != value_base(m)) == 0 &&
+            return __ballot(!none && value_base(mc) != value_base(m)) == 0 &&
                 values_end(
                     rm, r, anchor(m, r.c), S, s.chunk, cl, part, h,
                     [&](int c, int p, uint32_t(&n)[VB_PER]) {
@@ -252,19 +247,13 @@ __device__ __forceinline__ void split_end(RowSmem<T, SM_W>& rm, const SampleRows
                         h.load(x + i0, (int32_t)(a.V - i0 < s.chunk ? a.V - i0 : s.chunk));
                     },
                     val, idx);
-            if (!ok) {
-                __syncthreads();
-                sample_row(sm, src, r, val, idx);
-            }
-            return;
         }
     }
     // (the histograms leave out what is below 2^-64 of the largest weight; only a u at
     // the very ends of [0, 1] can fall there)
     const bool ends = r.u < 0x1p-30 || r.u > 1.0 - 0x1p-30;
     if (filtered && (__ballot(!none && cold((double)mc * r.c)) != 0 || ends)) {
-        sample_row(sm, src, r, val, idx);
-        return;
+        return false;
     }
     const Anchor an = anchor(m, r.c);
     // bins of the row's histogram that its own starts below, and its weights' factor
@@ -356,10 +345,7 @@ __device__ __forceinline__ void split_end(RowSmem<T, SM_W>& rm, const SampleRows
                     }
                 }
             });
-        if (!f.ok) {
-            sample_row(sm, src, r, val, idx);
-            return;
-        }
+        if (!f.ok) return false;
         cut = f.cut;
         // the kept weights of each chunk: of the bins kept whole, and of the list
         const int n = f.sure < BINS - 1 ? sm.n : 0;
@@ -397,17 +383,13 @@ __device__ __forceinline__ void split_end(RowSmem<T, SM_W>& rm, const SampleRows
     Held<T, SM_W, R> h;
     h.load(x + i0, (int32_t)(a.V - i0 < s.chunk ? a.V - i0 : s.chunk));
     __syncthreads();
-    const bool found = locate<true>(sm, h,
+    return locate<true>(sm, h,
                                     [&](float v, uint32_t i) {
                                         const double w = an.weight(v);
                                         return cut.keeps(v, (uint32_t)i0 + i) && w >= r.q ? w
                                                                                             : 0.0;
                                     },
                                     rem, total, (uint32_t)i0, val, idx);
-    if (!found) {
-        __syncthreads();
-        sample_row(sm, src, r, val, idx);
-    }
 }
 
 // A chunk of a row a workgroup.  Workgroups go to the eight dies in turn, and there to
@@ -498,7 +480,9 @@ __global__ __launch_bounds__(SM_BLOCK, OSM_SPW) void sample_split(const SampleRo
     __syncthreads();
     if (done != s.S - 1) return;
     if (tid == 0) __hip_atomic_store(s.ctr + rel, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    split_end<T, R>(rm, a, s, x, r, parts, mass, counts, a.vals + row, a.idx + row);
+    if (split_end<T, R>(rm, a, s, x, r, parts, mass, counts, a.vals + row, a.idx + row)) return;
+    __syncthreads();
+    sample_row(sm, RowSource<T>{x, a.V}, r, a.vals + row, a.idx + row);
 }
 
 // ------------------------------------------------------------------------ plan

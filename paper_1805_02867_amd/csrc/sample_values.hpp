@@ -98,6 +98,31 @@ struct ClassSum {
     uint32_t mid_n, tail_n;
 };
 
+// A thread's bins, one after the other in a loop: f(number, weight, position).  The
+// registers turn (see Held::each): the end of a row runs once in a while, and what
+// bounds it is the fetching of its code, not its work.
+struct Bins {
+    uint32_t n[VB_PER];
+    double w[VB_PER];
+    template <typename F>
+    __device__ __forceinline__ void each(const F& f) {
+        int p = VB_PER * (int)threadIdx.x;
+#pragma unroll 1
+        for (int j = 0; j < VB_PER; ++j, ++p) {
+            f(n[0], w[0], p);
+            const uint32_t n0 = n[0];
+            const double w0 = w[0];
+#pragma unroll
+            for (int i = 0; i + 1 < VB_PER; ++i) {
+                n[i] = n[i + 1];
+                w[i] = w[i + 1];
+            }
+            n[VB_PER - 1] = n0;
+            w[VB_PER - 1] = w0;
+        }
+    }
+};
+
 // The row's end.  count8(c, p, n): the numbers of chunk c at positions p .. p + 7;
 // classes of chunk `lane`, whose maximum's weight in the row is `part`, in cl.
 // hold(c): makes h hold chunk c, from index c * chunk on.  False if the bins do not
@@ -111,14 +136,8 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
     auto& s = sm.s;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int base = value_base((float)an.m), p0 = VB_PER * tid;
-    // the bins of the row, their weights, and the classes
-    uint32_t n[VB_PER];
-    double w[VB_PER];
-#pragma unroll
-    for (int j = 0; j < VB_PER; ++j) n[j] = 0;
     constexpr int AT_ONCE = 4;  // chunks whose loads are in flight
-    for (int c0 = 0; c0 < S; c0 += AT_ONCE) {
-        uint32_t m[AT_ONCE][VB_PER];
+    const auto counts_of = [&](int c0, uint32_t(&m)[AT_ONCE][VB_PER]) {
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
 #pragma unroll
@@ -126,19 +145,27 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
             if (c0 + k < S && lane_value(part, c0 + k < S ? c0 + k : 0) > 0.0)
                 count8(c0 + k, p0, m[k]);
         }
+    };
+    // the bins of the row, their weights, and the classes
+    Bins bin;
+#pragma unroll
+    for (int j = 0; j < VB_PER; ++j) bin.n[j] = 0;
+#pragma unroll 1
+    for (int c0 = 0; c0 < S; c0 += AT_ONCE) {
+        uint32_t m[AT_ONCE][VB_PER];
+        counts_of(c0, m);
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k)
 #pragma unroll
-            for (int j = 0; j < VB_PER; ++j) n[j] += m[k][j];
+            for (int j = 0; j < VB_PER; ++j) bin.n[j] += m[k][j];
     }
     uint32_t count = 0;
     double mass = 0.0;
-#pragma unroll
-    for (int j = 0; j < VB_PER; ++j) {
-        w[j] = n[j] ? an.weight(position_value(p0 + j, base)) : 0.0;
-        count += n[j];
-        mass += (double)n[j] * w[j];
-    }
+    bin.each([&](uint32_t n, double& w, int p) {
+        w = n ? an.weight(position_value(p, base)) : 0.0;
+        count += n;
+        mass += (double)n * w;
+    });
     const double mid_c = (double)cl.mid * 0x1p-48 * part, tail_c = (double)cl.tail * 0x1p-48 * part;
     const double mid = group_sum<64>(mid_c), tail = group_sum<64>(tail_c);
     const uint32_t mid_n = lane_value(wave_scan(part > 0.0 ? cl.mid_n : 0u), 63);
@@ -156,13 +183,16 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
     if (tid == 0) s.found = VB_BINS;
     __syncthreads();
     uint32_t cbefore = cincl - count;
-    double mbefore = lane_before(mincl), window = 0.0;
+    double mbefore = lane_before(mincl), window = 0.0, positive = 0.0;
+    uint32_t bins_n = 0;
 #pragma unroll
     for (int v = 0; v < W; ++v) {
-        if (v < wv) {
-            cbefore += s.wave32[v];
-            mbefore += s.waved[v];
+        if (v == wv) {
+            cbefore += bins_n;
+            mbefore += window;
         }
+        if (v == W / 2) positive = window;
+        bins_n += s.wave32[v];
         window += s.waved[v];
     }
     const bool behind = tid >= VB_SIDE / VB_PER;
@@ -176,75 +206,62 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
     double all = window + mid + tail;
     if (r.k) {
         uint32_t b = cbefore;
-#pragma unroll
-        for (int j = 0; j < VB_PER; ++j) {
-            if ((int64_t)b < r.k && r.k <= (int64_t)b + n[j]) {
-                s.found = p0 + j;
+        double d = mbefore;
+        bin.each([&](uint32_t n, double w, int p) {
+            if ((int64_t)b < r.k && r.k <= (int64_t)b + n) {
+                s.found = p;
                 s.above = (uint64_t)(r.k - b);
+                s.base = d + (double)(r.k - b) * w;
             }
-            b += n[j];
-        }
+            b += n;
+            d += (double)n * w;
+        });
         __syncthreads();
         cut = s.found;
         if (cut < VB_BINS) {
             keep = (uint32_t)s.above;
-#pragma unroll
-            for (int j = 0; j < VB_PER; ++j) {
-                if (p0 + j == cut) {
-                    double a = mbefore;
-                    for (int i = 0; i < j; ++i) a += (double)n[i] * w[i];
-                    s.base = a + (double)keep * w[j];
-                }
-            }
+            all = s.base;
+        } else if (tail_n != 0 || r.k <= (int64_t)bins_n + mid_n) {
+            return false;  // not among the bins: in the middle class, or beyond the end
         }
-        __syncthreads();
-        // not among the bins: in the middle class, or beyond the end
-        const uint32_t bins_n = s.wave32[0] + s.wave32[1] + s.wave32[2] + s.wave32[3] + s.wave32[4] +
-                                s.wave32[5] + s.wave32[6] + s.wave32[7];
-        if (cut == VB_BINS && (tail_n != 0 || r.k <= (int64_t)bins_n + mid_n)) return false;
-        if (cut < VB_BINS) all = s.base;
         __syncthreads();
     }
     if (r.p < 1.0) {
         const double target = r.p * all;
         if (tid == 0) s.found = VB_BINS;
         __syncthreads();
-        double b = mbefore;
+        double b = mbefore, b_at = 0.0, w_at = 0.0;
+        uint32_t m_at = 0;
+        int at = VB_BINS;
         // (the lowest position that reaches the target; the class in between is not one)
-#pragma unroll
-        for (int j = 0; j < VB_PER; ++j) {
-            const uint32_t m = p0 + j < cut ? n[j] : p0 + j == cut ? keep : 0u;
-            const double a = b + (double)m * w[j];
-            if (m != 0 && a >= target) atomicMin(&s.found, p0 + j);
-            b = a;
-        }
-        __syncthreads();
-        const int at = s.found;
-        if (at < VB_BINS) {
-            b = mbefore;
-#pragma unroll
-            for (int j = 0; j < VB_PER; ++j) {
-                const uint32_t m = p0 + j < cut ? n[j] : p0 + j == cut ? keep : 0u;
-                if (p0 + j == at) {
-                    const double need = __builtin_ceil((target - b) / w[j]);
-                    uint32_t want = need >= 1.0 ? (need < (double)m ? (uint32_t)need : m) : 1;
-                    // (the quotient may be a step off: the smallest that reaches it)
-                    while (want > 1 && b + (double)(want - 1) * w[j] >= target) --want;
-                    while (want < m && b + (double)want * w[j] < target) ++want;
-                    s.above = want;
-                    s.base = b;
-                }
-                b += (double)m * w[j];
+        bin.each([&](uint32_t n, double w, int p) {
+            const uint32_t m = p < cut ? n : p == cut ? keep : 0u;
+            const double a = b + (double)m * w;
+            if (m != 0 && a >= target && at == VB_BINS) {
+                at = p;
+                b_at = b;
+                w_at = w;
+                m_at = m;
             }
+            b = a;
+        });
+        if (at < VB_BINS) atomicMin(&s.found, at);
+        __syncthreads();
+        const bool mine = at == s.found;
+        at = s.found;
+        if (mine && at < VB_BINS) {
+            const double need = __builtin_ceil((target - b_at) / w_at);
+            uint32_t want = need >= 1.0 ? (need < (double)m_at ? (uint32_t)need : m_at) : 1;
+            // (the quotient may be a step off: the smallest that reaches it)
+            if (want > 1 && b_at + (double)(want - 1) * w_at >= target) --want;
+            else if (want < m_at && b_at + (double)want * w_at < target) ++want;
+            s.above = want;
         }
         __syncthreads();
-        if (at >= VB_SIDE && cut >= VB_SIDE && mid_n != 0) {
-            // reached within the class that stands before it?
-            double pos = 0.0;  // of the positive bins
-#pragma unroll
-            for (int v = 0; v < W / 2; ++v) pos += s.waved[v];
-            if (pos < target && pos + mid >= target) return false;
-        }
+        // reached within the class that stands before it?
+        if (at >= VB_SIDE && cut >= VB_SIDE && mid_n != 0 && positive < target &&
+            positive + mid >= target)
+            return false;
         if (at < VB_BINS) {
             cut = at;
             keep = (uint32_t)s.above;
@@ -268,34 +285,32 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
         }
     }
     // the kept weights of each chunk
-#pragma unroll
-    for (int j = 0; j < VB_PER; ++j)
-        if (p0 + j > cut || w[j] < r.q) w[j] = 0.0;
+    bin.each([&](uint32_t, double& w, int p) { w = p > cut || w < r.q ? 0.0 : w; });
     const int at_cut = cut - p0;  // in [0, 8): this thread has the cut's bin
     uint32_t left = keep;
+#pragma unroll 1
     for (int c0 = 0; c0 < S; c0 += AT_ONCE) {
         uint32_t m[AT_ONCE][VB_PER];
-#pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k) {
-#pragma unroll
-            for (int j = 0; j < VB_PER; ++j) m[k][j] = 0;
-            if (c0 + k < S && lane_value(part, c0 + k < S ? c0 + k : 0) > 0.0)
-                count8(c0 + k, p0, m[k]);
-        }
+        counts_of(c0, m);
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             if (c0 + k >= S) break;
             double sum = 0.0;
+            uint32_t have = 0;
 #pragma unroll
             for (int j = 0; j < VB_PER; ++j) {
-                if (j == at_cut) {
-                    const uint32_t take = m[k][j] < left ? m[k][j] : left;
-                    sm.have[c0 + k] = m[k][j];
-                    sm.take[c0 + k] = take;
-                    left -= take;
-                    m[k][j] = take;
-                }
-                sum += (double)m[k][j] * w[j];
+                sum += (double)m[k][j] * bin.w[j];
+                have = j == at_cut ? m[k][j] : have;
+            }
+            if (at_cut >= 0 && at_cut < VB_PER) {
+                const uint32_t take = have < left ? have : left;
+                sm.have[c0 + k] = have;
+                sm.take[c0 + k] = take;
+                left -= take;
+                double w = 0.0;
+#pragma unroll
+                for (int j = 0; j < VB_PER; ++j) w = j == at_cut ? bin.w[j] : w;
+                sum -= (double)(have - take) * w;
             }
             sum = group_sum<64>(sum);
             if (lane == 0) sm.part[wv][c0 + k] = sum;
