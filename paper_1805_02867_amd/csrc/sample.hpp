@@ -924,8 +924,8 @@ __device__ __forceinline__ Filtered filter_row(ListSmem<W>& sm, const Rule& r, c
 }
 
 // The token of a row of which `h` holds all, or the part that the target falls into:
-// the first element, in index order, at which the running sum of wt(x, index) passes
-// the target u * sum (PART: rem, of a row whose sum is `total`).  base: added to
+// the first element, in index order, at which the running sum of the weights that
+// wt(vector, index of its first element, weights) gives passes the target u * sum (PART: rem, of a row whose sum is `total`).  base: added to
 // the index.  False if no element has a weight.
 template <bool PART, typename T, int W, int R, typename Wt>
 __device__ __forceinline__ bool locate(SampleSmem<W>& sm, Held<T, W, R>& h, const Wt& wt,
@@ -937,17 +937,16 @@ __device__ __forceinline__ bool locate(SampleSmem<W>& sm, Held<T, W, R>& h, cons
     // in the one that the target falls into, by the wavefront that has it
     u32x4 q = h.q[0];
     uint32_t i0 = (uint32_t)h.first;
-    double w[h.E], v, found_sum = 0.0;
+    constexpr int E = Held<T, W, R>::E;
+    double w[E], v, found_sum = 0.0;
     bool reached = false;
     int turn = 0;
 #pragma unroll 1
     for (;; ++turn) {
+        wt(q, i0, w);
         v = 0.0;
 #pragma unroll
-        for (int e = 0; e < h.E; ++e) {
-            w[e] = wt(h.at(q, e), i0 + e);
-            v += w[e];
-        }
+        for (int e = 0; e < h.E; ++e) v += w[e];
         if (turn == R) break;
         const double s = group_sum<64>(v);
         if (lane == 0) sm.seg[turn * W + wv] = s;

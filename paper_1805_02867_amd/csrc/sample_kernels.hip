@@ -105,9 +105,12 @@ __device__ __forceinline__ bool held_row(RowSmem<T, W>& rm, const T* x, int32_t 
         cut = f.cut;
     }
     return locate<false>(sm, h,
-                  [&](float v, uint32_t i) {
-                      const double w = an.weight(v);
-                      return cut.keeps(v, i) && w >= r.q ? w : 0.0;
+                  [&](const u32x4& v, uint32_t i, double(&w)[Vec<T>::N]) {
+#pragma unroll
+                      for (int e = 0; e < Vec<T>::N; ++e) {
+                          w[e] = an.weight(h.at(v, e));
+                          w[e] = cut.keeps(h.at(v, e), i + e) && w[e] >= r.q ? w[e] : 0.0;
+                      }
                   },
                   r.u, 0.0, 0, val, idx);
 }
@@ -384,12 +387,15 @@ __device__ __forceinline__ bool split_end(RowSmem<T, SM_W>& rm, const SampleRows
     h.load(x + i0, (int32_t)(a.V - i0 < s.chunk ? a.V - i0 : s.chunk));
     __syncthreads();
     return locate<true>(sm, h,
-                                    [&](float v, uint32_t i) {
-                                        const double w = an.weight(v);
-                                        return cut.keeps(v, (uint32_t)i0 + i) && w >= r.q ? w
-                                                                                            : 0.0;
-                                    },
-                                    rem, total, (uint32_t)i0, val, idx);
+                        [&](const u32x4& v, uint32_t i, double(&w)[E]) {
+#pragma unroll
+                            for (int e = 0; e < E; ++e) {
+                                w[e] = an.weight(h.at(v, e));
+                                const bool in = cut.keeps(h.at(v, e), (uint32_t)i0 + i + e);
+                                w[e] = in && w[e] >= r.q ? w[e] : 0.0;
+                            }
+                        },
+                        rem, total, (uint32_t)i0, val, idx);
 }
 
 // A chunk of a row a workgroup.  Workgroups go to the eight dies in turn, and there to

@@ -21,7 +21,9 @@ static_assert(VB_PER == 8, "eight bins are one 16-byte load of a chunk's counts"
 
 struct ValueSmem {
     SampleSmem<8> s;
-    uint32_t values[VB_BINS];  // of a pattern: sign * 2048 + (magnitude - base)
+    // of a pattern: sign * 2048 + (magnitude - base); one more for those outside
+    uint32_t values[VB_BINS + 1];
+    double weights[VB_BINS];   // what an element of a bin weighs, if it is kept
     uint64_t mid, tail;        // weights of the classes, in units of 2^-48
     uint32_t mid_n, tail_n;
     double part[8][64];        // kept weights by wavefront and chunk
@@ -30,6 +32,7 @@ struct ValueSmem {
     float val;
     int32_t idx;
 };
+
 
 // Magnitude (the pattern without its sign) of the first bins: 15 octaves below the octave
 // of m, or of 2^5 if that is larger, in steps of four octaves (so that the chunks of
@@ -56,36 +59,47 @@ __device__ __forceinline__ void clear_values(ValueSmem& sm) {
     }
 }
 
+// The bin of a pattern, VB_BINS outside of them.
+__device__ __forceinline__ uint32_t value_bin(uint32_t bits, uint32_t base) {
+    const uint32_t rel = (bits & 0x7FFFu) - base;
+    return rel < (uint32_t)VB_SIDE ? (bits >> 4 & (uint32_t)VB_SIDE) | rel : (uint32_t)VB_BINS;
+}
+
+__device__ __forceinline__ uint32_t pattern(const u32x4& v, int e) {
+    return e & 1 ? v[e >> 1] >> 16 : v[e >> 1] & 0xFFFFu;
+}
+
 // Adds the held elements.  Those whose weight vanishes count nowhere.
 template <int R>
 __device__ __forceinline__ void add_values(ValueSmem& sm, Held<bf16_t, 8, R>& h, const Anchor& an) {
-    const int base = value_base((float)an.m);
-    // magnitude of negative elements from which on the weight is below 2^-1100
+    const uint32_t base = (uint32_t)value_base((float)an.m);
+    // patterns of negative elements whose weight is below 2^-1100 (-inf: always)
     const float zero = (float)(an.m - 1100.0 / an.c);
-    const uint32_t gone = zero < 0.0f && an.c > 0.0 ? (__float_as_uint(-zero) >> 16) + 1
-                          : an.c > 0.0              ? 0u
-                                                    : 0x7F80u;
+    const uint32_t gone = 0x8000u + (!(an.c > 0.0)  ? 0x7F80u
+                                     : zero < 0.0f ? (__float_as_uint(-zero) >> 16) + 1
+                                                   : 0u);
     h.each([&](const u32x4& v, int32_t) {
         bool odd = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t bits = e & 1 ? v[e >> 1] >> 16 : v[e >> 1] & 0xFFFFu;
-            const uint32_t mag = bits & 0x7FFFu, rel = mag - (uint32_t)base;
-            if (rel < (uint32_t)VB_SIDE)
-                atomicAdd(&sm.values[(bits >> 15) * VB_SIDE + rel], 1u);
-            else
-                odd |= !(bits >= 0x8000u && mag >= gone);
+            const uint32_t bin = value_bin(pattern(v, e), base);
+            atomicAdd(&sm.values[bin], 1u);
+            odd |= bin == (uint32_t)VB_BINS;
         }
+        if (!__any(odd)) return;
+        odd = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            odd |= value_bin(pattern(v, e), base) == (uint32_t)VB_BINS && pattern(v, e) < gone;
         if (!__any(odd)) return;
 #pragma unroll 1
         for (int e = 0; e < 8; ++e) {
             const uint32_t word = e < 2 ? v[0] : e < 4 ? v[1] : e < 6 ? v[2] : v[3];
             const uint32_t bits = e & 1 ? word >> 16 : word & 0xFFFFu;
-            const uint32_t rel = (bits & 0x7FFFu) - (uint32_t)base;
             const double t = an.t(__uint_as_float(bits << 16));
-            if (rel < (uint32_t)VB_SIDE || t <= -1080.0) continue;
+            if (value_bin(bits, base) != (uint32_t)VB_BINS || t <= -1080.0) continue;
             const uint64_t w = fixed48(an.exp2(t));
-            const bool middle = (int)rel < 0;
+            const bool middle = (bits & 0x7FFFu) < base;
             add_bin(middle ? sm.mid : sm.tail, w);
             atomicAdd(middle ? &sm.mid_n : &sm.tail_n, 1u);
         }
@@ -285,7 +299,10 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
         }
     }
     // the kept weights of each chunk
-    bin.each([&](uint32_t, double& w, int p) { w = p > cut || w < r.q ? 0.0 : w; });
+    bin.each([&](uint32_t, double& w, int p) {
+        w = p > cut || w < r.q ? 0.0 : w;
+        sm.weights[p < VB_SIDE ? VB_SIDE - 1 - p : p] = w;
+    });
     const int at_cut = cut - p0;  // in [0, 8): this thread has the cut's bin
     uint32_t left = keep;
 #pragma unroll 1
@@ -330,29 +347,54 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
     const int c = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(some);
     const double rem = past ? target - (c ? lane_value(incl, c - 1) : 0.0) : __builtin_inf();
     hold(c);
-    // the chunk's cut: of the equal ones, the first `take`
+    // of the elements that hold the cut's value, the chunk's first `take`
     const uint32_t i0 = (uint32_t)(c * chunk);
-    Cut stop = no_cut();
+    uint32_t last = 0xFFFFFFFFu, partly = VB_BINS + 1;  // the bin that is cut within this chunk
+    __syncthreads();
     if (cut < VB_BINS) {
-        const float v = position_value(cut, base);
         const uint32_t take = sm.take[c], have = sm.have[c];
-        stop = take == have ? Cut{v, 0xFFFFFFFFu} : Cut{order_value(order_key(v) + 1), 0xFFFFFFFFu};
+        const int b = cut < VB_SIDE ? VB_SIDE - 1 - cut : cut;
+        if (take == 0 && tid == 0) sm.weights[b] = 0.0;
         if (take != 0 && take != have) {
-            __syncthreads();
-            const bool ok = locate<true>(s, h, [&](float x, uint32_t) { return x == v ? 1.0 : 0.0; },
-                                         (double)take - 0.5, 1.0, 0, &sm.val, &sm.idx);
+            const float v = position_value(cut, base);
+            const bool ok = locate<true>(
+                s, h,
+                [&](const u32x4& q, uint32_t, double(&y)[8]) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = h.at(q, e) == v ? 1.0 : 0.0;
+                },
+                (double)take - 0.5, 1.0, 0, &sm.val, &sm.idx);
             __syncthreads();
             if (!ok) return false;
-            stop = Cut{v, (uint32_t)sm.idx};
+            last = (uint32_t)sm.idx;
+            partly = (uint32_t)b;
         }
     }
     __syncthreads();
-    return locate<true>(s, h,
-                        [&](float x, uint32_t i) {
-                            const double y = an.weight(x);
-                            return stop.keeps(x, i) && y >= r.q ? y : 0.0;
-                        },
-                        rem, total, i0, val, idx);
+    const bool classes = mid_stays || tail_stays;
+    return locate<true>(
+        s, h,
+        [&](const u32x4& q, uint32_t i, double(&y)[8]) {
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t b = value_bin(pattern(q, e), (uint32_t)base);
+                const bool in = b < (uint32_t)VB_BINS && !(b == partly && i + e > last);
+                const double x = sm.weights[b < (uint32_t)VB_BINS ? b : 0];
+                y[e] = in ? x : 0.0;
+                odd |= b == (uint32_t)VB_BINS;
+            }
+            if (classes && __any(odd)) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t p = pattern(q, e);
+                    const bool of = (p & 0x7FFFu) < (uint32_t)base ? mid_stays : tail_stays;
+                    if (of && value_bin(p, (uint32_t)base) == (uint32_t)VB_BINS)
+                        y[e] = an.weight(h.at(q, e));
+                }
+            }
+        },
+        rem, total, i0, val, idx);
 }
 
 }  // namespace osm
