@@ -32,15 +32,6 @@
 
 namespace osm {
 
-#ifndef OSM_ROUTE_BLOCKS
-#define OSM_ROUTE_BLOCKS 4
-#endif
-#ifndef OSM_ROUTE_EACH
-#define OSM_ROUTE_EACH 8
-#endif
-#ifndef OSM_ROUTE_EACH_BWD
-#define OSM_ROUTE_EACH_BWD 4
-#endif
 constexpr int RT_BLOCK = 256;
 constexpr int RT_WAVES = RT_BLOCK / 64;
 
@@ -622,7 +613,7 @@ hipError_t launch_route_r(const RouteRows& a, unsigned blocks, hipStream_t st) {
 template <typename T, bool BWD, int LANES, int VEC>
 hipError_t launch_route_l(const RouteRows& a, hipStream_t st) {
     const int64_t want = (a.N + RT_WAVES * (64 / LANES) - 1) / (RT_WAVES * (64 / LANES));
-    const int64_t most = (int64_t)a.cus * OSM_ROUTE_BLOCKS;
+    const int64_t most = (int64_t)a.cus * (BWD ? 5 : 4);
     const unsigned blocks = (unsigned)(want < most ? want : most);
     const int r = (a.E + LANES - 1) / LANES;
     if constexpr (VEC == 1) {
@@ -643,7 +634,10 @@ hipError_t launch_route_t(const RouteRows& a, hipStream_t st) {
                      a.E >= 32;
 #define OSM_LANES(L) \
     return vec ? launch_route_l<T, BWD, L, 4>(a, st) : launch_route_l<T, BWD, L, 1>(a, st)
-    switch (route_lanes(a, BWD ? OSM_ROUTE_EACH_BWD : OSM_ROUTE_EACH)) {
+    // eight experts a lane once the batch fills the chip: the steps over the lanes then serve
+    // twice as many rows (16384 x 256 binary32: 26.5 us, with four 36.9; the gradient 10.8 and
+    // 14.4); else four (16 x 64: 3.8 and 4.3)
+    switch (route_lanes(a, a.N * a.E >= (int64_t)a.cus * 4096 ? 8 : 4)) {
         case 8: OSM_LANES(8);
         case 16: OSM_LANES(16);
         case 32: OSM_LANES(32);

@@ -44,8 +44,8 @@ struct SampleShape {
     static constexpr int BINS = 1 << LOG_BINS;
     static constexpr int SUB = BINS / 64;
     static constexpr int PER = BINS / THREADS;  // bins a thread scans
-    // elements of a cut's bin that are held; a team of one holds its whole row
-    static constexpr int CAP = W == 1 ? 1024 : 3840;
+    // elements of a cut's bin that are held
+    static constexpr int CAP = W == 1 ? 512 : 3840;
 };
 
 template <int W>
@@ -64,8 +64,9 @@ struct SampleSmem {
     double waved[W];
     float wavef[W];
     uint32_t wave32[W];
-    uint64_t chunk[64];  // (split rows) kept weights of each chunk: of the list,
-    double whole[64];  // and of the bins kept whole
+    // (split rows) kept weights of each chunk: of the list, and of the bins kept whole
+    uint64_t chunk[W > 1 ? 64 : 1];
+    double whole[W > 1 ? 64 : 1];
     int found, n;
     uint64_t above, here;
     double base;
@@ -601,10 +602,10 @@ template <typename T, int W, int R>
 __device__ __forceinline__ double sum_weights(SampleSmem<W>& sm, Held<T, W, R>& h,
                                               const Anchor& an) {
     double z = 0.0;
-    h.each([&](const u32x4& v, int32_t) {
 #pragma unroll
-        for (int e = 0; e < h.E; ++e) z += an.weight(h.at(v, e));
-    });
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int e = 0; e < h.E; ++e) z += an.weight(h.at(h.q[r], e));
     return team_sum(sm, z);
 }
 
@@ -848,6 +849,7 @@ __device__ __forceinline__ Filtered filter_row(ListSmem<W>& sm, const Rule& r, c
     int held0 = 0, held1 = -1, n = 0;  // bins whose elements are in the list
     double extra = 0.0;
     int limit = BINS - 1;
+    const double log_q = r.q > 0.0 ? (double)__builtin_log2f((float)r.q) : -1100.0;
     // one after the other: top-k, top-p, min-p; each wants the elements of some bins
 #pragma unroll 1
     for (int step = 0; step < 3; ++step) {
@@ -873,12 +875,14 @@ __device__ __forceinline__ Filtered filter_row(ListSmem<W>& sm, const Rule& r, c
             if (!(r.p < 1.0)) continue;
             double all;
             const int b = find_mass(sm, limit, extra, r.p, &all, &need);
+            // (min-p alone cuts where its bin is clearly before this one)
+            if (b < BINS && an.bin<W>(log_q) + 1 < b) continue;
             if (b < BINS) lo = hi = b;
             else if (limit == BINS - 1) continue;  // (a rounding: nothing to cut off)
         } else {
             if (!sums) break;
             if (r.q > 0.0) {  // w >= q, somewhere in the bins around that
-                const int b = an.bin<W>((double)__builtin_log2f((float)r.q));
+                const int b = an.bin<W>(log_q);
                 f.sure = b - 1 < f.sure ? (b > 1 ? b - 1 : 0) : f.sure;
                 f.last = b + 1 < f.last ? b + 1 : f.last;
                 f.sure = f.sure < f.last ? f.sure : f.last;

@@ -8,9 +8,6 @@ namespace osm {
 
 constexpr int SM_W = 8;  // wavefronts of a workgroup that has a row, or a chunk, to itself
 constexpr int SM_BLOCK = 64 * SM_W;
-#ifndef OSM_SPW
-#define OSM_SPW 4
-#endif
 
 __device__ __forceinline__ void no_token(float* val, int32_t* idx) {
     *val = __builtin_nanf("");
@@ -18,6 +15,7 @@ __device__ __forceinline__ void no_token(float* val, int32_t* idx) {
 }
 
 __device__ __forceinline__ SampleSmem<SM_W>& smem_of(ValueSmem& sm) { return sm.s; }
+__device__ __forceinline__ SampleSmem<SM_W>& smem_of(SampleSmem<SM_W>& sm) { return sm; }
 template <int W>
 __device__ __forceinline__ SampleSmem<W>& smem_of(ListSmem<W>& sm) {
     return sm;
@@ -27,6 +25,8 @@ __device__ __forceinline__ SampleSmem<W>& smem_of(ListSmem<W>& sm) {
 // (bfloat16 rows of a workgroup by their values, others by the bins of their weights)
 template <typename T, int W>
 using RowSmem = std::conditional_t<W == SM_W && std::is_same_v<T, bf16_t>, ValueSmem, ListSmem<W>>;
+template <typename T, bool FILTERS>
+using SplitSmem = std::conditional_t<FILTERS, RowSmem<T, SM_W>, SampleSmem<SM_W>>;
 
 template <typename T, int W, int R>
 __device__ __forceinline__ bool held_row(RowSmem<T, W>& rm, const T* x, int32_t V, const Rule& r,
@@ -118,7 +118,7 @@ __device__ __forceinline__ bool held_row(RowSmem<T, W>& rm, const T* x, int32_t 
 // Short rows, a wavefront each.
 constexpr int SM_SHORT = 1024;  // elements
 template <typename T>
-__global__ __launch_bounds__(256) void sample_short(const SampleRows a) {
+__global__ __launch_bounds__(256, 4) void sample_short(const SampleRows a) {
     constexpr int R = SM_SHORT / 64 / Vec<T>::N;
     __shared__ ListSmem<1> sm[4];
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -185,15 +185,15 @@ __device__ __forceinline__ uint32_t get(const uint32_t* p) {
 
 // The row's end, by the workgroup that put its last chunk.  False: the row has to be done
 // the slow way.
-template <typename T, int R>
-__device__ __forceinline__ bool split_end(RowSmem<T, SM_W>& rm, const SampleRows& a,
+template <typename T, int R, bool FILTERS>
+__device__ __forceinline__ bool split_end(SplitSmem<T, FILTERS>& rm, const SampleRows& a,
                                           const SampleSplit& s, const T* x, const Rule& r,
                                           const uint64_t* parts, const uint64_t* mass,
                                           const uint32_t* counts, float* val, int32_t* idx) {
     constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
     constexpr int SUB = SampleShape<SM_W>::SUB, E = Vec<T>::N;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, S = s.S;
-    constexpr bool VALUES = std::is_same_v<T, bf16_t>;
+    constexpr bool VALUES = FILTERS && std::is_same_v<T, bf16_t>;
     SampleSmem<SM_W>& sm = smem_of(rm);
     // every wavefront: chunk `lane`
     float mc = -__builtin_inff();
@@ -220,7 +220,7 @@ __device__ __forceinline__ bool split_end(RowSmem<T, SM_W>& rm, const SampleRows
     }
     // a chunk far below the row's maximum has no weight at all
     const bool none = mc == -__builtin_inff() || ((double)mc - (double)m) * r.c < -1100.0;
-    const bool filtered = r.k || r.p < 1.0 || r.q > 0.0;
+    const bool filtered = FILTERS && (r.k || r.p < 1.0 || r.q > 0.0);
     const double part = none ? 0.0 : exp2_wide(((double)mc - (double)m) * r.c);
     if constexpr (VALUES) {
         if (filtered) {
@@ -265,7 +265,7 @@ __device__ __forceinline__ bool split_end(RowSmem<T, SM_W>& rm, const SampleRows
     double kept = 0.0;  // of chunk `lane`
     if (!filtered) {
         kept = z * part;
-    } else if constexpr (!VALUES) {
+    } else if constexpr (FILTERS && !VALUES) {
         // the row's histograms
         bool tail = r.k && __ballot(lane < S && !none && at != 0) != 0;
         double sum[PER];
@@ -319,32 +319,36 @@ __device__ __forceinline__ bool split_end(RowSmem<T, SM_W>& rm, const SampleRows
             rm, r, an, tail, (uint32_t)a.V - 1, true, [&](const Range& g) {
                 const int h = (int)(((uintptr_t)x & 15) / sizeof(T));
                 const int64_t vecs = (a.V + h + E - 1) / E;
-                for (int64_t v0 = 0; v0 < vecs; v0 += 4 * SM_BLOCK) {
-                    u32x4 q[4];
-                    int64_t i0[4];
+                constexpr int AT_ONCE = 8;
+                for (int64_t v0 = 0; v0 < vecs; v0 += AT_ONCE * SM_BLOCK) {
+                    u32x4 q[AT_ONCE];
+                    int64_t i0 = (v0 + tid) * E - h;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        i0[j] = (v0 + j * SM_BLOCK + tid) * E - h;
-                        if (i0[j] >= 0 && i0[j] + E <= a.V)
-                            q[j] = *reinterpret_cast<const u32x4*>(x + i0[j]);
+                    for (int j = 0; j < AT_ONCE; ++j) {
+                        const int64_t i = i0 + j * SM_BLOCK * E;
+                        if (i >= 0 && i + E <= a.V) q[j] = *reinterpret_cast<const u32x4*>(x + i);
                     }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const bool whole = i0[j] >= 0 && i0[j] + E <= a.V;
+#pragma unroll 1
+                    for (int j = 0; j < AT_ONCE; ++j) {
+                        const bool whole = i0 >= 0 && i0 + E <= a.V;
                         float v[E];
                         bool any = false;
 #pragma unroll
                         for (int e = 0; e < E; ++e) {
-                            const int64_t i = i0[j] + e;
-                            v[e] = whole                ? elem(q[j], e, (T*)nullptr)
+                            const int64_t i = i0 + e;
+                            v[e] = whole                ? elem(q[0], e, (T*)nullptr)
                                    : i >= 0 && i < a.V ? load1(x + i)
                                                        : -__builtin_inff();
                             any |= near(g, v[e]);
                         }
-                        if (__ballot(any) == 0) continue;
+                        if (__ballot(any) != 0) {
 #pragma unroll
-                        for (int e = 0; e < E; ++e)
-                            append(rm, g, an, v[e], (uint32_t)(i0[j] + e));
+                            for (int e = 0; e < E; ++e)
+                                append(rm, g, an, v[e], (uint32_t)(i0 + e));
+                        }
+#pragma unroll
+                        for (int k = 0; k + 1 < AT_ONCE; ++k) q[k] = q[k + 1];
+                        i0 += SM_BLOCK * E;
                     }
                 }
             });
@@ -405,10 +409,11 @@ __device__ __forceinline__ bool split_end(RowSmem<T, SM_W>& rm, const SampleRows
 // 128256 bfloat16, four chunks a row: a fifth of the chip busy).  So the chunks of 32
 // rows are interleaved: rows end at 32 places in turn, and a row's chunks are on one
 // die, whose L2 has their sums.  Fewer than eight rows spread theirs over all dies.
-template <typename T, int R>
-__global__ __launch_bounds__(SM_BLOCK, OSM_SPW) void sample_split(const SampleRows a, const SampleSplit s) {
+// Without FILTERS every row draws from its whole distribution (or takes its maximum).
+template <typename T, int R, bool FILTERS>
+__global__ __launch_bounds__(SM_BLOCK, FILTERS ? 4 : 6) void sample_split(const SampleRows a, const SampleSplit s) {
     constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
-    __shared__ RowSmem<T, SM_W> rm;
+    __shared__ SplitSmem<T, FILTERS> rm;
     SampleSmem<SM_W>& sm = smem_of(rm);
     const int tid = threadIdx.x;
     const unsigned S = (unsigned)s.S, b = blockIdx.x, group = (unsigned)s.group;
@@ -431,8 +436,9 @@ __global__ __launch_bounds__(SM_BLOCK, OSM_SPW) void sample_split(const SampleRo
             p.at = index_of(sm, h, p.m) + (uint32_t)i0;
         } else if (live) {
             const Anchor an = anchor(p.m, r.c);
-            if (!(r.k || r.p < 1.0 || r.q > 0.0)) {
+            if (!FILTERS || !(r.k || r.p < 1.0 || r.q > 0.0)) {
                 p.z = sum_weights(sm, h, an);
+            } else if constexpr (!FILTERS) {
             } else if constexpr (std::is_same_v<T, bf16_t>) {
                 clear_values(rm);
                 __syncthreads();
@@ -486,9 +492,13 @@ __global__ __launch_bounds__(SM_BLOCK, OSM_SPW) void sample_split(const SampleRo
     __syncthreads();
     if (done != s.S - 1) return;
     if (tid == 0) __hip_atomic_store(s.ctr + rel, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (split_end<T, R>(rm, a, s, x, r, parts, mass, counts, a.vals + row, a.idx + row)) return;
-    __syncthreads();
-    sample_row(sm, RowSource<T>{x, a.V}, r, a.vals + row, a.idx + row);
+    const bool ok =
+        split_end<T, R, FILTERS>(rm, a, s, x, r, parts, mass, counts, a.vals + row, a.idx + row);
+    if constexpr (FILTERS) {  // (without filters the histograms have nothing to decide)
+        if (ok) return;
+        __syncthreads();
+        sample_row(sm, RowSource<T>{x, a.V}, r, a.vals + row, a.idx + row);
+    }
 }
 
 // ------------------------------------------------------------------------ plan
@@ -508,23 +518,32 @@ SamplePlan sample_plan(int64_t N, int64_t V, int64_t ld, bool aligned, int dtype
     const int64_t one = (int64_t)SM_BLOCK * E;  // a vector a lane
     if (room <= SM_SHORT) return {0, 1, V, 1};
     if (room <= 2 * one) return {2, 1, V, 1};
-    // chunks of whole vectors, at most eight a lane; with few rows more of them, of at
-    // least two vectors a lane
-    const int64_t least = (V + 8 * one - E - 1) / (8 * one - E);
+    // Chunks of whole vectors, at most four a lane: with eight the kernels take so many
+    // registers that half as many workgroups fit on a CU (256 x 128256 binary32 without
+    // filters 61.1 us, with four 52.7); eight where a row would have too many chunks.  Fewer
+    // rows than fill the chip are split further, into up to four chunks, whose sums the
+    // row's end has in flight at once (33 x 50257 binary32 top-p and min-p: 38.9 us with
+    // four, 43.7 with eight, 47.0 with twelve).
+    int64_t R = 4;
+    int64_t least = (V + R * one - E - 1) / (R * one - E);
+    if (least > kSplitMax) {
+        R = 8;
+        least = (V + R * one - E - 1) / (R * one - E);
+    }
     int64_t S = 2 * (int64_t)cus / (N > 0 ? N : 1);
-    const int64_t most = V / (2 * one);
-    S = S < 16 ? S : 16;
+    const int64_t most = V / one;
+    S = S < 4 ? S : 4;
     S = S < most ? S : most;
     S = S > least ? S : least;
     if (S > kSplitMax) return {-1, 1, V, 1};
-    if (S <= 1) return {8, 1, V, 1};
+    if (S <= 1) return {4, 1, V, 1};
     int64_t chunk = (V + S - 1) / S;
     chunk = (chunk + E - 1) / E * E;
     S = (V + chunk - 1) / chunk;
-    const int R = chunk + E <= 2 * one ? 2 : chunk + E <= 4 * one ? 4 : 8;
+    R = chunk + E <= 2 * one ? 2 : R;
     int64_t rows = kSplitChunks / S;
     rows = rows < N ? rows : N;
-    return {R, (int)S, chunk, rows > 0 ? rows : 1};
+    return {(int)R, (int)S, chunk, rows > 0 ? rows : 1};
 }
 
 size_t sample_scratch_bytes(const SamplePlan& p) {
@@ -544,12 +563,14 @@ static hipError_t launch_sample_t(const SampleRows& a, const SamplePlan& p, void
         else if (p.R == 2)
             hipLaunchKernelGGL((sample_rows<T, 2>), blocks(a.N), dim3(SM_BLOCK), 0, st, a);
         else if (p.R > 0)
-            hipLaunchKernelGGL((sample_rows<T, 8>), blocks(a.N), dim3(SM_BLOCK), 0, st, a);
+            hipLaunchKernelGGL((sample_rows<T, 4>), blocks(a.N), dim3(SM_BLOCK), 0, st, a);
         else
             hipLaunchKernelGGL(sample_streamed<T>, blocks(a.N), dim3(SM_BLOCK), 0, st, a);
         return hipGetLastError();
     }
     constexpr int64_t BINS = SampleShape<SM_W>::BINS;
+    const bool filters = a.top_k || a.top_p || a.min_p || (a.top_k_all > 0 && a.top_k_all < a.V) ||
+                         a.top_p_all < 1.0f || a.min_p_all > 0.0f;
     SampleSplit s;
     s.S = p.S;
     s.chunk = p.chunk;
@@ -562,9 +583,14 @@ static hipError_t launch_sample_t(const SampleRows& a, const SamplePlan& p, void
         s.rows = n;
         s.group = n < 8 ? 1 : n < 32 ? 8 : 32;
         const dim3 grid((unsigned)((n + s.group - 1) / s.group * s.group * p.S)), block(SM_BLOCK);
-        if (p.R == 2) hipLaunchKernelGGL((sample_split<T, 2>), grid, block, 0, st, a, s);
-        else if (p.R == 4) hipLaunchKernelGGL((sample_split<T, 4>), grid, block, 0, st, a, s);
-        else hipLaunchKernelGGL((sample_split<T, 8>), grid, block, 0, st, a, s);
+        const auto launch = [&](auto filters) {
+            constexpr bool F = decltype(filters)::value;
+            if (p.R == 2) hipLaunchKernelGGL((sample_split<T, 2, F>), grid, block, 0, st, a, s);
+            else if (p.R == 4) hipLaunchKernelGGL((sample_split<T, 4, F>), grid, block, 0, st, a, s);
+            else hipLaunchKernelGGL((sample_split<T, 8, F>), grid, block, 0, st, a, s);
+        };
+        if (filters) launch(std::true_type{});
+        else launch(std::false_type{});
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
