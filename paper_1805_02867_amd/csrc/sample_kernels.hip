@@ -63,10 +63,10 @@ __device__ __forceinline__ bool held_row(RowSmem<T, W>& rm, const T* x, int32_t 
                                  lane == 0 ? rm.mid_n : 0, lane == 0 ? rm.tail_n : 0};
             return values_end(
                 rm, r, an, 1, V, cl, lane == 0 ? 1.0 : 0.0, h,
-                [&](int, int p, uint32_t(&n)[VB_PER]) {
-#pragma unroll
-                    for (int j = 0; j < VB_PER; ++j)
-                        n[j] = rm.values[p < VB_SIDE ? VB_SIDE - 1 - p - j : p + j];
+                [&](int, int p, uint64_t(&q)[2]) {
+                    const uint32_t* v = rm.values + (p < VB_SIDE ? VB_SIDE - VB_PER - p : p);
+                    q[0] = (uint64_t)(v[2] | v[3] << 16) << 32 | (v[0] | v[1] << 16);
+                    q[1] = (uint64_t)(v[6] | v[7] << 16) << 32 | (v[4] | v[5] << 16);
                 },
                 [](int) {}, val, idx);
         }
@@ -234,16 +234,11 @@ __device__ __forceinline__ bool split_end(SplitSmem<T, FILTERS>& rm, const Sampl
             return __ballot(!none && value_base(mc) != value_base(m)) == 0 &&
                 values_end(
                     rm, r, anchor(m, r.c), S, s.chunk, cl, part, h,
-                    [&](int c, int p, uint32_t(&n)[VB_PER]) {
-                        // 16 bits a bin, eight bins in two words; positive ones from the last
+                    [&](int c, int p, uint64_t(&q)[2]) {
                         const int b = p < VB_SIDE ? VB_SIDE - VB_PER - p : p;
                         const uint64_t* at = mass + (int64_t)c * BINS + b / 4;
-                        const uint64_t q0 = get(at), q1 = get(at + 1);
-#pragma unroll
-                        for (int j = 0; j < VB_PER; ++j) {
-                            const int i = p < VB_SIDE ? VB_PER - 1 - j : j;
-                            n[j] = (uint32_t)((i < 4 ? q0 : q1) >> (i % 4 * 16)) & 0xFFFFu;
-                        }
+                        q[0] = get(at);
+                        q[1] = get(at + 1);
                     },
                     [&](int c) {
                         const int64_t i0 = (int64_t)c * s.chunk;

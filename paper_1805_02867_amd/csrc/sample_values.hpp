@@ -1,4 +1,4 @@
-// Sampling of bfloat16 rows by the values themselves.  Between 2^-10 and 2^6 there are
+// Sampling of bfloat16 rows by the values themselves.  Between 2^-11 and 2^5 there are
 // only 2 x 2048 of them, so the histogram has a bin for each and counts: no weight is
 // computed per element, every bin is exact, and the cuts (sample.hpp) follow from the
 // bins alone, to the number of equal elements that stay.  The few elements nearer to 0,
@@ -18,6 +18,7 @@ constexpr int VB_SIDE = 2048;           // bins of a sign: 16 octaves
 constexpr int VB_BINS = 2 * VB_SIDE;
 constexpr int VB_PER = VB_BINS / 512;   // bins a thread, in the order of the values
 static_assert(VB_PER == 8, "eight bins are one 16-byte load of a chunk's counts");
+static_assert(VB_SIDE * 4 == 1 << 13, "the sign's place in a byte address");
 
 struct ValueSmem {
     SampleSmem<8> s;
@@ -35,11 +36,11 @@ struct ValueSmem {
 
 
 // Magnitude (the pattern without its sign) of the first bins: 15 octaves below the octave
-// of m, or of 2^5 if that is larger, in steps of four octaves (so that the chunks of
+// of m, or of 2^4 if that is larger, in steps of four octaves (so that the chunks of
 // a row agree).
 __device__ __forceinline__ int value_base(float m) {
     const int e = (int)(__float_as_uint(m) >> 23 & 0xFF);
-    const int top = e <= 132 ? 132 : 132 + (e - 132 + 3) / 4 * 4;
+    const int top = e <= 131 ? 131 : 131 + (e - 131 + 3) / 4 * 4;
     return (top - 15) << 7;
 }
 
@@ -82,26 +83,34 @@ __device__ __forceinline__ void add_values(ValueSmem& sm, Held<bf16_t, 8, R>& h,
         bool odd = false;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const uint32_t bin = value_bin(pattern(v, e), base);
-            atomicAdd(&sm.values[bin], 1u);
-            odd |= bin == (uint32_t)VB_BINS;
+            // four times the bin: a byte address
+            const uint32_t word = v[e >> 1], mag = e & 1 ? word >> 16 & 0x7FFFu : word & 0x7FFFu;
+            const uint32_t sign = e & 1 ? word >> 31 : word >> 15 & 1u;
+            const uint32_t rel = (mag << 2) - (base << 2);
+            const bool out = rel >= 4u * VB_SIDE;
+            const uint32_t at = out ? 4u * VB_BINS : sign << 13 | rel;
+            atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(sm.values) + at), 1u);
+            odd |= out;
         }
         if (!__any(odd)) return;
-        odd = false;
+        uint32_t which = 0;  // the lane's elements of a class
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            odd |= value_bin(pattern(v, e), base) == (uint32_t)VB_BINS && pattern(v, e) < gone;
-        if (!__any(odd)) return;
-#pragma unroll 1
-        for (int e = 0; e < 8; ++e) {
+            which |= value_bin(pattern(v, e), base) == (uint32_t)VB_BINS && pattern(v, e) < gone
+                         ? 1u << e
+                         : 0u;
+        while (__any(which != 0)) {
+            const int e = which ? __builtin_ctz(which) : 0;
             const uint32_t word = e < 2 ? v[0] : e < 4 ? v[1] : e < 6 ? v[2] : v[3];
             const uint32_t bits = e & 1 ? word >> 16 : word & 0xFFFFu;
             const double t = an.t(__uint_as_float(bits << 16));
-            if (value_bin(bits, base) != (uint32_t)VB_BINS || t <= -1080.0) continue;
-            const uint64_t w = fixed48(an.exp2(t));
-            const bool middle = (bits & 0x7FFFu) < base;
-            add_bin(middle ? sm.mid : sm.tail, w);
-            atomicAdd(middle ? &sm.mid_n : &sm.tail_n, 1u);
+            if (which && t > -1080.0) {
+                const uint64_t w = fixed48(an.exp2(t));
+                const bool middle = (bits & 0x7FFFu) < base;
+                add_bin(middle ? sm.mid : sm.tail, w);
+                atomicAdd(middle ? &sm.mid_n : &sm.tail_n, 1u);
+            }
+            which &= which - 1;
         }
     });
 }
@@ -137,7 +146,8 @@ struct Bins {
     }
 };
 
-// The row's end.  count8(c, p, n): the numbers of chunk c at positions p .. p + 7;
+// The row's end.  count8(c, p, q): the numbers of chunk c at positions p .. p + 7, 16 bits
+// each, in the order of the patterns' bins (from the last for positive values);
 // classes of chunk `lane`, whose maximum's weight in the row is `part`, in cl.
 // hold(c): makes h hold chunk c, from index c * chunk on.  False if the bins do not
 // decide.
@@ -150,15 +160,19 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
     auto& s = sm.s;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int base = value_base((float)an.m), p0 = VB_PER * tid;
-    constexpr int AT_ONCE = 4;  // chunks whose loads are in flight
-    const auto counts_of = [&](int c0, uint32_t(&m)[AT_ONCE][VB_PER]) {
+    constexpr int AT_ONCE = 8;  // chunks whose counts are in flight, and held if these are all
+    uint64_t held[AT_ONCE][2];
+    const auto load_counts = [&](int c0) {
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
-#pragma unroll
-            for (int j = 0; j < VB_PER; ++j) m[k][j] = 0;
+            held[k][0] = held[k][1] = 0;
             if (c0 + k < S && lane_value(part, c0 + k < S ? c0 + k : 0) > 0.0)
-                count8(c0 + k, p0, m[k]);
+                count8(c0 + k, p0, held[k]);
         }
+    };
+    const auto number = [&](int k, int j) {  // of position p0 + j in chunk k of those
+        const int i = p0 < VB_SIDE ? VB_PER - 1 - j : j;
+        return (uint32_t)((i < 4 ? held[k][0] : held[k][1]) >> (i % 4 * 16)) & 0xFFFFu;
     };
     // the bins of the row, their weights, and the classes
     Bins bin;
@@ -166,12 +180,13 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
     for (int j = 0; j < VB_PER; ++j) bin.n[j] = 0;
 #pragma unroll 1
     for (int c0 = 0; c0 < S; c0 += AT_ONCE) {
-        uint32_t m[AT_ONCE][VB_PER];
-        counts_of(c0, m);
+        load_counts(c0);
 #pragma unroll
-        for (int k = 0; k < AT_ONCE; ++k)
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (c0 + k >= S) break;
 #pragma unroll
-            for (int j = 0; j < VB_PER; ++j) bin.n[j] += m[k][j];
+            for (int j = 0; j < VB_PER; ++j) bin.n[j] += number(k, j);
+        }
     }
     uint32_t count = 0;
     double mass = 0.0;
@@ -307,8 +322,7 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
     uint32_t left = keep;
 #pragma unroll 1
     for (int c0 = 0; c0 < S; c0 += AT_ONCE) {
-        uint32_t m[AT_ONCE][VB_PER];
-        counts_of(c0, m);
+        if (S > AT_ONCE) load_counts(c0);
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
             if (c0 + k >= S) break;
@@ -316,8 +330,9 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
             uint32_t have = 0;
 #pragma unroll
             for (int j = 0; j < VB_PER; ++j) {
-                sum += (double)m[k][j] * bin.w[j];
-                have = j == at_cut ? m[k][j] : have;
+                const uint32_t n = number(k, j);
+                sum += (double)n * bin.w[j];
+                have = j == at_cut ? n : have;
             }
             if (at_cut >= 0 && at_cut < VB_PER) {
                 const uint32_t take = have < left ? have : left;
