@@ -172,6 +172,43 @@ def test_far_values(dtype, dev):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("V", [9001, 40000, 300000])
+def test_values_of_every_kind(V, dtype, dev):
+    """What a histogram over the values themselves could get wrong: elements next to 0 (and a
+    cut among them), beyond its ends, rows far from 0 whose parts lie in different octaves,
+    rows all negative, and equal elements cut in the middle, in any part of the row."""
+    g = torch.Generator().manual_seed(V)
+    r = torch.randn(16, V, generator=g)
+    x = r.clone()
+    x[0] = 2.0 ** -13 * r[0]                           # all next to 0
+    x[1] = torch.where(r[1] > 1.0, r[1], 2.0 ** -14 * r[1])
+    x[2] = 0.0
+    x[3] = r[3].clamp(max=0.0)                         # half of them 0, at the top
+    x[4] = 1000.0 + 20.0 * r[4]
+    x[4, : V // 2] = x[4, : V // 2].clamp(max=1010.0)  # 2^10 is reached in one half only
+    x[5] = -700.0 + r[5]
+    x[6] = -30.0 - 25.0 * r[6].abs()                   # beyond the negative end
+    x[7] = 31.0 + 2.0 * r[7]                           # both sides of 2^5
+    x[8] = (2.0 * r[8]).round()                        # a dozen values
+    x[9] = r[9] * 2.0 ** -10
+    x[10] = 3e38 * r[10].clamp(-1, 1)
+    x[11] = r[11] * 1e-40
+    x[12] = torch.where(r[12] > 2.5, 5.0, -40.0)
+    x[13] = torch.where(r[13] > 0.0, -2.0 ** -20, 2.0 ** -20)
+    x[14] = 100.0 * r[14]
+    x[15, : V - 3] = -INF
+    x = x.to(TYPES[dtype]).to(dev)
+    u = uniform(16, V, dev)
+    u[3], u[8] = 0.0, 1.0
+    for kw in (dict(), dict(top_p=0.5), dict(top_p=0.9999), dict(top_k=V // 3), dict(top_k=17),
+               dict(top_k=V - 2, top_p=0.7), dict(min_p=0.7), dict(top_p=0.9, min_p=1e-6),
+               dict(temperature=0.02, top_p=0.9), dict(temperature=40.0, top_p=0.8, min_p=0.3),
+               dict(temperature=40.0, top_k=V // 2), dict(temperature=INF, top_p=0.25),
+               dict(temperature=1e-35, top_p=0.5, top_k=V // 2)):
+        check(x, u, dev, **kw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("V,ld,first", [(1000, 1003, 1), (50257, 50304, 0), (4097, 5000, 3),
                                         (1, 64, 5), (33, 33, 1)])
 def test_rows_apart_and_unaligned(V, ld, first, dtype, dev):
