@@ -1,7 +1,7 @@
 """Python binding of libosoftmax (online-normalizer softmax, fused softmax +
-top-k, sampling and expert routing on MI355X).  Argument marshalling only: every step of the computation
-runs in the library's HIP kernels, reached through its C ABI
-(``include/osoftmax.h``).  PyTorch supplies device memory and the current
+top-k, sampling and expert routing on MI355X).  Argument marshalling only:
+every step of the computation runs in the library's HIP kernels, reached
+through its C ABI (``include/osoftmax.h``).  PyTorch supplies device memory and the current
 stream.  There is no fallback: if the library is missing, every call raises.
 """
 from __future__ import annotations
@@ -513,7 +513,8 @@ def route_bwd(x: torch.Tensor, idx: torch.Tensor, dvals: torch.Tensor, score="so
     elif not _like(dx, x):
         raise ValueError("dx must be a contiguous tensor like x")
     rc = lib().route_bwd(x.data_ptr(), idx.data_ptr(), dvals.data_ptr(), dx.data_ptr(), N, E, K,
-                         _DTYPES[x.dtype], _route(_score(score), 1, 1, 1, bool(renorm), float(scale)),
+                         _DTYPES[x.dtype],
+                         _route(_score(score), 1, 1, 1, bool(renorm), float(scale)),
                          _stream(stream))
     if rc != OK:
         raise OsmError(rc, "route_bwd")

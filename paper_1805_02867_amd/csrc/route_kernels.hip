@@ -35,8 +35,8 @@ namespace osm {
 constexpr int RT_BLOCK = 256;
 constexpr int RT_WAVES = RT_BLOCK / 64;
 
-// 1 / d for 1/2 <= d <= 64: the hardware's estimate and two Newton steps (each squares
-// the error 2^-26 or less).
+// 1 / d for 1/2 <= d <= 64: the hardware's estimate, to 2^-23, and two Newton steps (each
+// squares the error).
 __device__ __forceinline__ double reciprocal(double d) {
     double r = __builtin_amdgcn_rcp(d);
     r = __builtin_fma(__builtin_fma(-d, r, 1.0), r, r);
@@ -503,7 +503,9 @@ __global__ __launch_bounds__(RT_BLOCK) void route_bwd_rows(const RouteRows a) {
             own = g * (exp2_wide((xc - mx) * kLog2eD) * rsum);
             // (a row without any place, whatever it holds, has no gradient)
             const uint64_t who = __ballot(in);
-            const bool any = (LANES == 64 ? who : who >> (team * LANES) & ((1ull << (LANES & 63)) - 1)) != 0;
+            const uint64_t row_mask = LANES == 64 ? ~0ull
+                                                  : ((1ull << (LANES & 63)) - 1) << (team * LANES);
+            const bool any = (who & row_mask) != 0;
             const double dot = group_sum<LANES>(in ? own : 0.0) * rsum;
 #pragma unroll
             for (int j = 0; j < R; ++j) d[j] = any ? -d[j] * dot : 0.0;

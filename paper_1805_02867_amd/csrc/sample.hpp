@@ -16,7 +16,16 @@
 // the bin's weights (and for top-k their number); its running sums say in
 // which bin a cut falls, and only that bin's elements are looked at one by one:
 // ranked among each other if they are few, else by further histograms over
-// their ordered bits and, among equal ones, their indices.
+// their ordered bits and, among equal ones, their indices.  (bfloat16 rows longer than
+// a wavefront's go by their values instead: sample_values.hpp.)
+//
+// A binary64 weight is 20 instructions and a bin 10 more.  At 256 x 128256 binary32
+// without filters (52 us; the 131 MB alone 27) the passes over the chunks run at the
+// memory's rate and the rest is the ends of the rows, about 10 us each, of which
+// the last ones have the chip to themselves.  Few rows are bound by that end: 33 x
+// 50257 binary32 with top-p and min-p 39 us, 1 x 32000 bfloat16 with top-k and top-p
+// 20.  Short rows (4000 x 1000 binary32 top-k 29 us, the 16 MB 3) are bound by the
+// wavefront's own chain of steps.
 //
 // Weights are binary64 and the sums of a histogram are in fixed point: in
 // binary32 the sums of 10^5 weights are off by more than the distance between the
@@ -451,9 +460,9 @@ struct Held {
             }
         }
     }
-    // f(vector, index of its first element) for each, in a loop over registers that turn:
-    // unrolled, the code of a pass over the row leaves the instruction cache, which
-    // bounded it (the moves are one instruction in ten)
+    // f(vector, index of its first element) for each, in a loop over registers that turn.
+    // Unrolled, the kernel's code is several times the instruction cache (211 KB), and the
+    // end of a row, which each CU runs a few times, waits for its code
     template <typename F>
     __device__ __forceinline__ void each(const F& f) {
         constexpr int STEP = R % 2 == 0 && E == 4 ? 2 : 1;
@@ -488,7 +497,8 @@ struct Held {
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int e = 0; e < E; e += 2)
-                m = __builtin_elementwise_maximum(__builtin_elementwise_maximum(at(q[r], e), at(q[r], e + 1)), m);
+                m = __builtin_elementwise_maximum(
+                    __builtin_elementwise_maximum(at(q[r], e), at(q[r], e + 1)), m);
         return m;
     }
 };
@@ -929,8 +939,9 @@ __device__ __forceinline__ Filtered filter_row(ListSmem<W>& sm, const Rule& r, c
 
 // The token of a row of which `h` holds all, or the part that the target falls into:
 // the first element, in index order, at which the running sum of the weights that
-// wt(vector, index of its first element, weights) gives passes the target u * sum (PART: rem, of a row whose sum is `total`).  base: added to
-// the index.  False if no element has a weight.
+// wt(vector, index of its first element, weights) gives passes the target u * sum (PART:
+// what is left of it, of a row whose sum is `total`).  base: added to the index.  False
+// if no element has a weight.
 template <bool PART, typename T, int W, int R, typename Wt>
 __device__ __forceinline__ bool locate(SampleSmem<W>& sm, Held<T, W, R>& h, const Wt& wt,
                                        double target, double total, uint32_t base, float* val,

@@ -21,13 +21,13 @@ __device__ __forceinline__ SampleSmem<W>& smem_of(ListSmem<W>& sm) {
     return sm;
 }
 
-// A row held by the team: loaded once.  False: it has to be done the slow way.
-// (bfloat16 rows of a workgroup by their values, others by the bins of their weights)
+// bfloat16 rows of a workgroup go by their values, others by the bins of their weights.
 template <typename T, int W>
 using RowSmem = std::conditional_t<W == SM_W && std::is_same_v<T, bf16_t>, ValueSmem, ListSmem<W>>;
 template <typename T, bool FILTERS>
 using SplitSmem = std::conditional_t<FILTERS, RowSmem<T, SM_W>, SampleSmem<SM_W>>;
 
+// A row held by the team: loaded once.  False: it has to be done the slow way.
 template <typename T, int W, int R>
 __device__ __forceinline__ bool held_row(RowSmem<T, W>& rm, const T* x, int32_t V, const Rule& r,
                                          float* val, int32_t* idx) {
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(SM_BLOCK) void sample_streamed(const SampleRows a) 
 // What a chunk leaves for the workgroup that completes the row, at the device's
 // coherence point: its maximum, the index of that (greedy rows) or whether elements
 // of some weight lie below its histogram, and the sum of its weights relative to
-// its own anchor (rows without a filter) or its histograms.
+// its own maximum (rows without a filter) or its histograms.
 constexpr int SAMPLE_PART = 6;  // 64-bit words of a chunk: its sum, and its classes
 static_assert(VB_BINS * 2 == SampleShape<SM_W>::BINS * 8, "counts take the place of masses");
 struct ChunkSum {
@@ -250,9 +250,7 @@ __device__ __forceinline__ bool split_end(SplitSmem<T, FILTERS>& rm, const Sampl
     // (the histograms leave out what is below 2^-64 of the largest weight; only a u at
     // the very ends of [0, 1] can fall there)
     const bool ends = r.u < 0x1p-30 || r.u > 1.0 - 0x1p-30;
-    if (filtered && (__ballot(!none && cold((double)mc * r.c)) != 0 || ends)) {
-        return false;
-    }
+    if (filtered && (__ballot(!none && cold((double)mc * r.c)) != 0 || ends)) return false;
     const Anchor an = anchor(m, r.c);
     // bins of the row's histogram that its own starts below, and its weights' factor
     const int down = none || !filtered ? 0 : (int)(an.a - anchor(mc, r.c).a) * SUB;
@@ -403,10 +401,12 @@ __device__ __forceinline__ bool split_end(SplitSmem<T, FILTERS>& rm, const Sampl
 // side every row ends at the same few places, for which the next ones then wait (512 x
 // 128256 bfloat16, four chunks a row: a fifth of the chip busy).  So the chunks of 32
 // rows are interleaved: rows end at 32 places in turn, and a row's chunks are on one
-// die, whose L2 has their sums.  Fewer than eight rows spread theirs over all dies.
+// die, whose L2 has their sums (341 -> 200 us).  Fewer than eight rows spread theirs over
+// all dies.
 // Without FILTERS every row draws from its whole distribution (or takes its maximum).
 template <typename T, int R, bool FILTERS>
-__global__ __launch_bounds__(SM_BLOCK, FILTERS ? 4 : 6) void sample_split(const SampleRows a, const SampleSplit s) {
+__global__ __launch_bounds__(SM_BLOCK, FILTERS ? 4 : 6) void sample_split(const SampleRows a,
+                                                                         const SampleSplit s) {
     constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
     __shared__ SplitSmem<T, FILTERS> rm;
     SampleSmem<SM_W>& sm = smem_of(rm);
@@ -580,9 +580,10 @@ static hipError_t launch_sample_t(const SampleRows& a, const SamplePlan& p, void
         const dim3 grid((unsigned)((n + s.group - 1) / s.group * s.group * p.S)), block(SM_BLOCK);
         const auto launch = [&](auto filters) {
             constexpr bool F = decltype(filters)::value;
-            if (p.R == 2) hipLaunchKernelGGL((sample_split<T, 2, F>), grid, block, 0, st, a, s);
-            else if (p.R == 4) hipLaunchKernelGGL((sample_split<T, 4, F>), grid, block, 0, st, a, s);
-            else hipLaunchKernelGGL((sample_split<T, 8, F>), grid, block, 0, st, a, s);
+            const auto kernel = p.R == 2   ? sample_split<T, 2, F>
+                                : p.R == 4 ? sample_split<T, 4, F>
+                                           : sample_split<T, 8, F>;
+            hipLaunchKernelGGL(kernel, grid, block, 0, st, a, s);
         };
         if (filters) launch(std::true_type{});
         else launch(std::false_type{});

@@ -6,8 +6,10 @@
 // beyond the negative end are weighed one by one, as two classes; a cut inside a class
 // leaves the row to the slow way.  Rows with larger values move the 16 octaves up.
 //
-// Against a histogram of weights this takes 9 instructions an element instead of 30, and no
-// second pass over the row: 512 x 128256 top-p 204 -> @V512@ us.
+// Against a histogram of weights this takes a third of the instructions an element and no
+// second pass over the row: 512 x 128256 top-p 204 -> 106 us, 64 x 128256 with a setting a
+// row 91 -> 36.  What bounds it now is not the 131 MB (27 us at a large copy's rate): half
+// is the elements' instructions and shared-memory additions, half the ends of the rows.
 #pragma once
 
 #include "sample.hpp"
@@ -22,8 +24,9 @@ static_assert(VB_SIDE * 4 == 1 << 13, "the sign's place in a byte address");
 
 struct ValueSmem {
     SampleSmem<8> s;
-    // of a pattern: sign * 2048 + (magnitude - base); one more for those outside
-    uint32_t values[VB_BINS + 1];
+    // of a pattern: sign * 2048 + (magnitude - base); for those outside one a lane, so
+    // that a masked row's additions do not wait for each other
+    uint32_t values[VB_BINS + 64];
     double weights[VB_BINS];   // what an element of a bin weighs, if it is kept
     uint64_t mid, tail;        // weights of the classes, in units of 2^-48
     uint32_t mid_n, tail_n;
@@ -79,6 +82,7 @@ __device__ __forceinline__ void add_values(ValueSmem& sm, Held<bf16_t, 8, R>& h,
     const uint32_t gone = 0x8000u + (!(an.c > 0.0)  ? 0x7F80u
                                      : zero < 0.0f ? (__float_as_uint(-zero) >> 16) + 1
                                                    : 0u);
+    const uint32_t outside = 4u * (VB_BINS + (threadIdx.x & 63));
     h.each([&](const u32x4& v, int32_t) {
         bool odd = false;
 #pragma unroll
@@ -88,7 +92,7 @@ __device__ __forceinline__ void add_values(ValueSmem& sm, Held<bf16_t, 8, R>& h,
             const uint32_t sign = e & 1 ? word >> 31 : word >> 15 & 1u;
             const uint32_t rel = (mag << 2) - (base << 2);
             const bool out = rel >= 4u * VB_SIDE;
-            const uint32_t at = out ? 4u * VB_BINS : sign << 13 | rel;
+            const uint32_t at = out ? outside : sign << 13 | rel;
             atomicAdd(reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(sm.values) + at), 1u);
             odd |= out;
         }

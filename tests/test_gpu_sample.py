@@ -76,7 +76,7 @@ def test_settings(V, dtype, dev):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("N,V", [(1, 128256), (3, 131073), (70, 32000), (600, 1000), (2, 1000003)])
+@pytest.mark.parametrize("N,V", [(1, 128256), (3, 131073), (70, 32000), (600, 1000), (2, 1000003), (2, 1200007)])
 def test_a_setting_a_row(N, V, dtype, dev):
     rng = np.random.default_rng(V + N)
     x = logits(N, V, dtype, N, dev)
