@@ -48,8 +48,12 @@ def test_workspace_sizes():
     assert size(4, 10, 0, None) == osm.EINVAL
     assert osm.sample_workspace(0, 128256) >= 0 and osm.sample_workspace(1000, 1000) == 0
     for V, rows in ((32000, (1, 64)), (128256, (1, 64, 4000)), (1000000, (1, 4000))):
-        for N in rows:   # a launch's rows at a time: 4096 chunks of 12 KB and a row's few
-            assert 0 < osm.sample_workspace(N, V) <= 4096 * (12 * 1024 + 16) + 256 + 4 * 4096
+        for N in rows:
+            # a launch's rows at a time, at most 4096 chunks: of each 1024 bins of 8 + 4 bytes
+            # and six words of 8 (its sum and maximum, and two classes of bfloat16 values);
+            # rounded up to 256; and 4 bytes for each row, of which there are no more than chunks
+            most = 4096 * (12 * 1024 + 6 * 8) + 256 + 4 * 4096
+            assert 0 < osm.sample_workspace(N, V) <= most
 
 
 def test_empty_batches_are_noops():
