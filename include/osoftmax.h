@@ -11,8 +11,9 @@
  *    elements after row r-1, or ldx where an entry point has it), each pointer
  *    aligned to its element size.
  *  - Element types (dtype): OSM_F32 = IEEE binary32, OSM_BF16 = bfloat16
- *    (16-bit patterns).  All arithmetic is binary32; bfloat16 inputs are
- *    widened exactly and bfloat16 outputs are rounded to nearest even.
+ *    (16-bit patterns).  Arithmetic is binary32 unless an entry point says
+ *    otherwise; bfloat16 inputs are widened exactly and bfloat16 outputs are
+ *    rounded to nearest even.
  *  - Calls are asynchronous: they validate the arguments on the host, enqueue
  *    work on `stream` (NULL = the default stream) and return.  A status other
  *    than OSM_OK means nothing was enqueued, except OSM_EHIP, which reports a
@@ -45,8 +46,9 @@
  *    first use and when it must grow.  Under HIP graph capture, either call
  *    once outside the capture on the same stream with the largest shape to
  *    be captured (the buffer is then reused and nothing is allocated), or use
- *    softmax_topk_ex_noalloc for the top-k: an allocation recorded into a
- *    graph would leave the stream's buffer owned by the graph.
+ *    softmax_topk_ex_noalloc for the top-k and softmax_sample_ws for
+ *    sampling: an allocation recorded into a graph would leave the stream's
+ *    buffer owned by the graph.
  */
 #ifndef OSOFTMAX_H
 #define OSOFTMAX_H
@@ -299,7 +301,11 @@ typedef struct osm_sample_params {
  * probability among the kept elements (w / sum).  u below 0 or NaN counts as 0,
  * above 1 as 1; elements of weight 0 are never taken.  Weights and sums are
  * binary64, so the choice is that of the formula but for numbers u within about
- * 1e-13 of a border; the same call gives the same result.
+ * 1e-13 of a border.  With filters some sums are of weights in fixed point, in units
+ * relative to the largest: then u within 2^-49 V of a border may take its
+ * neighbour, and top_p within the larger of 2^-49 V and 2^-62 V^2 may keep an
+ * element more or less (both are bounds of the worst row; roundings mostly
+ * cancel).  The same call gives the same result.
  * A row holding NaN or +inf, or only -inf, gives idx -1 and a NaN value.
  * x: row r starts at x + r * ldx elements, ldx >= V.  u: N binary32.  vals: N
  * binary32.  idx: N int32.  params NULL: temperature 1, no filter.

@@ -1,8 +1,9 @@
 """Python binding of libosoftmax (online-normalizer softmax, fused softmax +
 top-k, sampling and expert routing on MI355X).  Argument marshalling only:
 every step of the computation runs in the library's HIP kernels, reached
-through its C ABI (``include/osoftmax.h``).  PyTorch supplies device memory and the current
-stream.  There is no fallback: if the library is missing, every call raises.
+through its C ABI (``include/osoftmax.h``).  PyTorch supplies device memory
+and the current stream.  There is no fallback: if the library is missing,
+every call raises.
 """
 from __future__ import annotations
 
@@ -424,9 +425,14 @@ def softmax_sample(x: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, t
     be apart (``x[:, :V]`` of a padded batch).  ``workspace``: uint8, at least
     ``sample_workspace(N, V, dtype)`` bytes, used instead of the library's scratch
     (``softmax_sample_ws``); while the current stream is being captured into a graph,
-    one is taken from the graph's own memory."""
+    one is taken from the graph's own memory, which is in order on that stream alone: a
+    call on another ``stream`` then has to bring its workspace."""
     N, V, ld = _rows(x)
     _on_current_device(x, "x")
+    capturing = workspace is None and torch.cuda.is_current_stream_capturing()
+    if capturing and _stream(stream) != _stream(None):
+        raise ValueError("a captured call on another stream than the current one needs a "
+                         "workspace")
     _vector(u, torch.float32, x, N, "u")
     t, t_all = _setting(temperature, torch.float32, x, N, "temperature")
     k, k_all = _setting(top_k, torch.int32, x, N, "top_k")
@@ -435,7 +441,7 @@ def softmax_sample(x: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, t
     vals = _output(vals, (N,), torch.float32, x, "vals")
     idx = _output(idx, (N,), torch.int32, x, "idx")
     params = SampleParams(t, k, p, q, t_all, k_all, p_all, q_all)
-    if workspace is None and torch.cuda.is_current_stream_capturing():
+    if capturing:
         workspace = torch.empty(sample_workspace(N, V, x.dtype), dtype=torch.uint8,
                                 device=x.device)
     if workspace is None:

@@ -257,3 +257,22 @@ def test_captured_replays(dev):
         torch.cuda.synchronize()
         assert torch.equal(vals, rv) and torch.equal(idx, ri) and torch.equal(dx, rd)
         check_fwd(x, 4)
+
+
+@pytest.mark.parametrize("E", [1024, 1021])
+def test_offsets_past_32_bits(E, dev):
+    """A batch of more than 2^31 logits: its last rows."""
+    N, K, last = (1 << 31) // E + 100, 4, 64
+    x = torch.zeros(N, E, dtype=torch.bfloat16, device=dev)
+    x[-last:] = logits(last, E, "bf16", 1, dev)
+    g = torch.zeros(N, K, device=dev)
+    g[-last:] = logits(last, K, "f32", 2, dev)
+    vals, idx = osm.route_fwd(x, K)
+    dx = osm.route_bwd(x, idx, g)
+    rv, ri = pick_ref.route(host(x[-last:]), K)
+    assert np.array_equal(idx[-last:].cpu().numpy(), ri)
+    pick_ref.close(host(vals[-last:]), rv)
+    want = pick_ref.route_bwd(host(x[-last:]), ri, host(g[-last:]))
+    pick_ref.close(host(dx[-last:]), want, "bf16", 2.0 ** -44 * float(g.abs().max()))
+    assert (idx[:-last] == torch.arange(K, device=dev, dtype=torch.int32)).all()
+    assert not dx[:-last].any()

@@ -76,7 +76,8 @@ def test_settings(V, dtype, dev):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("N,V", [(1, 128256), (3, 131073), (70, 32000), (600, 1000), (2, 1000003), (2, 1200007)])
+@pytest.mark.parametrize("N,V", [(1, 128256), (3, 131073), (70, 32000), (600, 1000),
+                                 (2, 1000003), (2, 1200007)])
 def test_a_setting_a_row(N, V, dtype, dev):
     rng = np.random.default_rng(V + N)
     x = logits(N, V, dtype, N, dev)
@@ -326,3 +327,40 @@ def test_same_bits_every_time(dev):
         for _ in range(5):
             again = osm.softmax_sample(x, u, **kw)
             assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+def test_a_captured_call_on_another_stream_brings_its_workspace(dev):
+    """Else the graph's memory for it could be given to the current stream's next call."""
+    x, u = logits(3, 128256, "bf16", 1, dev), uniform(3, 1, dev)
+    n = osm.sample_workspace(3, 128256, torch.bfloat16)
+    ws = torch.empty(n, dtype=torch.uint8, device=dev)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        main = torch.cuda.current_stream()
+        with pytest.raises(ValueError):
+            osm.softmax_sample(x, u, top_p=0.9, stream=other)
+        other.wait_stream(main)
+        vals, idx = osm.softmax_sample(x, u, top_p=0.9, stream=other, workspace=ws)
+        main.wait_stream(other)
+    rv, ri = pick_ref.sample(host(x), host(u), top_p=0.9)
+    for _ in range(3):
+        idx.fill_(-5)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert np.array_equal(idx.cpu().numpy(), ri)
+        pick_ref.close(host(vals), rv)
+
+
+@pytest.mark.parametrize("dtype,V", [("bf16", 700), ("f32", 700), ("bf16", 6000), ("f32", 40000),
+                                     ("bf16", 40000)])
+def test_offsets_past_32_bits(dtype, V, dev):
+    """Rows 1.5 * 2^30 elements apart: the last one begins past 2^31."""
+    ld = 3 << 29
+    buf = torch.empty(2 * ld + V, dtype=TYPES[dtype], device=dev)
+    x = buf.as_strided((3, V), (ld, 1))
+    x.copy_(logits(3, V, dtype, 2, dev))
+    for kw in (dict(), dict(top_k=50, top_p=0.9)):
+        check(x, uniform(3, 3, dev), dev, **kw)
