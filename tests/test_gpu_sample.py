@@ -364,3 +364,23 @@ def test_offsets_past_32_bits(dtype, V, dev):
     x.copy_(logits(3, V, dtype, 2, dev))
     for kw in (dict(), dict(top_k=50, top_p=0.9)):
         check(x, uniform(3, 3, dev), dev, **kw)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_masked_chunks_and_a_workspace_of_any_contents(dtype, dev):
+    """Chunks that are masked as a whole write no sums: what the workspace held is not read."""
+    N, V = 4, 128256
+    x, u = logits(N, V, dtype, 5, dev), uniform(N, 5, dev)
+    x[0, 5000:] = -INF
+    x[1, :100000] = -INF
+    x[2, 40000:90000] = LOWEST[dtype]
+    x[3] = -INF
+    for kw in (dict(), dict(top_k=60), dict(top_k=60000), dict(top_k=30, top_p=0.9),
+               dict(top_p=0.99, min_p=1e-3), dict(temperature=0.0)):
+        want = pick_ref.sample(host(x), host(u), **kw)
+        for fill in (255, 1, 0):
+            ws = torch.full((osm.sample_workspace(N, V, x.dtype),), fill, dtype=torch.uint8,
+                            device=dev)
+            vals, idx = osm.softmax_sample(x, u, workspace=ws, **kw)
+            assert np.array_equal(idx.cpu().numpy(), want[1]), (kw, fill)
+            pick_ref.close(host(vals), want[0])
