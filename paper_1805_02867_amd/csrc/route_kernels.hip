@@ -323,7 +323,13 @@ __global__ __launch_bounds__(RT_BLOCK) void route_rows(const RouteRows a) {
                 second = fmaxf(fminf(best, v), fmaxf(second, v2));
                 best = fmaxf(best, v);
             }
-            if (sums && second > ninf) best += second;
+            if (sums && best > ninf) {
+                // a sum that leaves binary32 (two biases of the type's lowest value) is not
+                // that of a group without experts: the largest numbers stand for all beyond
+                // them, and groups that are equal here are ranked again in binary64
+                constexpr float most = __FLT_MAX__;
+                best = __builtin_amdgcn_fmed3f(second > ninf ? best + second : best, -most, most);
+            }
             if (g < G && lane % per == 0) go[g] = best;
             wave_sync();
             int ahead = 0;
