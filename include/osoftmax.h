@@ -381,6 +381,10 @@ OSM_API int route_fwd(const void* x, const float* bias, float* vals, int32_t* id
  * the same score, renorm and scale (the other members of r are not read).
  * Places whose idx is outside [0, E) take no part; a row without any other gets
  * zeros.  An index that occurs twice adds both.  Sums are binary64.
+ * The gradient is NaN where a NaN (for the softmax also +inf) stands among the
+ * logits that the weights depend on: those of the places with renorm, one place's
+ * own for the sigmoid without it, else the whole row.  Places that all have
+ * -inf get zeros with renorm.
  * x: N*E logits of dtype.  idx: N*K int32.  dvals: N*K binary32.  dx: N*E
  * elements of dtype, every one written.
  * Errors: as route_fwd, for the arguments it has. */

@@ -525,7 +525,7 @@ __global__ __launch_bounds__(RT_BLOCK) void route_bwd_rows(const RouteRows a) {
             for (int j = 0; j < R; ++j) d[j] = 0.0;
             const double e = exp_minus_abs(xc), f = reciprocal(1.0 + e);
             if (a.renorm) {
-                const double z = a.sigmoid ? __builtin_fmin(xc, 0.0) : xc;
+                const double z = a.sigmoid && xc > 0.0 ? 0.0 : xc;  // (NaN stays)
                 const double zm = (double)team_maximum<LANES>(in ? (float)z : -__builtin_inff());
                 double p = exp2_wide((z - zm) * kLog2eD);
                 if (a.sigmoid) p *= f;
@@ -533,9 +533,11 @@ __global__ __launch_bounds__(RT_BLOCK) void route_bwd_rows(const RouteRows a) {
                 const double all = group_sum<LANES>(p);
                 p = all > 0.0 ? p / all : 0.0;
                 own = p * (g - group_sum<LANES>(p * g));
+                // a chosen NaN (or the softmax of +inf) leaves no weight a number
+                if (!(zm < __builtin_inf())) own = __builtin_nan("");
                 if (a.sigmoid) own *= (xc >= 0.0 ? e : 1.0) * f;
             } else {
-                own = g * e * f * f;
+                own = xc == xc ? g * e * f * f : xc;
             }
         }
         // places to experts: each expert finds the place that it has, if any

@@ -40,3 +40,28 @@ def test_groups_by_sums_that_leave_binary32(E, score, dev):
         for bias in (b, single):
             for top in (1, 2, 3):
                 check_fwd(x, 2, bias, score=score, groups=8, top_groups=top, group_top=2)
+
+
+@pytest.mark.filterwarnings("ignore:invalid value")     # of the reference, on purpose
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("E,K", [(24, 4), (33, 3), (256, 8)])
+def test_gradient_of_logits_that_are_not_numbers(E, K, dtype, dev):
+    """A given index is taken as it is: where the weights' formula is not a number, so is its
+    gradient, and no place outside of what they depend on."""
+    x = router(7, E, dtype, E, dev)
+    idx = torch.arange(K, dtype=torch.int32, device=dev).repeat(7, 1)
+    x[0, 1] = NAN              # among the chosen
+    x[1, E - 1] = NAN          # not among them
+    x[2, 0] = INF
+    x[3, E - 1] = INF
+    x[4, 2] = -INF             # a share of 0
+    x[5, 1], x[5, 2] = -INF, NAN
+    g = router(7, K, "f32", 4, dev)
+    for score in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            dx = check_bwd(x, idx, g, dtype, score=score, renorm=renorm)
+            assert dx[0].isnan().any() and not dx[[4, 6]].isnan().any()
+            none = osm.route_bwd(torch.full_like(x, -INF), idx, g, score=score, renorm=renorm)
+            assert not none.any() or not renorm
+            outside = torch.tensor([-1], dtype=torch.int32, device=dev).expand(7, K).contiguous()
+            assert not osm.route_bwd(x, outside, g, score=score, renorm=renorm).any()
