@@ -411,7 +411,9 @@ def _setting(v, dtype, x: torch.Tensor, N: int, name: str):
     """(pointer, value for all rows) of a setting given as a tensor or a number."""
     if isinstance(v, torch.Tensor):
         return _vector(v, dtype, x, N, name).data_ptr(), 0
-    return None, int(v) if dtype is torch.int32 else float(v)
+    if dtype is not torch.int32:
+        return None, float(v)
+    return None, max(-1 << 31, min(int(v), (1 << 31) - 1))  # (a field would take the low 32 bits)
 
 
 def softmax_sample(x: torch.Tensor, u: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0,
@@ -471,6 +473,9 @@ def sample_workspace(N: int, V: int, dtype=torch.float32) -> int:
 @functools.lru_cache(maxsize=256)
 def _route(score, groups, top_groups, group_top, renorm, scale):
     """A reference to an ``osm_route`` of these values (building one takes 0.9 us)."""
+    for v in (score, groups, top_groups, group_top):
+        if not -1 << 31 <= v < 1 << 31:  # (a field would take the low 32 bits)
+            raise ValueError(f"{v} is no option of a router")
     return ctypes.byref(Route(score, groups, top_groups, group_top, renorm, scale))
 
 
