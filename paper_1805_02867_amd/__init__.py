@@ -471,12 +471,18 @@ def sample_workspace(N: int, V: int, dtype=torch.float32) -> int:
 
 
 @functools.lru_cache(maxsize=256)
-def _route(score, groups, top_groups, group_top, renorm, scale):
+def _made_route(score, groups, top_groups, group_top, renorm, scale):
     """A reference to an ``osm_route`` of these values (building one takes 0.9 us)."""
     for v in (score, groups, top_groups, group_top):
         if not -1 << 31 <= v < 1 << 31:  # (a field would take the low 32 bits)
             raise ValueError(f"{v} is no option of a router")
     return ctypes.byref(Route(score, groups, top_groups, group_top, renorm, scale))
+
+
+def _route(score, groups, top_groups, group_top, renorm, scale):
+    # (0.0 and -0.0 are one key)
+    make = _made_route if scale else _made_route.__wrapped__
+    return make(score, groups, top_groups, group_top, renorm, scale)
 
 
 def _score(score) -> int:

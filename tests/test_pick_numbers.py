@@ -23,3 +23,9 @@ def test_router_options_outside_of_their_type(place, value):
     args[place] = value
     with pytest.raises(ValueError):
         osm._route(*args, True, 1.0)
+
+
+def test_scales_that_compare_equal_are_told_apart():
+    def sign(scale):
+        return str(osm._route(0, 1, 1, 1, True, scale)._obj.scale)
+    assert [sign(0.0), sign(-0.0), sign(0.0)] == ["0.0", "-0.0", "0.0"]
