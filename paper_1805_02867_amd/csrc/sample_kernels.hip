@@ -62,13 +62,13 @@ __device__ __forceinline__ bool held_row(RowSmem<T, W>& rm, const T* x, int32_t 
             const ClassSum cl = {lane == 0 ? rm.mid : 0, lane == 0 ? rm.tail : 0,
                                  lane == 0 ? rm.mid_n : 0, lane == 0 ? rm.tail_n : 0};
             return values_end(
-                rm, r, an, 1, V, cl, lane == 0 ? 1.0 : 0.0, h,
+                rm, r, an, 1, V, cl, lane == 0 ? 1.0 : 0.0, 0, h,
                 [&](int, int p, uint64_t(&q)[2]) {
                     const uint32_t* v = rm.values + (p < VB_SIDE ? VB_SIDE - VB_PER - p : p);
                     q[0] = (uint64_t)(v[2] | v[3] << 16) << 32 | (v[0] | v[1] << 16);
                     q[1] = (uint64_t)(v[6] | v[7] << 16) << 32 | (v[4] | v[5] << 16);
                 },
-                [](int) {}, val, idx);
+                [](int, int, const uint64_t(&)[2]) {}, [](int) {}, val, idx);
         }
     } else if (r.k || r.p < 1.0) {
         if (cold((double)m * r.c)) return false;
@@ -188,7 +188,7 @@ __device__ __forceinline__ uint32_t get(const uint32_t* p) {
 template <typename T, int R, bool FILTERS>
 __device__ __forceinline__ bool split_end(SplitSmem<T, FILTERS>& rm, const SampleRows& a,
                                           const SampleSplit& s, const T* x, const Rule& r,
-                                          const uint64_t* parts, const uint64_t* mass,
+                                          const uint64_t* parts, uint64_t* mass,
                                           const uint32_t* counts, float* val, int32_t* idx) {
     constexpr int BINS = SampleShape<SM_W>::BINS, PER = SampleShape<SM_W>::PER;
     constexpr int SUB = SampleShape<SM_W>::SUB, E = Vec<T>::N;
@@ -231,20 +231,26 @@ __device__ __forceinline__ bool split_end(SplitSmem<T, FILTERS>& rm, const Sampl
                       (uint32_t)n, (uint32_t)(n >> 32)};
             }
             Held<T, SM_W, R> h;
-            return __ballot(!none && value_base(mc) != value_base(m)) == 0 &&
-                values_end(
-                    rm, r, anchor(m, r.c), S, s.chunk, cl, part, h,
-                    [&](int c, int p, uint64_t(&q)[2]) {
-                        const int b = p < VB_SIDE ? VB_SIDE - VB_PER - p : p;
-                        const uint64_t* at = mass + (int64_t)c * BINS + b / 4;
-                        q[0] = get(at);
-                        q[1] = get(at + 1);
-                    },
-                    [&](int c) {
-                        const int64_t i0 = (int64_t)c * s.chunk;
-                        h.load(x + i0, (int32_t)(a.V - i0 < s.chunk ? a.V - i0 : s.chunk));
-                    },
-                    val, idx);
+            return values_end(
+                rm, r, anchor(m, r.c), S, s.chunk, cl, part,
+                none ? 0 : value_base(m) - value_base(mc), h,
+                [&](int c, int p, uint64_t(&q)[2]) {
+                    const int b = p < VB_SIDE ? VB_SIDE - VB_PER - p : p;
+                    const uint64_t* at = mass + (int64_t)c * BINS + b / 4;
+                    q[0] = get(at);
+                    q[1] = get(at + 1);
+                },
+                [&](int c, int p, const uint64_t(&q)[2]) {
+                    const int b = p < VB_SIDE ? VB_SIDE - VB_PER - p : p;
+                    uint64_t* at = mass + (int64_t)c * BINS + b / 4;
+                    put(at, q[0]);
+                    put(at + 1, q[1]);
+                },
+                [&](int c) {
+                    const int64_t i0 = (int64_t)c * s.chunk;
+                    h.load(x + i0, (int32_t)(a.V - i0 < s.chunk ? a.V - i0 : s.chunk));
+                },
+                val, idx);
         }
     }
     // (the histograms leave out what is below 2^-64 of the largest weight; only a u at

@@ -4,7 +4,10 @@
 // bins alone, to the number of equal elements that stay.  The few elements nearer to 0,
 // which in the order stand between the positive and the negative bins, and those
 // beyond the negative end are weighed one by one, as two classes; a cut inside a class
-// leaves the row to the slow way.  Rows with larger values move the 16 octaves up.
+// leaves the row to the slow way.  Rows with larger values, or none near 0, move the 16
+// octaves up, and parts of a row that moved them elsewhere are brought into line at
+// its end (64 x 128256 with 20 added to all, where a row's parts have their maxima on both
+// sides of 2^5: 40 us; centred 38).
 //
 // Against a histogram of weights this takes a third of the instructions an element and no
 // second pass over the row: 512 x 128256 top-p 204 -> 106 us, 64 x 128256 with a setting a
@@ -39,12 +42,16 @@ struct ValueSmem {
 
 
 // Magnitude (the pattern without its sign) of the first bins: 15 octaves below the octave
-// of m, or of 2^4 if that is larger, in steps of four octaves (so that the chunks of
-// a row agree).
+// of m, or of 2^4 if that is larger; for m up to -8 the octave of m itself, since all
+// elements are at least as far from 0.  Both in steps of four octaves, so that the bins of
+// a row's chunks are the same ones but for a shift of whole 512.  A chunk whose bins
+// begin below the row's has a smaller maximum, or none above 0; one whose bins begin above
+// the row's has only negative elements, and none nearer to 0 than its bins.
 __device__ __forceinline__ int value_base(float m) {
     const int e = (int)(__float_as_uint(m) >> 23 & 0xFF);
-    const int top = e <= 131 ? 131 : 131 + (e - 131 + 3) / 4 * 4;
-    return (top - 15) << 7;
+    const int up = m > -8.0f ? (m < 0.0f ? 0 : (e - 128) / 4) : (e - 116) / 4;
+    const int first = 116 + 4 * (up > 0 ? up : 0);
+    return (first < 240 ? first : 240) << 7;
 }
 
 // The value of a bin in the order: positions 0 .. 2047 are the positive ones, largest
@@ -150,22 +157,75 @@ struct Bins {
     }
 };
 
-// The row's end.  count8(c, p, q): the numbers of chunk c at positions p .. p + 7, 16 bits
-// each, in the order of the patterns' bins (from the last for positive values);
-// classes of chunk `lane`, whose maximum's weight in the row is `part`, in cl.
-// hold(c): makes h hold chunk c, from index c * chunk on.  False if the bins do not
+// The row's end.  count8(c, p, q): the numbers of chunk c at positions p .. p + 7 of its own
+// bins, 16 bits each, in the order of the patterns' bins (from the last for positive
+// values); classes of chunk `lane`, whose maximum's weight in the row is `part`, in cl, and
+// how many bins the row's first is above its first in `off`; put8(c, p, q) puts numbers
+// back.  hold(c): makes h hold chunk c, from index c * chunk on.  False if the bins do not
 // decide.
-template <int R, typename Count8, typename Hold>
+template <int R, typename Count8, typename Put8, typename Hold>
 __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const Anchor& an, int S,
-                                           int64_t chunk, ClassSum cl, double part,
+                                           int64_t chunk, ClassSum cl, double part, int off,
                                            Held<bf16_t, 8, R>& h, const Count8& count8,
-                                           const Hold& hold, float* val, int32_t* idx) {
+                                           const Put8& put8, const Hold& hold, float* val,
+                                           int32_t* idx) {
     constexpr int W = 8;
     auto& s = sm.s;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int base = value_base((float)an.m), p0 = VB_PER * tid;
     constexpr int AT_ONCE = 8;  // chunks whose counts are in flight, and held if these are all
     uint64_t held[AT_ONCE][2];
+    double mid_c = (double)cl.mid * 0x1p-48 * part, tail_c = (double)cl.tail * 0x1p-48 * part;
+    const uint64_t moved = __ballot(part > 0.0 && off != 0);
+    if (moved != 0) {
+        // These chunks' counts are put where the row has their bins; bins that it has not join
+        // the class on their side.  (A chunk's own class on the other side would have to be
+        // told apart.)
+        if (__ballot(part > 0.0 && off != 0 && (off > 0 ? cl.tail_n : cl.mid_n) != 0) != 0)
+            return false;
+        if (tid < 64) {
+            sm.have[tid] = (uint32_t)off;
+            sm.take[tid] = 0;
+        }
+        // the least magnitude of the thread's bins, above the first one's
+        const int mag0 = p0 < VB_SIDE ? VB_SIDE - VB_PER - p0 : p0 - VB_SIDE;
+        __syncthreads();
+#pragma unroll 1
+        for (uint64_t rest = moved; rest != 0; rest &= rest - 1) {
+            const int c = __builtin_ctzll(rest), o = (int)sm.have[c];
+            uint64_t out[2] = {0, 0}, q[2] = {0, 0};
+            if (o > 0 ? mag0 < o : mag0 >= VB_SIDE + o) count8(c, p0, out);
+            if (mag0 + o >= 0 && mag0 + o < VB_SIDE) count8(c, p0 < VB_SIDE ? p0 - o : p0 + o, q);
+            uint32_t n = 0;
+            double sum = 0.0;
+            if (__ballot((out[0] | out[1]) != 0) != 0) {
+                uint32_t v = (uint32_t)(base - o + mag0) << 16 | (p0 < VB_SIDE ? 0u : 0x80000000u);
+#pragma unroll 1
+                for (int i = 0; i < VB_PER; ++i, v += 1u << 16) {
+                    const uint32_t ni = (uint32_t)out[0] & 0xFFFFu;
+                    const double w = an.weight(__uint_as_float(v));
+                    n += w > 0.0 ? ni : 0u;  // (what has no weight counts nowhere)
+                    sum += (double)ni * w;
+                    out[0] = out[0] >> 16 | out[1] << 48;
+                    out[1] >>= 16;
+                }
+                sum = group_sum<64>(sum);
+                if (n != 0) atomicAdd(&sm.take[c], n);
+            }
+            if (lane == 0) sm.part[wv][c] = sum;
+            __syncthreads();  // all have what they need of the chunk's counts
+            put8(c, p0, q);
+        }
+        __syncthreads();
+        if (moved >> lane & 1) {
+            double sum = 0.0;
+#pragma unroll
+            for (int v = 0; v < W; ++v) sum += sm.part[v][lane];
+            (off > 0 ? mid_c : tail_c) += sum;
+            (off > 0 ? cl.mid_n : cl.tail_n) += sm.take[lane];
+        }
+        __syncthreads();
+    }
     const auto load_counts = [&](int c0) {
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
@@ -199,7 +259,6 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
         count += n;
         mass += (double)n * w;
     });
-    const double mid_c = (double)cl.mid * 0x1p-48 * part, tail_c = (double)cl.tail * 0x1p-48 * part;
     const double mid = group_sum<64>(mid_c), tail = group_sum<64>(tail_c);
     const uint32_t mid_n = lane_value(wave_scan(part > 0.0 ? cl.mid_n : 0u), 63);
     const uint32_t tail_n = lane_value(wave_scan(part > 0.0 ? cl.tail_n : 0u), 63);

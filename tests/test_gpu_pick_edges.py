@@ -42,6 +42,64 @@ def test_groups_by_sums_that_leave_binary32(E, score, dev):
                 check_fwd(x, 2, bias, score=score, groups=8, top_groups=top, group_top=2)
 
 
+# top-p, top-k, min-p, and all of them
+FILTERS = (dict(top_p=0.9), dict(top_k=50), dict(min_p=0.02, top_p=0.98, temperature=1.3),
+           dict(top_k=3000, top_p=0.95, min_p=1e-3))
+
+
+@pytest.mark.parametrize("V", [128256, 32000, 9001, 5000])
+def test_bfloat16_rows_with_a_constant_added(V, dev):
+    """A softmax does not see it; the bins of the values do.  Chunks on both sides of where the
+    bins move, of either sign, by one step and by several."""
+    shift = [8, 12, 16, 20, 24, 29, 33, 200, 500, 3000, -3, -8, -13, -15, -20, -28, -33, -40, -100,
+             -520, -1e4, 1e30]
+    x = logits(len(shift), V, "f32", V, dev, 2.0)
+    x = (x + torch.tensor(shift, device=dev).unsqueeze(1)).to(torch.bfloat16)
+    u = uniform(len(shift), V, dev)
+    for kw in FILTERS:
+        check(x, u, dev, **kw)
+
+
+@pytest.mark.parametrize("T", [1.0, 30.0, 1000.0])
+def test_bfloat16_chunks_whose_bins_begin_elsewhere(T, dev):
+    """Parts of a row around levels of their own: what leaves the row's bins on either side
+    has weight at these temperatures, next to 0 and far below it."""
+    V, part = 40000, 2500
+    levels = [[40.0, 20.0, 20.0, 3.0], [700.0, 20.0, 1e-3, 300.0], [1e4, 1.0, 30.0, 600.0],
+              [1e30, 1e25, 3.0, -1.0], [5.0, -5.0, -50.0, -900.0], [0.02, -0.02, -0.3, -40.0],
+              [-0.05, -0.5, -40.0, -3e4], [-1e-3, -1.0, -1e3, -1e6], [-40.0, -600.0, -1e4, -1e9],
+              [600.0, 40.0, -40.0, -600.0], [33.0, -33.0, 33.0, -1e-6], [2.0, 1e-4, -1e-4, -0.1]]
+    g = torch.Generator().manual_seed(7)
+    x = torch.randn(len(levels), V, generator=g)
+    for r, at in enumerate(levels):
+        order = torch.randperm(4, generator=g)
+        for c in range(V // part):
+            a = at[order[c % 4]]
+            v = x[r, c * part:(c + 1) * part]
+            v.copy_(a - abs(a) * 0.1 * v.abs())
+    x = x.to(torch.bfloat16).to(dev)
+    for seed, kw in enumerate(FILTERS + (dict(top_p=0.5), dict(top_k=V // 2), dict(top_p=0.999),
+                                         dict(top_k=V // 3, top_p=0.8), dict(min_p=0.5))):
+        check(x, uniform(len(levels), seed, dev), dev, **(dict(temperature=T) | kw))
+
+
+@pytest.mark.parametrize("N", [64, 512])
+def test_a_constant_costs_bfloat16_rows_little(N, dev):
+    """The same batch with a constant added, by the fastest of several batches of calls."""
+    V = 128256
+    g = torch.Generator(device=dev).manual_seed(N)
+    r = torch.randn(N, V, device=dev, generator=g)
+    r = 2.0 * (r + 0.5 * (r - 2.0).clamp(min=0.0) ** 2)
+    u = uniform(N, 1, dev)
+
+    def us(shift):
+        x = (r + shift).to(torch.bfloat16)
+        return best_us(lambda: osm.softmax_sample(x, u, top_p=0.9), batches=5, calls=3)
+    centred = us(0.0)
+    for shift in (8.0, 12.0, 16.0, 20.0, -20.0, -28.0, -40.0, -100.0):
+        assert us(shift) < 2.0 * centred, shift
+
+
 @pytest.mark.filterwarnings("ignore:invalid value")     # of the reference, on purpose
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("E,K", [(24, 4), (33, 3), (256, 8)])
