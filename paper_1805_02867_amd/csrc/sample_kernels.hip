@@ -61,14 +61,14 @@ __device__ __forceinline__ bool held_row(RowSmem<T, W>& rm, const T* x, int32_t 
             __syncthreads();
             const ClassSum cl = {lane == 0 ? rm.mid : 0, lane == 0 ? rm.tail : 0,
                                  lane == 0 ? rm.mid_n : 0, lane == 0 ? rm.tail_n : 0};
-            return values_end(
-                rm, r, an, 1, V, cl, lane == 0 ? 1.0 : 0.0, 0, h,
-                [&](int, int p, uint64_t(&q)[2]) {
-                    const uint32_t* v = rm.values + (p < VB_SIDE ? VB_SIDE - VB_PER - p : p);
-                    q[0] = (uint64_t)(v[2] | v[3] << 16) << 32 | (v[0] | v[1] << 16);
-                    q[1] = (uint64_t)(v[6] | v[7] << 16) << 32 | (v[4] | v[5] << 16);
-                },
-                [](int, int, const uint64_t(&)[2]) {}, [](int) {}, val, idx);
+            const double part = lane == 0 ? 1.0 : 0.0;
+            const HeldCounts counts{rm.values};
+            const Classes classes = in_row(cl, part);
+            if (__builtin_expect(values_cut<false>(rm, r, an, 1, V, classes, part, h, counts,
+                                                   [](int) {}, val, idx),
+                                 1))
+                return true;
+            return values_lists<R>(rm, r, m, r.c, x, V, V, 1, classes, part, counts, val, idx);
         }
     } else if (r.k || r.p < 1.0) {
         if (cold((double)m * r.c)) return false;
@@ -170,19 +170,6 @@ struct ChunkSum {
     double z;
 };
 
-__device__ __forceinline__ void put(uint64_t* p, uint64_t v) {
-    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ void put(uint32_t* p, uint32_t v) {
-    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ uint64_t get(const uint64_t* p) {
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ uint32_t get(const uint32_t* p) {
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
 // The row's end, by the workgroup that put its last chunk.  False: the row has to be done
 // the slow way.
 template <typename T, int R, bool FILTERS>
@@ -230,27 +217,20 @@ __device__ __forceinline__ bool split_end(SplitSmem<T, FILTERS>& rm, const Sampl
                 cl = {get(parts + SAMPLE_PART * lane + 2), get(parts + SAMPLE_PART * lane + 3),
                       (uint32_t)n, (uint32_t)(n >> 32)};
             }
+            const ScratchCounts counts{mass};
+            const Anchor an = anchor(m, r.c);
+            Classes classes = in_row(cl, part);
+            if (!into_line(rm, an, classes, part, none ? 0 : value_base(m) - value_base(mc),
+                           counts))
+                return false;
             Held<T, SM_W, R> h;
-            return values_end(
-                rm, r, anchor(m, r.c), S, s.chunk, cl, part,
-                none ? 0 : value_base(m) - value_base(mc), h,
-                [&](int c, int p, uint64_t(&q)[2]) {
-                    const int b = p < VB_SIDE ? VB_SIDE - VB_PER - p : p;
-                    const uint64_t* at = mass + (int64_t)c * BINS + b / 4;
-                    q[0] = get(at);
-                    q[1] = get(at + 1);
-                },
-                [&](int c, int p, const uint64_t(&q)[2]) {
-                    const int b = p < VB_SIDE ? VB_SIDE - VB_PER - p : p;
-                    uint64_t* at = mass + (int64_t)c * BINS + b / 4;
-                    put(at, q[0]);
-                    put(at + 1, q[1]);
-                },
-                [&](int c) {
-                    const int64_t i0 = (int64_t)c * s.chunk;
-                    h.load(x + i0, (int32_t)(a.V - i0 < s.chunk ? a.V - i0 : s.chunk));
-                },
-                val, idx);
+            const RowParts<R> row{x, a.V, s.chunk};
+            if (__builtin_expect(values_cut<false>(rm, r, an, S, s.chunk, classes, part, h, counts,
+                                                   [&](int c) { row.hold(c, h); }, val, idx),
+                                 1))
+                return true;
+            return values_lists<R>(rm, r, m, r.c, x, a.V, s.chunk, S, classes, part, counts, val,
+                                   idx);
         }
     }
     // (the histograms leave out what is below 2^-64 of the largest weight; only a u at

@@ -3,8 +3,8 @@
 // computed per element, every bin is exact, and the cuts (sample.hpp) follow from the
 // bins alone, to the number of equal elements that stay.  The few elements nearer to 0,
 // which in the order stand between the positive and the negative bins, and those
-// beyond the negative end are weighed one by one, as two classes; a cut inside a class
-// leaves the row to the slow way.  Rows with larger values, or none near 0, move the 16
+// beyond the negative end are weighed one by one, as two classes, which are looked at again
+// only if a cut falls inside.  Rows with larger values, or none near 0, move the 16
 // octaves up, and parts of a row that moved them elsewhere are brought into line at
 // its end (64 x 128256 with 20 added to all, where a row's parts have their maxima on both
 // sides of 2^5: 40 us; centred 38).
@@ -30,7 +30,13 @@ struct ValueSmem {
     // of a pattern: sign * 2048 + (magnitude - base); for those outside one a lane, so
     // that a masked row's additions do not wait for each other
     uint32_t values[VB_BINS + 64];
-    double weights[VB_BINS];   // what an element of a bin weighs, if it is kept
+    union {
+        double weights[VB_BINS];  // what an element of a bin weighs, if it is kept
+        struct {                  // before that: the elements of a class in which a cut falls
+            float lx[VB_BINS];
+            uint32_t li[VB_BINS];
+        };
+    };
     uint64_t mid, tail;        // weights of the classes, in units of 2^-48
     uint32_t mid_n, tail_n;
     double part[8][64];        // kept weights by wavefront and chunk
@@ -157,75 +163,132 @@ struct Bins {
     }
 };
 
-// The row's end.  count8(c, p, q): the numbers of chunk c at positions p .. p + 7 of its own
-// bins, 16 bits each, in the order of the patterns' bins (from the last for positive
-// values); classes of chunk `lane`, whose maximum's weight in the row is `part`, in cl, and
-// how many bins the row's first is above its first in `off`; put8(c, p, q) puts numbers
-// back.  hold(c): makes h hold chunk c, from index c * chunk on.  False if the bins do not
-// decide.
-template <int R, typename Count8, typename Put8, typename Hold>
-__device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const Anchor& an, int S,
-                                           int64_t chunk, ClassSum cl, double part, int off,
+// The classes of chunk `lane` in the row's terms; part: what the chunk's maximum weighs there.
+struct Classes {
+    double mid, tail;
+    uint32_t mid_n, tail_n;
+};
+__device__ __forceinline__ Classes in_row(const ClassSum& c, double part) {
+    return Classes{(double)c.mid * 0x1p-48 * part, (double)c.tail * 0x1p-48 * part,
+                   part > 0.0 ? c.mid_n : 0u, part > 0.0 ? c.tail_n : 0u};
+}
+
+// Words that workgroups leave for each other, at the device's coherence point.
+__device__ __forceinline__ void put(uint64_t* p, uint64_t v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void put(uint32_t* p, uint32_t v) {
+    __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t get(const uint64_t* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint32_t get(const uint32_t* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The numbers of chunk c at positions p .. p + 7, 16 bits each, in the order of the patterns'
+// bins (from the last for positive values): in the scratch of a split row, or the bins of
+// a held one.
+struct ScratchCounts {
+    uint64_t* words;
+    __device__ __forceinline__ uint64_t* at(int c, int p) const {
+        return words + (int64_t)c * (VB_BINS / 4) +
+               (p < VB_SIDE ? VB_SIDE - VB_PER - p : p) / 4;
+    }
+    __device__ __forceinline__ void operator()(int c, int p, uint64_t (&q)[2]) const {
+        q[0] = get(at(c, p));
+        q[1] = get(at(c, p) + 1);
+    }
+    __device__ __forceinline__ void replace(int c, int p, const uint64_t (&q)[2]) const {
+        put(at(c, p), q[0]);
+        put(at(c, p) + 1, q[1]);
+    }
+};
+struct HeldCounts {
+    const uint32_t* values;
+    __device__ __forceinline__ void operator()(int, int p, uint64_t (&q)[2]) const {
+        const uint32_t* v = values + (p < VB_SIDE ? VB_SIDE - VB_PER - p : p);
+        q[0] = (uint64_t)(v[2] | v[3] << 16) << 32 | (v[0] | v[1] << 16);
+        q[1] = (uint64_t)(v[6] | v[7] << 16) << 32 | (v[4] | v[5] << 16);
+    }
+};
+
+// Chunks whose bins begin elsewhere, the row's first being `off` bins above theirs: their
+// counts are put where the row has their bins, and bins that it has not join the class
+// on their side.  False if a chunk's own class on the other side would have to be told
+// apart.
+__device__ __forceinline__ bool into_line(ValueSmem& sm, const Anchor& an, Classes& cl, double part,
+                                          int off, const ScratchCounts& count8) {
+    constexpr int W = 8;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+    const uint64_t moved = __ballot(part > 0.0 && off != 0);
+    if (moved == 0) return true;
+    if (__ballot(part > 0.0 && off != 0 && (off > 0 ? cl.tail_n : cl.mid_n) != 0) != 0)
+        return false;
+    if (tid < 64) {
+        sm.have[tid] = (uint32_t)off;
+        sm.take[tid] = 0;
+    }
+    const int base = value_base((float)an.m), p0 = VB_PER * tid;
+    // the least magnitude of the thread's bins, above the first one's
+    const int mag0 = p0 < VB_SIDE ? VB_SIDE - VB_PER - p0 : p0 - VB_SIDE;
+    __syncthreads();
+#pragma unroll 1
+    for (uint64_t rest = moved; rest != 0; rest &= rest - 1) {
+        const int c = __builtin_ctzll(rest), o = (int)sm.have[c];
+        uint64_t out[2] = {0, 0}, q[2] = {0, 0};
+        if (o > 0 ? mag0 < o : mag0 >= VB_SIDE + o) count8(c, p0, out);
+        if (mag0 + o >= 0 && mag0 + o < VB_SIDE) count8(c, p0 < VB_SIDE ? p0 - o : p0 + o, q);
+        uint32_t n = 0;
+        double sum = 0.0;
+        if (__ballot((out[0] | out[1]) != 0) != 0) {
+            uint32_t v = (uint32_t)(base - o + mag0) << 16 | (p0 < VB_SIDE ? 0u : 0x80000000u);
+#pragma unroll 1
+            for (int i = 0; i < VB_PER; ++i, v += 1u << 16) {
+                const uint32_t ni = (uint32_t)out[0] & 0xFFFFu;
+                const double w = an.weight(__uint_as_float(v));
+                n += w > 0.0 ? ni : 0u;  // (what has no weight counts nowhere)
+                sum += (double)ni * w;
+                out[0] = out[0] >> 16 | out[1] << 48;
+                out[1] >>= 16;
+            }
+            sum = group_sum<64>(sum);
+            if (n != 0) atomicAdd(&sm.take[c], n);
+        }
+        if (lane == 0) sm.part[wv][c] = sum;
+        // all have what they need of the chunk's counts
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        count8.replace(c, p0, q);
+    }
+    __syncthreads();
+    if (moved >> lane & 1) {
+        double sum = 0.0;
+#pragma unroll
+        for (int v = 0; v < W; ++v) sum += sm.part[v][lane];
+        (off > 0 ? cl.mid : cl.tail) += sum;
+        (off > 0 ? cl.mid_n : cl.tail_n) += sm.take[lane];
+    }
+    __syncthreads();
+    return true;
+}
+
+// The row's end: the cuts, and the token.  It goes by count8 (see there) and the classes.
+// hold(c): makes h hold chunk c, from index c * chunk on.  A cut that falls in a class
+// needs LISTS: the row's elements of that class are listed and ranked among each other,
+// unless there are too many.  False if it cannot be done.
+template <bool LISTS, int R, typename Count8, typename Hold>
+__device__ __forceinline__ bool values_cut(ValueSmem& sm, const Rule& r, const Anchor& an, int S,
+                                           int64_t chunk, Classes cl, double part,
                                            Held<bf16_t, 8, R>& h, const Count8& count8,
-                                           const Put8& put8, const Hold& hold, float* val,
-                                           int32_t* idx) {
+                                           const Hold& hold, float* val, int32_t* idx) {
     constexpr int W = 8;
     auto& s = sm.s;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
     const int base = value_base((float)an.m), p0 = VB_PER * tid;
     constexpr int AT_ONCE = 8;  // chunks whose counts are in flight, and held if these are all
     uint64_t held[AT_ONCE][2];
-    double mid_c = (double)cl.mid * 0x1p-48 * part, tail_c = (double)cl.tail * 0x1p-48 * part;
-    const uint64_t moved = __ballot(part > 0.0 && off != 0);
-    if (moved != 0) {
-        // These chunks' counts are put where the row has their bins; bins that it has not join
-        // the class on their side.  (A chunk's own class on the other side would have to be
-        // told apart.)
-        if (__ballot(part > 0.0 && off != 0 && (off > 0 ? cl.tail_n : cl.mid_n) != 0) != 0)
-            return false;
-        if (tid < 64) {
-            sm.have[tid] = (uint32_t)off;
-            sm.take[tid] = 0;
-        }
-        // the least magnitude of the thread's bins, above the first one's
-        const int mag0 = p0 < VB_SIDE ? VB_SIDE - VB_PER - p0 : p0 - VB_SIDE;
-        __syncthreads();
-#pragma unroll 1
-        for (uint64_t rest = moved; rest != 0; rest &= rest - 1) {
-            const int c = __builtin_ctzll(rest), o = (int)sm.have[c];
-            uint64_t out[2] = {0, 0}, q[2] = {0, 0};
-            if (o > 0 ? mag0 < o : mag0 >= VB_SIDE + o) count8(c, p0, out);
-            if (mag0 + o >= 0 && mag0 + o < VB_SIDE) count8(c, p0 < VB_SIDE ? p0 - o : p0 + o, q);
-            uint32_t n = 0;
-            double sum = 0.0;
-            if (__ballot((out[0] | out[1]) != 0) != 0) {
-                uint32_t v = (uint32_t)(base - o + mag0) << 16 | (p0 < VB_SIDE ? 0u : 0x80000000u);
-#pragma unroll 1
-                for (int i = 0; i < VB_PER; ++i, v += 1u << 16) {
-                    const uint32_t ni = (uint32_t)out[0] & 0xFFFFu;
-                    const double w = an.weight(__uint_as_float(v));
-                    n += w > 0.0 ? ni : 0u;  // (what has no weight counts nowhere)
-                    sum += (double)ni * w;
-                    out[0] = out[0] >> 16 | out[1] << 48;
-                    out[1] >>= 16;
-                }
-                sum = group_sum<64>(sum);
-                if (n != 0) atomicAdd(&sm.take[c], n);
-            }
-            if (lane == 0) sm.part[wv][c] = sum;
-            __syncthreads();  // all have what they need of the chunk's counts
-            put8(c, p0, q);
-        }
-        __syncthreads();
-        if (moved >> lane & 1) {
-            double sum = 0.0;
-#pragma unroll
-            for (int v = 0; v < W; ++v) sum += sm.part[v][lane];
-            (off > 0 ? mid_c : tail_c) += sum;
-            (off > 0 ? cl.mid_n : cl.tail_n) += sm.take[lane];
-        }
-        __syncthreads();
-    }
     const auto load_counts = [&](int c0) {
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
@@ -259,9 +322,9 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
         count += n;
         mass += (double)n * w;
     });
-    const double mid = group_sum<64>(mid_c), tail = group_sum<64>(tail_c);
-    const uint32_t mid_n = lane_value(wave_scan(part > 0.0 ? cl.mid_n : 0u), 63);
-    const uint32_t tail_n = lane_value(wave_scan(part > 0.0 ? cl.tail_n : 0u), 63);
+    const double mid = group_sum<64>(cl.mid), tail = group_sum<64>(cl.tail);
+    const uint32_t mid_n = lane_value(wave_scan(cl.mid_n), 63);
+    const uint32_t tail_n = lane_value(wave_scan(cl.tail_n), 63);
     // (units of 2^-48 lose the least weights of the classes, which a u at the very ends
     // of [0, 1] could still fall on)
     if ((mid_n != 0 || tail_n != 0) && (r.u < 0x1p-30 || r.u > 1.0 - 0x1p-30)) return false;
@@ -276,14 +339,17 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
     __syncthreads();
     uint32_t cbefore = cincl - count;
     double mbefore = lane_before(mincl), window = 0.0, positive = 0.0;
-    uint32_t bins_n = 0;
+    uint32_t bins_n = 0, positive_n = 0;
 #pragma unroll
     for (int v = 0; v < W; ++v) {
         if (v == wv) {
             cbefore += bins_n;
             mbefore += window;
         }
-        if (v == W / 2) positive = window;
+        if (v == W / 2) {
+            positive = window;
+            positive_n = bins_n;
+        }
         bins_n += s.wave32[v];
         window += s.waved[v];
     }
@@ -296,6 +362,71 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
     int cut = VB_BINS;          // position of the last kept value
     uint32_t keep = 0;          // elements of it that stay
     double all = window + mid + tail;
+    enum { NONE, MIDDLE, TAIL };
+    int split = NONE, listed = NONE;  // the class with a cut inside, and the listed one
+    Cut inner = no_cut();
+    const auto list_class = [&](int which) {
+        if constexpr (!LISTS) return false;
+        if (listed == which) return true;
+        const uint32_t have = which == MIDDLE ? cl.mid_n : cl.tail_n;
+        if ((which == MIDDLE ? mid_n : tail_n) > (uint32_t)VB_BINS) return false;
+        listed = which;
+        __syncthreads();
+        if (tid == 0) s.n = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (uint64_t rest = __ballot(have != 0); rest != 0; rest &= rest - 1) {
+            const int c = __builtin_ctzll(rest);
+            hold(c);
+            h.each([&](const u32x4& v, int32_t i) {
+                uint32_t in = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t bits = pattern(v, e);
+                    const bool middle = (bits & 0x7FFFu) < (uint32_t)base;
+                    in |= value_bin(bits, (uint32_t)base) == (uint32_t)VB_BINS &&
+                                  middle == (which == MIDDLE)
+                              ? 1u << e
+                              : 0u;
+                }
+                for (; __any(in != 0); in &= in - 1) {
+                    const int e = in ? __builtin_ctz(in) : 0;
+                    const uint32_t word = e < 2 ? v[0] : e < 4 ? v[1] : e < 6 ? v[2] : v[3];
+                    const float x = __uint_as_float(e & 1 ? word & 0xFFFF0000u : word << 16);
+                    if (in && an.weight(x) > 0.0) {
+                        const int j = atomicAdd(&s.n, 1);
+                        if (j < VB_BINS) {
+                            sm.lx[j] = x;
+                            sm.li[j] = (uint32_t)(c * chunk) + (uint32_t)(i + e);
+                        }
+                    }
+                }
+            });
+        }
+        __syncthreads();
+        return s.n > 0 && s.n <= VB_BINS;
+    };
+    const auto units = [&](float x) { return fixed48(an.weight(x)); };
+    const auto inside = [&](int j) {
+        return inner.keeps(sm.lx[j], sm.li[j]) && an.weight(sm.lx[j]) >= r.q;
+    };
+    const auto listed_sum = [&] {  // of what `inner` keeps, in units
+        uint64_t v = 0;
+        for (int j = tid; j < s.n; j += 64 * W)
+            if (inner.keeps(sm.lx[j], sm.li[j])) v += units(sm.lx[j]);
+        v = wave_total(v);
+        if (lane == 0) s.wave64[wv] = v;
+        __syncthreads();
+        v = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) v += s.wave64[w];
+        __syncthreads();
+        return v;
+    };
+    const auto source = [&] {
+        return ListSource{sm.lx, sm.li, s.n, (uint32_t)(S * chunk - 1)};
+    };
+    const uint32_t top = order_key((float)an.m), bottom = order_key(-__builtin_inff());
     if (r.k) {
         uint32_t b = cbefore;
         double d = mbefore;
@@ -313,8 +444,19 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
         if (cut < VB_BINS) {
             keep = (uint32_t)s.above;
             all = s.base;
-        } else if (tail_n != 0 || r.k <= (int64_t)bins_n + mid_n) {
-            return false;  // not among the bins: in the middle class, or beyond the end
+        } else if (r.k <= (int64_t)bins_n + mid_n + tail_n) {
+            // not among the bins: in the middle class, or beyond the end
+            const int which = r.k <= (int64_t)bins_n + mid_n ? MIDDLE : TAIL;
+            const int64_t k = r.k - (which == MIDDLE ? positive_n : bins_n + mid_n);
+            if (!list_class(which)) return false;
+            split = which;
+            inner = find_cut<false>(s, source(), bottom, top, inner,
+                                    (uint64_t)(k < s.n ? k : s.n), -1.0, units);
+            all = (split == MIDDLE ? positive : window + mid) + (double)listed_sum() * 0x1p-48;
+            if (split == MIDDLE) {
+                cut = VB_SIDE - 1;
+                keep = ~0u;
+            }
         }
         __syncthreads();
     }
@@ -327,7 +469,7 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
         int at = VB_BINS;
         // (the lowest position that reaches the target; the class in between is not one)
         bin.each([&](uint32_t n, double w, int p) {
-            const uint32_t m = p < cut ? n : p == cut ? keep : 0u;
+            const uint32_t m = p < cut ? n : p == cut ? (n < keep ? n : keep) : 0u;
             const double a = b + (double)m * w;
             if (m != 0 && a >= target && at == VB_BINS) {
                 at = p;
@@ -350,31 +492,64 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
             s.above = want;
         }
         __syncthreads();
-        // reached within the class that stands before it?
-        if (at >= VB_SIDE && cut >= VB_SIDE && mid_n != 0 && positive < target &&
-            positive + mid >= target)
-            return false;
-        if (at < VB_BINS) {
+        // or within a class: the one that stands before it, or beyond the end?
+        const bool middle = split == MIDDLE ? at == VB_BINS
+                                            : at >= VB_SIDE && cut >= VB_SIDE && mid_n != 0 &&
+                                                  positive < target && positive + mid >= target;
+        if (middle || (at == VB_BINS && tail_n != 0 && cut == VB_BINS)) {
+            if (!list_class(middle ? MIDDLE : TAIL)) return false;
+            split = middle ? MIDDLE : TAIL;
+            const uint64_t sum = listed_sum();
+            const double need =
+                __builtin_ceil((target - (middle ? positive : window + mid)) * 0x1p48);
+            const uint64_t want = need >= 1.0 ? (uint64_t)need : 1;
+            if (sum == 0) return false;
+            inner = find_cut<true>(s, source(), bottom, top, inner, want < sum ? want : sum, -1.0,
+                                   units);
+            if (middle) {
+                cut = VB_SIDE - 1;
+                keep = ~0u;
+            }
+        } else if (at < VB_BINS) {
             cut = at;
             keep = (uint32_t)s.above;
-        } else if (tail_n != 0 && cut == VB_BINS) {
-            return false;
+            split = NONE;
+            inner = no_cut();
         }
         __syncthreads();
     }
     // min-p, and what stays of the classes
-    bool mid_stays = mid_n != 0 && cut >= VB_SIDE, tail_stays = tail_n != 0 && cut == VB_BINS;
+    bool mid_stays = split == MIDDLE || (mid_n != 0 && cut >= VB_SIDE);
+    bool tail_stays = tail_n != 0 && cut == VB_BINS;
     if (r.q > 0.0) {
         const float tiny = __uint_as_float((uint32_t)base << 16);
         if (mid_stays) {
             const bool some = an.weight(tiny) >= r.q, every = an.weight(-tiny) >= r.q;
-            if (some && !every) return false;
-            mid_stays = every;
+            if (some && !every && split != MIDDLE) {  // (so the tail stays out)
+                if (!list_class(MIDDLE)) return false;
+                split = MIDDLE;
+                inner = no_cut();
+            }
+            mid_stays = some;
         }
         if (tail_stays) {
-            if (an.weight(position_value(VB_BINS - 1, base)) >= r.q) return false;
-            tail_stays = false;
+            tail_stays = an.weight(position_value(VB_BINS - 1, base)) >= r.q;
+            if (tail_stays && split != TAIL) {
+                if (!list_class(TAIL)) return false;
+                split = TAIL;
+            }
         }
+        if (split == TAIL && !tail_stays) split = NONE;
+        if (split == MIDDLE && !mid_stays) split = NONE;
+    }
+    if (split != NONE) {  // its kept weights by chunk, in the place of its whole ones
+        __syncthreads();
+        if (tid < 64) s.chunk[tid] = 0;
+        __syncthreads();
+        for (int j = tid; j < s.n; j += 64 * W)
+            if (inside(j)) add_bin(s.chunk[sm.li[j] / (uint32_t)chunk], units(sm.lx[j]));
+        __syncthreads();
+        (split == MIDDLE ? cl.mid : cl.tail) = (double)s.chunk[lane] * 0x1p-48;
     }
     // the kept weights of each chunk
     bin.each([&](uint32_t, double& w, int p) {
@@ -416,7 +591,7 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
     if (lane < S) {
 #pragma unroll
         for (int v = 0; v < W; ++v) kept += sm.part[v][lane];
-        kept += (mid_stays ? mid_c : 0.0) + (tail_stays ? tail_c : 0.0);
+        kept += (mid_stays ? cl.mid : 0.0) + (tail_stays ? cl.tail : 0.0);
     }
     const double incl = wave_scan(kept);
     const double total = lane_value(incl, 63), target = r.u * total;
@@ -467,12 +642,43 @@ __device__ __forceinline__ bool values_end(ValueSmem& sm, const Rule& r, const A
                 for (int e = 0; e < 8; ++e) {
                     const uint32_t p = pattern(q, e);
                     const bool of = (p & 0x7FFFu) < (uint32_t)base ? mid_stays : tail_stays;
-                    if (of && value_bin(p, (uint32_t)base) == (uint32_t)VB_BINS)
-                        y[e] = an.weight(h.at(q, e));
+                    if (of && value_bin(p, (uint32_t)base) == (uint32_t)VB_BINS &&
+                        inner.keeps(h.at(q, e), i0 + i + e)) {
+                        const double w = an.weight(h.at(q, e));
+                        y[e] = w >= r.q ? w : 0.0;
+                    }
                 }
             }
         },
         rem, total, i0, val, idx);
+}
+
+// The chunks of a row.
+template <int R>
+struct RowParts {
+    const bf16_t* x;
+    int64_t V, chunk;
+    __device__ __forceinline__ void hold(int c, Held<bf16_t, 8, R>& h) const {
+        const int64_t i0 = (int64_t)c * chunk;
+        h.load(x + i0, (int32_t)(V - i0 < chunk ? V - i0 : chunk));
+    }
+};
+
+// The same with lists, for the rows that need them (64 x 128256, a top-k among the 50
+// elements next to 0 in every row: 82 us, by passes over memory 428; with a cut elsewhere
+// 37).  In a function of its own: beside the common way its code and registers cost that 5%
+// of 512 x 128256.
+template <int R, typename Counts>
+__device__ __attribute__((noinline)) bool values_lists(ValueSmem& sm, Rule r, float m, double c,
+                                                       const bf16_t* x, int64_t V, int64_t chunk,
+                                                       int S, Classes cl, double part,
+                                                       Counts counts, float* val, int32_t* idx) {
+    const Anchor an = anchor(m, c);
+    const RowParts<R> row{x, V, chunk};
+    Held<bf16_t, 8, R> h;
+    __syncthreads();
+    return values_cut<true>(sm, r, an, S, chunk, cl, part, h, counts,
+                            [&](int c) { row.hold(c, h); }, val, idx);
 }
 
 }  // namespace osm

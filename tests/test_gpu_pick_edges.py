@@ -100,6 +100,79 @@ def test_a_constant_costs_bfloat16_rows_little(N, dev):
         assert us(shift) < 2.0 * centred, shift
 
 
+def near_zero(N, V, g, dev):
+    """Rows of which a hundredth lies within 2^-11 of 0, on both sides; and how many lie
+    above 2^-11, a row."""
+    x = torch.randn(N, V, device=dev, generator=g)
+    x = torch.where(torch.rand(N, V, device=dev, generator=g) < 0.01, 2.0 ** -12 * x.clamp(-1, 1), x)
+    x = x.to(torch.bfloat16)
+    return x, (x >= 2.0 ** -11).sum(dim=1)
+
+
+@pytest.mark.parametrize("V", [128256, 9001, 6000])
+def test_bfloat16_cuts_next_to_zero(V, dev):
+    """Cuts among the few elements between the positive and the negative bins: by top-k, by
+    top-p, by min-p and one after the other; equal elements there, and zeros of either sign."""
+    N = 24
+    g = torch.Generator(device=dev).manual_seed(V)
+    x, above = near_zero(N, V, g, dev)
+    x[1::4] = torch.where(x[1::4].abs() < 2.0 ** -11, torch.sign(x[1::4]) * 2.0 ** -13, x[1::4])
+    x[2::4] = torch.where(x[2::4].abs() < 2.0 ** -11, x[2::4] * 0.0, x[2::4])
+    mid = (x.abs() < 2.0 ** -11).sum(dim=1)
+    k = above + 1 + torch.arange(N, device=dev) * (mid - 1) // (N - 1)  # first to last of them
+    u = uniform(N, V, dev)
+    u[::3] = 1 - 2.0 ** -20
+    for T in (0.7, 1.5):
+        w = torch.exp(x.double() / T)
+        order = torch.sort(w, dim=1, descending=True).values
+        c = torch.cumsum(order, dim=1)
+        # between the sums before and at the k-th, so that no rounding decides
+        at = (torch.gather(c, 1, k.unsqueeze(1) - 1).squeeze(1) - 0.5)
+        p = (at / c[:, -1]).float()
+        pk = (at / torch.gather(c, 1, (above + mid).unsqueeze(1) - 1).squeeze(1)).float()
+        q = torch.exp(-x.double().amax(dim=1) / T).float()       # the weight of 0
+        kt, kall = k.int().tolist(), (above + mid).int().tolist()
+        for kw in (dict(top_k=kt), dict(top_p=p.tolist()), dict(min_p=q.tolist()),
+                   dict(top_k=kall, top_p=pk.tolist()), dict(top_k=kt, top_p=0.999999),
+                   dict(top_k=kt, top_p=0.5), dict(top_p=p.tolist(), min_p=q.tolist()),
+                   dict(top_k=(k + mid).int().tolist(), min_p=q.tolist())):
+            check(x, u, dev, temperature=T, **kw)
+
+
+@pytest.mark.parametrize("V", [40000, 7000])
+def test_bfloat16_cuts_beyond_the_bins(V, dev):
+    """Cuts among elements below -32 of rows that reach above 0, at temperatures that give
+    them weight."""
+    N = 12
+    g = torch.Generator(device=dev).manual_seed(V)
+    x = 5.0 * torch.randn(N, V, device=dev, generator=g)
+    x = torch.where(torch.rand(N, V, device=dev, generator=g) < 0.05, -40.0 - x.abs(), x)
+    x[3::4] = x[3::4].round()
+    x = x.clamp(max=31.0).to(torch.bfloat16)
+    low = (x <= -32.0).sum(dim=1)
+    k = (V - low + 1 + torch.arange(N, device=dev) * (low - 1) // (N - 1)).int().tolist()
+    u = uniform(N, V, dev)
+    u[::3] = 1 - 2.0 ** -20
+    for kw in (dict(top_k=k), dict(top_p=0.99), dict(top_p=0.9999), dict(top_k=k, top_p=0.9999),
+               dict(top_k=k, top_p=0.97), dict(min_p=0.15), dict(top_k=k, min_p=0.2),
+               dict(top_k=k, top_p=0.5)):
+        check(x, u, dev, temperature=40.0, **kw)
+
+
+@pytest.mark.parametrize("N", [64, 512])
+def test_cuts_next_to_zero_cost_bfloat16_rows_little(N, dev):
+    V = 128256
+    x = torch.randn(N, V, device=dev, generator=torch.Generator(device=dev).manual_seed(1))
+    x = x.to(torch.bfloat16)
+    above = (x >= 2.0 ** -11).sum(dim=1)
+    u = uniform(N, 1, dev)
+
+    def us(k):
+        k = k.int()
+        return best_us(lambda: osm.softmax_sample(x, u, top_k=k), batches=5, calls=3)
+    assert us(above + 5) < 3.0 * us(above // 2)
+
+
 @pytest.mark.filterwarnings("ignore:invalid value")     # of the reference, on purpose
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("E,K", [(24, 4), (33, 3), (256, 8)])
