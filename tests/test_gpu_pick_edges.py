@@ -196,3 +196,41 @@ def test_gradient_of_logits_that_are_not_numbers(E, K, dtype, dev):
             assert not none.any() or not renorm
             outside = torch.tensor([-1], dtype=torch.int32, device=dev).expand(7, K).contiguous()
             assert not osm.route_bwd(x, outside, g, score=score, renorm=renorm).any()
+
+
+@pytest.mark.parametrize("dtype,N,V", [("f32", 1400, 20000), ("bf16", 2100, 20000),
+                                       ("f32", 700, 50257), ("bf16", 1037, 50257)])
+def test_batches_of_more_than_one_launch(dtype, N, V, dev):
+    """4096 chunks a launch, in the same scratch: rows on both sides of each launch's border and
+    the last ones, and the whole batch the same with a workspace and once more."""
+    g = torch.Generator(device=dev).manual_seed(N)
+    r = torch.randn(N, V, device=dev, generator=g)
+    x = (2.0 * r).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    u = torch.rand(N, device=dev, generator=g)
+    rows = sorted({r for S in (2, 3, 4, 5, 7, 8) for b in range(4096 // S, N + 1, 4096 // S)
+                   for r in range(b - 3, b + 3) if 0 <= r < N} | set(range(4)) |
+                  set(range(N - 4, N)))
+    at = torch.tensor(rows, device=dev)
+    ws = torch.full((osm.sample_workspace(N, V, x.dtype),), 255, dtype=torch.uint8, device=dev)
+    assert 0 < ws.numel() == osm.sample_workspace(2 * N, V, x.dtype)   # a launch is full
+    for kw in (dict(), dict(top_p=0.9), dict(top_k=300, top_p=0.95, min_p=1e-3)):
+        vals, idx = osm.softmax_sample(x, u, **kw)
+        rv, ri = pick_ref.sample(host(x[at]), host(u[at]), **kw)
+        assert np.array_equal(idx[at].cpu().numpy(), ri)
+        pick_ref.close(host(vals[at]), rv)
+        for w in (ws, None):
+            v, i = osm.softmax_sample(x, u, workspace=w, **kw)
+            assert torch.equal(i, idx) and torch.equal(v, vals)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_streamed_rows(dtype, dev):
+    """Rows of more than 64 chunks."""
+    V = 2200003
+    assert osm.sample_workspace(3, V, torch.float32 if dtype == "f32" else torch.bfloat16) == 0
+    x, u = logits(3, V, dtype, 4, dev), uniform(3, 4, dev)
+    x[1, : V // 2] = -INF
+    x[2, 77] = NAN
+    for kw in (dict(), dict(top_p=0.9), dict(top_k=300), dict(min_p=0.01), dict(temperature=0.0),
+               dict(top_k=100000, top_p=0.99)):
+        check(x, u, dev, **kw)
