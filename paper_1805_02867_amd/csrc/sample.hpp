@@ -270,6 +270,20 @@ __device__ __forceinline__ Cut find_cut(SampleSmem<W>& sm, const Src& src, uint3
     }
 }
 
+template <int W>
+__device__ __forceinline__ uint32_t team_minimum(SampleSmem<W>& sm, uint32_t v) {
+    v = ~group_max<64>(~v);
+    if constexpr (W > 1) {
+        if ((threadIdx.x & 63) == 0) sm.wave32[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = sm.wave32[0];
+#pragma unroll
+        for (int w = 1; w < W; ++w) v = sm.wave32[w] < v ? sm.wave32[w] : v;
+        __syncthreads();
+    }
+    return v;
+}
+
 // ------------------------------------------------- a row too odd for the short way
 // Any row, by passes over memory: rows too long to be split, temperatures so low
 // that logits over T leave 2^30, bins that hold more elements than fit, and cuts
@@ -279,14 +293,16 @@ __device__ __forceinline__ void sample_row(SampleSmem<W>& sm, const RowSource<T>
                                            const Rule& r, float* val, int32_t* idx) {
     constexpr int BINS = SampleShape<W>::BINS, PER = SampleShape<W>::PER;
     const int tid = threadIdx.x % (64 * W), lane = tid & 63, wv = tid >> 6;
-    // the maximum with its lowest index, and whether a NaN or +inf is there
+    // the maximum with its lowest index, the minimum, and whether a NaN or +inf is there
     uint64_t best = 0;
+    uint32_t least = ~0u;
     int bad = 0;
     for (int64_t i = tid; i < src.n; i += 64 * W) {
         const float x = src.value(i);
         bad |= !(x < __builtin_inff());
         const uint64_t k = (uint64_t)order_key(x) << 32 | (uint32_t)~(uint32_t)i;
         best = k > best ? k : best;
+        least = (uint32_t)(k >> 32) < least ? (uint32_t)(k >> 32) : least;
     }
     best = group_max<64>(best);
     bad = __any(bad);
@@ -315,7 +331,7 @@ __device__ __forceinline__ void sample_row(SampleSmem<W>& sm, const RowSource<T>
     }
     const double m = mx, c = r.c;
     const auto wt = [m, c](float x) { return exp2_wide(((double)x - m) * c); };
-    const uint32_t top = (uint32_t)(best >> 32), bottom = order_key(-__builtin_inff());
+    const uint32_t top = (uint32_t)(best >> 32), bottom = team_minimum(sm, least);
     Cut cut = no_cut();
     // the largest weight, 1, in so many units that n of them sum below 2^63
     const double scale = __builtin_ldexp(1.0, 62 - (64 - __builtin_clzll((uint64_t)src.n)));
@@ -337,7 +353,10 @@ __device__ __forceinline__ void sample_row(SampleSmem<W>& sm, const RowSource<T>
     do {
         int64_t L = (b - a + BINS - 1) / BINS;
         L = (L + 63) / 64 * 64;
-        for (int s = wv; s < BINS; s += W) {
+        // (the segments past the range are empty)
+        for (int s = tid; s < BINS; s += 64 * W)
+            if (a + s * L >= b) sm.seg[s] = 0.0;
+        for (int s = wv; s < BINS && a + s * L < b; s += W) {
             double sum = 0.0;
             const int64_t e = a + (s + 1) * L < b ? a + (s + 1) * L : b;
             for (int64_t i = a + s * L + lane; i < e; i += 64) sum += kept(i);
@@ -523,20 +542,6 @@ __device__ __forceinline__ float team_maximum(SampleSmem<W>& sm, float v) {
         v = sm.wavef[0];
 #pragma unroll
         for (int w = 1; w < W; ++w) v = __builtin_elementwise_maximum(v, sm.wavef[w]);
-        __syncthreads();
-    }
-    return v;
-}
-
-template <int W>
-__device__ __forceinline__ uint32_t team_minimum(SampleSmem<W>& sm, uint32_t v) {
-    v = ~group_max<64>(~v);
-    if constexpr (W > 1) {
-        if ((threadIdx.x & 63) == 0) sm.wave32[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = sm.wave32[0];
-#pragma unroll
-        for (int w = 1; w < W; ++w) v = sm.wave32[w] < v ? sm.wave32[w] : v;
         __syncthreads();
     }
     return v;

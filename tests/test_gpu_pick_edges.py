@@ -198,6 +198,23 @@ def test_gradient_of_logits_that_are_not_numbers(E, K, dtype, dev):
             assert not osm.route_bwd(x, outside, g, score=score, renorm=renorm).any()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_flat_and_cold_short_rows_cost_little(dtype, dev):
+    """Rows whose cut lies among more elements than a list holds, or below the histogram,
+    against ordinary ones; and their tokens."""
+    N, V = 4000, 1000
+    x, u = logits(N, V, dtype, 3, dev, 1.0), uniform(N, 3, dev)
+    flat = torch.ones_like(x)
+
+    def us(x, **kw):
+        return best_us(lambda: osm.softmax_sample(x, u, **kw), batches=5, calls=3)
+    ordinary = us(x, top_p=0.9)
+    for y, kw in ((x, dict(top_p=0.9, temperature=30.0)), (x, dict(top_k=700, temperature=30.0)),
+                  (flat, dict(top_p=0.9)), (x, dict(top_k=50, temperature=0.05))):
+        check(y[:64], u[:64], dev, **kw)
+        assert us(y, **kw) < 3.0 * ordinary, kw
+
+
 @pytest.mark.parametrize("dtype,N,V", [("f32", 1400, 20000), ("bf16", 2100, 20000),
                                        ("f32", 700, 50257), ("bf16", 1037, 50257)])
 def test_batches_of_more_than_one_launch(dtype, N, V, dev):
