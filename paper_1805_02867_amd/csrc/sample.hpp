@@ -16,8 +16,8 @@
 // the bin's weights (and for top-k their number); its running sums say in
 // which bin a cut falls, and only that bin's elements are looked at one by one:
 // ranked among each other if they are few, else by further histograms over
-// their ordered bits and, among equal ones, their indices.  (bfloat16 rows longer than
-// a wavefront's go by their values instead: sample_values.hpp.)
+// their ordered bits and, among equal ones, their indices.  (bfloat16 rows of more than two
+// vectors a lane of a workgroup go by their values instead: sample_values.hpp.)
 //
 // A binary64 weight is 20 instructions and a bin 10 more.  At 256 x 128256 binary32
 // without filters (52 us; the 131 MB alone 27) the passes over the chunks run at the

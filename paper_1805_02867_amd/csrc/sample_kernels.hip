@@ -21,17 +21,22 @@ __device__ __forceinline__ SampleSmem<W>& smem_of(ListSmem<W>& sm) {
     return sm;
 }
 
-// bfloat16 rows of a workgroup go by their values, others by the bins of their weights.
-template <typename T, int W>
-using RowSmem = std::conditional_t<W == SM_W && std::is_same_v<T, bf16_t>, ValueSmem, ListSmem<W>>;
+// bfloat16 rows of more than two vectors a lane of a workgroup go by their values, others by
+// the bins of their weights: clearing and adding up 4096 bins takes shorter rows longer
+// than it saves (1000 x 2000 top-p 63 us by values, 43 by weights; 1000 x 12000 84 and 109).
+template <typename T, int W, int R>
+using RowSmem =
+    std::conditional_t<W == SM_W && R != 2 && std::is_same_v<T, bf16_t>, ValueSmem, ListSmem<W>>;
 template <typename T, bool FILTERS>
-using SplitSmem = std::conditional_t<FILTERS, RowSmem<T, SM_W>, SampleSmem<SM_W>>;
+using SplitSmem = std::conditional_t<
+    FILTERS, std::conditional_t<std::is_same_v<T, bf16_t>, ValueSmem, ListSmem<SM_W>>,
+    SampleSmem<SM_W>>;
 
 // A row held by the team: loaded once.  False: it has to be done the slow way.
 template <typename T, int W, int R>
-__device__ __forceinline__ bool held_row(RowSmem<T, W>& rm, const T* x, int32_t V, const Rule& r,
-                                         float* val, int32_t* idx) {
-    constexpr bool VALUES = std::is_same_v<RowSmem<T, W>, ValueSmem>;
+__device__ __forceinline__ bool held_row(RowSmem<T, W, R>& rm, const T* x, int32_t V,
+                                         const Rule& r, float* val, int32_t* idx) {
+    constexpr bool VALUES = std::is_same_v<RowSmem<T, W, R>, ValueSmem>;
     SampleSmem<W>& sm = smem_of(rm);
     constexpr int THREADS = 64 * W, PER = SampleShape<W>::PER;
     const int tid = threadIdx.x % THREADS;
@@ -135,7 +140,7 @@ __global__ __launch_bounds__(256, 4) void sample_short(const SampleRows a) {
 
 template <typename T, int R>
 __global__ __launch_bounds__(SM_BLOCK, 4) void sample_rows(const SampleRows a) {
-    __shared__ RowSmem<T, SM_W> sm;
+    __shared__ RowSmem<T, SM_W, R> sm;
     for (int64_t row = blockIdx.x; row < a.N; row += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + row * a.ld;
         const Rule r = row_rule(a, row);

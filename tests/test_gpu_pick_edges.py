@@ -215,6 +215,17 @@ def test_flat_and_cold_short_rows_cost_little(dtype, dev):
         assert us(y, **kw) < 3.0 * ordinary, kw
 
 
+@pytest.mark.parametrize("N,V", [(1000, 7000), (2000, 8000)])
+def test_bfloat16_rows_of_a_workgroup_take_no_longer_than_binary32(N, V, dev):
+    """Of as many elements a lane, in half the bytes."""
+    x, u = logits(N, V, "f32", 3, dev), uniform(N, 3, dev)
+
+    def us(x, kw):
+        return best_us(lambda: osm.softmax_sample(x, u, **kw), batches=5, calls=3)
+    for kw in (dict(), dict(top_p=0.9), dict(top_k=50), dict(temperature=0.0)):
+        assert us(x.to(torch.bfloat16), kw) < 1.25 * us(x, kw), kw
+
+
 @pytest.mark.parametrize("dtype,N,V", [("f32", 1400, 20000), ("bf16", 2100, 20000),
                                        ("f32", 700, 50257), ("bf16", 1037, 50257)])
 def test_batches_of_more_than_one_launch(dtype, N, V, dev):
