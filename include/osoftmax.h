@@ -328,7 +328,7 @@ OSM_API int softmax_sample_ws(const void* x, int64_t ldx, const float* u,
                               size_t workspace_bytes, hipStream_t stream);
 
 /* Bytes of workspace that softmax_sample_ws needs for this shape on the current device
- * (0 for rows that one workgroup takes), for any ldx and alignment.
+ * (0 for rows that one workgroup takes), for any ldx, alignment and settings.
  * Errors: OSM_EINVAL for bad sizes or dtype or NULL bytes. */
 OSM_API int osm_sample_workspace(int64_t N, int64_t V, int dtype, size_t* bytes);
 

@@ -692,7 +692,8 @@ int run_sample(const void* x, int64_t ldx, const float* u, const osm_sample_para
                             s.min_p,    s.temperature_all, s.top_k_all, s.top_p_all,
                             s.min_p_all, vals,      idx,               N,           V,
                             ldx};
-    const osm::SamplePlan p = osm::sample_plan(N, V, ldx, aligned(x, 16), dtype, ds->cus);
+    const osm::SamplePlan p = osm::sample_plan(N, V, ldx, aligned(x, 16), dtype,
+                                               osm::sample_filters(a), ds->cus);
     if (p.S <= 1) return hip_status(osm::launch_sample(a, p, dtype, nullptr, nullptr, stream));
     const size_t at = sample_counters_at(p);
     if (own) {
@@ -874,8 +875,13 @@ int osm_sample_workspace(int64_t N, int64_t V, int dtype, size_t* bytes) {
     if (!check_shape(N, V, dtype, &batch) || !bytes) return OSM_EINVAL;
     DeviceState* ds = device_state(nullptr);
     // (rows that are not aligned may take one path less, never a larger split)
-    const osm::SamplePlan p = osm::sample_plan(N, V, V, false, dtype, ds ? ds->cus : 256);
-    *bytes = p.S <= 1 ? 0 : sample_counters_at(p) + (size_t)p.rows * 4;
+    *bytes = 0;
+    for (const bool filters : {false, true}) {
+        const osm::SamplePlan p =
+            osm::sample_plan(N, V, V, false, dtype, filters, ds ? ds->cus : 256);
+        const size_t need = p.S <= 1 ? 0 : sample_counters_at(p) + (size_t)p.rows * 4;
+        *bytes = need > *bytes ? need : *bytes;
+    }
     return OSM_OK;
 }
 

@@ -131,7 +131,9 @@ struct SampleSplit {
     uint32_t* counts;
     uint32_t* ctr;
 };
-SamplePlan sample_plan(int64_t N, int64_t V, int64_t ld, bool aligned, int dtype, int cus);
+bool sample_filters(const SampleRows& a);  // whether any row may have one
+SamplePlan sample_plan(int64_t N, int64_t V, int64_t ld, bool aligned, int dtype, bool filters,
+                       int cus);
 size_t sample_scratch_bytes(const SamplePlan& p);
 hipError_t launch_sample(const SampleRows& a, const SamplePlan& p, int dtype, void* scratch,
                          uint32_t* ctr, hipStream_t st);

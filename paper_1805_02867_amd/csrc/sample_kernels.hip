@@ -498,7 +498,13 @@ constexpr int64_t held_elems(int R) {
 }
 }  // namespace
 
-SamplePlan sample_plan(int64_t N, int64_t V, int64_t ld, bool aligned, int dtype, int cus) {
+bool sample_filters(const SampleRows& a) {
+    return a.top_k || a.top_p || a.min_p || (a.top_k_all > 0 && a.top_k_all < a.V) ||
+           a.top_p_all < 1.0f || a.min_p_all > 0.0f;
+}
+
+SamplePlan sample_plan(int64_t N, int64_t V, int64_t ld, bool aligned, int dtype, bool filters,
+                       int cus) {
     const int E = dtype == 1 ? 8 : 4;
     const int64_t room = V + (aligned && ld % E == 0 ? 0 : E - 1);
     const int64_t one = (int64_t)SM_BLOCK * E;  // a vector a lane
@@ -510,11 +516,20 @@ SamplePlan sample_plan(int64_t N, int64_t V, int64_t ld, bool aligned, int dtype
     // rows than fill the chip are split further, into up to four chunks, whose sums the
     // row's end has in flight at once (33 x 50257 binary32 top-p and min-p: 38.9 us with
     // four, 43.7 with eight, 47.0 with twelve).
-    int64_t R = 4;
-    int64_t least = (V + R * one - E - 1) / (R * one - E);
-    if (least > kSplitMax) {
+    // Binary32 rows with filters take eight as well where that saves a launch (which waits for
+    // the one before) or, of more than four chunks, half a launch's: their histograms are what a
+    // row's end reads, and their kernels have the registers (top-p, us with eight and four:
+    // 128 x 128256 102 and 95, 250 x 128256 126 and 133, 300 x 128256 138 and 216; 1000 x 20000
+    // 134 and 121, 1400 x 20000 174 and 193, 2100 x 20000 282 and 252).
+    const auto chunks = [&](int64_t r) { return (V + r * one - E - 1) / (r * one - E); };
+    const auto launches = [&](int64_t s) { return (N + kSplitChunks / s - 1) / (kSplitChunks / s); };
+    int64_t R = 4, least = chunks(4);
+    const int64_t eight = chunks(8);
+    if (least > kSplitMax ||
+        (filters && dtype != 1 && eight > 1 &&
+         ((least > 4 && N * least > kSplitChunks / 2) || launches(eight) < launches(least)))) {
         R = 8;
-        least = (V + R * one - E - 1) / (R * one - E);
+        least = eight;
     }
     int64_t S = 2 * (int64_t)cus / (N > 0 ? N : 1);
     const int64_t most = V / one;
@@ -555,8 +570,7 @@ static hipError_t launch_sample_t(const SampleRows& a, const SamplePlan& p, void
         return hipGetLastError();
     }
     constexpr int64_t BINS = SampleShape<SM_W>::BINS;
-    const bool filters = a.top_k || a.top_p || a.min_p || (a.top_k_all > 0 && a.top_k_all < a.V) ||
-                         a.top_p_all < 1.0f || a.min_p_all > 0.0f;
+    const bool filters = sample_filters(a);
     SampleSplit s;
     s.S = p.S;
     s.chunk = p.chunk;
