@@ -649,10 +649,14 @@ hipError_t launch_route_t(const RouteRows& a, hipStream_t st) {
                      a.E >= 32;
 #define OSM_LANES(L) \
     return vec ? launch_route_l<T, BWD, L, 4>(a, st) : launch_route_l<T, BWD, L, 1>(a, st)
-    // eight experts a lane once the batch fills the chip: the steps over the lanes then serve
-    // twice as many rows (16384 x 256 binary32: 26.5 us, with four 36.9; the gradient 10.8 and
-    // 14.4); else four (16 x 64: 3.8 and 4.3)
-    switch (route_lanes(a, a.N * a.E >= (int64_t)a.cus * 4096 ? 8 : 4)) {
+    // Eight experts a lane once the batch fills the chip: the steps over the lanes then serve
+    // twice as many rows.  Else four.  us with eight and four, binary32 sigmoid with a bias
+    // and groups: 1024 x 256 8.8 and 8.0, 2048 x 256 9.4 and 9.5, 4096 x 128 9.7 and 9.7,
+    // 4096 x 160 9.2 and 11.1, 4096 x 256 10.7 and 12.7, 16384 x 256 29 and 42; softmax
+    // without scores 2048 x 256 6.7 and 6.0, 4096 x 160 6.7 and 7.0, 16384 x 256 16 and 22;
+    // the dense gradient 1024 x 256 4.0 and 3.7, 4096 x 160 4.8 and 4.9, 16384 x 256 10.2
+    // and 13.4.  (From 257 experts on both are the same.)
+    switch (route_lanes(a, a.N * a.E > (int64_t)a.cus * 2048 ? 8 : 4)) {
         case 8: OSM_LANES(8);
         case 16: OSM_LANES(16);
         case 32: OSM_LANES(32);

@@ -173,6 +173,17 @@ def test_cuts_next_to_zero_cost_bfloat16_rows_little(N, dev):
     assert us(above + 5) < 3.0 * us(above // 2)
 
 
+def test_routing_twice_the_rows_takes_longer(dev):
+    """4096 x 160 has the lanes of the larger batch (0.76 of its time; with half the experts a
+    lane 0.91)."""
+    def us(N):
+        x, b = router(N, 160, "f32", N, dev), 0.05 * router(1, 160, "f32", 1, dev).view(-1)
+        kw = dict(score="sigmoid", groups=8, top_groups=3, group_top=2)
+        vals, idx = osm.route_fwd(x, 6, b, **kw)
+        return best_us(lambda: osm.route_fwd(x, 6, b, vals=vals, idx=idx, **kw))
+    assert us(4096) < 0.84 * us(8192)
+
+
 @pytest.mark.filterwarnings("ignore:invalid value")     # of the reference, on purpose
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("E,K", [(24, 4), (33, 3), (256, 8)])
