@@ -46,11 +46,10 @@ __global__ void zero_u32(uint32_t* p, int64_t n) {
 
 struct DeviceState {
     std::once_flag once;
-    int cus = 0;
+    int dev = 0, cus = 0;
     void* scratch_ptr = nullptr;  // device address of `scratch` (null if the lookup failed)
-    hipMemPool_t pool = nullptr;
-    bool pool_ok = false;
-    std::mutex mu;  // guards the scratch and counter tables
+    hipMemPool_t pool = nullptr;  // made when it is first needed
+    std::mutex mu;                // guards it, and the scratch and counter tables
     ScratchSlot slots[kScratchSlots] = {};
     int nslots = 0;
     ScratchSlot cslots[kScratchSlots] = {};  // zeroed counter arrays, per stream
@@ -68,25 +67,34 @@ DeviceState* device_state(int* dev_out) {
             cus <= 0)
             cus = 256;
         s.cus = cus;
+        s.dev = dev;
         void* sp = nullptr;
         if (hipGetSymbolAddress(&sp, HIP_SYMBOL(scratch)) == hipSuccess && sp) s.scratch_ptr = sp;
-        // A library-owned stream-ordered pool keeps split-V scratch cheap to
-        // allocate and free on any stream without touching the device's
-        // default pool settings.
-        hipMemPoolProps props = {};
-        props.allocType = hipMemAllocationTypePinned;
-        props.handleTypes = hipMemHandleTypeNone;
-        props.location.type = hipMemLocationTypeDevice;
-        props.location.id = dev;
-        if (hipMemPoolCreate(&s.pool, &props) == hipSuccess) {
-            uint64_t keep = UINT64_MAX;
-            (void)hipMemPoolSetAttribute(s.pool, hipMemPoolAttrReleaseThreshold, &keep);
-            s.pool_ok = true;
-        }
         (void)hipGetLastError();
     });
     if (dev_out) *dev_out = dev;
     return &s;
+}
+
+// A library-owned stream-ordered pool keeps split-V scratch cheap to allocate
+// and free on any stream without touching the device's default pool settings.
+// It cannot be made while a stream is being captured, so a call that needs none
+// does not make it, and one that failed to is no reason for the next to fail.
+bool have_pool(DeviceState* ds) {
+    if (ds->pool) return true;
+    hipMemPoolProps props = {};
+    props.allocType = hipMemAllocationTypePinned;
+    props.handleTypes = hipMemHandleTypeNone;
+    props.location.type = hipMemLocationTypeDevice;
+    props.location.id = ds->dev;
+    hipMemPool_t pool = nullptr;
+    if (hipMemPoolCreate(&pool, &props) == hipSuccess && pool) {
+        uint64_t keep = UINT64_MAX;
+        (void)hipMemPoolSetAttribute(pool, hipMemPoolAttrReleaseThreshold, &keep);
+        ds->pool = pool;
+    }
+    (void)hipGetLastError();
+    return ds->pool != nullptr;
 }
 
 // The scratch and counter tables are guarded by the device's mutex, and a
@@ -115,8 +123,8 @@ ScratchSlot* find_slot(ScratchSlot* tab, int* n, hipStream_t stream) {
 // stream order after its launches.
 int acquire_scratch(DeviceState* ds, std::unique_lock<std::mutex>& lk, hipStream_t stream,
                     size_t bytes, void** out, bool* temp) {
-    if (!ds->pool_ok) return OSM_ENOMEM;
     if (!lk.owns_lock()) lk.lock();
+    if (!have_pool(ds)) return OSM_ENOMEM;
     ScratchSlot* slot = find_slot(ds->slots, &ds->nslots, stream);
     *temp = slot == nullptr;
     if (slot && slot->bytes >= bytes) {
@@ -150,8 +158,8 @@ int acquire_scratch(DeviceState* ds, std::unique_lock<std::mutex>& lk, hipStream
 // (*temp = true) to free after its launches.  Locking as acquire_scratch.
 int acquire_counters(DeviceState* ds, std::unique_lock<std::mutex>& lk, hipStream_t stream,
                      size_t count, uint32_t** out, bool* temp) {
-    if (!ds->pool_ok) return OSM_ENOMEM;
     if (!lk.owns_lock()) lk.lock();
+    if (!have_pool(ds)) return OSM_ENOMEM;
     ScratchSlot* slot = find_slot(ds->cslots, &ds->ncslots, stream);
     *temp = slot == nullptr;
     const size_t bytes = count * 4;
