@@ -28,10 +28,11 @@
 //   sigmoid:                dx_i = scale g_i s_i (1 - s_i)
 // and 0 elsewhere.  The choice itself has no gradient, and neither has the bias.
 //
-// What bounds them: 16384 x 256 binary32 sigmoid with a bias and groups takes 27 us, the 17
-// MB alone 3.6: about 600 vector instructions a row and the draws' dependent steps, at four
-// wavefronts a SIMD (more of them spill: 34 to 42 us).  The gradient of that batch, 10.6
-// us, is near its 34 MB (7.1).  Calls of some thousand logits are a launch, 3.3 to 3.6 us.
+// What bounds them: 16384 x 256 binary32 sigmoid with a bias and groups takes 25 to 28 us, the
+// 17 MB alone 2.6: 640 vector instructions a row and the draws' dependent steps, at four
+// wavefronts a SIMD (more of them spill: 34 to 42 us).  Without scores 10007 x 160 bfloat16
+// has 475 a row (10.8 us).  The gradient of the first batch, 10.5 us, is 62% of a large
+// copy's rate (its 34 MB 6.5).  Calls of some thousand logits are a launch, 3.3 to 4.0 us.
 #include "wide.hpp"
 #include "kernels.h"
 

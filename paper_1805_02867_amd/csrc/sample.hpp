@@ -19,13 +19,13 @@
 // their ordered bits and, among equal ones, their indices.  (bfloat16 rows of more than two
 // vectors a lane of a workgroup go by their values instead: sample_values.hpp.)
 //
-// A binary64 weight is 20 instructions and a bin 10 more.  At 256 x 128256 binary32
-// without filters (52 us; the 131 MB alone 27) the passes over the chunks run at the
-// memory's rate and the rest is the ends of the rows, about 10 us each, of which
-// the last ones have the chip to themselves.  Few rows are bound by that end: 33 x
-// 50257 binary32 with top-p and min-p 39 us, 1 x 32000 bfloat16 with top-k and top-p
-// 20.  Short rows (4000 x 1000 binary32 top-k 29 us, the 16 MB 3) are bound by the
-// wavefront's own chain of steps.
+// A binary64 weight is 20 instructions and a bin 10 more.  256 x 128256 binary32 without
+// filters takes 47 to 50 us (the 131 MB at a large read's rate 19): 38 of them, timed without
+// the ends of the rows, are the chunks, and the rest is what the ends add.  Few rows are
+// bound by the end: 33 x 50257 binary32 with top-p and min-p 38 us, the chunks 8 of them;
+// 1 x 32000 bfloat16 with top-k and top-p 18 and 5.  Short rows (4000 x 1000 binary32 top-k
+// 28 to 29 us, the 16 MB 2.3) are bound by the wavefront's own steps, 2640 vector
+// instructions a row.
 //
 // Weights are binary64 and the sums of a histogram are in fixed point: in
 // binary32 the sums of 10^5 weights are off by more than the distance between the
@@ -286,8 +286,10 @@ __device__ __forceinline__ uint32_t team_minimum(SampleSmem<W>& sm, uint32_t v) 
 
 // ------------------------------------------------- a row too odd for the short way
 // Any row, by passes over memory: rows too long to be split, temperatures so low
-// that logits over T leave 2^30, bins that hold more elements than fit, and cuts
-// below the histogram's 64 powers of two.
+// that logits over T leave 2^30, binary32 (or short) rows with a cut in a bin that holds
+// more elements than fit or below the histogram's 64 powers of two, and numbers u at the
+// very ends of [0, 1] of split rows with a filter.  A long row takes several times as long
+// (64 x 128256 binary32, a top-k of 50 at T 0.1: 450 us; at T 1 73).
 template <int W, typename T>
 __device__ __forceinline__ void sample_row(SampleSmem<W>& sm, const RowSource<T>& src,
                                            const Rule& r, float* val, int32_t* idx) {

@@ -389,11 +389,11 @@ __device__ __forceinline__ bool split_end(SplitSmem<T, FILTERS>& rm, const Sampl
 // A chunk of a row a workgroup.  Workgroups go to the eight dies in turn, and there to
 // groups of CUs in turn, each waiting for room where its turn is; and the one that
 // ends a row is as a rule the last of its chunks to start.  With a row's chunks side by
-// side every row ends at the same few places, for which the next ones then wait (512 x
-// 128256 bfloat16, four chunks a row: a fifth of the chip busy).  So the chunks of 32
-// rows are interleaved: rows end at 32 places in turn, and a row's chunks are on one
-// die, whose L2 has their sums (341 -> 200 us).  Fewer than eight rows spread theirs over
-// all dies.
+// side every row ends at the same few places, for which the next ones then wait.  So the
+// chunks of 32 rows are interleaved: rows end at 32 places in turn, and a row's chunks are
+// on one die, whose L2 has their sums (side by side and interleaved: 512 x 128256 bfloat16
+// top-p, eight chunks a row, 234 and 100 us; 256 x 128256 binary32 without filters 75 and
+// 47).  Fewer than eight rows spread theirs over all dies.
 // Without FILTERS every row draws from its whole distribution (or takes its maximum).
 template <typename T, int R, bool FILTERS>
 __global__ __launch_bounds__(SM_BLOCK, FILTERS ? 4 : 6) void sample_split(const SampleRows a,
@@ -510,19 +510,22 @@ SamplePlan sample_plan(int64_t N, int64_t V, int64_t ld, bool aligned, int dtype
     const int64_t one = (int64_t)SM_BLOCK * E;  // a vector a lane
     if (room <= SM_SHORT) return {0, 1, V, 1};
     if (room <= 2 * one) return {2, 1, V, 1};
-    // Chunks of whole vectors, at most four a lane: with eight the kernels take so many
-    // registers that half as many workgroups fit on a CU (256 x 128256 binary32 without
-    // filters 61.1 us, with four 52.7); eight where a row would have too many chunks.  Fewer
-    // rows than fill the chip are split further, into up to four chunks, whose sums the
-    // row's end has in flight at once (33 x 50257 binary32 top-p and min-p: 38.9 us with
-    // four, 43.7 with eight, 47.0 with twelve).
+    // Chunks of whole vectors, at most four a lane: with eight the kernels without filters
+    // take so many registers that fewer workgroups fit on a CU (256 x 128256 binary32 59 us,
+    // with four 47); eight where a row would have too many chunks.  Fewer rows than fill the
+    // chip are split further, into up to four chunks, whose sums the row's end has in flight
+    // at once (60 x 16000 binary32 top-p: 32.2 us with four, 33.5 with the two that it needs,
+    // 37.0 with seven).
     // Binary32 rows with filters take eight as well where that saves a launch (which waits for
     // the one before) or, of more than four chunks, half a launch's: their histograms are what a
     // row's end reads, and their kernels have the registers (top-p, us with eight and four:
     // 128 x 128256 102 and 95, 250 x 128256 126 and 133, 300 x 128256 138 and 216; 1000 x 20000
     // 134 and 121, 1400 x 20000 174 and 193, 2100 x 20000 282 and 252).
     const auto chunks = [&](int64_t r) { return (V + r * one - E - 1) / (r * one - E); };
-    const auto launches = [&](int64_t s) { return (N + kSplitChunks / s - 1) / (kSplitChunks / s); };
+    const auto launches = [&](int64_t s) {
+        const int64_t rows = kSplitChunks / s;
+        return (N + rows - 1) / rows;
+    };
     int64_t R = 4, least = chunks(4);
     const int64_t eight = chunks(8);
     if (least > kSplitMax ||

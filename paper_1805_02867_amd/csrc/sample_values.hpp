@@ -10,9 +10,10 @@
 // sides of 2^5: 40 us; centred 38).
 //
 // Against a histogram of weights this takes a third of the instructions an element and no
-// second pass over the row: 512 x 128256 top-p 204 -> 106 us, 64 x 128256 with a setting a
-// row 91 -> 36.  What bounds it now is not the 131 MB (27 us at a large copy's rate): half
-// is the elements' instructions and shared-memory additions, half the ends of the rows.
+// second pass over the row: 512 x 128256 top-p 204 -> 146 us when it came, 64 x 128256 with a
+// setting a row 91 -> 60; now 100 and 35.  What bounds it is not the 131 MB (19 us at a large
+// read's rate): the chunks take 57 of the 100 us, with 1000 vector instructions and 53
+// shared-memory ones a wavefront, ends included, and the ends of the rows the rest.
 #pragma once
 
 #include "sample.hpp"

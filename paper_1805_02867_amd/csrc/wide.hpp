@@ -1,8 +1,8 @@
 // Binary64 building blocks of the kernels whose choices must not depend on
 // rounding: sampling (a vocabulary of 10^5 has as many borders that a random
 // number can fall on) and routing (a bias brings scores close together).  CDNA
-// vector units take a binary64 fma at the rate of a binary32 one, so these cost
-// registers, not time.
+// vector units take a binary64 fma at the rate of a binary32 one; what these cost is
+// registers, and the instructions of a polynomial where binary32 has one for 2^t.
 #pragma once
 
 #include "md.hpp"

@@ -104,7 +104,8 @@ def near_zero(N, V, g, dev):
     """Rows of which a hundredth lies within 2^-11 of 0, on both sides; and how many lie
     above 2^-11, a row."""
     x = torch.randn(N, V, device=dev, generator=g)
-    x = torch.where(torch.rand(N, V, device=dev, generator=g) < 0.01, 2.0 ** -12 * x.clamp(-1, 1), x)
+    few = torch.rand(N, V, device=dev, generator=g) < 0.01
+    x = torch.where(few, 2.0 ** -12 * x.clamp(-1, 1), x)
     x = x.to(torch.bfloat16)
     return x, (x >= 2.0 ** -11).sum(dim=1)
 
