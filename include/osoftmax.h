@@ -299,7 +299,9 @@ typedef struct osm_sample_params {
  * there: idx[r] is the lowest kept index at which the running sum of w over the
  * kept elements, in index order, exceeds u[r] times their sum, and vals[r] its
  * probability among the kept elements (w / sum).  u below 0 or NaN counts as 0,
- * above 1 as 1; elements of weight 0 are never taken.  Weights and sums are
+ * above 1 as 1; elements of weight 0 are never taken.  At 1, which no running sum
+ * exceeds, it is the last kept index or one behind which less than 1e-13 of the sum
+ * (with filters, than the bounds below) is left.  Weights and sums are
  * binary64, so the choice is that of the formula but for numbers u within about
  * 1e-13 of a border.  With filters some sums are of weights in fixed point, in units
  * relative to the largest: then u within 2^-49 V of a border may take its
