@@ -1,6 +1,7 @@
 /*
  * osoftmax -- row-wise softmax with the online normalizer, fused softmax +
- * top-k, sampling and expert routing, for AMD Instinct MI355X (gfx950).
+ * top-k, sampling, log probabilities, expert routing and their gradients, for
+ * AMD Instinct MI355X (gfx950).
  *
  * Method: M. Milakov and N. Gimelshein, "Online normalizer calculation for
  * softmax" (arXiv:1805.02867, 2018).
@@ -46,9 +47,9 @@
  *    first use and when it must grow.  Under HIP graph capture, either call
  *    once outside the capture on the same stream with the largest shape to
  *    be captured (the buffer is then reused and nothing is allocated), or use
- *    softmax_topk_ex_noalloc for the top-k and softmax_sample_ws for
- *    sampling: an allocation recorded into a graph would leave the stream's
- *    buffer owned by the graph.
+ *    softmax_topk_ex_noalloc for the top-k and softmax_sample_ws,
+ *    logprob_fwd_ws and balance_fwd_ws for those: an allocation recorded into
+ *    a graph would leave the stream's buffer owned by the graph.
  */
 #ifndef OSOFTMAX_H
 #define OSOFTMAX_H
@@ -392,6 +393,138 @@ OSM_API int route_fwd(const void* x, const float* bias, float* vals, int32_t* id
  * Errors: as route_fwd, for the arguments it has. */
 OSM_API int route_bwd(const void* x, const int32_t* idx, const float* dvals, void* dx, int64_t N,
                       int64_t E, int K, int dtype, const osm_route* r, hipStream_t stream);
+
+/* Largest number of given tokens a row of logprob_fwd and logprob_bwd. */
+#define OSM_LOGPROB_TMAX 64
+
+/* What logprob_fwd is asked for.  Outputs that are NULL are not written; one of them
+ * at least is asked for.
+ *  tokens     : N*T given tokens, T a row; NULL where T is 0.
+ *  logp       : N*T.  Not NULL where T > 0.
+ *  entropy    : N, or NULL.
+ *  stats      : N*2, or NULL: what logprob_bwd takes.
+ *  top_logp   : N*K, top_idx: N*K.  Not NULL where K > 0.
+ *  T, K       : 0 <= T <= OSM_LOGPROB_TMAX, 0 <= K <= OSM_TOPK_KMAX, K <= V.
+ *  temperature: logits are divided by it; positive and finite. */
+typedef struct osm_logprob {
+    const int32_t* tokens;
+    float* logp;
+    float* entropy;
+    float* stats;
+    float* top_logp;
+    int32_t* top_idx;
+    int T;
+    int K;
+    float temperature;
+} osm_logprob;
+
+/* Log probabilities of given tokens, the entropy and the best alternatives of each
+ * row's softmax.  With z = x / temperature, m = max x and
+ * s = sum of e^{(x_j - m) / temperature} over all j but one that has x_j = m (the online
+ * pair's d - 1, which keeps its digits where one element has all the weight):
+ *   logp[i]    = (x[t_i] - m) / temperature - ln(1 + s)   for the given token t_i,
+ *   entropy    = -sum_j p_j ln p_j,  p = softmax(z),
+ *   stats      = (m, s),
+ *   top_idx[i] = the K indices of the largest x (Eq. 5: larger first, equal values in
+ *                increasing index order), top_logp[i] their log probabilities.
+ * A token outside [0, V) is ignored: its logp is 0.  Elements of -inf have no weight,
+ * and a log probability of -inf.  A row holding NaN or +inf, or only -inf, gives NaN
+ * (0 for ignored tokens) and top_idx -1.  x is read once; sums are binary32, the
+ * outputs are formed from them in binary64.
+ * x: row r starts at x + r * ldx elements, ldx >= V; (max x - min x) / temperature
+ * stays below 2.35e38 for finite elements.
+ * Errors: OSM_EINVAL for bad sizes, ldx < V, unknown dtype, NULL p, T, K or temperature
+ * outside of what osm_logprob says, no output, null (with N > 0), misaligned or
+ * overlapping buffers (the memory between rows is part of x). */
+OSM_API int logprob_fwd(const void* x, int64_t ldx, const osm_logprob* p, int64_t N, int64_t V,
+                        int dtype, hipStream_t stream);
+
+/* logprob_fwd with the caller's workspace instead of the library's scratch (as
+ * softmax_sample_ws): osm_logprob_workspace(N, V, K, dtype) bytes, aligned to 256, of any
+ * contents; NULL where that is 0.
+ * Errors: as logprob_fwd, OSM_EINVAL for a misaligned or overlapping workspace,
+ * OSM_ESCRATCH for one that is too small. */
+OSM_API int logprob_fwd_ws(const void* x, int64_t ldx, const osm_logprob* p, int64_t N, int64_t V,
+                           int dtype, void* workspace, size_t workspace_bytes,
+                           hipStream_t stream);
+
+/* Bytes of workspace that logprob_fwd_ws needs for this shape on the current device (0 for
+ * rows that one workgroup takes), for any ldx, alignment, T and outputs.
+ * Errors: OSM_EINVAL for bad sizes, K or dtype or NULL bytes. */
+OSM_API int osm_logprob_workspace(int64_t N, int64_t V, int K, int dtype, size_t* bytes);
+
+/* The gradient of logprob_fwd's logp and entropy with respect to the logits: with
+ * p = softmax(x / temperature), g the gradients dlogp of the row's tokens inside [0, V),
+ * G their sum, H the entropy and h its gradient dentropy,
+ *   dx_j = (sum of g_i over t_i = j  -  p_j G  -  h p_j (ln p_j + H)) / temperature.
+ * A token that occurs twice adds both; an element of -inf takes part with p_j = 0.  A row
+ * whose g are all 0 (or that has no token inside) and whose h is 0 gets zeros, whatever it
+ * holds; any other row with NaN stats (or h, or one of g) gets NaN.  The gradient of
+ * top_logp is that of the same indices given as tokens.
+ * x, ldx, tokens, T, temperature: as in logprob_fwd.  stats: N*2 and entropy: N, as
+ * logprob_fwd wrote them for this x and temperature (entropy is read with dentropy only, and may be NULL without it).
+ * dlogp: N*T, NULL where T is 0.  dentropy: N, or NULL (0).  dx: row r at dx + r * lddx
+ * elements of dtype, lddx >= V, every element of the rows written, none between them.
+ * Errors: OSM_EINVAL for bad sizes, ldx or lddx < V, unknown dtype, bad T or temperature,
+ * neither dlogp nor dentropy, null (with N > 0), misaligned or overlapping buffers. */
+OSM_API int logprob_bwd(const void* x, int64_t ldx, const int32_t* tokens, const float* stats,
+                        const float* entropy, const float* dlogp, const float* dentropy, void* dx,
+                        int64_t lddx, int64_t N, int64_t V, int T, int dtype, float temperature,
+                        hipStream_t stream);
+
+/* The loss that keeps a router's experts in use, for each of S sequences of tokens packed one
+ * behind the other: sequence i is rows starts[i] to starts[i + 1] - 1 of the batch, all of it
+ * with starts NULL and S 1.  With q the shares of a row's experts (OSM_SCORE_SOFTMAX: the
+ * softmax; OSM_SCORE_SIGMOID: 1 / (1 + e^-x) over its sum), over the n rows of the sequence
+ * that take part:
+ *   rows      = n,
+ *   counts[e] = how often e stands among their K indices,
+ *   probs[e]  = the mean of q_e,
+ *   loss      = scale * E / (K n) * sum_e counts[e] probs[e]  (scale for even counts).
+ * A row takes part if one of its indices is in [0, E); others, such as the -1 that
+ * route_fwd gives where it chooses none, are not counted.  So padding is a row of -1, or
+ * a row before starts[0] or from starts[S] on.  An index that occurs twice counts twice.  n = 0
+ * gives zeros.  A row that takes part and whose shares are no numbers (a NaN, only -inf, for
+ * the softmax +inf) makes its sequence's probs and loss NaN.
+ * x: N*E logits of dtype.  idx: N*K int32, as route_fwd gave them.  starts: S + 1 int32 that do
+ * not decrease, or NULL; numbers outside [0, N] are taken as the nearest inside, results for
+ * decreasing ones are unspecified.  loss: S binary32.  counts: S*E int32.  probs: S*E
+ * binary32.  rows: S int32.  Shares are binary32, sums over rows binary64.  N = 0 is no
+ * no-op here: the outputs are zeros.
+ * Errors: OSM_EINVAL for N < 0, E < 1, E > OSM_ROUTE_EMAX, K < 1, K > OSM_TOPK_KMAX, S < 1,
+ * N * K, S or S * E above 2^31 - 1, starts NULL with S > 1, unknown dtype or score, null
+ * (x and idx only with N > 0), misaligned or overlapping buffers; OSM_ENOMEM if the
+ * scratch cannot be allocated. */
+OSM_API int balance_fwd(const void* x, const int32_t* idx, const int32_t* starts, float* loss,
+                        int32_t* counts, float* probs, int32_t* rows, int64_t N, int64_t E, int K,
+                        int64_t S, int dtype, int score, float scale, hipStream_t stream);
+
+/* balance_fwd with the caller's workspace instead of the library's scratch (as
+ * softmax_sample_ws): osm_balance_workspace(N, E, S) bytes, aligned to 256, of any contents;
+ * NULL where that is 0.
+ * Errors: as balance_fwd, OSM_EINVAL for a misaligned or overlapping workspace, OSM_ESCRATCH
+ * for one that is too small. */
+OSM_API int balance_fwd_ws(const void* x, const int32_t* idx, const int32_t* starts, float* loss,
+                           int32_t* counts, float* probs, int32_t* rows, int64_t N, int64_t E,
+                           int K, int64_t S, int dtype, int score, float scale, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of workspace that balance_fwd_ws needs for this shape on the current device.
+ * Errors: OSM_EINVAL for bad sizes or NULL bytes. */
+OSM_API int osm_balance_workspace(int64_t N, int64_t E, int64_t S, size_t* bytes);
+
+/* The gradient of balance_fwd's loss with respect to the logits, through the shares (the
+ * counts have none): for a row that takes part in a sequence,
+ *   dx_j = dloss * scale * E / (K n^2) * q_j (counts[j] - sum_e counts[e] q_e),
+ * for the sigmoid times 1 - 1 / (1 + e^-x_j); zeros for every other row.
+ * counts: S*E and rows: S as balance_fwd gave them, or summed over all the ranks that share
+ * the loss.  dloss: S binary32.  dx: N*E elements of dtype, every one written.  The others: as
+ * in balance_fwd.  N = 0 is a no-op.
+ * Errors: as balance_fwd, for the arguments it has. */
+OSM_API int balance_bwd(const void* x, const int32_t* idx, const int32_t* starts,
+                        const int32_t* counts, const int32_t* rows, const float* dloss, void* dx,
+                        int64_t N, int64_t E, int K, int64_t S, int dtype, int score, float scale,
+                        hipStream_t stream);
 
 /* Reference streaming kernels, for measurement only (nothing of the method):
  * op 0 reads `bytes` bytes of x (y: a device buffer of at least 1 KB that

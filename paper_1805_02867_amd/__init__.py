@@ -1,5 +1,5 @@
 """Python binding of libosoftmax (online-normalizer softmax, fused softmax +
-top-k, sampling and expert routing on MI355X).  Argument marshalling only:
+top-k, sampling, log probabilities, expert routing and balance on MI355X).  Argument marshalling only:
 every step of the computation runs in the library's HIP kernels, reached
 through its C ABI (``include/osoftmax.h``).  PyTorch supplies device memory
 and the current stream.  There is no fallback: if the library is missing,
@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -25,6 +26,7 @@ NOALLOC_SCRATCH_BYTES = 1 << 20
 TOPK_KMAX = 64
 PROJ_KMAX = 16
 ROUTE_EMAX, ROUTE_GMAX = 1024, 64
+LOGPROB_TMAX = 64
 SCORES = {"softmax": 0, "sigmoid": 1}
 TOPK_ONLINE_FUSED, TOPK_SAFE_FUSED, TOPK_SAFE_UNFUSED, TOPK_ONLINE_UNFUSED, TOPK_VALUES = range(5)
 TOPK_ALGOS = {"online_fused": TOPK_ONLINE_FUSED, "safe_fused": TOPK_SAFE_FUSED,
@@ -50,6 +52,31 @@ class Route(ctypes.Structure):
     """``osm_route``."""
     _fields_ = [("score", ctypes.c_int), ("groups", ctypes.c_int), ("top_groups", ctypes.c_int),
                 ("group_top", ctypes.c_int), ("renorm", ctypes.c_int), ("scale", ctypes.c_float)]
+
+
+class Logprob(ctypes.Structure):
+    """``osm_logprob``."""
+    _fields_ = [("tokens", ctypes.c_void_p), ("logp", ctypes.c_void_p),
+                ("entropy", ctypes.c_void_p), ("stats", ctypes.c_void_p),
+                ("top_logp", ctypes.c_void_p), ("top_idx", ctypes.c_void_p),
+                ("T", ctypes.c_int), ("K", ctypes.c_int), ("temperature", ctypes.c_float)]
+
+
+class Logprobs(NamedTuple):
+    """What logprob_fwd returns; None for what it was not asked for."""
+    logp: torch.Tensor | None
+    entropy: torch.Tensor | None
+    stats: torch.Tensor | None
+    top_vals: torch.Tensor | None
+    top_idx: torch.Tensor | None
+
+
+class Balance(NamedTuple):
+    """What balance_fwd returns."""
+    loss: torch.Tensor
+    counts: torch.Tensor
+    probs: torch.Tensor
+    rows: torch.Tensor
 
 
 class OsmError(RuntimeError):
@@ -101,6 +128,23 @@ def lib() -> ctypes.CDLL:
     L.route_fwd.restype = i32
     L.route_bwd.argtypes = [vp, vp, vp, vp, i64, i64, i32, i32, vp, vp]
     L.route_bwd.restype = i32
+    size_t, f32 = ctypes.c_size_t, ctypes.c_float
+    L.logprob_fwd.argtypes = [vp, i64, vp, i64, i64, i32, vp]
+    L.logprob_fwd.restype = i32
+    L.logprob_fwd_ws.argtypes = [vp, i64, vp, i64, i64, i32, vp, size_t, vp]
+    L.logprob_fwd_ws.restype = i32
+    L.osm_logprob_workspace.argtypes = [i64, i64, i32, i32, ctypes.POINTER(size_t)]
+    L.osm_logprob_workspace.restype = i32
+    L.logprob_bwd.argtypes = [vp, i64, vp, vp, vp, vp, vp, vp, i64, i64, i64, i32, i32, f32, vp]
+    L.logprob_bwd.restype = i32
+    L.balance_fwd.argtypes = [vp] * 7 + [i64, i64, i32, i64, i32, i32, f32, vp]
+    L.balance_fwd.restype = i32
+    L.balance_fwd_ws.argtypes = [vp] * 7 + [i64, i64, i32, i64, i32, i32, f32, vp, size_t, vp]
+    L.balance_fwd_ws.restype = i32
+    L.osm_balance_workspace.argtypes = [i64, i64, i64, ctypes.POINTER(size_t)]
+    L.osm_balance_workspace.restype = i32
+    L.balance_bwd.argtypes = [vp] * 7 + [i64, i64, i32, i64, i32, i32, f32, vp]
+    L.balance_bwd.restype = i32
     L.osm_plan.argtypes = [i64, i64, i32, i32, ctypes.POINTER(i32), ctypes.POINTER(i64)]
     L.osm_plan.restype = i32
     L.osm_stream_release.argtypes = [vp]
@@ -535,4 +579,214 @@ def route_bwd(x: torch.Tensor, idx: torch.Tensor, dvals: torch.Tensor, score="so
                          _stream(stream))
     if rc != OK:
         raise OsmError(rc, "route_bwd")
+    return dx
+
+
+def _own_workspace(need, workspace, x: torch.Tensor, stream):
+    """The workspace that a call is given: the caller's, or while the current stream is being
+    captured one from the graph's own memory (None: the library's scratch)."""
+    if workspace is not None:
+        return _vector(workspace, torch.uint8, x, workspace.numel(), "workspace")
+    if not torch.cuda.is_current_stream_capturing():
+        return None
+    if _stream(stream) != _stream(None):
+        raise ValueError("a captured call on another stream than the current one needs a "
+                         "workspace")
+    return torch.empty(need(), dtype=torch.uint8, device=x.device)
+
+
+def _tokens(tokens, x: torch.Tensor, N: int, name: str = "tokens") -> int:
+    """T of a tensor of T given tokens for each of x's N rows: N, N x T, or T of a row."""
+    if not isinstance(tokens, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor")
+    shape = tokens.shape
+    T = shape[-1] if len(shape) == 2 or (len(shape) == 1 and x.dim() == 1) else 1
+    rows = shape[0] if len(shape) == 2 or x.dim() == 2 and len(shape) == 1 else 1
+    if len(shape) not in (1, 2) or rows != N:
+        raise ValueError(f"{name} must have a row for each of x's")
+    return T
+
+
+def _asked(t, shape, x: torch.Tensor, name: str):
+    """An output that is given, asked for (True) or not wanted (False, None)."""
+    if t is None or t is False:
+        return None
+    return _output(None if t is True else t, shape, torch.float32, x, name)
+
+
+def logprob_fwd(x: torch.Tensor, tokens: torch.Tensor | None = None, K: int = 0, entropy=False,
+                stats=False, temperature: float = 1.0, logp: torch.Tensor | None = None,
+                top_vals: torch.Tensor | None = None, top_idx: torch.Tensor | None = None,
+                workspace: torch.Tensor | None = None, stream=None) -> Logprobs:
+    """Log probabilities of each row's given tokens, its entropy and its K best alternatives,
+    as far as they are asked for (``logprob_fwd``).
+
+    ``tokens``: int32, N or N x T (T up to ``LOGPROB_TMAX``); one outside [0, V) is ignored, its
+    logp is 0.  ``entropy`` and ``stats`` (what logprob_bwd takes, N x 2) are True or the
+    tensor to write.  Rows may be apart (``x[:, :V]`` of a padded batch).  ``workspace``: uint8,
+    at least ``logprob_workspace(N, V, K, dtype)`` bytes, used instead of the library's
+    scratch (``logprob_fwd_ws``); under graph capture as in softmax_sample."""
+    N, V, ld = _rows(x)
+    _on_current_device(x, "x")
+    K, T, tp, lp, vp, ip = int(K), 0, None, None, None, None
+    if tokens is not None:
+        T = _tokens(tokens, x, N)
+        tp = _vector(tokens, torch.int32, x, N * T, "tokens").data_ptr()
+        if logp is None:
+            logp = torch.empty(tokens.shape, dtype=torch.float32, device=x.device)
+        lp = _vector(logp, torch.float32, x, N * T, "logp").data_ptr()
+    elif logp is not None:
+        raise ValueError("logp needs tokens")
+    if K > 0:
+        top_vals = _output(top_vals, (N, K), torch.float32, x, "top_vals")
+        top_idx = _output(top_idx, (N, K), torch.int32, x, "top_idx")
+        vp, ip = top_vals.data_ptr(), top_idx.data_ptr()
+    elif top_vals is not None or top_idx is not None:
+        raise ValueError("top_vals and top_idx need K")
+    entropy = _asked(entropy, (N,), x, "entropy")
+    stats = _asked(stats, (N, 2), x, "stats")
+    p = Logprob(tp, lp, None if entropy is None else entropy.data_ptr(),
+                None if stats is None else stats.data_ptr(), vp, ip, T, _int32(K, "K"),
+                float(temperature))
+    workspace = _own_workspace(lambda: logprob_workspace(N, V, K, x.dtype), workspace, x, stream)
+    if workspace is None:
+        rc = lib().logprob_fwd(x.data_ptr(), ld, ctypes.byref(p), N, V, _DTYPES[x.dtype],
+                               _stream(stream))
+    else:
+        rc = lib().logprob_fwd_ws(x.data_ptr(), ld, ctypes.byref(p), N, V, _DTYPES[x.dtype],
+                                  workspace.data_ptr(), workspace.numel(), _stream(stream))
+    if rc != OK:
+        raise OsmError(rc, "logprob_fwd")
+    return Logprobs(logp, entropy, stats, top_vals, top_idx)
+
+
+def _int32(v, name: str) -> int:
+    v = int(v)
+    if not -1 << 31 <= v < 1 << 31:  # (a field would take the low 32 bits)
+        raise ValueError(f"{name} is out of range")
+    return v
+
+
+def logprob_workspace(N: int, V: int, K: int = 0, dtype=torch.float32) -> int:
+    """Bytes of workspace of logprob_fwd for this shape (``osm_logprob_workspace``)."""
+    n = ctypes.c_size_t()
+    dt = _DTYPES[dtype] if isinstance(dtype, torch.dtype) else int(dtype)
+    rc = lib().osm_logprob_workspace(int(N), int(V), _int32(K, "K"), dt, ctypes.byref(n))
+    if rc != OK:
+        raise OsmError(rc, "osm_logprob_workspace")
+    return n.value
+
+
+def logprob_bwd(x: torch.Tensor, stats: torch.Tensor, tokens: torch.Tensor | None = None,
+                dlogp: torch.Tensor | None = None, entropy: torch.Tensor | None = None,
+                dentropy: torch.Tensor | None = None, temperature: float = 1.0,
+                dx: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """dx = gradient with respect to x of logprob_fwd's logp and entropy, whose own gradients are
+    ``dlogp`` (as ``tokens``) and ``dentropy`` (N); either pair may be left out (``logprob_bwd``).
+    ``stats`` and ``entropy`` are what logprob_fwd gave for this x and temperature.  dx has
+    x's shape; its rows are contiguous, and may be apart if it is given."""
+    N, V, ld = _rows(x)
+    _on_current_device(x, "x")
+    if (tokens is None) != (dlogp is None) or (dentropy is not None and entropy is None):
+        raise ValueError("dlogp goes with tokens, and dentropy with entropy")
+    T, tp, gp, hp, ep = 0, None, None, None, None
+    _vector(stats, torch.float32, x, 2 * N, "stats")
+    if tokens is not None:
+        T = _tokens(tokens, x, N)
+        tp = _vector(tokens, torch.int32, x, N * T, "tokens").data_ptr()
+        gp = _vector(dlogp, torch.float32, x, N * T, "dlogp").data_ptr()
+    if dentropy is not None:
+        hp = _vector(dentropy, torch.float32, x, N, "dentropy").data_ptr()
+        ep = _vector(entropy, torch.float32, x, N, "entropy").data_ptr()
+    if dx is None:
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        ldd = V
+    else:
+        if not isinstance(dx, torch.Tensor) or dx.shape != x.shape or dx.dtype != x.dtype or \
+                dx.get_device() != x.get_device():
+            raise ValueError("dx must match x in shape, dtype and device")
+        ldd = _rows(dx)[2]
+    rc = lib().logprob_bwd(x.data_ptr(), ld, tp, stats.data_ptr(), ep, gp, hp, dx.data_ptr(), ldd,
+                           N, V, T, _DTYPES[x.dtype], float(temperature), _stream(stream))
+    if rc != OK:
+        raise OsmError(rc, "logprob_bwd")
+    return dx
+
+
+def _sequences(x: torch.Tensor, idx, starts):
+    """(N, E, K, S, pointers of idx and starts) of a packed batch's routing."""
+    N, E = _batch(x)
+    _on_current_device(x, "x")
+    K = _tokens(idx, x, N, "idx")
+    _vector(idx, torch.int32, x, N * K, "idx")
+    if starts is None:
+        return N, E, K, 1, idx.data_ptr(), None
+    if not isinstance(starts, torch.Tensor) or starts.dim() != 1 or starts.numel() < 2:
+        raise ValueError("starts must have one more element than there are sequences")
+    S = starts.numel() - 1
+    return N, E, K, S, idx.data_ptr(), _vector(starts, torch.int32, x, S + 1, "starts").data_ptr()
+
+
+def balance_fwd(x: torch.Tensor, idx: torch.Tensor, starts: torch.Tensor | None = None,
+                score="softmax", scale: float = 1.0, loss: torch.Tensor | None = None,
+                counts: torch.Tensor | None = None, probs: torch.Tensor | None = None,
+                rows: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                stream=None) -> Balance:
+    """The balance loss of each packed sequence of router logits, with the counts of its experts
+    and their mean shares (``balance_fwd``): loss S, counts S x E int32, probs S x E and rows S
+    int32.
+
+    ``idx``: N x K int32, as route_fwd gave them; a row without any in [0, E) takes no part.
+    ``starts``: S + 1 int32, the rows where the sequences begin and where the last one ends
+    (None: one sequence, the whole batch).  ``workspace``: uint8, at least
+    ``balance_workspace(N, E, S)`` bytes, used instead of the library's scratch
+    (``balance_fwd_ws``); under graph capture as in softmax_sample."""
+    N, E, K, S, ip, sp = _sequences(x, idx, starts)
+    loss = _output(loss, (S,), torch.float32, x, "loss")
+    counts = _output(counts, (S, E), torch.int32, x, "counts")
+    probs = _output(probs, (S, E), torch.float32, x, "probs")
+    rows = _output(rows, (S,), torch.int32, x, "rows")
+    workspace = _own_workspace(lambda: balance_workspace(N, E, S), workspace, x, stream)
+    args = (x.data_ptr(), ip, sp, loss.data_ptr(), counts.data_ptr(), probs.data_ptr(),
+            rows.data_ptr(), N, E, K, S, _DTYPES[x.dtype], _int32(_score(score), "score"),
+            float(scale))
+    if workspace is None:
+        rc = lib().balance_fwd(*args, _stream(stream))
+    else:
+        rc = lib().balance_fwd_ws(*args, workspace.data_ptr(), workspace.numel(),
+                                  _stream(stream))
+    if rc != OK:
+        raise OsmError(rc, "balance_fwd")
+    return Balance(loss, counts, probs, rows)
+
+
+def balance_workspace(N: int, E: int, S: int = 1) -> int:
+    """Bytes of workspace of balance_fwd for this shape (``osm_balance_workspace``)."""
+    n = ctypes.c_size_t()
+    rc = lib().osm_balance_workspace(int(N), int(E), int(S), ctypes.byref(n))
+    if rc != OK:
+        raise OsmError(rc, "osm_balance_workspace")
+    return n.value
+
+
+def balance_bwd(x: torch.Tensor, idx: torch.Tensor, counts: torch.Tensor, rows: torch.Tensor,
+                dloss: torch.Tensor, starts: torch.Tensor | None = None, score="softmax",
+                scale: float = 1.0, dx: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """dx = gradient with respect to x of balance_fwd's losses, whose own gradient is ``dloss``
+    (S); ``counts`` and ``rows`` are what it gave, or their sums over the ranks that share the
+    loss (``balance_bwd``)."""
+    N, E, K, S, ip, sp = _sequences(x, idx, starts)
+    _vector(counts, torch.int32, x, S * E, "counts")
+    _vector(rows, torch.int32, x, S, "rows")
+    _vector(dloss, torch.float32, x, S, "dloss")
+    if dx is None:
+        dx = torch.empty_like(x)
+    elif not _like(dx, x):
+        raise ValueError("dx must be a contiguous tensor like x")
+    rc = lib().balance_bwd(x.data_ptr(), ip, sp, counts.data_ptr(), rows.data_ptr(),
+                           dloss.data_ptr(), dx.data_ptr(), N, E, K, S, _DTYPES[x.dtype],
+                           _int32(_score(score), "score"), float(scale),
+                           _stream(stream))
+    if rc != OK:
+        raise OsmError(rc, "balance_bwd")
     return dx

@@ -784,6 +784,202 @@ int run_route_bwd(const void* x, const int32_t* idx, const float* dvals, void* d
     return hip_status(osm::launch_route_bwd(a, dtype, stream));
 }
 
+// ---------------------------------------------- log probabilities and balance
+// Scratch of a split plan: the chunks' partials, then the row counters.
+size_t logprob_counters_at(const osm::LogprobPlan& p, int K) {
+    return (osm::logprob_scratch_bytes(p, K) + 255) / 256 * 256;
+}
+
+bool check_temperature(float t) { return t > 0.0f && t <= 3.402823466e38f; }
+
+// log2(e) / t, as a binary32 number that is not infinite (at temperatures near 0).
+bool scale_of(float t, float* c) {
+    const double v = 1.4426950408889634074 / (double)t;
+    *c = (float)v;
+    return v <= 3.402823466e38;
+}
+
+size_t rows_bytes(int64_t N, int64_t V, int64_t ld, size_t es) {
+    return ((size_t)(N - 1) * (size_t)ld + (size_t)V) * es;
+}
+
+// own: as in run_sample.
+int run_logprob(const void* x, int64_t ldx, const osm_logprob* p, int64_t N, int64_t V, int dtype,
+                bool own, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    size_t bytes = 0;
+    if (!check_shape(N, V, dtype, &bytes) || ldx < V || ldx > kMaxDim || !p) return OSM_EINVAL;
+    if (p->T < 0 || p->T > OSM_LOGPROB_TMAX || p->K < 0 || p->K > OSM_TOPK_KMAX || p->K > V)
+        return OSM_EINVAL;
+    osm::LogprobRows a{};
+    if (!check_temperature(p->temperature) || !scale_of(p->temperature, &a.c)) return OSM_EINVAL;
+    if (N == 0) return OSM_OK;
+    if (p->T == 0 && p->K == 0 && !p->entropy && !p->stats) return OSM_EINVAL;
+    if (!x || (p->T > 0 && (!p->tokens || !p->logp)) || (p->K > 0 && (!p->top_logp || !p->top_idx)))
+        return OSM_EINVAL;
+    a.x = x, a.N = N, a.V = V, a.ld = ldx, a.T = p->T, a.K = p->K;
+    a.inverse = 1.0 / (double)p->temperature;
+    a.entropy = p->entropy, a.stats = p->stats;
+    if (p->T > 0) a.tokens = p->tokens, a.logp = p->logp;
+    if (p->K > 0) a.top_vals = p->top_logp, a.top_idx = p->top_idx;
+    const size_t es = elem_size(dtype), nb = (size_t)N * 4;
+    if (!aligned(x, es) || !aligned(a.tokens, 4) || !aligned(a.logp, 4) || !aligned(a.entropy, 4) ||
+        !aligned(a.stats, 4) || !aligned(a.top_vals, 4) || !aligned(a.top_idx, 4))
+        return OSM_EINVAL;
+    // (an output that is not asked for has no bytes and overlaps nothing)
+    const Span out[] = {{a.logp, nb * (size_t)a.T},
+                        {a.entropy, a.entropy ? nb : 0},
+                        {a.stats, a.stats ? nb * 2 : 0},
+                        {a.top_vals, nb * (size_t)a.K},
+                        {a.top_idx, nb * (size_t)a.K}};
+    const Span in[] = {{x, rows_bytes(N, V, ldx, es)}, {a.tokens, nb * (size_t)a.T}};
+    if (any_overlap(out, in)) return OSM_EINVAL;
+    if (own && workspace) {
+        if (!aligned(workspace, 256)) return OSM_EINVAL;
+        const Span ws[] = {{workspace, workspace_bytes}};
+        const Span all[] = {in[0], in[1], out[0], out[1], out[2], out[3], out[4]};
+        if (any_overlap(ws, all)) return OSM_EINVAL;
+    }
+    DeviceState* ds = device_state(nullptr);
+    if (!ds) return OSM_EHIP;
+    const osm::LogprobPlan plan = osm::logprob_plan(N, V, a.K, dtype, ds->cus);
+    auto launch = [&](void* scratch, uint32_t* ctr) {
+        return dtype == OSM_BF16 ? osm::launch_logprob_bf16(a, plan, scratch, ctr, stream)
+                                 : osm::launch_logprob_f32(a, plan, scratch, ctr, stream);
+    };
+    if (plan.S <= 1) return hip_status(launch(nullptr, nullptr));
+    const size_t at = logprob_counters_at(plan, a.K);
+    if (own) {
+        if (!workspace || workspace_bytes < at + (size_t)plan.rows * 4) return OSM_ESCRATCH;
+        uint32_t* ctr = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + at);
+        hipLaunchKernelGGL(zero_u32, dim3((unsigned)((plan.rows + 255) / 256)), dim3(256), 0,
+                           stream, ctr, plan.rows);
+        if (hipGetLastError() != hipSuccess) return OSM_EHIP;
+        return hip_status(launch(workspace, ctr));
+    }
+    void* scratch = nullptr;
+    bool temp = false, ctemp = false;
+    uint32_t* ctr = nullptr;
+    std::unique_lock<std::mutex> lk(ds->mu, std::defer_lock);  // held until the launches are in
+    int st = acquire_scratch(ds, lk, stream, at, &scratch, &temp);
+    if (st != OSM_OK) return st;
+    st = acquire_counters(ds, lk, stream, (size_t)plan.rows, &ctr, &ctemp);
+    if (st != OSM_OK) {
+        if (temp) (void)hipFreeAsync(scratch, stream);
+        return st;
+    }
+    const hipError_t e = launch(scratch, ctr);
+    const hipError_t f = temp ? hipFreeAsync(scratch, stream) : hipSuccess;
+    const hipError_t g = ctemp ? hipFreeAsync(ctr, stream) : hipSuccess;
+    if (e != hipSuccess) return OSM_EHIP;
+    return hip_status(f != hipSuccess ? f : g);
+}
+
+int run_logprob_bwd(const void* x, int64_t ldx, const int32_t* tokens, const float* stats,
+                    const float* entropy, const float* dlogp, const float* dentropy, void* dx,
+                    int64_t lddx, int64_t N, int64_t V, int T, int dtype, float temperature,
+                    hipStream_t stream) {
+    size_t bytes = 0;
+    if (!check_shape(N, V, dtype, &bytes) || ldx < V || ldx > kMaxDim || lddx < V ||
+        lddx > kMaxDim || T < 0 || T > OSM_LOGPROB_TMAX)
+        return OSM_EINVAL;
+    osm::LogprobGrad a{};
+    if (!check_temperature(temperature) || !scale_of(temperature, &a.c)) return OSM_EINVAL;
+    if (N == 0) return OSM_OK;
+    if (!x || !stats || !dx || (T > 0 && (!tokens || !dlogp)) || (T == 0 && !dentropy) ||
+        (dentropy && !entropy))
+        return OSM_EINVAL;
+    a.x = x, a.stats = stats, a.dx = dx, a.N = N, a.V = V, a.ldx = ldx, a.lddx = lddx, a.T = T;
+    a.inverse = 1.0 / (double)temperature;
+    if (T > 0) a.tokens = tokens, a.dlogp = dlogp;
+    if (dentropy) a.entropy = entropy, a.dentropy = dentropy;
+    const size_t es = elem_size(dtype), nb = (size_t)N * 4;
+    if (!aligned(x, es) || !aligned(dx, es) || !aligned(a.tokens, 4) || !aligned(stats, 4) ||
+        !aligned(a.entropy, 4) || !aligned(a.dlogp, 4) || !aligned(a.dentropy, 4))
+        return OSM_EINVAL;
+    const Span out[] = {{dx, rows_bytes(N, V, lddx, es)}};
+    const Span in[] = {{x, rows_bytes(N, V, ldx, es)}, {a.tokens, nb * (size_t)T},
+                       {stats, nb * 2},                {a.entropy, nb},
+                       {a.dlogp, nb * (size_t)T},      {a.dentropy, nb}};
+    if (any_overlap(out, in)) return OSM_EINVAL;
+    return hip_status(osm::launch_logprob_bwd(a, dtype, stream));
+}
+
+bool check_balance(int64_t N, int64_t E, int K, int64_t S, int dtype, int score,
+                   const int32_t* starts) {
+    if (N < 0 || N > kMaxDim || E < 1 || E > OSM_ROUTE_EMAX || K < 1 || K > OSM_TOPK_KMAX)
+        return false;
+    if (S < 1 || S * E > kMaxDim || S > kMaxDim || N * K > kMaxDim) return false;
+    if (!starts && S > 1) return false;
+    if (dtype != OSM_F32 && dtype != OSM_BF16) return false;
+    return score == OSM_SCORE_SOFTMAX || score == OSM_SCORE_SIGMOID;
+}
+
+int run_balance(const osm::BalanceRows& rows, int dtype, bool own, void* workspace,
+                size_t workspace_bytes, hipStream_t stream) {
+    osm::BalanceRows a = rows;
+    const size_t es = elem_size(dtype);
+    if (!a.loss || !a.counts || !a.probs || !a.rows || (a.N > 0 && (!a.x || !a.idx)))
+        return OSM_EINVAL;
+    if (!aligned(a.x, es) || !aligned(a.idx, 4) || !aligned(a.starts, 4) || !aligned(a.loss, 4) ||
+        !aligned(a.counts, 4) || !aligned(a.probs, 4) || !aligned(a.rows, 4))
+        return OSM_EINVAL;
+    const size_t sb = (size_t)a.S * 4, eb = sb * (size_t)a.E;
+    const Span out[] = {{a.loss, sb}, {a.counts, eb}, {a.probs, eb}, {a.rows, sb}};
+    const Span in[] = {{a.x, (size_t)a.N * (size_t)a.E * es},
+                       {a.idx, (size_t)a.N * (size_t)a.K * 4},
+                       {a.starts, sb + 4}};
+    if (any_overlap(out, in)) return OSM_EINVAL;
+    if (own && workspace) {
+        if (!aligned(workspace, 256)) return OSM_EINVAL;
+        const Span ws[] = {{workspace, workspace_bytes}};
+        const Span all[] = {in[0], in[1], in[2], out[0], out[1], out[2], out[3]};
+        if (any_overlap(ws, all)) return OSM_EINVAL;
+    }
+    DeviceState* ds = device_state(nullptr);
+    if (!ds) return OSM_EHIP;
+    a.cus = ds->cus;
+    const size_t need = osm::balance_scratch_bytes(a.N, a.E, a.S, a.cus);
+    if (own) {
+        if (!workspace || workspace_bytes < need) return OSM_ESCRATCH;
+        return hip_status(osm::launch_balance_fwd(a, dtype, workspace, stream));
+    }
+    void* scratch = nullptr;
+    bool temp = false;
+    std::unique_lock<std::mutex> lk(ds->mu, std::defer_lock);  // held until the launches are in
+    const int st = acquire_scratch(ds, lk, stream, need, &scratch, &temp);
+    if (st != OSM_OK) return st;
+    const hipError_t e = osm::launch_balance_fwd(a, dtype, scratch, stream);
+    const hipError_t f = temp ? hipFreeAsync(scratch, stream) : hipSuccess;
+    return hip_status(e != hipSuccess ? e : f);
+}
+
+osm::BalanceRows balance_rows(const void* x, const int32_t* idx, const int32_t* starts, int64_t N,
+                              int64_t E, int K, int64_t S, int score, float scale) {
+    osm::BalanceRows a{};
+    a.x = x, a.idx = idx, a.starts = starts, a.N = N, a.E = (int)E, a.K = K, a.S = S;
+    a.sigmoid = score == OSM_SCORE_SIGMOID, a.scale = scale;
+    return a;
+}
+
+int run_balance_bwd(const osm::BalanceRows& rows, int dtype, hipStream_t stream) {
+    osm::BalanceRows a = rows;
+    const size_t es = elem_size(dtype);
+    if (!a.x || !a.idx || !a.counts || !a.rows || !a.dloss || !a.dx) return OSM_EINVAL;
+    if (!aligned(a.x, es) || !aligned(a.idx, 4) || !aligned(a.starts, 4) || !aligned(a.counts, 4) ||
+        !aligned(a.rows, 4) || !aligned(a.dloss, 4) || !aligned(a.dx, es))
+        return OSM_EINVAL;
+    const size_t sb = (size_t)a.S * 4, xb = (size_t)a.N * (size_t)a.E * es;
+    const Span out[] = {{a.dx, xb}};
+    const Span in[] = {{a.x, xb},        {a.idx, (size_t)a.N * (size_t)a.K * 4},
+                       {a.starts, sb + 4}, {a.counts, sb * (size_t)a.E},
+                       {a.rows, sb},     {a.dloss, sb}};
+    if (any_overlap(out, in)) return OSM_EINVAL;
+    DeviceState* ds = device_state(nullptr);
+    if (!ds) return OSM_EHIP;
+    a.cus = ds->cus;
+    return hip_status(osm::launch_balance_bwd(a, dtype, stream));
+}
+
 }  // namespace
 
 extern "C" {
@@ -901,6 +1097,75 @@ int route_fwd(const void* x, const float* bias, float* vals, int32_t* idx, int64
 int route_bwd(const void* x, const int32_t* idx, const float* dvals, void* dx, int64_t N,
               int64_t E, int K, int dtype, const osm_route* r, hipStream_t stream) {
     return run_route_bwd(x, idx, dvals, dx, N, E, K, dtype, r, stream);
+}
+
+int logprob_fwd(const void* x, int64_t ldx, const osm_logprob* p, int64_t N, int64_t V, int dtype,
+                hipStream_t stream) {
+    return run_logprob(x, ldx, p, N, V, dtype, false, nullptr, 0, stream);
+}
+
+int logprob_fwd_ws(const void* x, int64_t ldx, const osm_logprob* p, int64_t N, int64_t V,
+                   int dtype, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    return run_logprob(x, ldx, p, N, V, dtype, true, workspace, workspace_bytes, stream);
+}
+
+int osm_logprob_workspace(int64_t N, int64_t V, int K, int dtype, size_t* bytes) {
+    size_t batch = 0;
+    if (!check_shape(N, V, dtype, &batch) || K < 0 || K > OSM_TOPK_KMAX || K > V || !bytes)
+        return OSM_EINVAL;
+    *bytes = 0;
+    if (N == 0) return OSM_OK;
+    DeviceState* ds = device_state(nullptr);
+    const osm::LogprobPlan p = osm::logprob_plan(N, V, K, dtype, ds ? ds->cus : 256);
+    if (p.S > 1) *bytes = logprob_counters_at(p, K) + (size_t)p.rows * 4;
+    return OSM_OK;
+}
+
+int logprob_bwd(const void* x, int64_t ldx, const int32_t* tokens, const float* stats,
+                const float* entropy, const float* dlogp, const float* dentropy, void* dx,
+                int64_t lddx, int64_t N, int64_t V, int T, int dtype, float temperature,
+                hipStream_t stream) {
+    return run_logprob_bwd(x, ldx, tokens, stats, entropy, dlogp, dentropy, dx, lddx, N, V, T,
+                           dtype, temperature, stream);
+}
+
+int balance_fwd(const void* x, const int32_t* idx, const int32_t* starts, float* loss,
+                int32_t* counts, float* probs, int32_t* rows, int64_t N, int64_t E, int K,
+                int64_t S, int dtype, int score, float scale, hipStream_t stream) {
+    if (!check_balance(N, E, K, S, dtype, score, starts)) return OSM_EINVAL;
+    osm::BalanceRows a = balance_rows(x, idx, starts, N, E, K, S, score, scale);
+    a.loss = loss, a.counts = counts, a.probs = probs, a.rows = rows;
+    return run_balance(a, dtype, false, nullptr, 0, stream);
+}
+
+int balance_fwd_ws(const void* x, const int32_t* idx, const int32_t* starts, float* loss,
+                   int32_t* counts, float* probs, int32_t* rows, int64_t N, int64_t E, int K,
+                   int64_t S, int dtype, int score, float scale, void* workspace,
+                   size_t workspace_bytes, hipStream_t stream) {
+    if (!check_balance(N, E, K, S, dtype, score, starts)) return OSM_EINVAL;
+    osm::BalanceRows a = balance_rows(x, idx, starts, N, E, K, S, score, scale);
+    a.loss = loss, a.counts = counts, a.probs = probs, a.rows = rows;
+    return run_balance(a, dtype, true, workspace, workspace_bytes, stream);
+}
+
+int osm_balance_workspace(int64_t N, int64_t E, int64_t S, size_t* bytes) {
+    if (!check_balance(N, E, 1, 1, OSM_F32, OSM_SCORE_SOFTMAX, nullptr) || S < 1 || S > kMaxDim ||
+        S * E > kMaxDim || !bytes)
+        return OSM_EINVAL;
+    DeviceState* ds = device_state(nullptr);
+    *bytes = osm::balance_scratch_bytes(N, E, S, ds ? ds->cus : 256);
+    return OSM_OK;
+}
+
+int balance_bwd(const void* x, const int32_t* idx, const int32_t* starts, const int32_t* counts,
+                const int32_t* rows, const float* dloss, void* dx, int64_t N, int64_t E, int K,
+                int64_t S, int dtype, int score, float scale, hipStream_t stream) {
+    if (!check_balance(N, E, K, S, dtype, score, starts)) return OSM_EINVAL;
+    if (N == 0) return OSM_OK;
+    osm::BalanceRows a = balance_rows(x, idx, starts, N, E, K, S, score, scale);
+    a.counts = const_cast<int32_t*>(counts), a.rows = const_cast<int32_t*>(rows);
+    a.dloss = dloss, a.dx = dx;
+    return run_balance_bwd(a, dtype, stream);
 }
 
 int osm_stream_release(hipStream_t stream) {

@@ -155,4 +155,77 @@ struct RouteRows {
 hipError_t launch_route_fwd(const RouteRows& a, int dtype, hipStream_t st);
 hipError_t launch_route_bwd(const RouteRows& a, int dtype, hipStream_t st);
 
+// Log probabilities: rows of V elements, row r at x + r * ld (see osm_logprob).
+struct LogprobRows {
+    const void* x;
+    const int32_t* tokens;  // N * T
+    float* logp;
+    float* entropy;         // or null
+    float* stats;           // or null
+    float* top_vals;
+    int32_t* top_idx;
+    int64_t N, V, ld;
+    int T, K;
+    float c;                // log2(e) / temperature
+    double inverse;         // 1 / temperature
+};
+// How a batch is taken: W wavefronts a row (S = 1), or a workgroup of W for each of S chunks a
+// row of `chunk` elements, `rows` rows a launch, with scratch of logprob_scratch_bytes and
+// `rows` zeroed counters, which are left zeroed.
+struct LogprobPlan {
+    int W, S;
+    int64_t chunk, rows;
+};
+struct LogprobSplit {
+    uint64_t* states;  // two words a chunk
+    uint64_t* keys;    // K words a chunk
+    uint32_t* ctr;
+    int64_t row0, rows, chunk;
+    int S;
+};
+LogprobPlan logprob_plan(int64_t N, int64_t V, int K, int dtype, int cus);
+inline size_t logprob_scratch_bytes(const LogprobPlan& p, int K) {
+    return (size_t)p.rows * (size_t)p.S * (16 + 8 * (size_t)K);
+}
+hipError_t launch_logprob_f32(const LogprobRows& a, const LogprobPlan& p, void* scratch,
+                              uint32_t* ctr, hipStream_t st);
+hipError_t launch_logprob_bf16(const LogprobRows& a, const LogprobPlan& p, void* scratch,
+                               uint32_t* ctr, hipStream_t st);
+
+struct LogprobGrad {
+    const void* x;
+    const int32_t* tokens;
+    const float* stats;
+    const float* entropy;
+    const float* dlogp;
+    const float* dentropy;  // or null
+    void* dx;
+    int64_t N, V, ldx, lddx;
+    int T;
+    float c;
+    double inverse;
+};
+hipError_t launch_logprob_bwd(const LogprobGrad& a, int dtype, hipStream_t st);
+
+// Balance of a router's experts over S sequences of rows (see balance_fwd).
+struct BalanceRows {
+    const void* x;
+    const int32_t* idx;
+    const int32_t* starts;  // S + 1, or null
+    float* loss;            // forward: written
+    int32_t* counts;        // forward: written; backward: read
+    float* probs;           // forward: written
+    int32_t* rows;          // forward: written; backward: read
+    const float* dloss;     // backward
+    void* dx;               // backward: written
+    int64_t N, S;
+    int E, K;
+    bool sigmoid;
+    float scale;
+    int cus;
+};
+size_t balance_scratch_bytes(int64_t N, int64_t E, int64_t S, int cus);
+hipError_t launch_balance_fwd(const BalanceRows& a, int dtype, void* scratch, hipStream_t st);
+hipError_t launch_balance_bwd(const BalanceRows& a, int dtype, hipStream_t st);
+
 }  // namespace osm

@@ -1,0 +1,9 @@
+// Log probabilities of bf16 rows with alternatives.
+#include "logprob.hpp"
+
+namespace osm {
+hipError_t launch_logprob_top_bf16(const LogprobRows& a, const LogprobPlan& p, void* scratch,
+                                  uint32_t* ctr, hipStream_t st) {
+    return launch_logprob_t<bf16_t, true>(a, p, scratch, ctr, st);
+}
+}  // namespace osm

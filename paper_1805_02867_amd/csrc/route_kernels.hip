@@ -33,7 +33,7 @@
 // wavefronts a SIMD (more of them spill: 34 to 42 us).  Without scores 10007 x 160 bfloat16
 // has 475 a row (10.8 us).  The gradient of the first batch, 10.5 us, is 62% of a large
 // copy's rate (its 34 MB 6.5).  Calls of some thousand logits are a launch, 3.3 to 4.0 us.
-#include "wide.hpp"
+#include "experts.hpp"
 #include "kernels.h"
 
 namespace osm {
@@ -66,57 +66,6 @@ __device__ __forceinline__ double sigmoid_wide(double x) {
 // 22 additions (under 2^-19).  The sum with the bias rounds c.
 __device__ __forceinline__ float score_error(bool sigmoid, float bmax) {
     return (sigmoid ? 0x1p-20f : 0x1p-18f) + 0x1p-23f * (1.0f + bmax);
-}
-
-// The row team of a lane: LANES lanes, `lane` within it.  Lane l's j-th expert is
-// (j / VEC * LANES + l) * VEC + j % VEC: VEC neighbours are loaded together.
-template <int LANES, int VEC>
-__device__ __forceinline__ int expert(int lane, int j) {
-    return (j / VEC * LANES + lane) * VEC + j % VEC;
-}
-
-template <typename T, int LANES, int R, int VEC>
-__device__ __forceinline__ void load_experts(const T* xr, int E, bool live, int lane,
-                                             float (&x)[R]) {
-    if constexpr (VEC == 1) {
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int e = j * LANES + lane;
-            x[j] = live && e < E ? load1(xr + e) : -__builtin_inff();
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < R; j += 4) {
-            const int e = expert<LANES, VEC>(lane, j);
-#pragma unroll
-            for (int v = 0; v < 4; ++v) x[j + v] = -__builtin_inff();
-            if (!live || e >= E) continue;
-            if constexpr (sizeof(T) == 4) {
-                const f32x4 q = *reinterpret_cast<const f32x4*>(xr + e);
-#pragma unroll
-                for (int v = 0; v < 4; ++v) x[j + v] = q[v];
-            } else {
-                const uint2 q = *reinterpret_cast<const uint2*>(xr + e);
-                x[j] = bf16_lo(q.x);
-                x[j + 1] = bf16_hi(q.x);
-                x[j + 2] = bf16_lo(q.y);
-                x[j + 3] = bf16_hi(q.y);
-            }
-        }
-    }
-}
-
-template <int LANES>
-__device__ __forceinline__ float team_maximum(float v) {  // (NaN where there is one)
-    float a, b;
-#define OSM_STEP(S)                                              \
-    if constexpr (LANES > (1 << S)) {                            \
-        bfly_operands<S>(v, a, b);                               \
-        v = __builtin_elementwise_maximum(a, b);                 \
-    }
-    OSM_STEP(0) OSM_STEP(1) OSM_STEP(2) OSM_STEP(3) OSM_STEP(4) OSM_STEP(5)
-#undef OSM_STEP
-    return v;
 }
 
 // Sorts a lane's keys, which differ, largest first: Batcher's odd-even merge network.

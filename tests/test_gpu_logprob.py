@@ -1,0 +1,425 @@
+"""logprob_fwd and logprob_bwd against the plain binary64 implementation (loss_ref.py): every
+kernel shape and its borders, types, strides, masks, ties, ignored and repeated tokens, rows that
+are no numbers, streams, graphs and threads."""
+import threading
+
+import numpy as np
+import pytest
+import torch
+
+import loss_ref
+import paper_1805_02867_amd as osm
+
+pytestmark = pytest.mark.gpu
+INF, NAN = float("inf"), float("nan")
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need an MI355X; none is visible")
+    return torch.device("cuda:0")
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def logits(N, V, dtype, seed, dev, ld=0, offset=0, sigma=2.0):
+    """N x V logits in rows of ld elements, the first at an offset from an aligned place."""
+    ld = ld or V
+    g = torch.Generator().manual_seed(seed)
+    buf = torch.randn(N * ld + offset, generator=g) * sigma
+    return buf.to(DT[dtype]).to(dev)[offset:].view(N, ld)[:, :V]
+
+
+def some_tokens(N, V, T, seed, dev):
+    """Tokens of all kinds: among them ignored ones, repeated ones, the first and the last."""
+    g = torch.Generator().manual_seed(seed)
+    t = torch.randint(0, V, (N, T), generator=g)
+    t[torch.rand(N, T, generator=g) < 0.15] = -100
+    t[:, 0] = torch.tensor([0, V - 1, V, -1])[torch.arange(N) % 4]
+    if T > 2:
+        t[:, 2] = t[:, 1]
+    return t.int().to(dev)
+
+
+def check_fwd(x, tokens, K=0, temperature=1.0, what="", **kw):
+    """All outputs of a call, and the same from calls that ask for one thing only."""
+    got = osm.logprob_fwd(x, tokens, K=K, entropy=True, stats=True, temperature=temperature, **kw)
+    t = None if tokens is None else tokens.cpu().numpy().reshape(x.shape[0], -1)
+    want = loss_ref.logprob(host(x), t, K, temperature)
+    what = f"{what} {tuple(x.shape)} K={K}"
+    if tokens is not None:
+        loss_ref.check(host(got.logp).reshape(want["logp"].shape), want["logp"], want["logp_err"],
+                       what + " logp")
+    loss_ref.check(host(got.entropy), want["entropy"], want["entropy_err"], what + " entropy")
+    loss_ref.check(host(got.stats), want["stats"], want["stats_err"], what + " stats")
+    if K:
+        assert np.array_equal(got.top_idx.cpu().numpy(), want["top_idx"]), what
+        loss_ref.check(host(got.top_vals), want["top_vals"], want["top_vals_err"], what + " top")
+    return got
+
+
+def check_bwd(x, tokens, dlogp, dentropy=None, temperature=1.0, dtype="f32", dx=None, what=""):
+    r = osm.logprob_fwd(x, entropy=True, stats=True, temperature=temperature)
+    got = osm.logprob_bwd(x, r.stats, tokens, dlogp, r.entropy if dentropy is not None else None,
+                          dentropy, temperature=temperature, dx=dx)
+    N = x.shape[0]
+    t = None if tokens is None else tokens.cpu().numpy().reshape(N, -1)
+    want, err = loss_ref.logprob_bwd(host(x), t, None if dlogp is None else host(dlogp).reshape(N, -1),
+                                     None if dentropy is None else host(dentropy), temperature,
+                                     dtype)
+    loss_ref.check(host(got), want, err, f"{what} {tuple(x.shape)}")
+    return got
+
+
+# lengths around a vector, a wavefront's, a workgroup's and a chunk's share
+LENGTHS = [1, 2, 3, 5, 8, 9, 31, 64, 255, 257, 1000, 1023, 2049, 4096, 4097, 8191, 8200, 16385,
+           32768, 32771, 65537, 70001, 131075]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", LENGTHS)
+def test_rows(V, dtype, dev):
+    N = 5
+    print(f"rows {dtype} {V}", flush=True)
+    for ld, offset, T, K, tau in ((V, 0, 1, 0, 1.0), (V + 3, 1, 3, min(V, 5), 0.7),
+                                  (V + 8, 2, 64, min(V, 64), 1.3)):
+        x = logits(N, V, dtype, V + T, dev, ld, offset)
+        check_fwd(x, some_tokens(N, V, T, V, dev), K, tau, f"{dtype} ld {ld} offset {offset}")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V", [(1, 128256), (1, 1000003), (2, 300007), (700, 1500), (1500, 4000),
+                                 (3000, 300), (600, 9000), (260, 33000), (1030, 20)])
+def test_batches(N, V, dtype, dev):
+    """Batches that take the other plans: one long row, many short ones, more than the chip."""
+    print(f"batch {dtype} {N} {V}", flush=True)
+    x = logits(N, V, dtype, N, dev)
+    tok = some_tokens(N, V, 2, V, dev)
+    for K in (0, min(V, 20)):
+        got = osm.logprob_fwd(x, tok, K=K, entropy=True, stats=True)
+        rows = sorted(set(range(min(N, 6))) | {N // 2, N - 1})
+        at = torch.tensor(rows, device=dev)
+        want = loss_ref.logprob(host(x[at]), tok[at].cpu().numpy(), K)
+        for name in ("logp", "entropy", "stats") + (("top_vals",) if K else ()):
+            loss_ref.check(host(getattr(got, name)[at]), want[name], want[name + "_err"], name)
+        if K:
+            assert np.array_equal(got.top_idx[at].cpu().numpy(), want["top_idx"])
+        again = osm.logprob_fwd(x, tok, K=K, entropy=True, stats=True)
+        assert all(torch.equal(a, b) for a, b in zip(got, again) if a is not None)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [7, 1000, 40000, 300001])
+def test_masked_rows(V, dtype, dev):
+    """-inf almost everywhere, everywhere but in one place, everywhere; fewer elements left than
+    alternatives; the type's lowest value."""
+    low = torch.finfo(DT[dtype]).min
+    x = logits(7, V, dtype, V, dev)
+    g = torch.Generator().manual_seed(V)
+    few = (torch.rand(V, generator=g) < max(0.01, 2 / V)).to(dev)
+    x[0, ~few] = -INF
+    x[1] = -INF
+    x[1, V - 1] = -3.0
+    x[2] = -INF
+    x[3, : V // 2] = -INF
+    x[4, 1:] = low / 4
+    x[5] = low / 4
+    x[6, :] = -INF
+    x[6, V // 2] = 5.0
+    for K in (0, 1, min(V, 6), min(V, 64)):
+        check_fwd(x, some_tokens(7, V, 3, V, dev), K, what=dtype)
+    tok = some_tokens(7, V, 3, V, dev)
+    check_bwd(x, tok, torch.randn(7, 3, device=dev), torch.randn(7, device=dev), dtype=dtype)
+    check_bwd(x, tok, torch.randn(7, 3, device=dev), dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [5, 1200, 50001])
+def test_rows_that_are_no_numbers(V, dtype, dev):
+    x = logits(6, V, dtype, V, dev)
+    for r, (j, v) in enumerate([(0, NAN), (V - 1, NAN), (V // 2, INF), (0, INF)]):
+        x[r, j] = v
+    x[4, 0], x[4, 1] = NAN, INF
+    tok = some_tokens(6, V, 2, V, dev)
+    got = check_fwd(x, tok, min(V, 5), what=dtype)
+    assert (got.top_idx[:5] == -1).all() and (got.top_idx[5] >= 0).all()
+    # a gradient that is not 0 is not a number there; where none comes in it is 0
+    g = torch.ones(6, 2, device=dev)
+    check_bwd(x, tok, g, dtype=dtype)
+    dx = check_bwd(x, tok, torch.zeros_like(g), torch.zeros(6, device=dev), dtype=dtype)
+    assert not dx.any()
+    ignored = torch.full_like(tok, -100)
+    assert not check_bwd(x, ignored, g, dtype=dtype).any()
+    g[5, 0] = NAN
+    tok[5] = 1
+    assert check_bwd(x, tok, g, dtype=dtype)[5].isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [40, 3000, 66000])
+def test_ties(V, dtype, dev):
+    """Equal elements everywhere, at the top, at the line; -0.0 and 0.0; by index."""
+    x = logits(5, V, dtype, V, dev)
+    x[0] = 1.5
+    x[1, ::3] = 9.0
+    x[2] = (x[2] * 2).round() / 2
+    x[3] = 0.0
+    x[3, ::2] = -0.0
+    x[4, V // 2:] = x[4].max()
+    for K in (1, 5, min(V, 64)):
+        check_fwd(x, some_tokens(5, V, 3, V, dev), K, what=dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [10, 700, 33333, 140000])
+def test_sure_rows_keep_their_digits(V, dtype, dev):
+    """A token with almost all the weight: its log p, and 1 - p in its gradient, are numbers of
+    1e-3 to 1e-30 with the type's precision."""
+    x = logits(8, V, dtype, V, dev, sigma=1.0).float()
+    at = torch.tensor([0, 1, V - 1, V // 2, V // 3, 7, 8, 9], device=dev) % V
+    up = torch.tensor([5.0, 10.0, 16.0, 20.0, 30.0, 40.0, 60.0, 70.0], device=dev)
+    x.scatter_(1, at.unsqueeze(1), (x.amax(dim=1) + up).unsqueeze(1))
+    x = x.to(DT[dtype])
+    tok = at.int().unsqueeze(1).contiguous()
+    got = check_fwd(x, tok, 2, what=dtype)
+    assert (got.logp < 0).all()
+    dx = check_bwd(x, tok, torch.ones(8, 1, device=dev), dtype=dtype)
+    assert (torch.gather(dx, 1, at.unsqueeze(1)) > 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_logits_far_from_zero(dtype, dev):
+    """A constant added; magnitudes at which steps of the type are large; the largest numbers."""
+    x = logits(6, 9001, dtype, 3, dev)
+    for r, c in enumerate((1e2, -1e3, 1e4, 1e6)):
+        x[r] += c
+    x[4] = x[4] * 1e5
+    x[5] = x[5].sign() * 1e37
+    tok = some_tokens(6, 9001, 2, 1, dev)
+    for tau in (1.0, 0.5, 30.0):
+        check_fwd(x, tok, 4, tau, what=dtype)
+        check_bwd(x, tok, torch.randn(6, 2, device=dev), torch.randn(6, device=dev), tau, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", LENGTHS)
+def test_gradients(V, dtype, dev):
+    print(f"gradients {dtype} {V}", flush=True)
+    N = 5
+    g = torch.Generator().manual_seed(V)
+    for ld, ldd, off, T, tau in ((V, V, 0, 1, 1.0), (V + 3, V, 1, 3, 0.7),
+                                 (V + 8, V + 5, 2, 64, 1.0)):
+        x = logits(N, V, dtype, V + T, dev, ld, off)
+        tok = some_tokens(N, V, T, V, dev)
+        dlogp = torch.randn(N, T, generator=g).to(dev)
+        dent = torch.randn(N, generator=g).to(dev)
+        buf = torch.full((N * ldd + 3,), 7.0, dtype=DT[dtype], device=dev)
+        rows = buf[3:].view(N, ldd)
+        what = f"{dtype} ld {ld} {ldd}"
+        dx = check_bwd(x, tok, dlogp, None, tau, dtype, what=what)
+        assert torch.equal(check_bwd(x, tok, dlogp, None, tau, dtype, rows[:, :V], what), dx)
+        assert (rows[:, V:] == 7.0).all() and (buf[:3] == 7.0).all()
+        check_bwd(x, tok, dlogp, dent, tau, dtype, what=what)
+        check_bwd(x, None, None, dent, tau, dtype, what=what)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V", [(1, 128256), (3000, 300), (1030, 20), (300, 5000), (5000, 1)])
+def test_gradients_of_batches(N, V, dtype, dev):
+    x = logits(N, V, dtype, N, dev)
+    tok = some_tokens(N, V, 2, V, dev)
+    dlogp = torch.randn(N, 2, device=dev)
+    r = osm.logprob_fwd(x, stats=True)
+    dx = osm.logprob_bwd(x, r.stats, tok, dlogp)
+    rows = sorted(set(range(min(N, 6))) | {N // 2, N - 1})
+    at = torch.tensor(rows, device=dev)
+    want, err = loss_ref.logprob_bwd(host(x[at]), tok[at].cpu().numpy(), host(dlogp[at]),
+                                     dtype=dtype)
+    loss_ref.check(host(dx[at]), want, err, f"{N} {V}")
+    assert torch.equal(dx, osm.logprob_bwd(x, r.stats, tok, dlogp))
+
+
+def test_gradient_against_differences(dev):
+    """Of the kernels' own forward pass: a step of 1/8 in binary32, differences of sums of 12
+    outputs of order 10 (2^-20 each), and h^2 / 6 times third derivatives below 2."""
+    x = logits(3, 11, "f32", 1, dev, sigma=1.0)
+    tok = some_tokens(3, 11, 4, 2, dev)
+    g, h = torch.randn(3, 4, device=dev), torch.randn(3, device=dev)
+    r = osm.logprob_fwd(x, tok, entropy=True, stats=True)
+    dx = osm.logprob_bwd(x, r.stats, tok, g, r.entropy, h)
+
+    def value(x):
+        r = osm.logprob_fwd(x, tok, entropy=True)
+        return float((r.logp.double() * g.double()).sum() + (r.entropy.double() * h.double()).sum())
+    size = float(g.abs().sum() + h.abs().sum())
+    for n in range(3):
+        for j in range(11):
+            lo, hi = x.clone(), x.clone()
+            lo[n, j] -= 0.125
+            hi[n, j] += 0.125
+            step = float(hi[n, j] - lo[n, j])
+            diff = (value(hi) - value(lo)) / step
+            assert abs(diff - float(dx[n, j])) < size * (0.125 ** 2 / 3 + 2.0 ** -16)
+
+
+def test_what_is_asked_for(dev):
+    """Outputs do not depend on which others are asked for; given tensors are written; shapes."""
+    for V in (100, 50000):
+        x, tok = logits(4, V, "f32", 1, dev), some_tokens(4, V, 1, 1, dev)
+        full = check_fwd(x, tok, 5)
+        assert full.logp.shape == (4, 1) and full.top_idx.shape == (4, 5)
+        flat = osm.logprob_fwd(x, tok.view(4))
+        assert flat.logp.shape == (4,) and flat.entropy is None and flat.top_idx is None
+        assert torch.equal(flat.logp, full.logp.view(4))
+        assert torch.equal(osm.logprob_fwd(x, entropy=True).entropy, full.entropy)
+        assert torch.equal(osm.logprob_fwd(x, stats=True).stats, full.stats)
+        top = osm.logprob_fwd(x, K=5)
+        assert top.logp is None and torch.equal(top.top_idx, full.top_idx)
+        e, s = torch.empty(4, device=dev), torch.empty(4, 2, device=dev)
+        r = osm.logprob_fwd(x, tok, entropy=e, stats=s, logp=torch.empty(4, 1, device=dev))
+        assert r.entropy is e and torch.equal(e, full.entropy) and torch.equal(s, full.stats)
+        one = osm.logprob_fwd(x[0], tok.view(4)[:1], K=2)
+        assert torch.equal(one.logp, full.logp[0]) and one.top_idx.shape == (1, 2)
+
+
+def test_empty_and_refused(dev):
+    x = logits(4, 50, "f32", 1, dev)
+    tok = some_tokens(4, 50, 2, 1, dev)
+    r = osm.logprob_fwd(x[:0], tok[:0], K=3, entropy=True, stats=True)
+    assert r.logp.shape == (0, 2) and r.top_idx.shape == (0, 3)
+    assert osm.logprob_bwd(x[:0], r.stats, tok[:0], r.logp).shape == (0, 50)
+    stats, g = torch.zeros(4, 2, device=dev), torch.zeros(4, 2, device=dev)
+    for call in (lambda: osm.logprob_fwd(x, tok.long()), lambda: osm.logprob_fwd(x, tok[:3]),
+                 lambda: osm.logprob_fwd(x.half(), tok), lambda: osm.logprob_fwd(x.t(), tok),
+                 lambda: osm.logprob_fwd(x, tok.cpu()), lambda: osm.logprob_fwd(x, logp=g),
+                 lambda: osm.logprob_fwd(x, top_vals=g),
+                 lambda: osm.logprob_fwd(x, tok, logp=g.half()),
+                 lambda: osm.logprob_fwd(x, tok, stats=torch.zeros(4, device=dev)),
+                 lambda: osm.logprob_bwd(x, stats, tok), lambda: osm.logprob_bwd(x, g[:2], tok, g),
+                 lambda: osm.logprob_bwd(x, stats, tok, g, dentropy=g[:, 0].contiguous()),
+                 lambda: osm.logprob_bwd(x, stats, tok, g, dx=x.to(torch.bfloat16)),
+                 lambda: osm.logprob_bwd(x, stats, tok, g, dx=torch.empty(4, 49, device=dev))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: osm.logprob_fwd(x), lambda: osm.logprob_fwd(x, tok, K=51),
+                 lambda: osm.logprob_fwd(x, tok, temperature=0.0),
+                 lambda: osm.logprob_fwd(x, torch.zeros(4, 65, dtype=torch.int32, device=dev)),
+                 lambda: osm.logprob_bwd(x, stats), lambda: osm.logprob_bwd(x, stats, tok, g, dx=x)):
+        with pytest.raises(osm.OsmError) as e:
+            call()
+        assert e.value.status == osm.EINVAL
+
+
+def test_workspaces(dev):
+    """A workspace of any contents, one that is too small, and one shared by calls in turn."""
+    x, tok = logits(3, 200000, "f32", 1, dev), some_tokens(3, 200000, 2, 1, dev)
+    want = osm.logprob_fwd(x, tok, K=7, entropy=True)
+    n = osm.logprob_workspace(3, 200000, 7)
+    assert n > 0
+    ws = torch.full((n,), 255, dtype=torch.uint8, device=dev)
+    for _ in range(3):
+        got = osm.logprob_fwd(x, tok, K=7, entropy=True, workspace=ws)
+        assert all(torch.equal(a, b) for a, b in zip(got, want) if a is not None)
+    with pytest.raises(osm.OsmError) as e:
+        osm.logprob_fwd(x, tok, K=7, workspace=ws[:n - 1])
+    assert e.value.status == osm.ESCRATCH
+
+
+@pytest.mark.parametrize("V", [3000, 150000])
+def test_graphs_share_nothing(V, dev):
+    """Two graphs of the same shapes, captured without a call before, replayed on two streams at
+    once with other inputs, with eager calls between."""
+    xs = [logits(4, V, "bf16", s, dev) for s in range(2)]
+    toks = [some_tokens(4, V, 2, s, dev) for s in range(2)]
+    g = torch.randn(4, 2, device=dev)
+    outs, graphs, streams = [], [], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for s, x, t in zip(streams, xs, toks):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            r = osm.logprob_fwd(x, t, K=9, entropy=True, stats=True)
+            dx = osm.logprob_bwd(x, r.stats, t, g)
+        outs.append(tuple(r) + (dx,))
+        graphs.append(graph)
+    for rep in range(4):
+        for i, x in enumerate(xs):
+            x.copy_(logits(4, V, "bf16", 10 * rep + i, dev))
+        torch.cuda.synchronize()
+        for s, graph in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for x, t, out in zip(xs, toks, outs):
+            r = osm.logprob_fwd(x, t, K=9, entropy=True, stats=True)
+            want = tuple(r) + (osm.logprob_bwd(x, r.stats, t, g),)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, want)), f"replay {rep}"
+
+
+def test_a_captured_call_on_another_stream_brings_its_workspace(dev):
+    x = logits(4, 150000, "f32", 1, dev)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(ValueError):
+            osm.logprob_fwd(x, K=3, stream=other)
+        out = osm.logprob_fwd(x, K=3)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out.top_idx, osm.logprob_fwd(x, K=3).top_idx)
+
+
+def test_threads_and_streams(dev):
+    """Calls from several threads, on one stream and on their own."""
+    shapes = [(3, 200000, 5), (40, 70000, 0), (1, 128256, 20), (500, 900, 3)]
+    want, data = [], []
+    for i, (N, V, K) in enumerate(shapes):
+        x, t = logits(N, V, "f32", i, dev), some_tokens(N, V, 2, i, dev)
+        data.append((x, t, K))
+        want.append(osm.logprob_fwd(x, t, K=K, entropy=True, stats=True))
+    torch.cuda.synchronize()
+    shared, bad = torch.cuda.Stream(), []
+
+    def work(i, stream):
+        x, t, K = data[i]
+        with torch.cuda.stream(stream):
+            for _ in range(10):
+                got = osm.logprob_fwd(x, t, K=K, entropy=True, stats=True)
+        stream.synchronize()
+        bad.extend(i for a, b in zip(got, want[i]) if a is not None and not torch.equal(a, b))
+    for streams in ([shared] * 4, [torch.cuda.Stream() for _ in range(4)]):
+        threads = [threading.Thread(target=work, args=(i, s)) for i, s in enumerate(streams)]
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+        assert not bad
+        for s in set(streams):
+            osm.stream_release(s)
+
+
+def test_offsets_past_32_bits(dev):
+    """The last rows of a batch of more than 2^32 bytes, and elements past 2^31."""
+    N, V = 70, 33000000
+    x = torch.zeros(N, V, dtype=torch.bfloat16, device=dev)
+    g = torch.Generator(device=dev).manual_seed(1)
+    x[N - 1] = torch.randn(V, device=dev, generator=g).to(torch.bfloat16)
+    x[N - 1, V - 2] = 12.0
+    tok = torch.full((N,), V - 2, dtype=torch.int32, device=dev)
+    r = osm.logprob_fwd(x, tok, K=2, entropy=True, stats=True)
+    last = x[N - 1].double()
+    lse = torch.logsumexp(last, 0)
+    assert r.top_idx[N - 1].tolist()[0] == V - 2 and r.top_idx[0].tolist() == [0, 1]
+    # flat rows of V, a sum of V terms; 500 additions a lane, chunk and merge at most
+    assert abs(float(r.logp[N - 1]) - float(12.0 - lse)) < 700 * 2.0 ** -24 + 20 * 2.0 ** -24
+    assert abs(float(r.entropy[0]) - np.log(V)) < 700 * 2.0 ** -24 + 20 * 2.0 ** -24
+    dx = osm.logprob_bwd(x, r.stats, tok, torch.ones(N, device=dev))
+    p = torch.exp(last - lse)
+    p[V - 2] -= 1.0
+    d = (dx[N - 1].double() + p).abs()
+    assert bool((d <= (2.0 ** -8 + 2.0 ** -12) * p.abs()).all())
