@@ -939,6 +939,7 @@ int run_balance(const osm::BalanceRows& rows, int dtype, bool own, void* workspa
     if (!ds) return OSM_EHIP;
     a.cus = ds->cus;
     const size_t need = osm::balance_scratch_bytes(a.N, a.E, a.S, a.cus);
+    if (need == 0) return hip_status(osm::launch_balance_fwd(a, dtype, nullptr, stream));
     if (own) {
         if (!workspace || workspace_bytes < need) return OSM_ESCRATCH;
         return hip_status(osm::launch_balance_fwd(a, dtype, workspace, stream));

@@ -26,26 +26,27 @@
 
 namespace osm {
 
-constexpr int BL_BLOCK = 256;
+constexpr int BL_BLOCK = 256;   // of the gradient
 constexpr int BL_WAVES = BL_BLOCK / 64;
-constexpr int BL_JOIN = 1024;  // threads of the second kernel's workgroups
-constexpr int BL_EMAX = 1024;
+constexpr int BL_FLUSH = 64;    // rows of a team whose shares are added in binary32
 
+// A sequence's part of a span in scratch: for each expert the sum of its shares (binary32, upper
+// word) and its count, then the rows that took part.  Slot 2 i is of the sequence that span i has
+// from the span before, slot 2 i + 1 of the one that begins in it and goes on.
 struct BalanceSpans {
-    int64_t rows;    // of a span
+    int64_t rows;      // of a span
     uint32_t spans;
-    double* sums;    // spans * 2 * E: of the sequence before the span's first row, and of the last
-    int32_t* counts; // the same
-    int32_t* n;      // spans * 2
-    int32_t* leads;  // the sequence that begins in the span and ends behind it, or -1
+    uint64_t* slots;   // spans * 2 * (E + 1)
+    int2* leads;       // the sequence of slot 2 i + 1, or -1; the last span that has it
 };
 
-__device__ __forceinline__ int64_t seq_start(const BalanceRows& a, int64_t s) {
-    if (!a.starts) return s == 0 ? 0 : a.N;
-    const int64_t v = a.starts[s];
+__device__ __forceinline__ int64_t inside(const BalanceRows& a, int64_t v) {
     return v < 0 ? 0 : v > a.N ? a.N : v;
 }
-
+__device__ __forceinline__ int64_t seq_start(const BalanceRows& a, int64_t s) {
+    if (!a.starts) return s == 0 ? 0 : a.N;
+    return inside(a, a.starts[s]);
+}
 // The first sequence that ends behind `row` (S: none), by the whole wavefront: 64 places at a
 // time.
 __device__ __forceinline__ int64_t seq_after(const BalanceRows& a, int64_t row) {
@@ -55,7 +56,7 @@ __device__ __forceinline__ int64_t seq_after(const BalanceRows& a, int64_t row) 
     while (hi > lo) {
         const int64_t step = (hi - lo + 63) / 64;
         const int64_t s = lo + lane * step;
-        const bool behind = s < hi && seq_start(a, s + 1) > row;
+        const bool behind = s < hi && inside(a, a.starts[s + 1]) > row;
         const uint64_t who = __ballot(behind);
         // the first of the places that does
         if (who == 0) {
@@ -71,51 +72,110 @@ __device__ __forceinline__ int64_t seq_after(const BalanceRows& a, int64_t row) 
     return lo;
 }
 
+// Where sequences begin and end, by the whole wavefront: 64 of them in its lanes.
+struct Sequences {
+    int64_t base = 0;
+    int32_t from = 0, to = 0;  // of sequence base + lane
+
+    __device__ __forceinline__ void load(const BalanceRows& a, int64_t s) {
+        base = s;
+        if (!a.starts) {
+            from = 0, to = (int32_t)a.N;
+            return;
+        }
+        const int64_t i = s + (threadIdx.x & 63);
+        const int32_t v = a.starts[i < a.S ? i : a.S], w = a.starts[i < a.S ? i + 1 : a.S];
+        from = (int32_t)inside(a, v);
+        to = (int32_t)inside(a, w);
+        to = to > from ? to : from;
+    }
+    // The first one that ends behind `row`.
+    __device__ __forceinline__ int64_t after(const BalanceRows& a, int64_t row) {
+        if (a.S <= 64) {
+            load(a, 0);
+            const uint64_t who = __ballot((threadIdx.x & 63) < a.S && to > row);
+            return who ? __builtin_ctzll(who) : a.S;
+        }
+        const int64_t s = seq_after(a, row);
+        load(a, s);
+        return s;
+    }
+    __device__ __forceinline__ void bounds(const BalanceRows& a, int64_t s, int64_t& begin,
+                                           int64_t& end) {
+        if (s - base >= 64) load(a, s);
+        begin = __builtin_amdgcn_readlane(from, (int)(s - base));
+        end = __builtin_amdgcn_readlane(to, (int)(s - base));
+    }
+};
+
 // Shares of a row (see above), and for the gradient 1 - sigma of each expert.
 template <int LANES, int R, bool SLOPE>
 __device__ __forceinline__ void shares(const float (&x)[R], bool sigmoid, float (&q)[R],
                                        float (&slope)[R]) {
-    float m = x[0];
+    float sum = 0.0f;
     if (sigmoid) {
 #pragma unroll
-        for (int j = 1; j < R; ++j) m = fmaxf(m, x[j]);
-        m = fminf(group_max<LANES>(m), 0.0f);
+        for (int j = 0; j < R; ++j) {
+            const float e = exp2_hw(-x[j] * kLog2e);
+            q[j] = __builtin_amdgcn_rcpf(1.0f + e);
+            if constexpr (SLOPE) slope[j] = x[j] > 0.0f ? e * q[j] : 1.0f - q[j];
+            sum += q[j];
+        }
+        sum = group_sum<LANES>(sum);
+        if (__ballot(sum < 0x1p-60f) != 0) {  // only logits far below 0 (or an idle team)
+            float m = x[0];
+#pragma unroll
+            for (int j = 1; j < R; ++j) m = fmaxf(m, x[j]);
+            m = group_max<LANES>(m);
+            const bool low = sum < 0x1p-60f;
+            float t = 0.0f, p[R];
+#pragma unroll
+            for (int j = 0; j < R; ++j) {  // x < 0, where the sigmoid is e^x
+                p[j] = exp2_hw((x[j] - m) * kLog2e);
+                t += p[j];
+            }
+            t = group_sum<LANES>(t);
+            sum = low ? t : sum;
+#pragma unroll
+            for (int j = 0; j < R; ++j) q[j] = low ? p[j] : q[j];
+        }
     } else {
+        float m = x[0];
 #pragma unroll
         for (int j = 1; j < R; ++j) m = __builtin_elementwise_maximum(m, x[j]);
         m = team_maximum<LANES>(m);
-    }
-    float sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < R; ++j) {
-        if (sigmoid) {
-            const float e = exp2_hw(-__builtin_fabsf(x[j]) * kLog2e);
-            const float f = __builtin_amdgcn_rcpf(1.0f + e);
-            // (a NaN stays one: the minimum would give 0)
-            const float z = x[j] > 0.0f ? 0.0f : x[j];
-            q[j] = exp2_hw((z - m) * kLog2e) * f;
-            if constexpr (SLOPE) slope[j] = x[j] > 0.0f ? e * f : f;
-        } else {
+        for (int j = 0; j < R; ++j) {
             q[j] = exp2_hw((x[j] - m) * kLog2e);
             if constexpr (SLOPE) slope[j] = 1.0f;
+            sum += q[j];
         }
-        sum += q[j];
+        sum = group_sum<LANES>(sum);
     }
-    const float r = 1.0f / group_sum<LANES>(sum);
+    const float r = __builtin_amdgcn_rcpf(sum);
 #pragma unroll
     for (int j = 0; j < R; ++j) q[j] *= r;
 }
 
-// Whether one of a row's indices is an expert, for a team.  COUNT: they are counted.
+// The lane's first index of a row (every lane loads one).
+__device__ __forceinline__ int32_t first_index(const BalanceRows& a, int64_t row, int lane) {
+    return a.idx[row * a.K + (lane < a.K ? lane : 0)];
+}
+
+// Whether one of a row's indices is an expert, for a team that has them LANES at a time, the
+// first ones in `first`.  COUNT: they are counted.
 template <int LANES, bool COUNT>
 __device__ __forceinline__ bool takes_part(const BalanceRows& a, int64_t row, bool live, int lane,
-                                           int team, int32_t* counts) {
-    bool in = false;
-    for (int k = lane; k < a.K; k += LANES) {
-        const int32_t e = live ? a.idx[row * a.K + k] : -1;
-        const bool is = e >= 0 && e < a.E;
-        if (COUNT && is) atomicAdd(counts + e, 1);
-        in = in || is;
+                                           int team, int32_t first, int32_t* counts) {
+    bool in = live && lane < a.K && (uint32_t)first < (uint32_t)a.E;
+    if (COUNT && in) atomicAdd(counts + first, 1);
+    if (LANES < 64 && a.K > LANES) {
+        for (int k = LANES; k < a.K; k += LANES) {  // uniform
+            const int32_t e = live && k + lane < a.K ? a.idx[row * a.K + k + lane] : -1;
+            const bool is = (uint32_t)e < (uint32_t)a.E;
+            if (COUNT && is) atomicAdd(counts + e, 1);
+            in = in || is;
+        }
     }
     const uint64_t who = __ballot(in);
     const uint64_t mine = LANES == 64 ? ~0ull : ((1ull << (LANES & 63)) - 1) << (team * LANES);
@@ -147,166 +207,245 @@ __device__ __forceinline__ void finish(const BalanceRows& a, int64_t s, const do
     }
 }
 
-template <typename T, int LANES, int R, int VEC>
-__global__ __launch_bounds__(BL_BLOCK) void balance_spans(const BalanceRows a,
-                                                          const BalanceSpans b) {
-    constexpr int ROWS = 64 / LANES, TEAMS = BL_WAVES * ROWS;
+// Wavefronts of a span's workgroup: with 16 experts a lane half as many, for their sums in LDS.
+template <int R>
+constexpr int span_waves() { return R > 8 ? 8 : 16; }
+
+template <typename T, int LANES, int R, int VEC, bool FULL>
+__global__ __launch_bounds__(64 * span_waves<R>()) void balance_spans(const BalanceRows a,
+                                                                      const BalanceSpans b) {
+    constexpr int ROWS = 64 / LANES, WAVES = span_waves<R>(), TEAMS = WAVES * ROWS;
+    constexpr int THREADS = 64 * WAVES;
+    __shared__ float acc[WAVES][LANES * R];
     __shared__ double sums[LANES * R];
-    __shared__ double acc[BL_WAVES][LANES * R];
     __shared__ int32_t counts[LANES * R];
-    __shared__ int32_t part_rows[BL_WAVES];
-    __shared__ double part[BL_WAVES];
+    __shared__ int32_t part_rows[WAVES];
+    __shared__ double part[WAVES];
     const int tid = threadIdx.x, lane = tid % LANES, wv = tid >> 6, team = (tid & 63) / LANES;
     const int E = a.E;
+    const T* const x0 = static_cast<const T*>(a.x);
     const int64_t r0 = blockIdx.x * b.rows, r1 = r0 + b.rows < a.N ? r0 + b.rows : a.N;
+    // the first row is on its way before its sequence is known
+    RawExperts<T, LANES, R, VEC> raw, later;
+    int32_t first = -1, then;
+    auto fetch = [&](int64_t row, int64_t end) {
+        const int64_t at = row < end ? row : end - 1;
+        later.load(x0 + at * E, E, lane);
+        then = first_index(a, at, lane);
+    };
+    if (r0 < r1) {
+        fetch(r0 + wv * ROWS + team, r1);
+        raw = later;
+        first = then;
+    }
     // its sequences: those that end behind r0 (all that end at row 0 are the first span's)
-    int64_t s = blockIdx.x == 0 ? 0 : seq_after(a, r0);
-    int32_t lead = -1;
+    Sequences seq;
+    int64_t s = 0;
+    if (blockIdx.x == 0) seq.load(a, 0);
+    else s = seq.after(a, r0);
+    int2 lead = {-1, 0};
     for (; s < a.S; ++s) {
-        const int64_t from = seq_start(a, s), end = seq_start(a, s + 1);
-        const int64_t to = end > from ? end : from;
+        int64_t from, to;
+        seq.bounds(a, s, from, to);
         if (from > r1 || (from == r1 && to > from)) break;
         const int64_t p0 = from > r0 ? from : r0, p1 = to < r1 ? to : r1;
-        for (int e = tid; e < LANES * R; e += BL_BLOCK) counts[e] = 0;
+        for (int e = tid; e < LANES * R; e += THREADS) counts[e] = 0;
+        if (p0 != r0 && p0 < p1) {
+            fetch(p0 + wv * ROWS + team, p1);
+            raw = later;
+            first = then;
+        }
         __syncthreads();
-        float q[R], none[R];
-        double sum[R];
+        double total[R];
+        float sum[R];
         int32_t n = 0;
 #pragma unroll
-        for (int j = 0; j < R; ++j) sum[j] = 0.0;
+        for (int j = 0; j < R; ++j) total[j] = 0.0, sum[j] = 0.0f;
+        int added = 0;
+        // the next row is on its way while one is worked on
+        int64_t row = p0 + wv * ROWS + team;
         for (int64_t row0 = p0 + wv * ROWS; row0 < p1; row0 += TEAMS) {
-            const int64_t row = row0 + team;
-            const bool live = row < p1;
-            float x[R];
-            load_experts<T, LANES, R, VEC>(static_cast<const T*>(a.x) + (live ? row : p0) * E, E,
-                                           live, lane, x);
-            const bool in = takes_part<LANES, true>(a, row, live, lane, team, counts);
+            fetch(row + TEAMS, p1);
+            float x[R], q[R], none[R];
+            raw.template widen<FULL>(x, E, lane);
+            const bool in = takes_part<LANES, true>(a, row, row < p1, lane, team, first, counts);
             shares<LANES, R, false>(x, a.sigmoid, q, none);
 #pragma unroll
-            for (int j = 0; j < R; ++j) sum[j] += (double)(in ? q[j] : 0.0f);
+            for (int j = 0; j < R; ++j) sum[j] += in ? q[j] : 0.0f;
             n += in && lane == 0;
+            if (++added == BL_FLUSH) {
+                added = 0;
+#pragma unroll
+                for (int j = 0; j < R; ++j) total[j] += (double)sum[j], sum[j] = 0.0f;
+            }
+            row += TEAMS;
+            first = then;
+            raw = later;
         }
         // the wavefront's teams, then the wavefronts
 #pragma unroll
-        for (int d = LANES; d < 64; d *= 2) {
-#pragma unroll
-            for (int j = 0; j < R; ++j) sum[j] += __shfl_xor(sum[j], d);
+        for (int j = 0; j < R; ++j) {
+            const float v = sum_of_teams<LANES>((float)(total[j] + (double)sum[j]));
+            if (team == 0) acc[wv][expert<LANES, VEC>(lane, j)] = v;
         }
-        if (team == 0) {
-#pragma unroll
-            for (int j = 0; j < R; ++j) acc[wv][expert<LANES, VEC>(lane, j)] = sum[j];
-        }
-        for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
+        n = (int32_t)group_sum<64>((float)n);  // (below 2^24: a wavefront's rows of a span)
         if ((tid & 63) == 0) part_rows[wv] = n;
         __syncthreads();
         n = 0;
 #pragma unroll
-        for (int w = 0; w < BL_WAVES; ++w) n += part_rows[w];
+        for (int w = 0; w < WAVES; ++w) n += part_rows[w];
         const bool before = from < r0, behind = to > r1;
-        const int slot = before ? 0 : 1;
-        double* const out = before || behind ? b.sums + ((int64_t)blockIdx.x * 2 + slot) * E : sums;
-        for (int e = tid; e < E; e += BL_BLOCK) {
+        uint64_t* const slot = b.slots + ((int64_t)blockIdx.x * 2 + (before ? 0 : 1)) * (E + 1);
+        for (int e = tid; e < E; e += THREADS) {
             double v = 0.0;
 #pragma unroll
-            for (int w = 0; w < BL_WAVES; ++w) v += acc[w][e];
-            out[e] = v;
+            for (int w = 0; w < WAVES; ++w) v += (double)acc[w][e];
+            if (before || behind)
+                slot[e] = (uint64_t)__float_as_uint((float)v) << 32 | (uint32_t)counts[e];
+            else
+                sums[e] = v;
         }
         if (before || behind) {
-            int32_t* const oc = b.counts + ((int64_t)blockIdx.x * 2 + slot) * E;
-            for (int e = tid; e < E; e += BL_BLOCK) oc[e] = counts[e];
-            if (tid == 0) b.n[blockIdx.x * 2 + slot] = n;
-            if (!before) lead = (int32_t)s;
+            if (tid == 0) slot[E] = (uint32_t)n;
+            if (!before) lead = int2{(int32_t)s, (int32_t)((to - 1) / b.rows)};
         } else {
             __syncthreads();
-            finish<BL_BLOCK>(a, s, sums, counts, n, part);
+            finish<THREADS>(a, s, sums, counts, n, part);
         }
         __syncthreads();
         if (behind) break;
     }
-    if (tid == 0) b.leads[blockIdx.x] = lead;
+    if (tid == 0 && b.spans > 1) b.leads[blockIdx.x] = lead;
 }
 
-// Sequences that more than one span has: workgroup i joins the one that begins in span i.
-__global__ __launch_bounds__(BL_JOIN) void balance_join(const BalanceRows a,
+// Sequences that more than one span has: workgroup i joins the one that begins in span i.  Each
+// wavefront takes every so many-th slot, COLS experts a lane, several slots in flight.
+template <int COLS>
+constexpr int join_waves() { return COLS > 8 ? 8 : 16; }
+
+template <int COLS>
+__global__ __launch_bounds__(64 * join_waves<COLS>()) void balance_join(const BalanceRows a,
                                                         const BalanceSpans b) {
-    __shared__ double stripe[BL_JOIN];
-    __shared__ int32_t stripe_counts[BL_JOIN];
-    __shared__ double sums[BL_EMAX];
-    __shared__ int32_t counts[BL_EMAX];
-    __shared__ double part[BL_JOIN / 64];
-    __shared__ int32_t rows[BL_JOIN / 64];
-    const int64_t s = b.leads[blockIdx.x];
-    if (s < 0) return;
-    const int tid = threadIdx.x, E = a.E;
-    const int64_t end = seq_start(a, s + 1);
+    constexpr int WAVES = join_waves<COLS>(), DEEP = COLS > 4 ? 32 / COLS : 8;
+    __shared__ double stripe[WAVES][64 * COLS];
+    __shared__ int32_t stripe_counts[WAVES][64 * COLS];
+    __shared__ double sums[64 * COLS];
+    __shared__ int32_t counts[64 * COLS];
+    __shared__ double part[WAVES];
+    __shared__ int32_t rows[WAVES];
+    const int2 lead = b.leads[blockIdx.x];
+    if (lead.x < 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, E = a.E;
     // slots: the second one of this span, the first ones of the following
-    const int64_t i0 = blockIdx.x, more = (end - 1) / b.rows - i0;
-    auto slot = [&](int64_t j) { return j == 0 ? i0 * 2 + 1 : (i0 + j) * 2; };
-    const int cols = E < BL_JOIN ? E : BL_JOIN;
-    const int stripes = BL_JOIN / cols, st = tid / cols, e = tid % cols;
-    const int64_t each = (more + stripes) / stripes;  // slots of a stripe
-    double v = 0.0;
-    int32_t c = 0, n = 0;
-    if (st < stripes) {
-        const int64_t j1 = (st + 1) * each < more + 1 ? (st + 1) * each : more + 1;
-#pragma unroll 8
-        for (int64_t j = st * each; j < j1; ++j) {
-            v += b.sums[slot(j) * E + e];
-            c += b.counts[slot(j) * E + e];
+    const int64_t i0 = blockIdx.x;
+    const int last = lead.y < (int)b.spans ? lead.y - (int)i0 : (int)b.spans - 1 - (int)i0;
+    auto slot = [&](int j) { return b.slots + (j == 0 ? i0 * 2 + 1 : (i0 + j) * 2) * (E + 1); };
+    double v[COLS];
+    int32_t c[COLS], n = 0;
+#pragma unroll
+    for (int k = 0; k < COLS; ++k) v[k] = 0.0, c[k] = 0;
+    for (int j0 = wv; j0 <= last; j0 += WAVES * DEEP) {
+        uint64_t w[DEEP][COLS];
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d) {
+            const int j = j0 + d * WAVES;
+#pragma unroll
+            for (int k = 0; k < COLS; ++k) {
+                const int e = lane + 64 * k;
+                w[d][k] = j <= last && e < E ? slot(j)[e] : 0;
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < DEEP; ++d) {
+#pragma unroll
+            for (int k = 0; k < COLS; ++k) {
+                v[k] += (double)__uint_as_float((uint32_t)(w[d][k] >> 32));
+                c[k] += (int32_t)(uint32_t)w[d][k];
+            }
         }
     }
-    stripe[tid] = v;
-    stripe_counts[tid] = c;
-    for (int64_t j = tid; j <= more; j += BL_JOIN) n += b.n[slot(j)];
+    for (int j = tid; j <= last; j += 64 * WAVES) n += (int32_t)(uint32_t)slot(j)[E];
     for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
-    if ((tid & 63) == 0) rows[tid >> 6] = n;
+    if (lane == 0) rows[wv] = n;
+#pragma unroll
+    for (int k = 0; k < COLS; ++k) {
+        stripe[wv][lane + 64 * k] = v[k];
+        stripe_counts[wv][lane + 64 * k] = c[k];
+    }
     __syncthreads();
     n = 0;
-    for (int w = 0; w < BL_JOIN / 64; ++w) n += rows[w];
-    if (tid < cols) {
-        v = 0.0;
-        c = 0;
-        for (int i = 0; i < stripes; ++i) {
-            v += stripe[i * cols + tid];
-            c += stripe_counts[i * cols + tid];
+    for (int w = 0; w < WAVES; ++w) n += rows[w];
+    for (int e = tid; e < 64 * COLS; e += 64 * WAVES) {
+        double t = 0.0;
+        int32_t m = 0;
+        for (int w = 0; w < WAVES; ++w) {
+            t += stripe[w][e];
+            m += stripe_counts[w][e];
         }
-        sums[tid] = v;
-        counts[tid] = c;
+        sums[e] = t;
+        counts[e] = m;
     }
     __syncthreads();
-    finish<BL_JOIN>(a, s, sums, counts, n, part);
+    finish<64 * WAVES>(a, lead.x, sums, counts, n, part);
 }
 
-template <typename T, int LANES, int R, int VEC>
+template <typename T, int LANES, int R, int VEC, bool FULL>
 __global__ __launch_bounds__(BL_BLOCK) void balance_grad(const BalanceRows a, int64_t span) {
     constexpr int ROWS = 64 / LANES, TEAMS = BL_WAVES * ROWS;
     const int tid = threadIdx.x, lane = tid % LANES, wv = tid >> 6, team = (tid & 63) / LANES;
     const int E = a.E;
+    const T* const x0 = static_cast<const T*>(a.x);
     const int64_t r0 = blockIdx.x * span, r1 = r0 + span < a.N ? r0 + span : a.N;
-    int64_t s = seq_after(a, r0 + wv * ROWS), s_end = -1, s_from = 0;  // of this lane's row
+    // a row is on its way while the one before is worked on, the first one while its sequence
+    // is looked for
+    RawExperts<T, LANES, R, VEC> raw, later;
+    int32_t first, then;
+    auto fetch = [&](int64_t row) {
+        const int64_t at = row < r1 ? row : r1 - 1;
+        later.load(x0 + at * E, E, lane);
+        then = first_index(a, at, lane);
+    };
+    int64_t row = r0 + wv * ROWS + team;
+    fetch(row);
+    raw = later;
+    first = then;
+    // the sequence of this lane's row: none from s_end on
+    int64_t s = 0, s_from = INT64_MAX, s_end = INT64_MAX;
     float c[R], f = 0.0f;
+    auto enter = [&] {
+        const double n = (double)a.rows[s], mean = (double)a.K * n / E;
+        const double g = (double)a.dloss[s] * a.scale * E;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int e = expert<LANES, VEC>(lane, j);
+            const int32_t v = a.counts[s * E + (FULL || e < E ? e : 0)];
+            c[j] = FULL || e < E ? (float)((double)v - mean) : 0.0f;
+        }
+        f = n > 0.0 ? (float)(g / (a.K * n * n)) : 0.0f;
+    };
 #pragma unroll
     for (int j = 0; j < R; ++j) c[j] = 0.0f;
+    {
+        Sequences seq;
+        s = seq.after(a, r0 + wv * ROWS);
+        if (s < a.S) {
+            seq.bounds(a, s, s_from, s_end);
+            enter();
+        }
+    }
     for (int64_t row0 = r0 + wv * ROWS; row0 < r1; row0 += TEAMS) {
-        const int64_t row = row0 + team;
+        fetch(row + TEAMS);
         const bool live = row < r1;
         float x[R], q[R], slope[R];
-        load_experts<T, LANES, R, VEC>(static_cast<const T*>(a.x) + (live ? row : r0) * E, E, live,
-                                       lane, x);
-        const bool in = takes_part<LANES, false>(a, row, live, lane, team, nullptr);
+        raw.template widen<FULL>(x, E, lane);
+        const bool in = takes_part<LANES, false>(a, row, live, lane, team, first, nullptr);
         if (live && row >= s_end) {  // another sequence
             while (s < a.S && (s_end = seq_start(a, s + 1)) <= row) ++s;
             if (s < a.S) {
                 s_from = seq_start(a, s);
-                const double n = (double)a.rows[s], mean = (double)a.K * n / E;
-#pragma unroll
-                for (int j = 0; j < R; ++j) {
-                    const int e = expert<LANES, VEC>(lane, j);
-                    c[j] = e < E ? (float)((double)a.counts[s * E + e] - mean) : 0.0f;
-                }
-                f = n > 0.0 ? (float)((double)a.dloss[s] * a.scale * E / (a.K * n * n)) : 0.0f;
+                enter();
             } else {
-                s_from = s_end = INT64_MAX;  // behind the last
+                s_from = s_end = INT64_MAX;
             }
         }
         const bool part = in && row >= s_from;
@@ -315,12 +454,16 @@ __global__ __launch_bounds__(BL_BLOCK) void balance_grad(const BalanceRows a, in
 #pragma unroll
         for (int j = 0; j < R; ++j) dot = __builtin_fmaf(c[j], q[j], dot);
         dot = group_sum<LANES>(dot);
-        if (!live) continue;
-        T* dr = static_cast<T*>(a.dx) + row * E;
         float d[R];
 #pragma unroll
-        for (int j = 0; j < R; ++j) d[j] = part ? f * q[j] * (c[j] - dot) * slope[j] : 0.0f;
-        store_experts<T, LANES, R, VEC>(dr, E, lane, d);
+        for (int j = 0; j < R; ++j) {
+            const float v = f * q[j] * (c[j] - dot);
+            d[j] = part ? (a.sigmoid ? v * slope[j] : v) : 0.0f;
+        }
+        if (live) store_experts<T, LANES, R, VEC>(static_cast<T*>(a.dx) + row * E, E, lane, d);
+        row += TEAMS;
+        first = then;
+        raw = later;
     }
 }
 
@@ -331,11 +474,11 @@ static int balance_lanes(int E) {
     return lanes;
 }
 
-// Rows of a span: as many as give every CU a workgroup or two, and at least four a team.
+// Rows of a span: one workgroup a CU, and at least four rows a team.
 static int64_t balance_span(int64_t N, int E, int cus) {
-    const int64_t teams = BL_BLOCK / balance_lanes(E);
-    int64_t rows = (N + 2 * cus - 1) / (2 * (int64_t)cus);
-    rows = (rows + teams - 1) / teams * teams;
+    const int lanes = balance_lanes(E);
+    const int64_t teams = (lanes == 64 && E > 512 ? 8 : 16) * (64 / lanes);
+    const int64_t rows = ((N + cus - 1) / cus + teams - 1) / teams * teams;
     return rows < 4 * teams ? 4 * teams : rows;
 }
 
@@ -343,13 +486,14 @@ static uint32_t balance_spans_of(int64_t N, int64_t rows) {
     return N > 0 ? (uint32_t)((N + rows - 1) / rows) : 1;
 }
 
-static size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+static size_t slots_bytes(size_t spans, size_t E) {
+    return (spans * 2 * (E + 1) * 8 + 255) / 256 * 256;
+}
 
 size_t balance_scratch_bytes(int64_t N, int64_t E, int64_t S, int cus) {
     (void)S;
     const size_t spans = balance_spans_of(N, balance_span(N, (int)E, cus));
-    return up256(spans * 2 * (size_t)E * 8) + up256(spans * 2 * (size_t)E * 4) +
-           up256(spans * 2 * 4) + up256(spans * 4);
+    return spans > 1 ? slots_bytes(spans, (size_t)E) + spans * sizeof(int2) : 0;
 }
 
 // Teams of LANES lanes with R experts each, VEC neighbours at a time: f is called with them as
@@ -388,24 +532,30 @@ static hipError_t launch_balance_fwd_t(const BalanceRows& a, void* scratch, hipS
     BalanceSpans b{};
     b.rows = balance_span(a.N, a.E, a.cus);
     b.spans = balance_spans_of(a.N, b.rows);
-    char* at = static_cast<char*>(scratch);
-    b.sums = reinterpret_cast<double*>(at);
-    at += up256((size_t)b.spans * 2 * a.E * 8);
-    b.counts = reinterpret_cast<int32_t*>(at);
-    at += up256((size_t)b.spans * 2 * a.E * 4);
-    b.n = reinterpret_cast<int32_t*>(at);
-    at += up256((size_t)b.spans * 2 * 4);
-    b.leads = reinterpret_cast<int32_t*>(at);
+    b.slots = static_cast<uint64_t*>(scratch);
+    b.leads = reinterpret_cast<int2*>(static_cast<char*>(scratch) +
+                                      slots_bytes(b.spans, (size_t)a.E));
     auto go = [&](auto lanes, auto r, auto vec) {
-        hipLaunchKernelGGL((balance_spans<T, decltype(lanes)::value, decltype(r)::value,
-                                          decltype(vec)::value>),
-                           dim3(b.spans), dim3(BL_BLOCK), 0, st, a, b);
+        constexpr int R = decltype(r)::value;
+        constexpr int L = decltype(lanes)::value, V = decltype(vec)::value;
+        const dim3 grid(b.spans), block(64 * span_waves<R>());
+        if (a.E == L * R)
+            hipLaunchKernelGGL((balance_spans<T, L, R, V, true>), grid, block, 0, st, a, b);
+        else
+            hipLaunchKernelGGL((balance_spans<T, L, R, V, false>), grid, block, 0, st, a, b);
     };
     if (four(a, sizeof(T), false)) with_team<true>(a.E, go);
     else with_team<false>(a.E, go);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess || b.spans == 1) return e;
-    hipLaunchKernelGGL(balance_join, dim3(b.spans), dim3(BL_JOIN), 0, st, a, b);
+#define OSM_JOIN(C) hipLaunchKernelGGL((balance_join<C>), dim3(b.spans), dim3(64 * join_waves<C>()), 0, st, a, \
+                                       b)
+    if (a.E <= 64) OSM_JOIN(1);
+    else if (a.E <= 128) OSM_JOIN(2);
+    else if (a.E <= 256) OSM_JOIN(4);
+    else if (a.E <= 512) OSM_JOIN(8);
+    else OSM_JOIN(16);
+#undef OSM_JOIN
     return hipGetLastError();
 }
 
@@ -416,10 +566,12 @@ static hipError_t launch_balance_bwd_t(const BalanceRows& a, hipStream_t st) {
     const int64_t blocks = want < most ? want : most;
     const int64_t span = (a.N + blocks - 1) / blocks;
     auto go = [&](auto lanes, auto r, auto vec) {
-        hipLaunchKernelGGL((balance_grad<T, decltype(lanes)::value, decltype(r)::value,
-                                         decltype(vec)::value>),
-                           dim3((unsigned)((a.N + span - 1) / span)), dim3(BL_BLOCK), 0, st, a,
-                           span);
+        constexpr int L = decltype(lanes)::value, R = decltype(r)::value, V = decltype(vec)::value;
+        const dim3 grid((unsigned)((a.N + span - 1) / span)), block(BL_BLOCK);
+        if (a.E == L * R)
+            hipLaunchKernelGGL((balance_grad<T, L, R, V, true>), grid, block, 0, st, a, span);
+        else
+            hipLaunchKernelGGL((balance_grad<T, L, R, V, false>), grid, block, 0, st, a, span);
     };
     if (four(a, sizeof(T), true)) with_team<true>(a.E, go);
     else with_team<false>(a.E, go);

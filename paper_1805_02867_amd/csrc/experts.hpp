@@ -1,6 +1,8 @@
 // Rows of router logits in registers: a row by a team of 8 to 64 lanes.
 #pragma once
 
+#include <type_traits>
+
 #include "wide.hpp"
 
 namespace osm {
@@ -41,6 +43,66 @@ __device__ __forceinline__ void load_experts(const T* xr, int E, bool live, int 
             }
         }
     }
+}
+
+// A row's experts as they come from memory: every lane loads, from a place inside the row where
+// it has no expert, so that nothing waits; `widen` makes numbers of them, -inf where there is no
+// expert.
+template <typename T, int LANES, int R, int VEC>
+struct RawExperts {
+    using V4 = std::conditional_t<sizeof(T) == 4, f32x4, uint2>;
+    using V1 = std::conditional_t<sizeof(T) == 4, float, uint16_t>;
+    static constexpr int N = VEC == 4 ? R / 4 : R;
+    using V = std::conditional_t<VEC == 4, V4, V1>;
+    V q[N];
+
+    __device__ __forceinline__ void load(const T* xr, int E, int lane) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int e = expert<LANES, VEC>(lane, i * VEC);
+            q[i] = *reinterpret_cast<const V*>(xr + (e < E ? e : 0));
+        }
+    }
+    // FULL: there is an expert in every place.
+    template <bool FULL>
+    __device__ __forceinline__ void widen(float (&x)[R], int E, int lane) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool in = FULL || expert<LANES, VEC>(lane, i * VEC) < E;
+            float v[VEC];
+            if constexpr (VEC == 4 && sizeof(T) == 4) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = q[i][k];
+            } else if constexpr (VEC == 4) {
+                v[0] = bf16_lo(q[i].x), v[1] = bf16_hi(q[i].x);
+                v[2] = bf16_lo(q[i].y), v[3] = bf16_hi(q[i].y);
+            } else if constexpr (sizeof(T) == 4) {
+                v[0] = q[i];
+            } else {
+                v[0] = __uint_as_float((uint32_t)q[i] << 16);
+            }
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) x[i * VEC + k] = in ? v[k] : -__builtin_inff();
+        }
+    }
+};
+
+// Sum over the wavefront's teams of what the lanes with the same place in them hold.
+template <int LANES>
+__device__ __forceinline__ float sum_of_teams(float v) {
+    float a, b;
+    if constexpr (LANES <= 8)  // a rotation by 8 within 16 lanes
+        v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x128,
+                                                                   0xF, 0xF, false));
+    if constexpr (LANES <= 16) {
+        bfly_operands<4>(v, a, b);
+        v = a + b;
+    }
+    if constexpr (LANES <= 32) {
+        bfly_operands<5>(v, a, b);
+        v = a + b;
+    }
+    return v;
 }
 
 template <typename T, int LANES, int R, int VEC>

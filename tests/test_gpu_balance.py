@@ -228,7 +228,10 @@ def test_refused(dev):
         with pytest.raises(osm.OsmError) as e:
             call()
         assert e.value.status == osm.EINVAL
-    n = osm.balance_workspace(8, 12, 2)
+    x, idx, starts = logits(9000, 12, "f32", 1, dev), places(9000, 12, 2, 1, dev), None
+    r = osm.balance_fwd(x, idx)
+    n = osm.balance_workspace(9000, 12)
+    assert n > 0
     ws = torch.full((n,), 255, dtype=torch.uint8, device=dev)
     assert torch.equal(osm.balance_fwd(x, idx, starts, workspace=ws).loss, r.loss)
     with pytest.raises(osm.OsmError) as e:
