@@ -171,10 +171,12 @@ struct LogprobRows {
 };
 // How a batch is taken: W wavefronts a row (S = 1), or a workgroup of W for each of S chunks a
 // row of `chunk` elements, `rows` rows a launch, with scratch of logprob_scratch_bytes and
-// `rows` zeroed counters, which are left zeroed.
+// `rows` zeroed counters, which are left zeroed.  stream: rows or chunks by workgroups of so many
+// wavefronts that stream them (without alternatives).
 struct LogprobPlan {
     int W, S;
     int64_t chunk, rows;
+    int stream;
 };
 struct LogprobSplit {
     uint64_t* states;  // two words a chunk

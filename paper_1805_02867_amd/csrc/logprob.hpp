@@ -14,8 +14,12 @@
 //   s = s + (s' + 1) r,   w = w + (w' + (M - m') c (s' + 1)) r.
 // An empty state is (-inf, -1, 0): its s' + 1 is 0.
 //
-// Exponents are formed as (x - m) c, not as one fma with m c: the difference is exact near the
-// maximum at any magnitude of the logits, and the largest element's exponent is 0.
+// Exponents.  A wavefront's are t = fma(x, c, -S) with S = m c rounded: one rounding of the
+// difference, at any magnitude.  What S lacks, delta = m c - S (exact in an fma), is put right
+// in its sums: with t = (x - m) c + delta, s is 2^-delta times the sum of 2^t, and so is w.  From
+// |S| = 2^22 on delta would not be small: there the elements are replaced by x - m, and m by 0,
+// ahead of the same loop.  (In the elements' type: where x - m rounds in bfloat16, x is so far
+// from m that its weight is 0.)
 #pragma once
 
 #include "topk_held.hpp"
@@ -63,13 +67,15 @@ __device__ __forceinline__ LogState log_merge_wave(LogState v, float c) {
 // in w, where -inf times 0 would be no number.
 constexpr float kLogFloor = -200.0f;
 
-// Adds a vector's weights and falls.  skip: an element of value m is left out, the first.
-template <bool SKIP, int E>
-__device__ __forceinline__ void log_add(const float (&x)[E], float m, float c, float& s, float& w) {
+// Adds the weights of a vector, and (ENT) minus their falls.  SKIP: an element of value m is
+// left out, the first.
+template <bool ENT, bool SKIP, int E>
+__device__ __forceinline__ void log_add(const float (&x)[E], float m, float c, float S, float& s,
+                                        float& w) {
     bool done = !SKIP;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        const float t = (x[e] - m) * c;
+        const float t = __builtin_fmaf(x[e], c, -S);
         float p = exp2_hw(t);
         if constexpr (SKIP) {
             const bool is = !done && x[e] == m;
@@ -77,27 +83,55 @@ __device__ __forceinline__ void log_add(const float (&x)[E], float m, float c, f
             done = done || is;
         }
         s += p;
-        w = __builtin_fmaf(p, -__builtin_fmaxf(t, kLogFloor), w);
+        if constexpr (ENT) w = __builtin_fmaf(p, __builtin_fmaxf(t, kLogFloor), w);
     }
 }
 
-// What lane l < T of a wavefront knows of its row's l-th token.
-struct LogToken {
-    float x;
-    bool in;
-};
+// The largest of a vector of bfloat16 elements as integers of 16 bits: the largest element if
+// that is not negative, else some negative number.
+__device__ __forceinline__ int signed_max(u32x4 q) {
+    typedef short s16x2 __attribute__((ext_vector_type(2)));
+    const s16x2 a = __builtin_elementwise_max(__builtin_bit_cast(s16x2, (uint32_t)q.x),
+                                              __builtin_bit_cast(s16x2, (uint32_t)q.y));
+    const s16x2 b = __builtin_elementwise_max(__builtin_bit_cast(s16x2, (uint32_t)q.z),
+                                              __builtin_bit_cast(s16x2, (uint32_t)q.w));
+    const s16x2 c = __builtin_elementwise_max(a, b);
+    return c.x > c.y ? c.x : c.y;
+}
 
+// x - m in the elements' type.
 template <typename T>
-__device__ __forceinline__ LogToken log_token(const LogprobRows& a, const T* xr, int64_t row,
-                                              int lane) {
-    LogToken t{0.0f, false};
-    if (lane < a.T) {
-        const int32_t i = a.tokens[row * a.T + lane];
-        t.in = i >= 0 && (int64_t)i < a.V;
-        if (t.in) t.x = load1(xr + i);
-    }
-    return t;
+__device__ __forceinline__ u32x4 less(u32x4 q, float m) {
+    float v[Vec<T>::N];
+    widen<T>(q, v);
+#pragma unroll
+    for (int e = 0; e < Vec<T>::N; ++e) v[e] -= m;
+    if constexpr (Vec<T>::N == 8)
+        return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                     pack_bf16x2(v[6], v[7])};
+    else
+        return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+                     __float_as_uint(v[3])};
 }
+
+// What lane l < T of a wavefront knows of its row's l-th token.  The index is asked for ahead of
+// the row, the element behind it: neither is waited for then.
+struct LogToken {
+    int32_t i = -1;
+    float x = 0.0f;
+    bool in = false;
+
+    __device__ __forceinline__ void index(const LogprobRows& a, int64_t row, int lane) {
+        if (a.T > 0) i = a.tokens[row * a.T + (lane < a.T ? lane : 0)];
+    }
+    template <typename T>
+    __device__ __forceinline__ void element(const LogprobRows& a, const T* xr, int lane) {
+        if (a.T > 0) {
+            in = lane < a.T && i >= 0 && (int64_t)i < a.V;
+            x = load1(xr + (in ? i : 0));
+        }
+    }
+};
 
 // A row's outputs by one wavefront, from its state, lane l's token and (SEL) l-th key.
 template <bool SEL>
@@ -156,11 +190,45 @@ __device__ __forceinline__ LogState log_get(const uint64_t* p) {
             __uint_as_float((uint32_t)w)};
 }
 
+// Leaves chunk vr's state at the device's coherence point, by one wavefront, then counts it:
+// whether it is the row's last.
+__device__ __forceinline__ bool log_arrive(const LogprobSplit& p, int64_t vr, uint32_t in_launch,
+                                           LogState v) {
+    const int lane = threadIdx.x & 63;
+    if (lane == 0) log_put(p.states + vr * 2, v);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    uint32_t done = 0;
+    if (lane == 0)
+        done = __hip_atomic_fetch_add(p.ctr + in_launch, 1u, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT);
+    return __builtin_amdgcn_readfirstlane(done) == (uint32_t)p.S - 1;
+}
+
+// The state of a row whose chunks are all in, by one wavefront; its count is left at 0.
+__device__ __forceinline__ LogState log_join(const LogprobSplit& p, uint32_t in_launch, float c) {
+    const int lane = threadIdx.x & 63;
+    const int64_t first = (int64_t)in_launch * p.S;
+    LogState v = log_empty();
+    for (int j = lane; j < p.S; j += 64) v = log_merge(v, log_get(p.states + (first + j) * 2), c);
+    v = log_merge_wave(v, c);
+    if (lane == 0)
+        __hip_atomic_store(p.ctr + in_launch, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return v;
+}
+
+// Wavefronts per SIMD asked of the compiler.
+template <typename T, int W, int R, bool SEL, bool PART>
+constexpr int log_waves() {
+    constexpr bool bf = Vec<T>::N == 8;
+    if (SEL && R >= 6) return R > 12 ? 4 : R > 8 ? (bf ? 4 : 5) : R > 6 ? (bf ? 6 : 7) : 7;
+    return held_waves<T, W, R, PART>();
+}
+
 // Rows (PART = false) or chunks of rows (PART = true: workgroup b has chunk b % S of row
 // row0 + b / S) of at most 64 W R whole 16-byte vectors, W wavefronts each (W = 1: four rows a
-// workgroup).  SEL: with alternatives, selected as topk_held.hpp does.
-template <typename T, int W, int R, bool SEL, bool PART>
-__global__ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (held_waves<T, W, R, PART>())) void logprob_held(
+// workgroup).  SEL: with alternatives, selected as topk_held.hpp does.  ENT: with w.
+template <typename T, int W, int R, bool SEL, bool ENT, bool PART>
+__global__ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (log_waves<T, W, R, SEL, PART>())) void logprob_held(
     const LogprobRows a, const LogprobSplit p) {
     static_assert(!PART || W > 1, "chunks take a workgroup each");
     constexpr int E = Vec<T>::N, TR = 64 * W;
@@ -180,38 +248,59 @@ __global__ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (held_waves<T, W, R, PA
     const int nvec = sp.nvec;
     const float ninf = -__builtin_inff(), c = a.c;
 
+    LogToken tok;
+    if (wv == 0 || W == 1) tok.index(a, row, lane);
     // all loads first; lanes past the row load its last vector and mask it
     u32x4 buf[R];
-    if (nvec > 0) {
+    auto load = [&] {
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int v = tr + i * TR;
             buf[i] = __builtin_nontemporal_load(sp.vb + (v < nvec ? v : nvec - 1));
         }
+    };
+    if (nvec > 0) {
+        load();
     } else {
 #pragma unroll
         for (int i = 0; i < R; ++i) buf[i] = u32x4{0, 0, 0, 0};
     }
     const float ex = tr < sp.ne ? load1(sp.xr + sp.extra(tr)) : ninf;
-    LogToken tok{0.0f, false};
-    if (wv == 0 || W == 1) tok = log_token(a, xr, row, lane);
+    if (wv == 0 || W == 1) tok.element(a, xr, lane);
 
-    // 1. maxima by vector, and the wavefront's
-    float vm[R];
-    float lm = __builtin_fmaxf(ex, ninf);  // a NaN element gives -inf
+    // 1. maxima by vector, and the wavefront's.  bfloat16 ones by two elements at a time as
+    // integers, which order numbers that are not negative: where the wavefront has one, and only the
+    // largest is asked for, that is all.
+    float vm[R], lm = __builtin_fmaxf(ex, ninf), wm;  // a NaN element gives -inf
+    constexpr bool FAST = E == 8 && !SEL;
+    if constexpr (FAST) {
+        int im = ex >= 0.0f ? (int)(__float_as_uint(ex) >> 16) : -1;
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        vm[i] = tr + i * TR < nvec ? held_vmax<T, TK_VALUES>(buf[i]) : ninf;
-        lm = max3_raw(lm, vm[i], ninf);
+        for (int i = 0; i < R; ++i) {
+            const int v = tr + i * TR < nvec ? signed_max(buf[i]) : -1;
+            vm[i] = __uint_as_float((uint32_t)v << 16);
+            im = v > im ? v : im;
+        }
+        wm = __builtin_amdgcn_ballot_w64(im >= 0) != 0
+                 ? wave_max_f(im >= 0 ? __uint_as_float((uint32_t)im << 16) : ninf)
+                 : ninf;
     }
-    const float wm = wave_max_f(lm);
+    if (!FAST || !(wm > ninf)) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            opaque(buf[i]);
+            vm[i] = tr + i * TR < nvec ? held_vmax<T, TK_VALUES>(buf[i]) : ninf;
+            lm = max3_raw(lm, vm[i], ninf);
+        }
+        wm = wave_max_f(lm);
+    }
     // 2. the wavefront's state.  The element that is left out: the head or tail element of
     // the first lane that has the maximum there, else in that lane's vector `left_out`, which is
     // looked at again by itself.
     LogState st;
     {
-        const float m = wm > ninf ? wm : 0.0f;  // (no elements, or only -inf)
-        float s = 0.0f, w = 0.0f;
+        float m = wm > ninf ? wm : 0.0f;  // (no elements, or only -inf)
+        float s = 0.0f, w = 0.0f, x1[1] = {ex};
         const uint64_t at_ex = __builtin_amdgcn_ballot_w64(ex == m);
         uint64_t owner = at_ex;
         int left_out = -1;
@@ -225,10 +314,15 @@ __global__ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (held_waves<T, W, R, PA
             }
         }
         const bool mine = wm > ninf && owner != 0 && lane == __builtin_ctzll(owner | 1ull << 63);
-        {
-            const float x1[1] = {ex};
-            if (!(mine && at_ex != 0)) log_add<false>(x1, m, c, s, w);
+        const bool far = __builtin_fabsf(m * c) >= 0x1p22f;
+        if (rare(far)) {
+            x1[0] -= m;
+#pragma unroll
+            for (int i = 0; i < R; ++i) buf[i] = less<T>(buf[i], m);
+            m = 0.0f;
         }
+        const float S = m * c, delta = __builtin_fmaf(m, c, -S);
+        if (!(mine && at_ex != 0)) log_add<ENT, false>(x1, m, c, S, s, w);
         u32x4 again = buf[0];
 #pragma unroll
         for (int i = 0; i < R; ++i) {
@@ -236,26 +330,29 @@ __global__ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (held_waves<T, W, R, PA
             if (i == 0 || i * TR < nvec) {  // uniform
                 float xv[E], ps = 0.0f, pw = 0.0f;
                 widen<T>(buf[i], xv);
-                log_add<false>(xv, m, c, ps, pw);
+                log_add<ENT, false>(xv, m, c, S, ps, pw);
                 bool counts = tr + i * TR < nvec;
                 if (i == left_out) {  // uniform
                     again = buf[i];
                     counts = counts && !mine;
                 }
                 s += counts ? ps : 0.0f;
-                w += counts ? pw : 0.0f;
+                if constexpr (ENT) w += counts ? pw : 0.0f;
             }
         }
         if (left_out >= 0) {
             float xv[E], ps = 0.0f, pw = 0.0f;
             widen<T>(again, xv);
-            log_add<true>(xv, m, c, ps, pw);
+            log_add<ENT, true>(xv, m, c, S, ps, pw);
             s += mine ? ps : 0.0f;
-            w += mine ? pw : 0.0f;
+            if constexpr (ENT) w += mine ? pw : 0.0f;
         }
         s = group_sum<64>(s);
-        w = group_sum<64>(w);
+        const float back = exp2_hw(-delta);
+        if constexpr (ENT) w = back * __builtin_fmaf(delta, s, -group_sum<64>(w));
+        s *= back;
         st = LogState{wm, wm > ninf ? s : s - 1.0f, w};
+        if (SEL && rare(far) && nvec > 0) load();
     }
     uint64_t key = 0;
     if constexpr (SEL) {
@@ -333,17 +430,10 @@ __global__ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (held_waves<T, W, R, PA
                 if (SEL && lane < a.K)
                     __hip_atomic_store(p.keys + vr * a.K + lane, key, __ATOMIC_RELAXED,
                                        __HIP_MEMORY_SCOPE_AGENT);
-                if (lane == 0) log_put(p.states + vr * 2, st);
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-                uint32_t done = 0;
-                if (lane == 0)
-                    done = __hip_atomic_fetch_add(p.ctr + in_launch, 1u, __ATOMIC_RELAXED,
-                                                  __HIP_MEMORY_SCOPE_AGENT);
-                last = __builtin_amdgcn_readfirstlane(done) == (uint32_t)p.S - 1;
+                last = log_arrive(p, vr, in_launch, st);
             }
         }
         if constexpr (PART) {
-            const int64_t first = (int64_t)in_launch * p.S;  // the row's first chunk
             if constexpr (!SEL) {
                 if (!last) return;
                 // every chunk of the row is in
@@ -357,7 +447,7 @@ __global__ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (held_waves<T, W, R, PA
                     __syncthreads();
                 }
                 if (!last) return;
-                const uint64_t* pk = p.keys + first * a.K;
+                const uint64_t* pk = p.keys + (int64_t)in_launch * p.S * a.K;
                 const int64_t n = (int64_t)p.S * a.K;
                 MD none;
                 if (wide) {
@@ -369,18 +459,231 @@ __global__ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (held_waves<T, W, R, PA
                                                                     a.K, &key, &none);
                 }
             }
-            LogState v = log_empty();
-            for (int j = lane; j < p.S; j += 64)
-                v = log_merge(v, log_get(p.states + (first + j) * 2), c);
-            log_store<SEL>(a, row, log_merge_wave(v, c), tok, key);
-            if (lane == 0)
-                __hip_atomic_store(p.ctr + in_launch, 0u, __ATOMIC_RELAXED,
-                                   __HIP_MEMORY_SCOPE_AGENT);
+            log_store<SEL>(a, row, log_join(p, in_launch, c), tok, key);
         }
     }
 }
 
-template <typename T, int W, bool SEL, bool PART>
+// ------------------------------------------------------------------ streamed rows
+// Rows or chunks by a workgroup of W wavefronts that stream them, U vectors a lane on their
+// way while as many are worked on: memory is never left waiting for a reduction, which rows held
+// in registers do between their loads.
+//
+// A wavefront's reference is its own maximum so far: one comparison a step finds whether that
+// changes (of bfloat16 elements as integers of 16 bits, where the maximum is not negative).  Each
+// lane sums all of its elements.  The one that s leaves out has weight 1 in its lane's sum; where
+// the others of the wavefront add less than that, that lane's elements are read once more at the
+// end, the largest apart, by the whole wavefront.
+constexpr int LS_U = 4;  // vectors of a step
+
+template <typename T, bool ENT>
+struct LogStream {
+    static constexpr int E = Vec<T>::N;
+    float c;
+    float m = -__builtin_inff();   // the wavefront's maximum
+    float lm = -__builtin_inff();  // this lane's, where it is the wavefront's
+    float S = 0.0f;                // m c, rounded
+    float d = 0.0f, w = 0.0f;      // this lane's sums, relative to S
+    bool far = false;              // |m c| has reached 2^22
+
+    static __device__ __forceinline__ u32x4 nothing() {
+        const uint32_t v = E == 8 ? 0xFF80FF80u : 0xFF800000u;
+        return u32x4{v, v, v, v};
+    }
+    // The largest element of a step, if that is above the maximum.
+    template <int U>
+    __device__ __forceinline__ float largest(const u32x4 (&q)[U]) const {
+        if constexpr (E == 8) {
+            if (m >= 0.0f) {
+                int v = -1;
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int i = signed_max(q[u]);
+                    v = i > v ? i : v;
+                }
+                return __uint_as_float((uint32_t)v << 16);  // (NaN for -1)
+            }
+        }
+        float v = -__builtin_inff();
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            u32x4 t = q[u];
+            if (E == 8) opaque(t);  // (or it is widened ahead of the test above)
+            v = max3_raw(v, held_vmax<T, TK_VALUES>(t), v);
+        }
+        return v;
+    }
+    template <int U>
+    __device__ __forceinline__ void step(const u32x4 (&q)[U]) {
+        const float v = largest(q);
+        lm = v > lm ? v : lm;
+        if (rare(__builtin_amdgcn_ballot_w64(v > m) != 0)) {
+#pragma clang fp contract(off)  // (the step between the references as they are, both rounded)
+            const float top = wave_max_f(lm), S2 = top * c, fall = S - S2;
+            if (m > -__builtin_inff()) {
+                const float r = exp2_hw(fall);
+                if constexpr (ENT) w = r * __builtin_fmaf(fall, d, w);
+                d *= r;
+            } else if constexpr (ENT) {
+                w = d;  // 0, or NaN
+            }
+            m = top;
+            S = S2;
+            far = far || !(__builtin_fabsf(S2) < 0x1p22f);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float x[E];
+            widen<T>(q[u], x);
+            log_add<ENT, false>(x, 0.0f, c, S, d, w);
+        }
+    }
+    // The wavefront's state.  ex: the lane's head or tail element; the others are its vectors
+    // first + lane, first + lane + stride, ... of n from vb.
+    __device__ __forceinline__ LogState end(float ex, const u32x4* vb, int first, int stride,
+                                            int n) const {
+        const int lane = threadIdx.x & 63;
+        if (!(m > -__builtin_inff())) return {m, group_sum<64>(d) - 1.0f, 0.0f};
+        const float delta = __builtin_fmaf(m, c, -S), one = exp2_hw(delta);
+        const uint64_t who = __builtin_amdgcn_ballot_w64(lm == m);
+        const int owner = who != 0 ? __builtin_ctzll(who) : 0;
+        const bool mine = lane == owner;
+        const float rest = group_sum<64>(mine ? 0.0f : d);
+        // (the one's own exponent is delta)
+        float s = rest + (lane_value(d, owner) - one);
+        float fall = __builtin_fmaf(-delta, one, group_sum<64>(w));
+        if (s < 1.0f) {
+            float ps = 0.0f, pw = 0.0f;
+            const float oex = lane_value(ex, owner);
+            bool out = oex == m;
+            if (!out && lane == 0) {
+                const float x1[1] = {oex};
+                log_add<ENT, false>(x1, m, c, S, ps, pw);
+            }
+            for (int i = first + owner; i < n; i += 64 * stride) {
+                const int v = i + lane * stride;
+                float x[E], top = -__builtin_inff();
+                widen<T>(v < n ? vb[v] : nothing(), x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) top = __builtin_fmaxf(top, x[e]);
+                const uint64_t has = __builtin_amdgcn_ballot_w64(top == m);
+                if (!out && has != 0 && lane == __builtin_ctzll(has | 1ull << 63))
+                    log_add<ENT, true>(x, m, c, S, ps, pw);
+                else
+                    log_add<ENT, false>(x, m, c, S, ps, pw);
+                out = out || has != 0;
+            }
+            s = rest + group_sum<64>(ps);
+            fall = group_sum<64>(mine ? 0.0f : w) + group_sum<64>(pw);
+        }
+        const float r = exp2_hw(-delta);
+        return {m, s * r, ENT ? r * __builtin_fmaf(delta, s, -fall) : 0.0f};
+    }
+};
+
+// A vector's state by one lane, whatever its magnitude.
+template <typename T>
+__device__ __forceinline__ LogState log_of_vector(u32x4 q, float c) {
+    constexpr int E = Vec<T>::N;
+    float x[E];
+    widen<T>(q, x);
+    const float m = held_vmax<T, TK_VALUES>(q), at = m > -__builtin_inff() ? m : 0.0f;
+    LogState v{m, 0.0f, 0.0f};
+    bool done = false;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const float t = (x[e] - at) * c;
+        const bool is = !done && x[e] == m;
+        done = done || is;
+        const float p = is && m > -__builtin_inff() ? 0.0f : exp2_hw(t);
+        v.s += p;
+        v.w = __builtin_fmaf(p, -__builtin_fmaxf(t, kLogFloor), v.w);
+    }
+    if (!(m > -__builtin_inff())) v.s -= 1.0f;
+    return v;
+}
+
+template <typename T, bool ENT, int W>
+__global__ __launch_bounds__(64 * W, 5) void logprob_stream(const LogprobRows a,
+                                                            const LogprobSplit p) {
+    constexpr int E = Vec<T>::N, TR = 64 * W, U = LS_U;
+    __shared__ LogSmem<W, false> sm;
+    const int tr = threadIdx.x, lane = tr & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(tr >> 6);
+    const uint32_t in_launch = blockIdx.x / (uint32_t)p.S;
+    const int64_t row = p.row0 + in_launch;
+    const int64_t start = (blockIdx.x - in_launch * (uint32_t)p.S) * p.chunk;
+    const int64_t left = a.V - start;
+    const T* xr = static_cast<const T*>(a.x) + row * a.ld;
+    const HeldSpan<T> sp(xr, 0, start, 0, (int)(p.chunk < left ? p.chunk : left));
+    const int nvec = sp.nvec;
+    LogStream<T, ENT> st;
+    st.c = a.c;
+    // Steps of U vectors a lane, all whole but the last; of that, a lane loads the chunk's last
+    // vector where it has none, and counts it as nothing.
+    const int whole = nvec / (TR * U), steps = (nvec + TR * U - 1) / (TR * U);
+    auto load = [&](u32x4 (&to)[U], int k) {
+        if (k < whole) {
+            const u32x4* const at = sp.vb + (int64_t)k * (TR * U);
+#pragma unroll
+            for (int u = 0; u < U; ++u) to[u] = __builtin_nontemporal_load(at + u * TR + tr);
+        } else if (k < steps) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int v = tr + (k * U + u) * TR;
+                to[u] = __builtin_nontemporal_load(sp.vb + (v < nvec ? v : nvec - 1));
+            }
+        }
+    };
+    auto step = [&](u32x4 (&q)[U], int k) {
+        if (k == whole) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (tr + (k * U + u) * TR >= nvec) q[u] = st.nothing();
+        }
+        st.step(q);
+    };
+    LogToken tok;
+    if (wv == 0) tok.index(a, row, lane);
+    u32x4 q0[U], q1[U];
+    load(q0, 0);
+    const float ex = tr < sp.ne ? load1(sp.xr + sp.extra(tr)) : -__builtin_inff();
+    if (wv == 0) tok.element(a, xr, lane);
+    u32x4 extra = st.nothing();
+    extra.x = E == 8 ? (0xFF800000u | __float_as_uint(ex) >> 16) : __float_as_uint(ex);
+    if (sp.ne > 0) {
+        u32x4 one[1] = {extra};
+        st.step(one);
+    }
+    for (int k = 0; k < steps; k += 2) {
+        load(q1, k + 1);
+        step(q0, k);
+        if (k + 1 == steps) break;
+        load(q0, k + 2);
+        step(q1, k + 1);
+    }
+    LogState v;
+    if (rare(st.far)) {  // again, one vector after the other
+        v = log_of_vector<T>(extra, a.c);
+        for (int i = tr; i < nvec; i += TR) v = log_merge(v, log_of_vector<T>(sp.vb[i], a.c), a.c);
+        v = log_merge_wave(v, a.c);
+    } else {
+        v = st.end(ex, sp.vb, wv * 64, TR, nvec);
+    }
+    if (lane == 0) sm.state[wv] = v;
+    __syncthreads();
+    if (wv != 0) return;
+    v = sm.state[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) v = log_merge(v, sm.state[i], a.c);
+    if (p.S > 1) {
+        if (!log_arrive(p, blockIdx.x, in_launch, v)) return;
+        v = log_join(p, in_launch, a.c);
+    }
+    log_store<false>(a, row, v, tok, 0);
+}
+
+template <typename T, int W, bool SEL, bool ENT, bool PART>
 hipError_t launch_logprob_w(const LogprobRows& a, const LogprobSplit& p, hipStream_t st) {
     const int64_t nv = (PART ? p.chunk : a.V) / Vec<T>::N;
     const int64_t r = (nv + 64 * W - 1) / (64 * W);
@@ -388,16 +691,20 @@ hipError_t launch_logprob_w(const LogprobRows& a, const LogprobSplit& p, hipStre
                                   : PART ? p.rows * p.S : a.N;
     const dim3 grid((unsigned)blocks), block(W == 1 ? TK_BLOCK : 64 * W);
 #define OSM_LOG(R_) \
-    hipLaunchKernelGGL((logprob_held<T, W, R_, SEL, PART>), grid, block, 0, st, a, p)
+    hipLaunchKernelGGL((logprob_held<T, W, R_, SEL, ENT, PART>), grid, block, 0, st, a, p)
     if constexpr (W <= 4) {
         if (r <= 1) OSM_LOG(1);
         else if (r <= 2) OSM_LOG(2);
         else if (r <= 4) OSM_LOG(4);
         else if (r <= 6) OSM_LOG(6);
         else if (r <= 8) OSM_LOG(8);
-        else if (r <= 12) OSM_LOG(12);
-        else if (r <= TH_RMAX) OSM_LOG(16);
-        else return hipErrorInvalidValue;
+        else if constexpr (W == 4 && SEL) {
+            if (r <= 12) OSM_LOG(12);
+            else if (r <= TH_RMAX) OSM_LOG(16);
+            else return hipErrorInvalidValue;
+        } else {
+            return hipErrorInvalidValue;
+        }
     } else {
         if (r <= 8) OSM_LOG(8);
         else if (r <= 12) OSM_LOG(12);
@@ -408,17 +715,18 @@ hipError_t launch_logprob_w(const LogprobRows& a, const LogprobSplit& p, hipStre
     return hipGetLastError();
 }
 
-template <typename T, bool SEL>
+template <typename T, bool SEL, bool ENT>
 hipError_t launch_logprob_t(const LogprobRows& a, const LogprobPlan& plan, void* scratch,
                             uint32_t* ctr, hipStream_t st) {
     LogprobSplit p{};
     p.chunk = plan.chunk;
     p.S = plan.S;
-    if (plan.S <= 1) {
+    if (plan.S <= 1 && !plan.stream) {
         switch (plan.W) {
-            case 1: return launch_logprob_w<T, 1, SEL, false>(a, p, st);
-            case 4: return launch_logprob_w<T, 4, SEL, false>(a, p, st);
-            case 8: return launch_logprob_w<T, 8, SEL, false>(a, p, st);
+            case 1: return launch_logprob_w<T, 1, SEL, ENT, false>(a, p, st);
+            case 4: return launch_logprob_w<T, 4, SEL, ENT, false>(a, p, st);
+            case 8:
+                if constexpr (SEL) return launch_logprob_w<T, 8, SEL, ENT, false>(a, p, st);
             default: return hipErrorInvalidValue;
         }
     }
@@ -427,8 +735,18 @@ hipError_t launch_logprob_t(const LogprobRows& a, const LogprobPlan& plan, void*
     p.ctr = ctr;
     for (p.row0 = 0; p.row0 < a.N; p.row0 += plan.rows) {
         p.rows = a.N - p.row0 < plan.rows ? a.N - p.row0 : plan.rows;
-        const hipError_t e = plan.W == 4 ? launch_logprob_w<T, 4, SEL, true>(a, p, st)
-                                         : launch_logprob_w<T, 8, SEL, true>(a, p, st);
+        hipError_t e;
+        if (plan.stream) {
+            if constexpr (SEL) return hipErrorInvalidValue;
+            const dim3 grid((unsigned)(p.rows * p.S));
+            if (plan.stream == 8)
+                hipLaunchKernelGGL((logprob_stream<T, ENT, 8>), grid, dim3(512), 0, st, a, p);
+            else
+                hipLaunchKernelGGL((logprob_stream<T, ENT, 4>), grid, dim3(256), 0, st, a, p);
+            e = hipGetLastError();
+        } else {
+            e = launch_logprob_w<T, 4, SEL, ENT, true>(a, p, st);
+        }
         if (e != hipSuccess) return e;
     }
     return hipSuccess;

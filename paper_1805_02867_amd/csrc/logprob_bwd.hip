@@ -5,9 +5,9 @@
 // and h the entropy's:
 //   dx_j = (-p_j G - h p_j (ln p_j + H) + sum of g over the tokens that are j) / temperature
 //        = p_j (alpha + beta (x_j - m) c) + ...,  alpha, beta a row's constants.
-// Every element gets the first part; the lane that stored a token's element then stores it
-// again, from binary64: where p_t is close to 1, g (1 - p_t) is formed with
-// 1 - p_t = -expm1(ln p_t), which the difference of binary32 numbers has lost.
+// Every element gets the first part; then the tokens' elements are stored again, from binary64:
+// where p_t is close to 1, g (1 - p_t) is formed with 1 - p_t = -expm1(ln p_t), which the
+// difference of binary32 numbers has lost.
 //
 // What bounds it is memory: an element is read and written once, with a subtraction, an
 // exponential and four other operations.
@@ -35,7 +35,6 @@ __device__ __forceinline__ Vec<T> load_any(const T* p) {
 // A row's constants.
 struct GradRow {
     float m, c, alpha, beta;
-    bool zero;  // no gradient comes in
 };
 
 template <bool ENT>
@@ -78,24 +77,32 @@ __global__ __launch_bounds__(LB_BLOCK) void logprob_grad(const LogprobGrad a, ui
         }
     }
     const float ex = tr < extras ? load1(xr + extra(tr)) : 0.0f;
-
+    const float m = a.stats[row * 2], s = a.stats[row * 2 + 1];
+    const float h = ENT ? a.dentropy[row] : 0.0f;
+    const double H = ENT ? (double)a.entropy[row] : 0.0;
+    // lane l has the l-th token
     int32_t tok = -1;
     float g = 0.0f;
-    if (lane < a.T) {
-        tok = a.tokens[row * a.T + lane];
-        const bool in = tok >= 0 && (int64_t)tok < a.V;
-        tok = in ? tok : -1;
-        if (in) g = a.dlogp[row * a.T + lane];
+    if (a.T > 0) {
+        const int64_t at = row * a.T + (lane < a.T ? lane : 0);
+        const int32_t t = a.tokens[at];
+        const float v = a.dlogp[at];
+        const bool in = lane < a.T && t >= 0 && (int64_t)t < a.V;
+        tok = in ? t : -1;
+        g = in ? v : 0.0f;
     }
-    const double G = group_sum<64>((double)g);
-    const float h = ENT ? a.dentropy[row] : 0.0f;
-    const float m = a.stats[row * 2], s = a.stats[row * 2 + 1];
-    const double ln_d = log1p((double)s), rd = 1.0 / (1.0 + (double)s);
-    const double H = ENT ? (double)a.entropy[row] : 0.0;
+    // those among this piece's elements
+    const int64_t tv = (int64_t)tok >= head ? (tok - head) / E : nvec;  // (nvec: none)
+    const bool here = tok >= 0 && (tv < nvec ? tv >= v0 && tv < v0 + TR * U : piece == 0);
+    const bool any = __builtin_amdgcn_ballot_w64(here) != 0;
+    const float tx = here ? load1(xr + tok) : 0.0f;
+
+    const double G = group_sum<64>((double)g), rd = 1.0 / (1.0 + (double)s);
+    const double ln_d = ENT || any ? log1p((double)s) : 0.0;
+    const bool zero = __builtin_amdgcn_ballot_w64(!(g == 0.0f)) == 0 && h == 0.0f;
     GradRow r;
     r.m = m;
     r.c = a.c;
-    r.zero = __builtin_amdgcn_ballot_w64(!(g == 0.0f)) == 0 && h == 0.0f;
     r.alpha = (float)(-a.inverse * rd * (G + (ENT ? (double)h * (H - ln_d) : 0.0)));
     r.beta = ENT ? (float)(-a.inverse * rd * (double)h * 0.69314718055994530942) : 0.0f;
 
@@ -105,35 +112,33 @@ __global__ __launch_bounds__(LB_BLOCK) void logprob_grad(const LogprobGrad a, ui
         if (v >= nvec) continue;
         Vec<T> out;
 #pragma unroll
-        for (int e = 0; e < E; ++e) out.v[e] = r.zero ? 0.0f : grad_of<ENT>(r, buf[i].v[e]);
+        for (int e = 0; e < E; ++e) out.v[e] = zero ? 0.0f : grad_of<ENT>(r, buf[i].v[e]);
         out.store_nt(dr + head + v * E);
     }
-    if (tr < extras) store1(dr + extra(tr), r.zero ? 0.0f : grad_of<ENT>(r, ex));
-    if (r.zero) return;
+    if (tr < extras) store1(dr + extra(tr), zero ? 0.0f : grad_of<ENT>(r, ex));
+    if (zero || !any) return;  // (the same in the piece's wavefronts)
 
-    // the tokens' own elements
-    for (int i = 0; i < a.T; ++i) {
-        const int32_t t = __builtin_amdgcn_readlane(tok, i);
-        if (t < 0) continue;
-        // who stored it
-        int64_t at;
-        const int64_t v = (int64_t)t >= head ? (t - head) / E : -1;
-        if (v < 0 || v >= nvec) {
-            if (piece != 0) continue;
-            at = v < 0 ? t : t - nvec * E;
-        } else {
-            if (v < v0 || v >= v0 + TR * U) continue;
-            at = (v - v0) % TR;
-        }
-        const uint64_t same = __builtin_amdgcn_ballot_w64(tok == t);
-        if ((same & ((1ull << i) - 1)) != 0) continue;  // done with its first place
-        const double gt = group_sum<64>(tok == t ? (double)g : 0.0);
-        const double lp = ((double)load1(xr + t) - (double)m) * a.inverse - ln_d;
-        const double p = exp(lp);
-        double d = gt * -expm1(lp) - p * (G - gt);
-        if (ENT && p > 0.0) d -= (double)h * p * (lp + H);
-        if (tr == (int)at) store1(dr + t, (float)(d * a.inverse));
+    // The tokens' own elements, a lane each, by the piece's first wavefront once they are
+    // stored.  A token that occurs twice is its first lane's.
+    if constexpr (TR > 64) {
+        __syncthreads();
+        if (threadIdx.x >= 64) return;
+    } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     }
+    double gt = 0.0;
+    bool first = here;
+    for (int i = 0; i < a.T; ++i) {
+        const bool same = __builtin_amdgcn_readlane(tok, i) == tok;
+        const float v = lane_value(g, i);
+        gt += same ? (double)v : 0.0;
+        first = first && !(same && i < lane);
+    }
+    if (!first) return;
+    const double lp = ((double)tx - (double)m) * a.inverse - ln_d, p = exp(lp);
+    double d = gt * -expm1(lp) - p * (G - gt);
+    if (ENT && p > 0.0) d -= (double)h * p * (lp + H);
+    store1(dr + tok, (float)(d * a.inverse));
 }
 
 template <typename T>
@@ -177,33 +182,60 @@ hipError_t launch_logprob_bwd(const LogprobGrad& a, int dtype, hipStream_t st) {
     return dtype == 1 ? launch_logprob_bwd_t<bf16_t>(a, st) : launch_logprob_bwd_t<float>(a, st);
 }
 
-// Rows that a wavefront holds take one where there are enough of them to fill the chip; longer
-// ones a workgroup of four or eight; rows that eight wavefronts do not hold, or too few to
-// fill the chip, are split.
+// How a batch is taken, by its rows' 16-byte vectors.  us of one call among others, f: binary32, b:
+// bfloat16 with the entropy; "held w" / "stream w": a workgroup of w wavefronts a row (w = 1: four
+// rows), xS: for each of S chunks.
+//
+// Up to 512 vectors: a wavefront a row where there are rows for all of them (1024 x 1000 f held 1
+// 4.1, held 4 4.7; 8192 x 1000 f 11.4 / 15.3; 8192 x 4000 b 20.4 / 23.6; but 512 x 1000 f 4.0 /
+// 3.8, 256 x 4000 b 5.5 / 4.1).  Up to 2048: held 4 (256 x 8000 f 5.3, stream 4 5.3, held 4 x2
+// 6.6).  Beyond that streams, by eight wavefronts (256 x 16000 f stream 8 6.2, stream 4 6.9, held 8
+// 7.0; 1024 x 128256 f 79.6 / 79.4 / 95; 2048 x 128256 b 84.7 / 90.6 / 105), or by four
+// where rows are not long and there are more of them than CUs (400 x 32000 b stream 4 10.5, 8
+// 10.6; 8192 x 50257 b 139 / 153; 8192 x 16000 b 48.3 / 52.5).
+//
+// Few long rows are split into as many chunks as give each CU one, of at least 4096 vectors, or up
+// to four in any case (64 x 128256 f stream 8 x4 10.4, x8 11.2; 16 x 128256 f x8 7.8, x6 8.2; 128
+// x 65536 f x2 9.9, x1 10.5; 16 x 65536 f x4 6.9); eight rows and fewer into up to 64 of at
+// least 512 vectors (1 x 128256 f held 4 x32 5.2, x16 5.7; 1 x 50257 f x32 4.9, x8 5.5).
+//
+// With alternatives (5 of them) rows are always held: by eight wavefronts from 2048 vectors on (16 x
+// 16000 f held 8 7.2, held 4 7.5; but 4096 x 16000 f 50.9 / 47.1), beyond 8192 vectors in chunks that
+// four hold (1024 x 128256 f x8 99, x4 by eight 125; 4096 x 128256 b x4 215, x2 262), and in
+// chunks of about 2048 where rows are few (64 x 128256 b x8 14.6, x4 15.0).
 LogprobPlan logprob_plan(int64_t N, int64_t V, int K, int dtype, int cus) {
-    const int64_t E = dtype == 1 ? 8 : 4;
+    const int64_t E = dtype == 1 ? 8 : 4, c = cus;
     const int64_t nv = (V + E - 1) / E;
     const int64_t hold4 = 256 * 16, hold8 = 512 * 16;  // vectors
-    LogprobPlan p{4, 1, V, N};
-    int64_t S = (nv + hold8 - 1) / hold8;
-    if (nv > 1024 && N < 2 * (int64_t)cus) {
-        const int64_t want = (2 * (int64_t)cus + N - 1) / N, most = (nv + 511) / 512;
-        const int64_t more = want < most ? want : most;
-        S = S > more ? S : more;
+    LogprobPlan p{4, 1, V, N, 0};
+    int64_t S = 1;
+    if (nv > 4096 && N <= 8) {
+        const int64_t most = K > 16 ? 32 : 64;
+        S = nv / 512 < most ? nv / 512 : most;
+    } else if (K == 0 && nv > 4096 && N < c) {
+        const int64_t most = nv / 4096 > 4 ? nv / 4096 : 4;
+        S = c / N < most ? c / N : most;
+    } else if (K > 0 && nv > hold8) {
+        const int64_t want = 2 * c / N, most = nv / 2048;
+        S = want < most ? want : most;
     }
-    if (S <= 1) {
-        if (nv <= 1024 && (nv <= 64 || N >= 4 * (int64_t)cus)) p.W = 1;
-        else p.W = nv <= hold4 ? 4 : 8;
-        return p;
-    }
+    // chunks that the registers hold, where they have to
+    if (K > 0 && nv > hold8 && S < (nv + hold4 - 1) / hold4) S = (nv + hold4 - 1) / hold4;
     const int64_t vecs = (nv + S - 1) / S;
-    p.chunk = vecs * E;
-    p.S = (int)((V + p.chunk - 1) / p.chunk);
-    p.W = vecs <= hold4 ? 4 : 8;
+    if (K == 0 && vecs > 2048) {
+        p.stream = nv <= hold8 && 2 * N >= 3 * c ? 4 : 8;
+    } else if (S == 1) {
+        p.W = nv <= 512 && N >= 4 * c ? 1
+              : nv <= 2048 || (nv <= hold4 && N >= 8 * c) ? 4 : 8;
+    }
+    if (S > 1) {
+        p.chunk = vecs * E;
+        S = (V + p.chunk - 1) / p.chunk;
+    }
+    p.S = (int)S;
     // 2^16 chunks a launch, or one row
-    const int64_t rows = ((int64_t)1 << 16) / p.S;
-    p.rows = rows < 1 ? 1 : rows < N ? rows : N;
-    (void)K;
+    const int64_t rows = ((int64_t)1 << 16) / S;
+    if (S > 1 || p.stream) p.rows = rows < 1 ? 1 : rows < N ? rows : N;
     return p;
 }
 

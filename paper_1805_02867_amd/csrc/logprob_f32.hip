@@ -1,13 +1,17 @@
-// Log probabilities of f32 rows (one source per element type and selection, so that the build
-// compiles them in parallel; the one with alternatives is logprob_top_f32.hip).
+// Log probabilities of f32 rows.  The kernels are instantiated in one source each for plain ones,
+// with the entropy and with alternatives (which come with the entropy), so that the build
+// compiles them in parallel.
 #include "logprob.hpp"
 
 namespace osm {
+hipError_t launch_logprob_entropy_f32(const LogprobRows& a, const LogprobPlan& p, void* scratch,
+                                      uint32_t* ctr, hipStream_t st);
 hipError_t launch_logprob_top_f32(const LogprobRows& a, const LogprobPlan& p, void* scratch,
                                   uint32_t* ctr, hipStream_t st);
 hipError_t launch_logprob_f32(const LogprobRows& a, const LogprobPlan& p, void* scratch,
                               uint32_t* ctr, hipStream_t st) {
-    return a.K > 0 ? launch_logprob_top_f32(a, p, scratch, ctr, st)
-                   : launch_logprob_t<float, false>(a, p, scratch, ctr, st);
+    if (a.K > 0) return launch_logprob_top_f32(a, p, scratch, ctr, st);
+    if (a.entropy) return launch_logprob_entropy_f32(a, p, scratch, ctr, st);
+    return launch_logprob_t<float, false, false>(a, p, scratch, ctr, st);
 }
 }  // namespace osm

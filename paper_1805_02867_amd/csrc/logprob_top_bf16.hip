@@ -3,7 +3,7 @@
 
 namespace osm {
 hipError_t launch_logprob_top_bf16(const LogprobRows& a, const LogprobPlan& p, void* scratch,
-                                  uint32_t* ctr, hipStream_t st) {
-    return launch_logprob_t<bf16_t, true>(a, p, scratch, ctr, st);
+                                   uint32_t* ctr, hipStream_t st) {
+    return launch_logprob_t<bf16_t, true, true>(a, p, scratch, ctr, st);
 }
 }  // namespace osm
