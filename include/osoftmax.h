@@ -462,8 +462,8 @@ OSM_API int osm_logprob_workspace(int64_t N, int64_t V, int K, int dtype, size_t
  * holds; any other row with NaN stats (or h, or one of g) gets NaN.  The gradient of
  * top_logp is that of the same indices given as tokens.
  * x, ldx, tokens, T, temperature: as in logprob_fwd.  stats: N*2 and entropy: N, as
- * logprob_fwd wrote them for this x and temperature (entropy is read with dentropy only, and may be NULL without it).
- * dlogp: N*T, NULL where T is 0.  dentropy: N, or NULL (0).  dx: row r at dx + r * lddx
+ * logprob_fwd wrote them for this x and temperature (entropy is read with dentropy only, and
+ * may be NULL without it).  dlogp: N*T, NULL where T is 0.  dentropy: N, or NULL (0).  dx: row r at dx + r * lddx
  * elements of dtype, lddx >= V, every element of the rows written, none between them.
  * Errors: OSM_EINVAL for bad sizes, ldx or lddx < V, unknown dtype, bad T or temperature,
  * neither dlogp nor dentropy, null (with N > 0), misaligned or overlapping buffers. */
@@ -489,8 +489,8 @@ OSM_API int logprob_bwd(const void* x, int64_t ldx, const int32_t* tokens, const
  * x: N*E logits of dtype.  idx: N*K int32, as route_fwd gave them.  starts: S + 1 int32 that do
  * not decrease, or NULL; numbers outside [0, N] are taken as the nearest inside, results for
  * decreasing ones are unspecified.  loss: S binary32.  counts: S*E int32.  probs: S*E
- * binary32.  rows: S int32.  Shares are binary32, sums over rows binary64.  N = 0 is no
- * no-op here: the outputs are zeros.
+ * binary32.  rows: S int32.  Shares are binary32, sums over rows binary64 but for
+ * 64 rows at a time at most.  N = 0 is no no-op here: the outputs are zeros.
  * Errors: OSM_EINVAL for N < 0, E < 1, E > OSM_ROUTE_EMAX, K < 1, K > OSM_TOPK_KMAX, S < 1,
  * N * K, S or S * E above 2^31 - 1, starts NULL with S > 1, unknown dtype or score, null
  * (x and idx only with N > 0), misaligned or overlapping buffers; OSM_ENOMEM if the

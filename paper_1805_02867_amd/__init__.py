@@ -1,9 +1,9 @@
 """Python binding of libosoftmax (online-normalizer softmax, fused softmax +
-top-k, sampling, log probabilities, expert routing and balance on MI355X).  Argument marshalling only:
-every step of the computation runs in the library's HIP kernels, reached
-through its C ABI (``include/osoftmax.h``).  PyTorch supplies device memory
-and the current stream.  There is no fallback: if the library is missing,
-every call raises.
+top-k, sampling, log probabilities, expert routing and balance on MI355X).
+Argument marshalling only: every step of the computation runs in the library's
+HIP kernels, reached through its C ABI (``include/osoftmax.h``).  PyTorch
+supplies device memory and the current stream.  There is no fallback: if the
+library is missing, every call raises.
 """
 from __future__ import annotations
 
@@ -446,7 +446,7 @@ def _vector(t, dtype, x: torch.Tensor, n: int, name: str) -> torch.Tensor:
 def _output(t, shape, dtype, x: torch.Tensor, name: str) -> torch.Tensor:
     """The caller's output, or a new one (which needs no checks: they take 0.5 us)."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=x.device)
+        return x.new_empty(shape, dtype=dtype)
     n = shape[0] * shape[1] if len(shape) == 2 else shape[0]
     return _vector(t, dtype, x, n, name)
 
@@ -582,17 +582,21 @@ def route_bwd(x: torch.Tensor, idx: torch.Tensor, dvals: torch.Tensor, score="so
     return dx
 
 
-def _own_workspace(need, workspace, x: torch.Tensor, stream):
+_capturing = getattr(torch._C, "_cuda_isCurrentStreamCapturing", None)
+
+
+def _own_workspace(workspace, x: torch.Tensor, stream, need, *shape):
     """The workspace that a call is given: the caller's, or while the current stream is being
-    captured one from the graph's own memory (None: the library's scratch)."""
+    captured one of need(*shape) bytes from the graph's own memory (None: the library's
+    scratch)."""
     if workspace is not None:
         return _vector(workspace, torch.uint8, x, workspace.numel(), "workspace")
-    if not torch.cuda.is_current_stream_capturing():
+    if not (_capturing or torch.cuda.is_current_stream_capturing)():
         return None
     if _stream(stream) != _stream(None):
         raise ValueError("a captured call on another stream than the current one needs a "
                          "workspace")
-    return torch.empty(need(), dtype=torch.uint8, device=x.device)
+    return torch.empty(need(*shape), dtype=torch.uint8, device=x.device)
 
 
 def _tokens(tokens, x: torch.Tensor, N: int, name: str = "tokens") -> int:
@@ -609,7 +613,7 @@ def _tokens(tokens, x: torch.Tensor, N: int, name: str = "tokens") -> int:
 
 def _asked(t, shape, x: torch.Tensor, name: str):
     """An output that is given, asked for (True) or not wanted (False, None)."""
-    if t is None or t is False:
+    if not isinstance(t, torch.Tensor) and not t:
         return None
     return _output(None if t is True else t, shape, torch.float32, x, name)
 
@@ -633,8 +637,10 @@ def logprob_fwd(x: torch.Tensor, tokens: torch.Tensor | None = None, K: int = 0,
         T = _tokens(tokens, x, N)
         tp = _vector(tokens, torch.int32, x, N * T, "tokens").data_ptr()
         if logp is None:
-            logp = torch.empty(tokens.shape, dtype=torch.float32, device=x.device)
-        lp = _vector(logp, torch.float32, x, N * T, "logp").data_ptr()
+            logp = x.new_empty((N, T) if tokens.dim() == 2 else (N * T,), dtype=torch.float32)
+        else:
+            _vector(logp, torch.float32, x, N * T, "logp")
+        lp = logp.data_ptr()
     elif logp is not None:
         raise ValueError("logp needs tokens")
     if K > 0:
@@ -648,7 +654,7 @@ def logprob_fwd(x: torch.Tensor, tokens: torch.Tensor | None = None, K: int = 0,
     p = Logprob(tp, lp, None if entropy is None else entropy.data_ptr(),
                 None if stats is None else stats.data_ptr(), vp, ip, T, _int32(K, "K"),
                 float(temperature))
-    workspace = _own_workspace(lambda: logprob_workspace(N, V, K, x.dtype), workspace, x, stream)
+    workspace = _own_workspace(workspace, x, stream, logprob_workspace, N, V, K, x.dtype)
     if workspace is None:
         rc = lib().logprob_fwd(x.data_ptr(), ld, ctypes.byref(p), N, V, _DTYPES[x.dtype],
                                _stream(stream))
@@ -746,7 +752,7 @@ def balance_fwd(x: torch.Tensor, idx: torch.Tensor, starts: torch.Tensor | None 
     counts = _output(counts, (S, E), torch.int32, x, "counts")
     probs = _output(probs, (S, E), torch.float32, x, "probs")
     rows = _output(rows, (S,), torch.int32, x, "rows")
-    workspace = _own_workspace(lambda: balance_workspace(N, E, S), workspace, x, stream)
+    workspace = _own_workspace(workspace, x, stream, balance_workspace, N, E, S)
     args = (x.data_ptr(), ip, sp, loss.data_ptr(), counts.data_ptr(), probs.data_ptr(),
             rows.data_ptr(), N, E, K, S, _DTYPES[x.dtype], _int32(_score(score), "score"),
             float(scale))

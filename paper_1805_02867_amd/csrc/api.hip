@@ -938,7 +938,7 @@ int run_balance(const osm::BalanceRows& rows, int dtype, bool own, void* workspa
     DeviceState* ds = device_state(nullptr);
     if (!ds) return OSM_EHIP;
     a.cus = ds->cus;
-    const size_t need = osm::balance_scratch_bytes(a.N, a.E, a.S, a.cus);
+    const size_t need = osm::balance_scratch_bytes(a.N, a.E, a.cus);
     if (need == 0) return hip_status(osm::launch_balance_fwd(a, dtype, nullptr, stream));
     if (own) {
         if (!workspace || workspace_bytes < need) return OSM_ESCRATCH;
@@ -1154,7 +1154,7 @@ int osm_balance_workspace(int64_t N, int64_t E, int64_t S, size_t* bytes) {
         S * E > kMaxDim || !bytes)
         return OSM_EINVAL;
     DeviceState* ds = device_state(nullptr);
-    *bytes = osm::balance_scratch_bytes(N, E, S, ds ? ds->cus : 256);
+    *bytes = osm::balance_scratch_bytes(N, E, ds ? ds->cus : 256);
     return OSM_OK;
 }
 

@@ -9,16 +9,21 @@
 // Balanced counts are all about K n / E and cancel in the gradient: they are taken less that
 // number, which changes nothing as the shares sum to 1.
 //
-// Forward.  Workgroup b takes a span of rows; a row by a team of LANES lanes that hold R
-// experts each, so that a lane sums the shares of its own experts over rows in registers (binary64:
-// a sequence may be long), and counts go to LDS as integers, whose additions may come in any order.  At the end of each
-// sequence's part of the span the teams' sums are joined in their order, in binary64.  A
-// sequence that lies within the span is finished there.  Of others the parts go to scratch, and a
-// second kernel joins them in the order of the spans, so that the result is the same every
-// time.
+// Forward.  Workgroup i takes a span of rows; a row by a team of LANES lanes that hold R experts
+// each, so that a lane sums the shares of its own experts over rows in registers (binary32, of at
+// most 64 rows of a team), and counts go to LDS as integers, whose additions may come in any
+// order.  At the end of each sequence's part of the span the teams' sums are joined in their order,
+// in binary64.  A sequence within the span is finished there: by the workgroup, or one of few rows
+// by a wavefront alone, so that several are worked on at once.  Of others the parts go to scratch,
+// and a second kernel joins them in the order of the spans: the result is the same every time.
 //
-// What bounds both is memory (a row is read once, the gradient written once), and for small
-// batches the launches.
+// Gradient: a row by a team as well, a lane keeps its experts' counts of the sequence that its row
+// is in.
+//
+// What bounds them.  65536 x 256 bfloat16 sigmoid in 24 sequences takes 18 us, its 36 MB 5.2 at
+// 6.9 TB/s: the arithmetic (an exponential and a reciprocal an element, about 14 instructions; 7 us
+// of it), the chain ahead of and behind the rows (5 us, a batch of 16 rows) and the join, a launch
+// (5 us).  The gradient of 65536 x 256 binary32 takes 25 us for 134 MB, a large copy's rate.
 #include <type_traits>
 
 #include "experts.hpp"
@@ -28,7 +33,8 @@ namespace osm {
 
 constexpr int BL_BLOCK = 256;   // of the gradient
 constexpr int BL_WAVES = BL_BLOCK / 64;
-constexpr int BL_FLUSH = 64;    // rows of a team whose shares are added in binary32
+constexpr int SPAN_WAVES = 16;  // of a span's workgroup
+constexpr int BL_ADDED = 64;    // rows of a team whose shares are added in binary32
 
 // A sequence's part of a span in scratch: for each expert the sum of its shares (binary32, upper
 // word) and its count, then the rows that took part.  Slot 2 i is of the sequence that span i has
@@ -37,7 +43,10 @@ struct BalanceSpans {
     int64_t rows;      // of a span
     uint32_t spans;
     uint64_t* slots;   // spans * 2 * (E + 1)
-    int2* leads;       // the sequence of slot 2 i + 1, or -1; the last span that has it
+    // of slot 2 i + 1: its sequence, or -1; the last span that has it; how many parts of its
+    // experts are joined
+    int4* leads;
+    double* dots;      // 4 a span, 16 of the first: sums of counts times mean shares of those parts
 };
 
 __device__ __forceinline__ int64_t inside(const BalanceRows& a, int64_t v) {
@@ -108,10 +117,11 @@ struct Sequences {
     }
 };
 
-// Shares of a row (see above), and for the gradient 1 - sigma of each expert.
+// Shares of a row (see above) times a number: returns that times the factor.  For the gradient
+// also 1 - sigma of each expert.
 template <int LANES, int R, bool SLOPE>
-__device__ __forceinline__ void shares(const float (&x)[R], bool sigmoid, float (&q)[R],
-                                       float (&slope)[R]) {
+__device__ __forceinline__ float shares(const float (&x)[R], bool sigmoid, float (&q)[R],
+                                        float (&slope)[R]) {
     float sum = 0.0f;
     if (sigmoid) {
 #pragma unroll
@@ -122,7 +132,7 @@ __device__ __forceinline__ void shares(const float (&x)[R], bool sigmoid, float 
             sum += q[j];
         }
         sum = group_sum<LANES>(sum);
-        if (__ballot(sum < 0x1p-60f) != 0) {  // only logits far below 0 (or an idle team)
+        if (__ballot(sum < 0x1p-60f) != 0) {  // only logits far below 0
             float m = x[0];
 #pragma unroll
             for (int j = 1; j < R; ++j) m = fmaxf(m, x[j]);
@@ -143,24 +153,50 @@ __device__ __forceinline__ void shares(const float (&x)[R], bool sigmoid, float 
         float m = x[0];
 #pragma unroll
         for (int j = 1; j < R; ++j) m = __builtin_elementwise_maximum(m, x[j]);
-        m = team_maximum<LANES>(m);
+        m = team_maximum<LANES>(m) * kLog2e;  // (its rounding is the same in all)
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            q[j] = exp2_hw((x[j] - m) * kLog2e);
+            q[j] = exp2_hw(__builtin_fmaf(x[j], kLog2e, -m));
             if constexpr (SLOPE) slope[j] = 1.0f;
             sum += q[j];
         }
         sum = group_sum<LANES>(sum);
     }
-    const float r = __builtin_amdgcn_rcpf(sum);
-#pragma unroll
-    for (int j = 0; j < R; ++j) q[j] *= r;
+    return __builtin_amdgcn_rcpf(sum);
 }
 
-// The lane's first index of a row (every lane loads one).
-__device__ __forceinline__ int32_t first_index(const BalanceRows& a, int64_t row, int lane) {
-    return a.idx[row * a.K + (lane < a.K ? lane : 0)];
-}
+// A team's rows as they come from memory, every so many-th of a span: their experts, and the lane's
+// first index (every lane loads one).  Places are counted from the span's first row in 32 bits, and
+// rows behind the last one are that.
+template <typename T, int LANES, int R, int VEC>
+struct TeamRows {
+    RawExperts<T, LANES, R, VEC> raw;
+    int32_t first;
+    const char *x, *idx;           // of the span's first row
+    uint32_t at, at_last, at_step;  // in bytes
+    uint32_t i, i_last, i_step;
+
+    __device__ __forceinline__ void span(const BalanceRows& a, int64_t r0) {
+        x = reinterpret_cast<const char*>(static_cast<const T*>(a.x) + r0 * a.E);
+        idx = reinterpret_cast<const char*>(a.idx + r0 * a.K);
+    }
+    // From row r of the span on, in steps of `step`, to row end - 1.
+    __device__ __forceinline__ void begin(const BalanceRows& a, uint32_t r, uint32_t step,
+                                          uint32_t end, int lane) {
+        const uint32_t xb = (uint32_t)a.E * (uint32_t)sizeof(T), ib = (uint32_t)a.K * 4;
+        r = r < end ? r : end - 1;
+        const uint32_t l = (uint32_t)(lane < a.K ? lane : 0) * 4;
+        at = r * xb, at_last = (end - 1) * xb, at_step = step * xb;
+        i = r * ib + l, i_last = (end - 1) * ib + l, i_step = step * ib;
+        fetch(a, lane);
+    }
+    __device__ __forceinline__ void fetch(const BalanceRows& a, int lane) {
+        raw.load(x, at, a.E, lane);
+        first = *reinterpret_cast<const int32_t*>(idx + i);
+        at = at + at_step < at_last ? at + at_step : at_last;
+        i = i + i_step < i_last ? i + i_step : i_last;
+    }
+};
 
 // Whether one of a row's indices is an expert, for a team that has them LANES at a time, the
 // first ones in `first`.  COUNT: they are counted.
@@ -207,143 +243,181 @@ __device__ __forceinline__ void finish(const BalanceRows& a, int64_t s, const do
     }
 }
 
-// Wavefronts of a span's workgroup: with 16 experts a lane half as many, for their sums in LDS.
-template <int R>
-constexpr int span_waves() { return R > 8 ? 8 : 16; }
-
 template <typename T, int LANES, int R, int VEC, bool FULL>
-__global__ __launch_bounds__(64 * span_waves<R>()) void balance_spans(const BalanceRows a,
-                                                                      const BalanceSpans b) {
-    constexpr int ROWS = 64 / LANES, WAVES = span_waves<R>(), TEAMS = WAVES * ROWS;
+__global__ __launch_bounds__(64 * SPAN_WAVES) void balance_spans(
+    const BalanceRows a, const BalanceSpans b) {
+    constexpr int ROWS = 64 / LANES, WAVES = SPAN_WAVES, TEAMS = WAVES * ROWS;
     constexpr int THREADS = 64 * WAVES;
-    __shared__ float acc[WAVES][LANES * R];
+    __shared__ float acc[WAVES][LANES * R];  // a wavefront's sums; its counts, where it is alone
     __shared__ double sums[LANES * R];
     __shared__ int32_t counts[LANES * R];
     __shared__ int32_t part_rows[WAVES];
     __shared__ double part[WAVES];
-    const int tid = threadIdx.x, lane = tid % LANES, wv = tid >> 6, team = (tid & 63) / LANES;
+    const int tid = threadIdx.x, lane = tid % LANES, team = (tid & 63) / LANES;
+    const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int E = a.E;
-    const T* const x0 = static_cast<const T*>(a.x);
     const int64_t r0 = blockIdx.x * b.rows, r1 = r0 + b.rows < a.N ? r0 + b.rows : a.N;
-    // the first row is on its way before its sequence is known
-    RawExperts<T, LANES, R, VEC> raw, later;
-    int32_t first = -1, then;
-    auto fetch = [&](int64_t row, int64_t end) {
-        const int64_t at = row < end ? row : end - 1;
-        later.load(x0 + at * E, E, lane);
-        then = first_index(a, at, lane);
-    };
-    if (r0 < r1) {
-        fetch(r0 + wv * ROWS + team, r1);
-        raw = later;
-        first = then;
-    }
+    // a row is on its way while the one before is worked on, the first one before its sequence
+    // is known
+    TeamRows<T, LANES, R, VEC> rows;
+    rows.span(a, r0);
+    if (r0 < r1) rows.begin(a, wv * ROWS + team, TEAMS, (uint32_t)(r1 - r0), lane);
     // its sequences: those that end behind r0 (all that end at row 0 are the first span's)
     Sequences seq;
-    int64_t s = 0;
+    int64_t begin = 0;
     if (blockIdx.x == 0) seq.load(a, 0);
-    else s = seq.after(a, r0);
-    int2 lead = {-1, 0};
-    for (; s < a.S; ++s) {
-        int64_t from, to;
-        seq.bounds(a, s, from, to);
-        if (from > r1 || (from == r1 && to > from)) break;
-        const int64_t p0 = from > r0 ? from : r0, p1 = to < r1 ? to : r1;
-        for (int e = tid; e < LANES * R; e += THREADS) counts[e] = 0;
-        if (p0 != r0 && p0 < p1) {
-            fetch(p0 + wv * ROWS + team, p1);
-            raw = later;
-            first = then;
+    else begin = seq.after(a, r0);
+    int4 lead = {-1, 0, 0, 0};
+    bool ahead = true;  // `rows` has the span's first ones
+    // 64 sequences at a time: first those that the workgroup takes together, then the ones of few
+    // rows, within the span and not all of it, that a wavefront takes alone
+    for (bool more = true; more; seq.load(a, seq.base + 64)) {
+        uint64_t todo, few;
+        {
+            const int64_t s = seq.base + (tid & 63), n = seq.to - seq.from;
+            const bool ok = s >= begin && s < a.S &&
+                            (seq.from < r1 || (seq.from == r1 && n == 0));
+            const bool is = ok && n <= 8 * ROWS && n < r1 - r0 && seq.from >= r0 && seq.to <= r1;
+            few = __ballot(is);
+            todo = __ballot(ok) & ~few;
+            more = __ballot(ok) >> 63;
         }
-        __syncthreads();
-        double total[R];
-        float sum[R];
-        int32_t n = 0;
+        for (int phase = 0; phase < 2; ++phase) {
+            const bool alone = phase == 1;
+            // (every so many-th of them is this wavefront's)
+            if (alone) todo = few & 0x0001000100010001ull << wv;
+            for (; todo != 0; todo &= todo - 1) {
+                const int at = __builtin_ctzll(todo);
+                const int64_t s = seq.base + at;
+                const int64_t from = __builtin_amdgcn_readlane(seq.from, at);
+                const int64_t to = __builtin_amdgcn_readlane(seq.to, at);
+                const bool before = from < r0, behind = to > r1;
+                const int64_t p0 = from > r0 ? from : r0, p1 = to < r1 ? to : r1;
+                int32_t* const own = alone ? reinterpret_cast<int32_t*>(acc[wv]) : counts;
+                const int64_t step = alone ? ROWS : TEAMS;
+                int64_t row0 = p0 + (alone ? 0 : wv * ROWS);
+                if ((!ahead || p0 != r0 || p1 != r1 || alone) && p0 < p1)
+                    rows.begin(a, (uint32_t)(row0 + team - r0), (uint32_t)step,
+                               (uint32_t)(p1 - r0), lane);
+                ahead = false;
+                if (alone) {
+                    for (int e = tid & 63; e < LANES * R; e += 64) own[e] = 0;
+                    wave_sync();
+                } else {
+                    for (int e = tid; e < LANES * R; e += THREADS) own[e] = 0;
+                    __syncthreads();
+                }
+                float sum[R];
+                int32_t n = 0;
 #pragma unroll
-        for (int j = 0; j < R; ++j) total[j] = 0.0, sum[j] = 0.0f;
-        int added = 0;
-        // the next row is on its way while one is worked on
-        int64_t row = p0 + wv * ROWS + team;
-        for (int64_t row0 = p0 + wv * ROWS; row0 < p1; row0 += TEAMS) {
-            fetch(row + TEAMS, p1);
-            float x[R], q[R], none[R];
-            raw.template widen<FULL>(x, E, lane);
-            const bool in = takes_part<LANES, true>(a, row, row < p1, lane, team, first, counts);
-            shares<LANES, R, false>(x, a.sigmoid, q, none);
+                for (int j = 0; j < R; ++j) sum[j] = 0.0f;
+                for (; row0 < p1; row0 += step) {
+                    const int64_t row = row0 + team;
+                    const RawExperts<T, LANES, R, VEC> raw = rows.raw;
+                    const int32_t first = rows.first;
+                    rows.fetch(a, lane);
+                    float x[R], q[R], none[R];
+                    raw.template widen<FULL>(x, E, lane);
+                    const bool in =
+                        takes_part<LANES, true>(a, row, row < p1, lane, team, first, own);
+                    float r = shares<LANES, R, false>(x, a.sigmoid, q, none);
+                    if (__ballot(!in) != 0) {  // (its shares may be anything)
+                        r = in ? r : 0.0f;
 #pragma unroll
-            for (int j = 0; j < R; ++j) sum[j] += in ? q[j] : 0.0f;
-            n += in && lane == 0;
-            if (++added == BL_FLUSH) {
-                added = 0;
+                        for (int j = 0; j < R; ++j) q[j] = in ? q[j] : 0.0f;
+                    }
 #pragma unroll
-                for (int j = 0; j < R; ++j) total[j] += (double)sum[j], sum[j] = 0.0f;
+                    for (int j = 0; j < R; ++j) sum[j] = __builtin_fmaf(q[j], r, sum[j]);
+                    n += in && lane == 0;
+                }
+                n = (int32_t)group_sum<64>((float)n);
+#pragma unroll
+                for (int j = 0; j < R; ++j) sum[j] = sum_of_teams<LANES>(sum[j]);
+                if (alone) {
+                    wave_sync();
+                    const double rn = n > 0 ? 1.0 / (double)n : 0.0;
+                    double dot = 0.0;
+#pragma unroll
+                    for (int j = 0; j < R; ++j) {
+                        const int e = expert<LANES, VEC>(lane, j);
+                        if (team != 0 || e >= E) continue;
+                        const double mean = (double)sum[j] * rn;
+                        const int32_t c = own[e];
+                        a.probs[s * E + e] = (float)mean;
+                        a.counts[s * E + e] = c;
+                        dot += (double)c * mean;
+                    }
+                    dot = group_sum<64>(dot);
+                    if ((tid & 63) == 0) {
+                        a.loss[s] = (float)((double)a.scale * E / a.K * rn * dot);
+                        a.rows[s] = n;
+                    }
+                    wave_sync();
+                    continue;
+                }
+                // the teams' sums, wavefront by wavefront
+#pragma unroll
+                for (int j = 0; j < R; ++j)
+                    if (team == 0) acc[wv][expert<LANES, VEC>(lane, j)] = sum[j];
+                if ((tid & 63) == 0) part_rows[wv] = n;
+                __syncthreads();
+                n = 0;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) n += part_rows[w];
+                uint64_t* const slot =
+                    b.slots + ((int64_t)blockIdx.x * 2 + (before ? 0 : 1)) * (E + 1);
+                for (int e = tid; e < E; e += THREADS) {
+                    double v = 0.0;
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) v += (double)acc[w][e];
+                    if (before || behind)
+                        slot[e] = (uint64_t)__float_as_uint((float)v) << 32 | (uint32_t)counts[e];
+                    else
+                        sums[e] = v;
+                }
+                if (before || behind) {
+                    if (tid == 0) slot[E] = (uint32_t)n;
+                    if (!before) lead = int4{(int32_t)s, (int32_t)((to - 1) / b.rows), 0, 0};
+                } else {
+                    __syncthreads();
+                    finish<THREADS>(a, s, sums, counts, n, part);
+                }
+                __syncthreads();
             }
-            row += TEAMS;
-            first = then;
-            raw = later;
         }
-        // the wavefront's teams, then the wavefronts
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const float v = sum_of_teams<LANES>((float)(total[j] + (double)sum[j]));
-            if (team == 0) acc[wv][expert<LANES, VEC>(lane, j)] = v;
-        }
-        n = (int32_t)group_sum<64>((float)n);  // (below 2^24: a wavefront's rows of a span)
-        if ((tid & 63) == 0) part_rows[wv] = n;
-        __syncthreads();
-        n = 0;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) n += part_rows[w];
-        const bool before = from < r0, behind = to > r1;
-        uint64_t* const slot = b.slots + ((int64_t)blockIdx.x * 2 + (before ? 0 : 1)) * (E + 1);
-        for (int e = tid; e < E; e += THREADS) {
-            double v = 0.0;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) v += (double)acc[w][e];
-            if (before || behind)
-                slot[e] = (uint64_t)__float_as_uint((float)v) << 32 | (uint32_t)counts[e];
-            else
-                sums[e] = v;
-        }
-        if (before || behind) {
-            if (tid == 0) slot[E] = (uint32_t)n;
-            if (!before) lead = int2{(int32_t)s, (int32_t)((to - 1) / b.rows)};
-        } else {
-            __syncthreads();
-            finish<THREADS>(a, s, sums, counts, n, part);
-        }
-        __syncthreads();
-        if (behind) break;
+        if (more) __syncthreads();
     }
     if (tid == 0 && b.spans > 1) b.leads[blockIdx.x] = lead;
 }
 
-// Sequences that more than one span has: workgroup i joins the one that begins in span i.  Each
-// wavefront takes every so many-th slot, COLS experts a lane, several slots in flight.
-template <int COLS>
-constexpr int join_waves() { return COLS > 8 ? 8 : 16; }
+// Sequences that more than one span has: workgroup (i, part) joins 64 COLS experts of the one that
+// begins in span i.  Each wavefront takes every so many-th slot, COLS experts a lane, eight slots
+// in flight.  The last part of a sequence to arrive has its loss.  All rows as one sequence are
+// joined 64 experts a workgroup (65536 x 256: 17.8 us, with one workgroup 22.0); of others a
+// workgroup takes 256, so that few are launched in vain (in 24 sequences 17.8 us, with four
+// workgroups a span 22.4).
+constexpr int JOIN_COLS = 4;  // at most
 
 template <int COLS>
-__global__ __launch_bounds__(64 * join_waves<COLS>()) void balance_join(const BalanceRows a,
-                                                        const BalanceSpans b) {
-    constexpr int WAVES = join_waves<COLS>(), DEEP = COLS > 4 ? 32 / COLS : 8;
-    __shared__ double stripe[WAVES][64 * COLS];
-    __shared__ int32_t stripe_counts[WAVES][64 * COLS];
-    __shared__ double sums[64 * COLS];
-    __shared__ int32_t counts[64 * COLS];
-    __shared__ double part[WAVES];
+__global__ __launch_bounds__(1024) void balance_join(const BalanceRows a, const BalanceSpans b) {
+    constexpr int WAVES = 16, DEEP = 8, WIDE = 64 * COLS;
+    __shared__ double stripe[WAVES][WIDE];
+    __shared__ int32_t stripe_counts[WAVES][WIDE];
     __shared__ int32_t rows[WAVES];
-    const int2 lead = b.leads[blockIdx.x];
+    __shared__ double dots[WAVES];
+    const int4 lead = b.leads[blockIdx.x];
     if (lead.x < 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, E = a.E;
+    const int e0 = (int)blockIdx.y * WIDE;
     // slots: the second one of this span, the first ones of the following
     const int64_t i0 = blockIdx.x;
-    const int last = lead.y < (int)b.spans ? lead.y - (int)i0 : (int)b.spans - 1 - (int)i0;
+    const int last = (lead.y < (int)b.spans ? lead.y : (int)b.spans - 1) - (int)i0;
     auto slot = [&](int j) { return b.slots + (j == 0 ? i0 * 2 + 1 : (i0 + j) * 2) * (E + 1); };
     double v[COLS];
     int32_t c[COLS], n = 0;
 #pragma unroll
     for (int k = 0; k < COLS; ++k) v[k] = 0.0, c[k] = 0;
+    for (int j = tid; j <= last; j += 64 * WAVES) n += (int32_t)(uint32_t)slot(j)[E];
     for (int j0 = wv; j0 <= last; j0 += WAVES * DEEP) {
         uint64_t w[DEEP][COLS];
 #pragma unroll
@@ -351,7 +425,7 @@ __global__ __launch_bounds__(64 * join_waves<COLS>()) void balance_join(const Ba
             const int j = j0 + d * WAVES;
 #pragma unroll
             for (int k = 0; k < COLS; ++k) {
-                const int e = lane + 64 * k;
+                const int e = e0 + lane + 64 * k;
                 w[d][k] = j <= last && e < E ? slot(j)[e] : 0;
             }
         }
@@ -364,7 +438,6 @@ __global__ __launch_bounds__(64 * join_waves<COLS>()) void balance_join(const Ba
             }
         }
     }
-    for (int j = tid; j <= last; j += 64 * WAVES) n += (int32_t)(uint32_t)slot(j)[E];
     for (int d = 1; d < 64; d *= 2) n += __shfl_xor(n, d);
     if (lane == 0) rows[wv] = n;
 #pragma unroll
@@ -375,18 +448,43 @@ __global__ __launch_bounds__(64 * join_waves<COLS>()) void balance_join(const Ba
     __syncthreads();
     n = 0;
     for (int w = 0; w < WAVES; ++w) n += rows[w];
-    for (int e = tid; e < 64 * COLS; e += 64 * WAVES) {
+    const int64_t s = lead.x;
+    const double rn = n > 0 ? 1.0 / (double)n : 0.0;
+    double dot = 0.0;
+    if (tid < WIDE && e0 + tid < E) {
         double t = 0.0;
         int32_t m = 0;
         for (int w = 0; w < WAVES; ++w) {
-            t += stripe[w][e];
-            m += stripe_counts[w][e];
+            t += stripe[w][tid];
+            m += stripe_counts[w][tid];
         }
-        sums[e] = t;
-        counts[e] = m;
+        t *= rn;
+        a.probs[s * E + e0 + tid] = (float)t;
+        a.counts[s * E + e0 + tid] = m;
+        dot = (double)m * t;
     }
+    dot = group_sum<64>(dot);
+    if (lane == 0) dots[wv] = dot;
     __syncthreads();
-    finish<64 * WAVES>(a, lead.x, sums, counts, n, part);
+    if (tid != 0) return;
+    dot = 0.0;
+    for (int w = 0; w < COLS; ++w) dot += dots[w];
+    const int parts = gridDim.y;
+    if (parts > 1) {
+        uint64_t* const at = reinterpret_cast<uint64_t*>(b.dots + i0 * 4);
+        __hip_atomic_store(at + blockIdx.y, __builtin_bit_cast(uint64_t, dot), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        const int32_t arrived = __hip_atomic_fetch_add(&b.leads[i0].z, 1, __ATOMIC_RELAXED,
+                                                       __HIP_MEMORY_SCOPE_AGENT);
+        if (arrived != parts - 1) return;
+        dot = 0.0;
+        for (int i = 0; i < parts; ++i)
+            dot += __builtin_bit_cast(double, __hip_atomic_load(at + i, __ATOMIC_RELAXED,
+                                                                __HIP_MEMORY_SCOPE_AGENT));
+    }
+    a.loss[s] = (float)((double)a.scale * E / a.K * rn * dot);
+    a.rows[s] = n;
 }
 
 template <typename T, int LANES, int R, int VEC, bool FULL>
@@ -394,21 +492,13 @@ __global__ __launch_bounds__(BL_BLOCK) void balance_grad(const BalanceRows a, in
     constexpr int ROWS = 64 / LANES, TEAMS = BL_WAVES * ROWS;
     const int tid = threadIdx.x, lane = tid % LANES, wv = tid >> 6, team = (tid & 63) / LANES;
     const int E = a.E;
-    const T* const x0 = static_cast<const T*>(a.x);
     const int64_t r0 = blockIdx.x * span, r1 = r0 + span < a.N ? r0 + span : a.N;
     // a row is on its way while the one before is worked on, the first one while its sequence
     // is looked for
-    RawExperts<T, LANES, R, VEC> raw, later;
-    int32_t first, then;
-    auto fetch = [&](int64_t row) {
-        const int64_t at = row < r1 ? row : r1 - 1;
-        later.load(x0 + at * E, E, lane);
-        then = first_index(a, at, lane);
-    };
+    TeamRows<T, LANES, R, VEC> rows;
+    rows.span(a, r0);
+    rows.begin(a, wv * ROWS + team, TEAMS, (uint32_t)(r1 - r0), lane);
     int64_t row = r0 + wv * ROWS + team;
-    fetch(row);
-    raw = later;
-    first = then;
     // the sequence of this lane's row: none from s_end on
     int64_t s = 0, s_from = INT64_MAX, s_end = INT64_MAX;
     float c[R], f = 0.0f;
@@ -434,7 +524,9 @@ __global__ __launch_bounds__(BL_BLOCK) void balance_grad(const BalanceRows a, in
         }
     }
     for (int64_t row0 = r0 + wv * ROWS; row0 < r1; row0 += TEAMS) {
-        fetch(row + TEAMS);
+        const RawExperts<T, LANES, R, VEC> raw = rows.raw;
+        const int32_t first = rows.first;
+        rows.fetch(a, lane);
         const bool live = row < r1;
         float x[R], q[R], slope[R];
         raw.template widen<FULL>(x, E, lane);
@@ -449,37 +541,46 @@ __global__ __launch_bounds__(BL_BLOCK) void balance_grad(const BalanceRows a, in
             }
         }
         const bool part = in && row >= s_from;
-        shares<LANES, R, true>(x, a.sigmoid, q, slope);
+        const float r = shares<LANES, R, true>(x, a.sigmoid, q, slope);
         float dot = 0.0f;
 #pragma unroll
         for (int j = 0; j < R; ++j) dot = __builtin_fmaf(c[j], q[j], dot);
-        dot = group_sum<LANES>(dot);
+        dot = group_sum<LANES>(dot) * r;
         float d[R];
+        const float k = r * f;
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            const float v = f * q[j] * (c[j] - dot);
-            d[j] = part ? (a.sigmoid ? v * slope[j] : v) : 0.0f;
+            d[j] = q[j] * k * (c[j] - dot);
+            if (a.sigmoid) d[j] *= slope[j];
+        }
+        if (__ballot(!part) != 0) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) d[j] = part ? d[j] : 0.0f;
         }
         if (live) store_experts<T, LANES, R, VEC>(static_cast<T*>(a.dx) + row * E, E, lane, d);
         row += TEAMS;
-        first = then;
-        raw = later;
     }
 }
 
-// Lanes of a row: eight experts a lane or few more.
+// Lanes of a row: 8 experts a lane, in at least 8 and at most 64 lanes (16 experts a lane are not
+// faster at any size tried).
 static int balance_lanes(int E) {
     int lanes = 8;
     while (lanes < 64 && lanes * 8 < E) lanes *= 2;
     return lanes;
 }
 
-// Rows of a span: one workgroup a CU, and at least four rows a team.
+// Rows of a span: one for all where a team has at most four, else a workgroup a CU, or for every
+// second one where a team would have less than four (one workgroup joins a sequence, and for longer
+// the more spans it has: 16384 x 256 in 128 of them 14.9 us, in 256 17.6), and at most BL_ADDED a
+// team.
 static int64_t balance_span(int64_t N, int E, int cus) {
-    const int lanes = balance_lanes(E);
-    const int64_t teams = (lanes == 64 && E > 512 ? 8 : 16) * (64 / lanes);
-    const int64_t rows = ((N + cus - 1) / cus + teams - 1) / teams * teams;
-    return rows < 4 * teams ? 4 * teams : rows;
+    const int64_t teams = SPAN_WAVES * (64 / balance_lanes(E));
+    if (N <= 4 * teams) return 4 * teams;
+    auto of = [&](int64_t spans) { return ((N + spans - 1) / spans + teams - 1) / teams * teams; };
+    int64_t rows = of(cus);
+    if (rows < 4 * teams) rows = of(cus / 2 + 1) < 4 * teams ? of(cus / 2 + 1) : 4 * teams;
+    return rows < BL_ADDED * teams ? rows : BL_ADDED * teams;
 }
 
 static uint32_t balance_spans_of(int64_t N, int64_t rows) {
@@ -490,10 +591,11 @@ static size_t slots_bytes(size_t spans, size_t E) {
     return (spans * 2 * (E + 1) * 8 + 255) / 256 * 256;
 }
 
-size_t balance_scratch_bytes(int64_t N, int64_t E, int64_t S, int cus) {
-    (void)S;
+size_t balance_scratch_bytes(int64_t N, int64_t E, int cus) {
     const size_t spans = balance_spans_of(N, balance_span(N, (int)E, cus));
-    return spans > 1 ? slots_bytes(spans, (size_t)E) + spans * sizeof(int2) : 0;
+    return spans > 1 ? slots_bytes(spans, (size_t)E) + spans * (sizeof(int4) + 4 * sizeof(double)) +
+                           12 * sizeof(double)
+                     : 0;
 }
 
 // Teams of LANES lanes with R experts each, VEC neighbours at a time: f is called with them as
@@ -503,15 +605,17 @@ static void with_team(int E, F f) {
     constexpr int VEC = VEC4 ? 4 : 1;
     auto r = [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
-        const int each = (E + L - 1) / L;
         auto call = [&](auto n) { f(lanes, n, std::integral_constant<int, VEC>{}); };
-        if constexpr (VEC == 1) {
-            if (each <= 1) return call(std::integral_constant<int, 1>{});
-            if (each <= 2) return call(std::integral_constant<int, 2>{});
+        if constexpr (L == 8) {
+            if constexpr (VEC == 1) {
+                if (E <= 8) return call(std::integral_constant<int, 1>{});
+                if (E <= 16) return call(std::integral_constant<int, 2>{});
+            }
+            if (E <= 32) return call(std::integral_constant<int, 4>{});
         }
-        if (each <= 4) return call(std::integral_constant<int, 4>{});
-        if (L < 64 || each <= 8) return call(std::integral_constant<int, 8>{});
-        if constexpr (L == 64) call(std::integral_constant<int, 16>{});
+        if constexpr (L == 64)
+            if (E > 512) return call(std::integral_constant<int, 16>{});
+        call(std::integral_constant<int, 8>{});
     };
     switch (balance_lanes(E)) {
         case 8: return r(std::integral_constant<int, 8>{});
@@ -533,12 +637,13 @@ static hipError_t launch_balance_fwd_t(const BalanceRows& a, void* scratch, hipS
     b.rows = balance_span(a.N, a.E, a.cus);
     b.spans = balance_spans_of(a.N, b.rows);
     b.slots = static_cast<uint64_t*>(scratch);
-    b.leads = reinterpret_cast<int2*>(static_cast<char*>(scratch) +
+    b.leads = reinterpret_cast<int4*>(static_cast<char*>(scratch) +
                                       slots_bytes(b.spans, (size_t)a.E));
+    b.dots = reinterpret_cast<double*>(b.leads + b.spans);
     auto go = [&](auto lanes, auto r, auto vec) {
         constexpr int R = decltype(r)::value;
         constexpr int L = decltype(lanes)::value, V = decltype(vec)::value;
-        const dim3 grid(b.spans), block(64 * span_waves<R>());
+        const dim3 grid(b.spans), block(64 * SPAN_WAVES);
         if (a.E == L * R)
             hipLaunchKernelGGL((balance_spans<T, L, R, V, true>), grid, block, 0, st, a, b);
         else
@@ -548,13 +653,13 @@ static hipError_t launch_balance_fwd_t(const BalanceRows& a, void* scratch, hipS
     else with_team<false>(a.E, go);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || b.spans == 1) return e;
-#define OSM_JOIN(C) hipLaunchKernelGGL((balance_join<C>), dim3(b.spans), dim3(64 * join_waves<C>()), 0, st, a, \
-                                       b)
-    if (a.E <= 64) OSM_JOIN(1);
-    else if (a.E <= 128) OSM_JOIN(2);
-    else if (a.E <= 256) OSM_JOIN(4);
-    else if (a.E <= 512) OSM_JOIN(8);
-    else OSM_JOIN(16);
+    const int cols = (a.E + 63) / 64;
+#define OSM_JOIN(C)                                                                         \
+    hipLaunchKernelGGL((balance_join<C>), dim3(a.starts ? b.spans : 1, (cols + C - 1) / C), \
+                       dim3(1024), 0, st, a, b)
+    if (cols <= 1 || !a.starts) OSM_JOIN(1);
+    else if (cols <= 2) OSM_JOIN(2);
+    else OSM_JOIN(JOIN_COLS);
 #undef OSM_JOIN
     return hipGetLastError();
 }
@@ -564,7 +669,8 @@ static hipError_t launch_balance_bwd_t(const BalanceRows& a, hipStream_t st) {
     const int64_t teams = BL_BLOCK / balance_lanes(a.E);
     const int64_t want = (a.N + teams - 1) / teams, most = 8 * (int64_t)a.cus;
     const int64_t blocks = want < most ? want : most;
-    const int64_t span = (a.N + blocks - 1) / blocks;
+    int64_t span = (a.N + blocks - 1) / blocks;
+    if (span > 1 << 16) span = 1 << 16;  // (places within it in 32 bits)
     auto go = [&](auto lanes, auto r, auto vec) {
         constexpr int L = decltype(lanes)::value, R = decltype(r)::value, V = decltype(vec)::value;
         const dim3 grid((unsigned)((a.N + span - 1) / span)), block(BL_BLOCK);

@@ -56,11 +56,13 @@ struct RawExperts {
     using V = std::conditional_t<VEC == 4, V4, V1>;
     V q[N];
 
-    __device__ __forceinline__ void load(const T* xr, int E, int lane) {
+    // at: the row's place behind `base`, in bytes.
+    __device__ __forceinline__ void load(const char* base, uint32_t at, int E, int lane) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int e = expert<LANES, VEC>(lane, i * VEC);
-            q[i] = *reinterpret_cast<const V*>(xr + (e < E ? e : 0));
+            q[i] = *reinterpret_cast<const V*>(base + (at + (uint32_t)(e < E ? e : 0) *
+                                                                (uint32_t)sizeof(T)));
         }
     }
     // FULL: there is an expert in every place.
@@ -92,8 +94,8 @@ template <int LANES>
 __device__ __forceinline__ float sum_of_teams(float v) {
     float a, b;
     if constexpr (LANES <= 8)  // a rotation by 8 within 16 lanes
-        v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x128,
-                                                                   0xF, 0xF, false));
+        v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(
+            0, (int)__float_as_uint(v), 0x128, 0xF, 0xF, false));
     if constexpr (LANES <= 16) {
         bfly_operands<4>(v, a, b);
         v = a + b;

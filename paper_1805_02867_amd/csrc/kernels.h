@@ -226,7 +226,7 @@ struct BalanceRows {
     float scale;
     int cus;
 };
-size_t balance_scratch_bytes(int64_t N, int64_t E, int64_t S, int cus);
+size_t balance_scratch_bytes(int64_t N, int64_t E, int cus);
 hipError_t launch_balance_fwd(const BalanceRows& a, int dtype, void* scratch, hipStream_t st);
 hipError_t launch_balance_bwd(const BalanceRows& a, int dtype, hipStream_t st);
 

@@ -39,7 +39,8 @@ __device__ __forceinline__ LogState log_merge(LogState a, LogState b, float c) {
     // (empty states are infinitely far: a bound keeps 0 times it 0)
     const float fall = __builtin_fminf((hi.m - lo.m) * c, 0x1p60f);
     const float r = exp2_hw(-fall), d = lo.s + 1.0f;
-    return {hi.m, __builtin_fmaf(d, r, hi.s), __builtin_fmaf(__builtin_fmaf(fall, d, lo.w), r, hi.w)};
+    return {hi.m, __builtin_fmaf(d, r, hi.s),
+            __builtin_fmaf(__builtin_fmaf(fall, d, lo.w), r, hi.w)};
 }
 
 template <int STEP>
@@ -228,7 +229,8 @@ constexpr int log_waves() {
 // row0 + b / S) of at most 64 W R whole 16-byte vectors, W wavefronts each (W = 1: four rows a
 // workgroup).  SEL: with alternatives, selected as topk_held.hpp does.  ENT: with w.
 template <typename T, int W, int R, bool SEL, bool ENT, bool PART>
-__global__ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (log_waves<T, W, R, SEL, PART>())) void logprob_held(
+__global__
+__launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (log_waves<T, W, R, SEL, PART>())) void logprob_held(
     const LogprobRows a, const LogprobSplit p) {
     static_assert(!PART || W > 1, "chunks take a workgroup each");
     constexpr int E = Vec<T>::N, TR = 64 * W;
@@ -269,8 +271,8 @@ __global__ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (log_waves<T, W, R, SEL
     if (wv == 0 || W == 1) tok.element(a, xr, lane);
 
     // 1. maxima by vector, and the wavefront's.  bfloat16 ones by two elements at a time as
-    // integers, which order numbers that are not negative: where the wavefront has one, and only the
-    // largest is asked for, that is all.
+    // integers, which order numbers that are not negative: where the wavefront has one, and only
+    // the largest is asked for, that is all.
     float vm[R], lm = __builtin_fmaxf(ex, ninf), wm;  // a NaN element gives -inf
     constexpr bool FAST = E == 8 && !SEL;
     if constexpr (FAST) {

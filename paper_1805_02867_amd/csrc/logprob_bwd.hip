@@ -199,10 +199,10 @@ hipError_t launch_logprob_bwd(const LogprobGrad& a, int dtype, hipStream_t st) {
 // x 65536 f x2 9.9, x1 10.5; 16 x 65536 f x4 6.9); eight rows and fewer into up to 64 of at
 // least 512 vectors (1 x 128256 f held 4 x32 5.2, x16 5.7; 1 x 50257 f x32 4.9, x8 5.5).
 //
-// With alternatives (5 of them) rows are always held: by eight wavefronts from 2048 vectors on (16 x
-// 16000 f held 8 7.2, held 4 7.5; but 4096 x 16000 f 50.9 / 47.1), beyond 8192 vectors in chunks that
-// four hold (1024 x 128256 f x8 99, x4 by eight 125; 4096 x 128256 b x4 215, x2 262), and in
-// chunks of about 2048 where rows are few (64 x 128256 b x8 14.6, x4 15.0).
+// With alternatives (5 of them) rows are always held: by eight wavefronts from 2048 vectors on
+// (16 x 16000 f held 8 7.2, held 4 7.5; but 4096 x 16000 f 50.9 / 47.1), beyond 8192 vectors in
+// chunks that four hold (1024 x 128256 f x8 99, x4 by eight 125; 4096 x 128256 b x4 215, x2 262),
+// and in chunks of about 2048 where rows are few (64 x 128256 b x8 14.6, x4 15.0).
 LogprobPlan logprob_plan(int64_t N, int64_t V, int K, int dtype, int cus) {
     const int64_t E = dtype == 1 ? 8 : 4, c = cus;
     const int64_t nv = (V + E - 1) / E;

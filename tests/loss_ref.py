@@ -121,7 +121,9 @@ def shares(X, score):
     t = np.where(np.isfinite(z), z, 0.0) * LOG2E
     # an exponential; for the sigmoid another one, an addition and a reciprocal; the sum of at
     # most 16 a lane and 6 steps, its reciprocal, the product
-    one = power(t) + (power(np.where(np.isfinite(X), X, 0.0) * LOG2E) + 4 * U) * (score != "softmax")
+    one = power(t)
+    if score != "softmax":
+        one = one + power(np.where(np.isfinite(X), X, 0.0) * LOG2E) + 4 * U
     err = one + (q * one).sum(axis=1, keepdims=True) + 28 * U
     return q, slope, err
 
@@ -154,7 +156,8 @@ def balance(X, idx, starts=None, score="softmax", scale=1.0):
         q, _, err = shares(X[a:b][took], score)
         P = q.sum(axis=0) / n
         r["probs"][i] = P
-        r["probs_err"][i] = (q * err).sum(axis=0) / n + U * P
+        # (up to 64 rows are added in binary32, and the sums of a wavefront's teams)
+        r["probs_err"][i] = (q * err).sum(axis=0) / n + (64 + 3 + 2) * U * P
         f = scale * E / (K * n)
         r["loss"][i] = f * (r["counts"][i] * P).sum()
         r["loss_err"][i] = (abs(f) * (r["counts"][i] * r["probs_err"][i]).sum() +

@@ -56,8 +56,8 @@ def check(x, idx, starts=None, score="softmax", scale=1.0, dtype="f32", seed=0, 
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("E", [1, 2, 7, 8, 9, 32, 60, 64, 65, 128, 130, 160, 256, 384, 511, 512, 513,
-                               1000, 1024])
+@pytest.mark.parametrize("E", [1, 2, 7, 8, 9, 32, 60, 64, 65, 128, 130, 160, 256, 384, 511, 512,
+                               513, 1000, 1024])
 def test_experts(E, dtype, dev):
     print(f"experts {dtype} {E}", flush=True)
     for N, K, lengths in ((1, 1, None), (37, 3, None), (500, 5, [100, 0, 1, 250, 100]),
@@ -92,6 +92,22 @@ def test_sequences(score, dev):
         x, idx = logits(N, E, "f32", E, dev, sigma=1.0), places(N, E, 2, 3, dev)
         _, dx = check(x, idx, offsets(lengths, dev, first), score)
         assert not dx[:first].any() and not dx[first + sum(lengths):].any()
+
+
+@pytest.mark.parametrize("E", [8, 64, 65, 128, 130, 256, 300, 512, 513, 1024])
+def test_sequences_of_many_spans(E, dev):
+    """All rows as one sequence, one that begins late, two; the same every time, also with scratch
+    memory that held something else."""
+    N = 9000 if E <= 64 else 5000
+    x, idx = logits(N, E, "bf16", E, dev), places(N, E, 3, 4, dev)
+    for lengths, first in ((None, 0), ([N - 8], 8), ([N - 100], 0), ([N // 2, N // 3], N // 6)):
+        starts = None if lengths is None else offsets(lengths, dev, first)
+        r, _ = check(x, idx, starts, "sigmoid", dtype="bf16", what=str(lengths))
+        n = osm.balance_workspace(N, E, 1 if lengths is None else len(lengths))
+        for fill in (0, 255):
+            ws = torch.full((n,), fill, dtype=torch.uint8, device=dev)
+            again = osm.balance_fwd(x, idx, starts, "sigmoid", workspace=ws)
+            assert all(torch.equal(a, b) for a, b in zip(r, again))
 
 
 def test_every_place_of_a_border(dev):
@@ -212,7 +228,8 @@ def test_refused(dev):
     r = osm.balance_fwd(x, idx, starts)
     g = torch.ones(2, device=dev)
     for call in (lambda: osm.balance_fwd(x, idx.long()), lambda: osm.balance_fwd(x, idx[:7]),
-                 lambda: osm.balance_fwd(x.t(), idx), lambda: osm.balance_fwd(x, idx, starts.long()),
+                 lambda: osm.balance_fwd(x.t(), idx),
+                 lambda: osm.balance_fwd(x, idx, starts.long()),
                  lambda: osm.balance_fwd(x, idx, starts[:1]),
                  lambda: osm.balance_fwd(x, idx, score="tanh"),
                  lambda: osm.balance_fwd(x, idx, score=1 << 32),

@@ -68,7 +68,8 @@ def check_bwd(x, tokens, dlogp, dentropy=None, temperature=1.0, dtype="f32", dx=
                           dentropy, temperature=temperature, dx=dx)
     N = x.shape[0]
     t = None if tokens is None else tokens.cpu().numpy().reshape(N, -1)
-    want, err = loss_ref.logprob_bwd(host(x), t, None if dlogp is None else host(dlogp).reshape(N, -1),
+    g = None if dlogp is None else host(dlogp).reshape(N, -1)
+    want, err = loss_ref.logprob_bwd(host(x), t, g,
                                      None if dentropy is None else host(dentropy), temperature,
                                      dtype)
     loss_ref.check(host(got), want, err, f"{what} {tuple(x.shape)}")
@@ -110,6 +111,74 @@ def test_batches(N, V, dtype, dev):
             assert np.array_equal(got.top_idx[at].cpu().numpy(), want["top_idx"])
         again = osm.logprob_fwd(x, tok, K=K, entropy=True, stats=True)
         assert all(torch.equal(a, b) for a, b in zip(got, again) if a is not None)
+
+
+@pytest.mark.filterwarnings("ignore:invalid value")     # of the reference, on purpose
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,nv,offset", [(16, 2049, 0), (16, 3001, 1), (16, 20011, 0),
+                                         (16, 33000, 3), (400, 2500, 0), (300, 8200, 1)])
+def test_long_rows_of_every_kind(N, nv, offset, dtype, dev):
+    """Rows that do not fit into registers, whole and in chunks, by nv 16-byte vectors: masked ones,
+    ties, sure tokens, logits far from 0, rows that are no numbers; and their gradients."""
+    V = nv * (4 if dtype == "f32" else 8) - 2
+    print(f"long rows {dtype} {N} {V}", flush=True)
+    x = logits(16, V, "f32", V, dev)
+    at = torch.randint(0, V, (16,), generator=torch.Generator().manual_seed(nv)).to(dev)
+    x[0] = -INF
+    x[1] = -INF
+    x[1, at[1]] = -3.0
+    x[2, : at[2]] = -INF
+    x[3, torch.arange(V, device=dev) % 97 != 5] = -INF
+    x[4] = torch.finfo(DT[dtype]).min / 4
+    x[4, at[4]] = 0.0
+    x[5, at[5]] = NAN
+    x[6, at[6]] = INF
+    x[7] = 1.5
+    x[8, ::3] = 9.0
+    for r, up in ((9, 20.0), (10, 45.0)):
+        x[r, at[r]] = x[r].max() + up
+    x[11] += 1e4
+    x[12] = x[12] * 1e5 - 1e7
+    x[13, V - 1] = 12.0
+    x[14, 0] = 12.0
+    tok = some_tokens(16, V, 3, V, dev)
+    tok[:, 1] = at.int()
+    ld = V + (3 if offset else 2)
+    rows = torch.arange(N, device=dev) % 16
+    each = rows.cpu().numpy()
+    buf = torch.zeros(N * ld + offset, dtype=DT[dtype], device=dev)
+    y = buf[offset:].view(N, ld)[:, :V]
+    y.copy_(x[rows])
+    got = osm.logprob_fwd(y, tok[rows], entropy=True, stats=True, temperature=0.8)
+    first = y[:16].contiguous()
+    want = loss_ref.logprob(host(first), tok.cpu().numpy(), 0, 0.8)
+    for name in ("logp", "entropy", "stats"):
+        loss_ref.check(host(getattr(got, name)), want[name][each], want[name + "_err"][each], name)
+    only = osm.logprob_fwd(y, tok[rows], temperature=0.8)
+    loss_ref.check(host(only.logp), want["logp"][each], want["logp_err"][each], "logp alone")
+    g = torch.Generator().manual_seed(nv)
+    dlogp, dent = torch.randn(16, 3, generator=g).to(dev), torch.randn(16, generator=g).to(dev)
+    dx = osm.logprob_bwd(y, got.stats, tok[rows], dlogp[rows], got.entropy, dent[rows],
+                         temperature=0.8)
+    d, err = loss_ref.logprob_bwd(host(first), tok.cpu().numpy(), host(dlogp), host(dent), 0.8,
+                                  dtype)
+    loss_ref.check(host(dx), d[each], err[each], "gradient")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,nv", [(12, 1900), (12, 2100), (12, 8190), (12, 8300), (300, 2500)])
+def test_alternatives_of_long_rows(N, nv, dtype, dev):
+    """With alternatives rows are held: by four wavefronts, by eight, in chunks."""
+    V = nv * (4 if dtype == "f32" else 8) - 1
+    print(f"alternatives {dtype} {N} {V}", flush=True)
+    x = logits(N, V, dtype, V, dev)
+    x[1, : V // 2] = -INF
+    x[2] = 1.5
+    x[3] = -INF
+    x[3, V - 1] = 2.0
+    x[4, ::5] = 9.0
+    for K in (5, 40):
+        check_fwd(x, some_tokens(N, V, 3, V, dev), K, what=dtype)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -308,7 +377,8 @@ def test_empty_and_refused(dev):
     for call in (lambda: osm.logprob_fwd(x), lambda: osm.logprob_fwd(x, tok, K=51),
                  lambda: osm.logprob_fwd(x, tok, temperature=0.0),
                  lambda: osm.logprob_fwd(x, torch.zeros(4, 65, dtype=torch.int32, device=dev)),
-                 lambda: osm.logprob_bwd(x, stats), lambda: osm.logprob_bwd(x, stats, tok, g, dx=x)):
+                 lambda: osm.logprob_bwd(x, stats),
+                 lambda: osm.logprob_bwd(x, stats, tok, g, dx=x)):
         with pytest.raises(osm.OsmError) as e:
             call()
         assert e.value.status == osm.EINVAL

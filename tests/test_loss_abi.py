@@ -28,7 +28,8 @@ def _fwd(x=X, ld=10, p=None, N=4, V=10, dtype=0, **kw):
 @pytest.mark.parametrize("bad", [
     dict(N=-1), dict(N=1 << 31), dict(V=0, ld=1), dict(V=1 << 31, ld=1 << 31), dict(ld=9),
     dict(ld=1 << 31), dict(dtype=2), dict(dtype=-1), dict(x=0), dict(tokens=0), dict(logp=0),
-    dict(top=0), dict(idx=0), dict(T=-1), dict(T=65), dict(K=-1), dict(K=11), dict(K=65, V=100, ld=100),
+    dict(top=0), dict(idx=0), dict(T=-1), dict(T=65), dict(K=-1), dict(K=11),
+    dict(K=65, V=100, ld=100),
     dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=INF), dict(temperature=NAN),
     dict(temperature=1e-45),
     dict(x=X + 2), dict(tokens=T_ + 1), dict(logp=L + 2), dict(entropy=H + 3), dict(stats=S_ + 1),
@@ -105,8 +106,8 @@ def test_balance_bwd_refuses(bad):
 
 def test_balance_refuses_bad_workspaces():
     for ws in (W + 128, X, H):
-        assert osm.lib().balance_fwd_ws(X, I_, T_, L, H, V_, S_, 4, 10, 2, 3, 0, 0, 1.0, ws, 1 << 20,
-                                        None) == osm.EINVAL
+        assert osm.lib().balance_fwd_ws(X, I_, T_, L, H, V_, S_, 4, 10, 2, 3, 0, 0, 1.0, ws,
+                                        1 << 20, None) == osm.EINVAL
 
 
 def test_empty_batches_are_noops():
@@ -137,7 +138,11 @@ def test_workspace_sizes():
     assert size(4, 10, 0, ctypes.byref(n)) == osm.EINVAL
     assert size(-1, 10, 1, ctypes.byref(n)) == osm.EINVAL
     assert size(4, 10, 1, None) == osm.EINVAL
-    assert osm.balance_workspace(0, 8) == 0 and 0 < osm.balance_workspace(1 << 24, 256, 9) < 1 << 24
+    assert osm.balance_workspace(0, 8) == 0
+    # at most 64 rows a team, 32 teams a workgroup: of each two slots of E + 1 words of 8 bytes
+    spans = (1 << 24) // (64 * 32)
+    most = spans * (2 * 257 * 8 + 64) + 512
+    assert 0 < osm.balance_workspace(1 << 24, 256, 9) <= most
 
 
 def test_constants_match_the_header():
