@@ -134,10 +134,15 @@ struct LogToken {
     }
 };
 
-// A row's outputs by one wavefront, from its state, lane l's token and (SEL) l-th key.
-template <bool SEL>
-__device__ __forceinline__ void log_store(const LogprobRows& a, int64_t row, LogState v,
-                                          LogToken t, uint64_t key) {
+// What a row's alternatives need of its state.
+struct LogEnd {
+    double m, ln_d;
+    bool good;
+};
+
+// A row's outputs but for the alternatives, by one wavefront, from its state and lane l's token.
+__device__ __forceinline__ LogEnd log_store(const LogprobRows& a, int64_t row, LogState v,
+                                            LogToken t) {
     const int lane = threadIdx.x & 63;
     const bool good = __builtin_fabsf(v.m) < __builtin_inff() && v.s == v.s;
     const float nan = __builtin_nanf("");
@@ -156,19 +161,25 @@ __device__ __forceinline__ void log_store(const LogprobRows& a, int64_t row, Log
             a.stats[row * 2 + 1] = good ? v.s : nan;
         }
     }
-    if constexpr (SEL) {
-        if (lane < a.K) {
-            const float lp = (float)(((double)key_value(key) - m) * a.inverse - ln_d);
-            a.top_vals[row * a.K + lane] = good ? lp : nan;
-            a.top_idx[row * a.K + lane] = good ? key_index(key) : -1;
-        }
-    }
+    return {m, ln_d, good};
+}
+
+// Lane l has the l-th alternative.
+__device__ __forceinline__ void log_store_top(const LogprobRows& a, int64_t row, LogEnd v,
+                                              uint64_t key) {
+    const int lane = threadIdx.x & 63;
+    if (lane >= a.K) return;
+    const float lp = (float)(((double)key_value(key) - v.m) * a.inverse - v.ln_d);
+    a.top_vals[row * a.K + lane] = v.good ? lp : __builtin_nanf("");
+    a.top_idx[row * a.K + lane] = v.good ? key_index(key) : -1;
 }
 
 // LDS of a workgroup.
 template <int W, bool SEL>
 struct LogSmem {
     LogState state[W];
+    LogEnd end;
+    bool last;
     HeldSmem<W> top;
 };
 template <int W>
@@ -217,6 +228,68 @@ __device__ __forceinline__ LogState log_join(const LogprobSplit& p, uint32_t in_
     return v;
 }
 
+// The end of a workgroup's row or (PART) chunk: its wavefronts' states and (SEL) lists are in
+// LDS.  The chunk that completes a row merges it.
+template <typename T, int W, bool SEL, bool PART>
+__device__ __forceinline__ void log_end(const LogprobRows& a, const LogprobSplit& p,
+                                        LogSmem<W, SEL>& sm, int64_t row, uint32_t in_launch,
+                                        int64_t vr, LogToken tok) {
+    constexpr uint32_t GRAN = Vec<T>::N == 8 ? 1u << 16 : 1u;
+    const int lane = threadIdx.x & 63;
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const float c = a.c;
+    auto state = [&] {
+        LogState v = sm.state[0];
+#pragma unroll
+        for (int i = 1; i < W; ++i) v = log_merge(v, sm.state[i], c);
+        return v;
+    };
+    if constexpr (!SEL) {
+        if (wv != 0) return;
+        LogState v = state();
+        if constexpr (PART) {
+            if (!log_arrive(p, vr, in_launch, v)) return;
+            v = log_join(p, in_launch, c);
+        }
+        log_store(a, row, v, tok);
+    } else {
+        uint64_t key = 0;
+        if (wv == 0) key = held_finish<W>(sm.top.list, sm.top.cnt, a.K);
+        if constexpr (PART) {
+            // the partial, at the device's coherence point; then the row's count
+            if (wv == 0) {
+                if (lane < a.K)
+                    __hip_atomic_store(p.keys + vr * a.K + lane, key, __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
+                const bool last = log_arrive(p, vr, in_launch, state());
+                if (lane == 0) sm.last = last;
+            }
+            __syncthreads();
+            if (!sm.last) return;
+            // every chunk of the row is in; a merge of more partial keys than one wavefront
+            // holds takes them all
+            const int64_t n = (int64_t)p.S * a.K;
+            const uint64_t* pk = p.keys + (int64_t)in_launch * n;
+            MD none;
+            if (n > 64 * TK_MERGE_B)
+                held_merge<TK_VALUES, W, TK_MERGE_B, GRAN, true>(sm.top, wv, pk, nullptr, n, 0,
+                                                                 a.K, &key, &none);
+            else if (wv == 0)
+                held_merge<TK_VALUES, 1, TK_MERGE_B, GRAN, true>(sm.top, 0, pk, nullptr, n, 0,
+                                                                 a.K, &key, &none);
+        }
+        if (wv == 1) {
+            LogState v;
+            if constexpr (PART) v = log_join(p, in_launch, c);
+            else v = state();
+            const LogEnd end = log_store(a, row, v, tok);
+            if (lane == 0) sm.end = end;
+        }
+        __syncthreads();
+        if (wv == 0) log_store_top(a, row, sm.end, key);
+    }
+}
+
 // Wavefronts per SIMD asked of the compiler.
 template <typename T, int W, int R, bool SEL, bool PART>
 constexpr int log_waves() {
@@ -251,7 +324,9 @@ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (log_waves<T, W, R, SEL, PART>()))
     const float ninf = -__builtin_inff(), c = a.c;
 
     LogToken tok;
-    if (wv == 0 || W == 1) tok.index(a, row, lane);
+    // with alternatives the second wavefront has the row's state while the first one sorts them
+    constexpr int OWN = SEL ? 1 : 0;
+    if (wv == OWN || W == 1) tok.index(a, row, lane);
     // all loads first; lanes past the row load its last vector and mask it
     u32x4 buf[R];
     auto load = [&] {
@@ -268,7 +343,7 @@ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (log_waves<T, W, R, SEL, PART>()))
         for (int i = 0; i < R; ++i) buf[i] = u32x4{0, 0, 0, 0};
     }
     const float ex = tr < sp.ne ? load1(sp.xr + sp.extra(tr)) : ninf;
-    if (wv == 0 || W == 1) tok.element(a, xr, lane);
+    if (wv == OWN || W == 1) tok.element(a, xr, lane);
 
     // 1. maxima by vector, and the wavefront's.  bfloat16 ones by two elements at a time as
     // integers, which order numbers that are not negative: where the wavefront has one, and only
@@ -415,54 +490,12 @@ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (log_waves<T, W, R, SEL, PART>()))
     }
     // 4. the row's outputs, or the chunk's partial
     if constexpr (W == 1) {
-        log_store<SEL>(a, row, st, tok, key);
+        const LogEnd end = log_store(a, row, st, tok);
+        if constexpr (SEL) log_store_top(a, row, end, key);
     } else {
         if (lane == 0) sm.state[wv] = st;
         __syncthreads();
-        bool last = false;
-        if (wv == 0) {
-            st = sm.state[0];
-#pragma unroll
-            for (int i = 1; i < W; ++i) st = log_merge(st, sm.state[i], c);
-            if constexpr (SEL) key = held_finish<W>(sm.top.list, sm.top.cnt, a.K);
-            if constexpr (!PART) {
-                log_store<SEL>(a, row, st, tok, key);
-            } else {
-                // the partial, at the device's coherence point; then the row's count
-                if (SEL && lane < a.K)
-                    __hip_atomic_store(p.keys + vr * a.K + lane, key, __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_AGENT);
-                last = log_arrive(p, vr, in_launch, st);
-            }
-        }
-        if constexpr (PART) {
-            if constexpr (!SEL) {
-                if (!last) return;
-                // every chunk of the row is in
-            } else {
-                // a merge of more partial keys than one wavefront holds takes them all
-                const bool wide = (int64_t)p.S * a.K > 64 * TK_MERGE_B;
-                if (wide) {
-                    if (wv == 0 && lane == 0) sm.top.cnt[0] = last;
-                    __syncthreads();
-                    last = sm.top.cnt[0] != 0;
-                    __syncthreads();
-                }
-                if (!last) return;
-                const uint64_t* pk = p.keys + (int64_t)in_launch * p.S * a.K;
-                const int64_t n = (int64_t)p.S * a.K;
-                MD none;
-                if (wide) {
-                    if (!held_merge<TK_VALUES, W, TK_MERGE_B, GRAN, true>(sm.top, wv, pk, nullptr,
-                                                                         n, 0, a.K, &key, &none))
-                        return;
-                } else {
-                    held_merge<TK_VALUES, 1, TK_MERGE_B, GRAN, true>(sm.top, 0, pk, nullptr, n, 0,
-                                                                    a.K, &key, &none);
-                }
-            }
-            log_store<SEL>(a, row, log_join(p, in_launch, c), tok, key);
-        }
+        log_end<T, W, SEL, PART>(a, p, sm, row, in_launch, vr, tok);
     }
 }
 
@@ -674,15 +707,8 @@ __global__ __launch_bounds__(64 * W, 5) void logprob_stream(const LogprobRows a,
     }
     if (lane == 0) sm.state[wv] = v;
     __syncthreads();
-    if (wv != 0) return;
-    v = sm.state[0];
-#pragma unroll
-    for (int i = 1; i < W; ++i) v = log_merge(v, sm.state[i], a.c);
-    if (p.S > 1) {
-        if (!log_arrive(p, blockIdx.x, in_launch, v)) return;
-        v = log_join(p, in_launch, a.c);
-    }
-    log_store<false>(a, row, v, tok, 0);
+    if (p.S > 1) log_end<T, W, false, true>(a, p, sm, row, in_launch, blockIdx.x, tok);
+    else log_end<T, W, false, false>(a, p, sm, row, in_launch, blockIdx.x, tok);
 }
 
 template <typename T, int W, bool SEL, bool ENT, bool PART>
