@@ -172,7 +172,7 @@ struct LogprobRows {
 // How a batch is taken: W wavefronts a row (S = 1), or a workgroup of W for each of S chunks a
 // row of `chunk` elements, `rows` rows a launch, with scratch of logprob_scratch_bytes and
 // `rows` zeroed counters, which are left zeroed.  stream: rows or chunks by workgroups of so many
-// wavefronts that stream them (without alternatives).
+// wavefronts that stream them (four, where there are alternatives).
 struct LogprobPlan {
     int W, S;
     int64_t chunk, rows;

@@ -525,11 +525,11 @@ struct LogStream {
         const uint32_t v = E == 8 ? 0xFF80FF80u : 0xFF800000u;
         return u32x4{v, v, v, v};
     }
-    // The largest element of a step, if that is above the maximum.
+    // The largest element of a step, if that is above the maximum or from `th` on.
     template <int U>
-    __device__ __forceinline__ float largest(const u32x4 (&q)[U]) const {
+    __device__ __forceinline__ float largest(const u32x4 (&q)[U], float th) const {
         if constexpr (E == 8) {
-            if (m >= 0.0f) {
+            if (m >= 0.0f && th >= 0.0f) {
                 int v = -1;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -548,9 +548,10 @@ struct LogStream {
         }
         return v;
     }
+    // (returns that largest element)
     template <int U>
-    __device__ __forceinline__ void step(const u32x4 (&q)[U]) {
-        const float v = largest(q);
+    __device__ __forceinline__ float step(const u32x4 (&q)[U], float th) {
+        const float v = largest(q, th);
         lm = v > lm ? v : lm;
         if (rare(__builtin_amdgcn_ballot_w64(v > m) != 0)) {
 #pragma clang fp contract(off)  // (the step between the references as they are, both rounded)
@@ -572,6 +573,7 @@ struct LogStream {
             widen<T>(q[u], x);
             log_add<ENT, false>(x, 0.0f, c, S, d, w);
         }
+        return v;
     }
     // The wavefront's state.  ex: the lane's head or tail element; the others are its vectors
     // first + lane, first + lane + stride, ... of n from vb.
@@ -638,11 +640,128 @@ __device__ __forceinline__ LogState log_of_vector(u32x4 q, float c) {
     return v;
 }
 
-template <typename T, bool ENT, int W>
+// The alternatives of a streamed row or chunk.  `th` is a value that K elements of the team's
+// first step reach.  Where a step has elements of at least that, only the lanes that have them are
+// noted; at the end, when the K-th largest of the lanes' maxima bounds the result far better, the
+// vectors of the few whose largest element reaches it are read once more, and their elements
+// offered to the wavefront's list (HeldList, topk_held.hpp).
+template <typename T, int W>
+struct LogPicks {
+    static constexpr int E = Vec<T>::N, TR = 64 * W, U = LS_U;
+    static constexpr uint32_t GRAN = E == 8 ? 1u << 16 : 1u;
+    HeldList hl;
+    uint64_t* notes;  // TH_LIST of them: image of the lane's largest element, step * 64 + lane
+    int n;            // noted (wave-uniform), at most TH_CUT between steps
+    float th;         // smaller elements are not among the K largest
+    float th0;        // nor are such head and tail elements
+    float lm;         // the lane's largest element, where that is at least th
+
+    static __device__ __forceinline__ float word_value(uint32_t w) {
+        return key_value((uint64_t)w << 32);
+    }
+    // From the first step's vectors (those behind the last one are not looked at) and the lanes'
+    // head or tail elements, by the whole workgroup.
+    __device__ __forceinline__ void begin(HeldSmem<W>& sm, uint64_t* mine, int wv, int K,
+                                          const HeldSpan<T>& sp, const u32x4 (&q)[U], float ex) {
+        const int tr = threadIdx.x;
+        hl = HeldList{sm.list[wv], K, 0, 0ull};
+        notes = mine;
+        n = 0;
+        lm = __builtin_fmaxf(ex, -__builtin_inff());
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            u32x4 t = q[u];
+            opaque(t);
+            if (tr + u * TR < sp.nvec) lm = __builtin_fmaxf(lm, held_vmax<T, TK_VALUES>(t));
+        }
+        const KthBound b = team_bound<W, GRAN>(sm, order_word(lm), K);
+        th = th0 = word_value(b.lo);
+        if (rare(b.tied && sp.nvec >= K)) {
+            // (equal head elements, ahead of the ties in vectors, are offered at the end)
+            const float up = word_value(b.up);
+            if (held_ties<T, W, U>(sm, hl, sp, q, tr, th, up)) th = up;
+        }
+    }
+    // v: the lane's largest element of step k, where that is at least th.
+    __device__ __forceinline__ void step(const HeldSpan<T>& sp, int k, float v) {
+        const uint64_t who = __builtin_amdgcn_ballot_w64(v >= th);
+        if (who == 0) return;
+        const int lane = threadIdx.x & 63;
+        const uint32_t below = __builtin_amdgcn_mbcnt_hi(
+            (uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0u));
+        if (v >= th) notes[n + below] = (uint64_t)order_word(v) << 32 | (uint32_t)(k * 64 + lane);
+        n += __builtin_popcountll(who);
+        lm = __builtin_fmaxf(lm, v);
+        if (rare(n > TH_CUT)) {
+            const uint32_t g[1] = {order_word(lm)};
+            th = __builtin_fmaxf(th, word_value(kth_bound<1, GRAN>(g, wave_hi(g), hl.K).lo));
+            keep();
+            if (n > TH_CUT) look(sp);
+        }
+    }
+    // Only the notes that reach th stay.
+    __device__ __forceinline__ void keep() {
+        const int lane = threadIdx.x & 63, had = n;
+        const uint32_t t = order_word(th);
+        uint64_t k[3];
+        wave_sync();
+#pragma unroll
+        for (int j = 0; j < 3; ++j) k[j] = lane + 64 * j < had ? notes[lane + 64 * j] : 0ull;
+        wave_sync();
+        n = 0;
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            const bool p = lane + 64 * j < had && (uint32_t)(k[j] >> 32) >= t;
+            const uint64_t mask = __builtin_amdgcn_ballot_w64(p);
+            const uint32_t below = __builtin_amdgcn_mbcnt_hi(
+                (uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u));
+            if (p) notes[n + below] = k[j];
+            n += __builtin_popcountll(mask);
+        }
+        wave_sync();
+    }
+    // The elements of at least th of the noted lanes' vectors go to the list.
+    __device__ __forceinline__ void look(const HeldSpan<T>& sp) {
+        const int lane = threadIdx.x & 63, first = (threadIdx.x & ~63);
+        wave_sync();
+        for (int i = 0; i < n; i += 64 / U) {
+            const int at = i + lane / U;
+            const uint32_t note = at < n ? (uint32_t)notes[at] : 0;
+            const int64_t v64 = (int64_t)(note >> 6) * (TR * U) + (lane % U) * TR + first +
+                                (int)(note & 63);
+            const bool in = at < n && v64 < sp.nvec;
+            const int v = in ? (int)v64 : 0;
+            u32x4 q[1] = {sp.vb[v]};
+            u32x4 t = q[0];
+            opaque(t);
+            held_offer<T, 1, TR>(hl, sp, q, v, in && held_vmax<T, TK_VALUES>(t) >= th, th, 0.0f);
+        }
+        n = 0;
+        wave_sync();
+    }
+    __device__ __forceinline__ void end(HeldSmem<W>& sm, int wv, const HeldSpan<T>& sp, float ex) {
+        const int tr = threadIdx.x;
+        __syncthreads();  // (the maxima of the beginning have been read)
+        const float t = word_value(team_bound<W, GRAN>(sm, order_word(lm), hl.K).lo);
+        th = __builtin_fmaxf(th, t);
+        if (n > 0) {
+            keep();
+            if (n > 0) look(sp);
+        }
+        hl.offer(tr < sp.ne && ex >= __builtin_fmaxf(th0, t),
+                 make_key(ex, sp.base + (uint32_t)sp.extra(tr)));
+        if (rare(hl.n > TH_CUT)) hl.cut();
+        if ((tr & 63) == 0) sm.cnt[wv] = hl.n;
+    }
+};
+struct NoPicks {};
+
+template <typename T, bool SEL, bool ENT, int W>
 __global__ __launch_bounds__(64 * W, 5) void logprob_stream(const LogprobRows a,
                                                             const LogprobSplit p) {
-    constexpr int E = Vec<T>::N, TR = 64 * W, U = LS_U;
-    __shared__ LogSmem<W, false> sm;
+    constexpr int E = Vec<T>::N, TR = 64 * W, U = LS_U, OWN = SEL ? 1 : 0;
+    __shared__ LogSmem<W, SEL> sm;
+    __shared__ uint64_t notes[SEL ? W : 1][SEL ? TH_LIST : 1];
     const int tr = threadIdx.x, lane = tr & 63;
     const int wv = __builtin_amdgcn_readfirstlane(tr >> 6);
     const uint32_t in_launch = blockIdx.x / (uint32_t)p.S;
@@ -670,26 +789,33 @@ __global__ __launch_bounds__(64 * W, 5) void logprob_stream(const LogprobRows a,
             }
         }
     };
+    std::conditional_t<SEL, LogPicks<T, W>, NoPicks> picks;
     auto step = [&](u32x4 (&q)[U], int k) {
         if (k == whole) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (tr + (k * U + u) * TR >= nvec) q[u] = st.nothing();
         }
-        st.step(q);
+        if constexpr (SEL) {
+            const float v = st.step(q, picks.th);
+            picks.step(sp, k, v);
+        } else {
+            st.step(q, 0.0f);
+        }
     };
     LogToken tok;
-    if (wv == 0) tok.index(a, row, lane);
+    if (wv == OWN) tok.index(a, row, lane);
     u32x4 q0[U], q1[U];
     load(q0, 0);
     const float ex = tr < sp.ne ? load1(sp.xr + sp.extra(tr)) : -__builtin_inff();
-    if (wv == 0) tok.element(a, xr, lane);
+    if (wv == OWN) tok.element(a, xr, lane);
     u32x4 extra = st.nothing();
     extra.x = E == 8 ? (0xFF800000u | __float_as_uint(ex) >> 16) : __float_as_uint(ex);
     if (sp.ne > 0) {
         u32x4 one[1] = {extra};
-        st.step(one);
+        st.step(one, 0.0f);
     }
+    if constexpr (SEL) picks.begin(sm.top, notes[wv], wv, a.K, sp, q0, ex);
     for (int k = 0; k < steps; k += 2) {
         load(q1, k + 1);
         step(q0, k);
@@ -705,10 +831,11 @@ __global__ __launch_bounds__(64 * W, 5) void logprob_stream(const LogprobRows a,
     } else {
         v = st.end(ex, sp.vb, wv * 64, TR, nvec);
     }
+    if constexpr (SEL) picks.end(sm.top, wv, sp, ex);
     if (lane == 0) sm.state[wv] = v;
     __syncthreads();
-    if (p.S > 1) log_end<T, W, false, true>(a, p, sm, row, in_launch, blockIdx.x, tok);
-    else log_end<T, W, false, false>(a, p, sm, row, in_launch, blockIdx.x, tok);
+    if (p.S > 1) log_end<T, W, SEL, true>(a, p, sm, row, in_launch, blockIdx.x, tok);
+    else log_end<T, W, SEL, false>(a, p, sm, row, in_launch, blockIdx.x, tok);
 }
 
 template <typename T, int W, bool SEL, bool ENT, bool PART>
@@ -765,12 +892,17 @@ hipError_t launch_logprob_t(const LogprobRows& a, const LogprobPlan& plan, void*
         p.rows = a.N - p.row0 < plan.rows ? a.N - p.row0 : plan.rows;
         hipError_t e;
         if (plan.stream) {
-            if constexpr (SEL) return hipErrorInvalidValue;
             const dim3 grid((unsigned)(p.rows * p.S));
-            if (plan.stream == 8)
-                hipLaunchKernelGGL((logprob_stream<T, ENT, 8>), grid, dim3(512), 0, st, a, p);
-            else
-                hipLaunchKernelGGL((logprob_stream<T, ENT, 4>), grid, dim3(256), 0, st, a, p);
+            if constexpr (SEL) {
+                hipLaunchKernelGGL((logprob_stream<T, SEL, ENT, 4>), grid, dim3(256), 0, st, a, p);
+            } else {
+                if (plan.stream == 8)
+                    hipLaunchKernelGGL((logprob_stream<T, SEL, ENT, 8>), grid, dim3(512), 0, st, a,
+                                       p);
+                else
+                    hipLaunchKernelGGL((logprob_stream<T, SEL, ENT, 4>), grid, dim3(256), 0, st, a,
+                                       p);
+            }
             e = hipGetLastError();
         } else {
             e = launch_logprob_w<T, 4, SEL, ENT, true>(a, p, st);

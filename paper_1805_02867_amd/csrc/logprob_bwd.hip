@@ -199,17 +199,24 @@ hipError_t launch_logprob_bwd(const LogprobGrad& a, int dtype, hipStream_t st) {
 // x 65536 f x2 9.9, x1 10.5; 16 x 65536 f x4 6.9); eight rows and fewer into up to 64 of at
 // least 512 vectors (1 x 128256 f held 4 x32 5.2, x16 5.7; 1 x 50257 f x32 4.9, x8 5.5).
 //
-// With alternatives (5 of them) rows are always held: by eight wavefronts from 2048 vectors on
-// (16 x 16000 f held 8 7.2, held 4 7.5; but 4096 x 16000 f 50.9 / 47.1), beyond 8192 vectors in
-// chunks that four hold (1024 x 128256 f x8 99, x4 by eight 125; 4096 x 128256 b x4 215, x2 262),
-// and in chunks of about 2048 where rows are few (64 x 128256 b x8 14.6, x4 15.0).
+// With alternatives (5 of them) rows are held by eight wavefronts from 2048 vectors on (16 x 16000 f
+// held 8 7.2, held 4 7.5; but 4096 x 16000 f 50.9 / 47.1), beyond 8192 vectors in chunks that four
+// hold, of about 2048 where rows are few (64 x 128256 b x8 14.2, x4 15.0).  Batches of 3 rows for 2
+// CUs and more are streamed from 4096 vectors on (held / stream 4: 512 x 25000 f 16.0 / 15.4, 4096 x
+// 50000 b 102 / 83, 1024 x 128256 f 105 / 84, 2048 x 128256 b 125 / 93; but 256 x 50000 b 13.5 /
+// 14.0, 4096 x 16000 f 49.1 / 51.2), of a row a CU from 8192 on, in two chunks from 16384 on (256 x
+// 100000 b 22.8 / 20.2, 256 x 256512 b 39.8 / 33.8): up to 32 alternatives, which the maxima of 64
+// lanes bound well (1024 x 128256 b top-20 72 / 54, top-50 76 / 86).
 LogprobPlan logprob_plan(int64_t N, int64_t V, int K, int dtype, int cus) {
     const int64_t E = dtype == 1 ? 8 : 4, c = cus;
     const int64_t nv = (V + E - 1) / E;
     const int64_t hold4 = 256 * 16, hold8 = 512 * 16;  // vectors
     LogprobPlan p{4, 1, V, N, 0};
     int64_t S = 1;
-    if (nv > 4096 && N <= 8) {
+    if (K > 0 && K <= 32 && ((nv > hold8 && N >= c) || (nv > hold4 && 2 * N >= 3 * c))) {
+        p.stream = 4;
+        S = 2 * N < 3 * c && nv >= 2 * hold8 ? 2 : 1;
+    } else if (nv > 4096 && N <= 8) {
         const int64_t most = K > 16 ? 32 : 64;
         S = nv / 512 < most ? nv / 512 : most;
     } else if (K == 0 && nv > 4096 && N < c) {
@@ -220,9 +227,12 @@ LogprobPlan logprob_plan(int64_t N, int64_t V, int K, int dtype, int cus) {
         S = want < most ? want : most;
     }
     // chunks that the registers hold, where they have to
-    if (K > 0 && nv > hold8 && S < (nv + hold4 - 1) / hold4) S = (nv + hold4 - 1) / hold4;
+    if (K > 0 && !p.stream && nv > hold8 && S < (nv + hold4 - 1) / hold4)
+        S = (nv + hold4 - 1) / hold4;
     const int64_t vecs = (nv + S - 1) / S;
-    if (K == 0 && vecs > 2048) {
+    if (p.stream) {
+        // (streamed with alternatives)
+    } else if (K == 0 && vecs > 2048) {
         p.stream = nv <= hold8 && 2 * N >= 3 * c ? 4 : 8;
     } else if (S == 1) {
         p.W = nv <= 512 && N >= 4 * c ? 1

@@ -181,6 +181,48 @@ def test_alternatives_of_long_rows(N, nv, dtype, dev):
         check_fwd(x, some_tokens(N, V, 3, V, dev), K, what=dtype)
 
 
+@pytest.mark.filterwarnings("ignore:invalid value")     # of the reference, on purpose
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,nv,offset", [(400, 4200, 1), (256, 8300, 0), (270, 16500, 3)])
+def test_alternatives_of_large_batches(N, nv, offset, dtype, dev):
+    """Streamed rows and chunks with up to 32 alternatives: rows that rise and fall, of few values,
+    masked ones with the rest at the front, at the end and anywhere, no numbers."""
+    V = nv * (4 if dtype == "f32" else 8) - 3
+    print(f"alternatives {dtype} {N} {V}", flush=True)
+    x = logits(16, V, "f32", V, dev)
+    at = torch.randint(0, V, (16,), generator=torch.Generator().manual_seed(nv)).to(dev)
+    x[0] = -INF
+    x[1] = -INF
+    x[1, at[1]] = -3.0
+    x[2, 20:] = -INF
+    x[3, :-20] = -INF
+    x[4, torch.arange(V, device=dev) % 997 != 5] = -INF
+    x[5] = x[5].sort().values
+    x[6] = x[6].sort(descending=True).values
+    x[7] = x[7].round()
+    x[8] = -1.25
+    x[9, V // 2:] = 9.0
+    x[10] = torch.arange(V, device=dev) // 5000
+    x[11, at[11]] = NAN
+    x[12] = x[12] - 50.0
+    x[13, -1], x[13, 0], x[13, 1] = 20.0, 20.0, 21.0
+    x[14] = x[14].sort().values.view(-1, 1)[:, 0].round()
+    rows = torch.arange(N, device=dev) % 16
+    each = rows.cpu().numpy()
+    ld = V + (3 if offset else 0)
+    buf = torch.zeros(N * ld + offset, dtype=DT[dtype], device=dev)
+    y = buf[offset:].view(N, ld)[:, :V]
+    y.copy_(x[rows])
+    tok = some_tokens(16, V, 2, V, dev)
+    for K in (1, 6, 32):
+        got = osm.logprob_fwd(y, tok[rows], K=K, entropy=True, stats=True)
+        want = loss_ref.logprob(host(y[:16].contiguous()), tok.cpu().numpy(), K)
+        assert np.array_equal(got.top_idx.cpu().numpy(), want["top_idx"][each]), K
+        for name in ("logp", "entropy", "stats", "top_vals"):
+            loss_ref.check(host(getattr(got, name)), want[name][each], want[name + "_err"][each],
+                           f"{name} K={K}")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [7, 1000, 40000, 300001])
 def test_masked_rows(V, dtype, dev):
