@@ -134,6 +134,23 @@ struct LogToken {
     }
 };
 
+// ln(1 + s), s >= 0, to 2^-24 of itself and 2^-26: with r, a power of two times a number of 11
+// bits next to 1 / (1 + s), that is -ln r + ln(1 + t) with t = (1 + s) r - 1, exact in binary64 and
+// below 2^-10; where s is small r is 1, and t = s.  (A row of 1000 elements takes 247 instructions;
+// with the library's binary64 function it took 361: 16385 x 1000 binary32 14.1 us for 16.0.)
+__device__ __forceinline__ double ln_1p(float s) {
+    const float d = 1.0f + s;
+    const int e = __builtin_amdgcn_frexp_expf(d * 0.70710678f);  // d 2^-e in [1/sqrt 2, sqrt 2]
+    const float f = __builtin_ldexpf(d, -e);
+    const float r = __uint_as_float(
+        (__float_as_uint(__builtin_amdgcn_rcpf(f)) + (1u << 12)) & ~((1u << 13) - 1));
+    const double k = (double)__builtin_ldexpf(r, -e);
+    const double t = __builtin_fma((double)s, k, k - 1.0);
+    const double p = t * __builtin_fma(t, __builtin_fma(t, 1.0 / 3.0, -0.5), 1.0);
+    const double l = (double)e - (double)__builtin_amdgcn_logf(r);
+    return __builtin_fma(l, 0.69314718055994530942, p);
+}
+
 // What a row's alternatives need of its state.
 struct LogEnd {
     double m, ln_d;
@@ -146,14 +163,15 @@ __device__ __forceinline__ LogEnd log_store(const LogprobRows& a, int64_t row, L
     const int lane = threadIdx.x & 63;
     const bool good = __builtin_fabsf(v.m) < __builtin_inff() && v.s == v.s;
     const float nan = __builtin_nanf("");
-    const double s = (double)v.s, ln_d = log1p(s), m = (double)v.m;
+    const double ln_d = ln_1p(v.s), m = (double)v.m;
     if (lane < a.T) {
         const float lp = (float)(((double)t.x - m) * a.inverse - ln_d);
         a.logp[row * a.T + lane] = !t.in ? 0.0f : good ? lp : nan;
     }
     if (lane == 0) {
         if (a.entropy) {
-            const double h = ln_d + 0.69314718055994530942 * (double)v.w / (1.0 + s);
+            const double d = 1.0 + (double)v.s, q = (double)__builtin_amdgcn_rcpf((float)d);
+            const double h = ln_d + 0.69314718055994530942 * (double)v.w * (q * (2.0 - d * q));
             a.entropy[row] = good ? (float)h : nan;
         }
         if (a.stats) {
