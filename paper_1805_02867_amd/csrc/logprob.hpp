@@ -316,8 +316,8 @@ constexpr int log_waves() {
     return held_waves<T, W, R, PART>();
 }
 
-// Rows (PART = false) or chunks of rows (PART = true: workgroup b has chunk b % S of row
-// row0 + b / S) of at most 64 W R whole 16-byte vectors, W wavefronts each (W = 1: four rows a
+// Rows (PART = false: from row0 on) or chunks of rows (PART = true: workgroup b has chunk b % S of
+// row row0 + b / S) of at most 64 W R whole 16-byte vectors, W wavefronts each (W = 1: four rows a
 // workgroup).  SEL: with alternatives, selected as topk_held.hpp does.  ENT: with w.
 template <typename T, int W, int R, bool SEL, bool ENT, bool PART>
 __global__
@@ -331,9 +331,9 @@ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (log_waves<T, W, R, SEL, PART>()))
     const int wv = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int tr = W == 1 ? lane : tid;
     const int64_t vr = W == 1 ? (int64_t)blockIdx.x * (TK_BLOCK / 64) + wv : (int64_t)blockIdx.x;
-    if (W == 1 && vr >= a.N) return;  // whole wavefronts; no barrier follows
+    if (W == 1 && vr >= p.rows) return;  // whole wavefronts; no barrier follows
     const uint32_t in_launch = PART ? blockIdx.x / (uint32_t)p.S : 0;
-    const int64_t row = PART ? p.row0 + in_launch : vr;
+    const int64_t row = p.row0 + (PART ? in_launch : vr);
     const int64_t start = PART ? (blockIdx.x - in_launch * (uint32_t)p.S) * p.chunk : 0;
     const int64_t left = a.V - start;
     const T* xr = static_cast<const T*>(a.x) + row * a.ld;
@@ -860,8 +860,8 @@ template <typename T, int W, bool SEL, bool ENT, bool PART>
 hipError_t launch_logprob_w(const LogprobRows& a, const LogprobSplit& p, hipStream_t st) {
     const int64_t nv = (PART ? p.chunk : a.V) / Vec<T>::N;
     const int64_t r = (nv + 64 * W - 1) / (64 * W);
-    const int64_t blocks = W == 1 ? (a.N + TK_BLOCK / 64 - 1) / (TK_BLOCK / 64)
-                                  : PART ? p.rows * p.S : a.N;
+    const int64_t blocks = W == 1 ? (p.rows + TK_BLOCK / 64 - 1) / (TK_BLOCK / 64)
+                                  : PART ? p.rows * p.S : p.rows;
     const dim3 grid((unsigned)blocks), block(W == 1 ? TK_BLOCK : 64 * W);
 #define OSM_LOG(R_) \
     hipLaunchKernelGGL((logprob_held<T, W, R_, SEL, ENT, PART>), grid, block, 0, st, a, p)
@@ -894,15 +894,6 @@ hipError_t launch_logprob_t(const LogprobRows& a, const LogprobPlan& plan, void*
     LogprobSplit p{};
     p.chunk = plan.chunk;
     p.S = plan.S;
-    if (plan.S <= 1 && !plan.stream) {
-        switch (plan.W) {
-            case 1: return launch_logprob_w<T, 1, SEL, ENT, false>(a, p, st);
-            case 4: return launch_logprob_w<T, 4, SEL, ENT, false>(a, p, st);
-            case 8:
-                if constexpr (SEL) return launch_logprob_w<T, 8, SEL, ENT, false>(a, p, st);
-            default: return hipErrorInvalidValue;
-        }
-    }
     p.states = static_cast<uint64_t*>(scratch);
     p.keys = p.states + 2 * plan.rows * plan.S;
     p.ctr = ctr;
@@ -922,8 +913,15 @@ hipError_t launch_logprob_t(const LogprobRows& a, const LogprobPlan& plan, void*
                                        p);
             }
             e = hipGetLastError();
-        } else {
+        } else if (plan.S > 1) {
             e = launch_logprob_w<T, 4, SEL, ENT, true>(a, p, st);
+        } else if (plan.W == 1) {
+            e = launch_logprob_w<T, 1, SEL, ENT, false>(a, p, st);
+        } else if (plan.W == 4) {
+            e = launch_logprob_w<T, 4, SEL, ENT, false>(a, p, st);
+        } else {
+            if constexpr (SEL) e = launch_logprob_w<T, 8, SEL, ENT, false>(a, p, st);
+            else e = hipErrorInvalidValue;
         }
         if (e != hipSuccess) return e;
     }

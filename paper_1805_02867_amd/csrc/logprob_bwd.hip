@@ -243,9 +243,9 @@ LogprobPlan logprob_plan(int64_t N, int64_t V, int K, int dtype, int cus) {
         S = (V + p.chunk - 1) / p.chunk;
     }
     p.S = (int)S;
-    // 2^16 chunks a launch, or one row
-    const int64_t rows = ((int64_t)1 << 16) / S;
-    if (S > 1 || p.stream) p.rows = rows < 1 ? 1 : rows < N ? rows : N;
+    // 2^16 chunks a launch, or one row; 2^22 rows (a launch has fewer than 2^32 threads)
+    const int64_t rows = S > 1 ? ((int64_t)1 << 16) / S : (int64_t)1 << 22;
+    p.rows = rows < 1 ? 1 : rows < N ? rows : N;
     return p;
 }
 

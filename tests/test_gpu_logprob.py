@@ -535,3 +535,26 @@ def test_offsets_past_32_bits(dev):
     p[V - 2] -= 1.0
     d = (dx[N - 1].double() + p).abs()
     assert bool((d <= (2.0 ** -8 + 2.0 ** -12) * p.abs()).all())
+
+
+def test_more_rows_than_a_launch_has_threads_for(dev):
+    """2^26 rows and a few: 2^32 threads and more."""
+    N = (1 << 26) + 5
+    x = torch.zeros(N, 2, device=dev)
+    at = [0, 1, (1 << 22) - 1, 1 << 22, (1 << 26) - 1, 1 << 26, N - 1]
+    for i, r in enumerate(at):
+        x[r, 1] = i + 1.0
+    tok = torch.ones(N, dtype=torch.int32, device=dev)
+    got = osm.logprob_fwd(x, tok, K=1, stats=True)
+    only = osm.logprob_fwd(x, tok)
+    rows = torch.tensor(at, device=dev)
+    want = loss_ref.logprob(host(x[rows]), tok[rows].cpu().numpy().reshape(-1, 1), 1)
+    for r in (got, only):
+        loss_ref.check(host(r.logp[rows])[:, None], want["logp"], want["logp_err"], "logp")
+        assert int((r.logp == r.logp[2]).sum()) == N - len(at)
+    assert got.top_idx[rows].tolist() == [[1]] * len(at)
+    assert int(got.top_idx.sum()) == len(at)
+    dx = osm.logprob_bwd(x, got.stats, tok, torch.ones(N, device=dev))
+    d, err = loss_ref.logprob_bwd(host(x[rows]), np.ones((len(at), 1), int),
+                                  np.ones((len(at), 1)))
+    loss_ref.check(host(dx[rows]), d, err, "gradient")
