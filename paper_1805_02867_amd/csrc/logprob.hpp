@@ -1,5 +1,11 @@
 // Log probabilities of given tokens, the entropy and the best alternatives of rows (or chunks
-// of rows) held in registers: one read of every element.
+// of rows) held in registers or streamed: one read of every element.
+//
+// What bounds them: large batches memory (2048 x 128256 bfloat16 with the entropy 86 us for 525
+// MB, 6.1 TB/s, a plain read of as much 75.5; 300 x 32000 binary32 10.6 us for 38 MB, 8.3), short
+// rows the arithmetic around the elements' own (16385 x 1000 binary32 14.1 us for 66 MB, 12.3; 247
+// vector instructions a row, 70 of them on its elements), and a few rows the chain of a chunk and
+// of the join (1 x 128256 5.1 us, with five alternatives 8.2).
 //
 // A row's state is (m, s, w) with c = log2(e) / temperature:
 //   m = max x,
