@@ -85,6 +85,7 @@ def test_sequences(score, dev):
             (40000, 64, [1, 0, 0, 20000, 7, 0, 19992, 0], 0), (40000, 64, [39999], 1),
             (30000, 16, [10000, 0, 15000], 3000), (5000, 256, [1] * 5000, 0),
             (20000, 60, torch.randint(0, 300, (130,), generator=g).tolist(), 5),
+            (12000, 256, torch.randint(0, 70, (300,), generator=g).tolist(), 9),
             (9000, 8, [0] * 300 + [9000] + [0] * 300, 0), (100, 8, [0] * 70, 50),
             (66000, 32, [32768, 1, 32767, 64, 64], 300), (100, 24, [100], 0)):
         print(N, E, len(lengths), flush=True)
