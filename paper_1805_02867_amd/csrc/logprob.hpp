@@ -140,23 +140,6 @@ struct LogToken {
     }
 };
 
-// ln(1 + s), s >= 0, to 2^-24 of itself and 2^-26: with r, a power of two times a number of 11
-// bits next to 1 / (1 + s), that is -ln r + ln(1 + t) with t = (1 + s) r - 1, exact in binary64 and
-// below 2^-10; where s is small r is 1, and t = s.  (A row of 1000 elements takes 247 instructions;
-// with the library's binary64 function it took 361: 16385 x 1000 binary32 14.1 us for 16.0.)
-__device__ __forceinline__ double ln_1p(float s) {
-    const float d = 1.0f + s;
-    const int e = __builtin_amdgcn_frexp_expf(d * 0.70710678f);  // d 2^-e in [1/sqrt 2, sqrt 2]
-    const float f = __builtin_ldexpf(d, -e);
-    const float r = __uint_as_float(
-        (__float_as_uint(__builtin_amdgcn_rcpf(f)) + (1u << 12)) & ~((1u << 13) - 1));
-    const double k = (double)__builtin_ldexpf(r, -e);
-    const double t = __builtin_fma((double)s, k, k - 1.0);
-    const double p = t * __builtin_fma(t, __builtin_fma(t, 1.0 / 3.0, -0.5), 1.0);
-    const double l = (double)e - (double)__builtin_amdgcn_logf(r);
-    return __builtin_fma(l, 0.69314718055994530942, p);
-}
-
 // What a row's alternatives need of its state.
 struct LogEnd {
     double m, ln_d;

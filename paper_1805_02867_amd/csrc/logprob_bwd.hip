@@ -18,7 +18,10 @@
 namespace osm {
 
 constexpr int LB_BLOCK = 256;
-constexpr int LB_U = 4;  // vectors a lane
+constexpr int LB_U = 4;     // vectors a lane
+// Lanes of a row of up to 64 vectors: four rows a wavefront (100000 x 64 binary32 70.7 us with a
+// wavefront a row, 19.1 so).
+constexpr int LB_FEW = 16;
 
 // Sixteen bytes at any element's address.
 typedef u32x4 u32x4_any __attribute__((aligned(2)));
@@ -47,17 +50,29 @@ __device__ __forceinline__ float grad_of(const GradRow& r, float x) {
 }
 
 // Piece b of a row by TR lanes: U vectors a lane from the first 16-byte boundary of dx on,
-// piece 0 with the elements in front of it and behind the last whole vector.
+// piece 0 with the elements in front of it and behind the last whole vector.  (T <= TR.)
 template <typename T, int TR, bool ENT>
 __global__ __launch_bounds__(LB_BLOCK) void logprob_grad(const LogprobGrad a, uint32_t pieces) {
     constexpr int E = Vec<T>::N, U = LB_U, TEAMS = LB_BLOCK / TR;
-    const int lane = threadIdx.x & 63;
+    constexpr int TL = TR < 64 ? TR : 64;  // lanes of a row or piece in one wavefront
+    const int lane = threadIdx.x % TL;
     const int tr = threadIdx.x % TR;
-    const int64_t unit = (int64_t)blockIdx.x * TEAMS +
-                         (TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TR) : 0);
-    const int64_t row = unit / pieces;
-    if (row >= a.N) return;  // whole wavefronts; no barrier follows
-    const uint32_t piece = (uint32_t)(unit - row * pieces);
+    const uint64_t team = TL == 64 ? ~0ull
+                                   : ((1ull << TL) - 1) << ((threadIdx.x & 63) / TL * TL);
+    int64_t row = blockIdx.x;
+    uint32_t piece = 0;
+    bool live = true;
+    if constexpr (TR < 64) {  // (a row is one piece)
+        row = row * TEAMS + threadIdx.x / TR;
+        live = row < a.N;  // the others do the last row again, and store nothing
+        row = live ? row : a.N - 1;
+    } else {
+        const int64_t unit =
+            row * TEAMS + (TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TR) : 0);
+        row = unit / pieces;
+        if (row >= a.N) return;  // whole wavefronts; no barrier follows
+        piece = (uint32_t)(unit - row * pieces);
+    }
     const T* xr = static_cast<const T*>(a.x) + row * a.ldx;
     T* dr = static_cast<T*>(a.dx) + row * a.lddx;
     int64_t head = (int64_t)(((16 - (((uintptr_t)dr) & 15)) & 15) / sizeof(T));
@@ -98,9 +113,10 @@ __global__ __launch_bounds__(LB_BLOCK) void logprob_grad(const LogprobGrad a, ui
     const bool any = __builtin_amdgcn_ballot_w64(here) != 0;
     const float tx = here ? load1(xr + tok) : 0.0f;
 
-    const double G = group_sum<64>((double)g), rd = 1.0 / (1.0 + (double)s);
-    const double ln_d = ENT || any ? log1p((double)s) : 0.0;
-    const bool zero = __builtin_amdgcn_ballot_w64(!(g == 0.0f)) == 0 && h == 0.0f;
+    const double G = group_sum<TL>((double)g), d1 = 1.0 + (double)s;
+    const double rd0 = (double)__builtin_amdgcn_rcpf((float)d1), rd = rd0 * (2.0 - d1 * rd0);
+    const double ln_d = ENT || any ? ln_1p(s) : 0.0;
+    const bool zero = (__builtin_amdgcn_ballot_w64(!(g == 0.0f)) & team) == 0 && h == 0.0f;
     GradRow r;
     r.m = m;
     r.c = a.c;
@@ -110,14 +126,14 @@ __global__ __launch_bounds__(LB_BLOCK) void logprob_grad(const LogprobGrad a, ui
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int64_t v = v0 + tr + i * TR;
-        if (v >= nvec) continue;
+        if (v >= nvec || !live) continue;
         Vec<T> out;
 #pragma unroll
         for (int e = 0; e < E; ++e) out.v[e] = zero ? 0.0f : grad_of<ENT>(r, buf[i].v[e]);
         out.store_nt(dr + head + v * E);
     }
-    if (tr < extras) store1(dr + extra(tr), zero ? 0.0f : grad_of<ENT>(r, ex));
-    if (zero || !any) return;  // (the same in the piece's wavefronts)
+    if (tr < extras && live) store1(dr + extra(tr), zero ? 0.0f : grad_of<ENT>(r, ex));
+    if (!any || (TR >= 64 && zero)) return;  // (the same in the piece's wavefronts)
 
     // The tokens' own elements, a lane each, by the piece's first wavefront once they are
     // stored.  A token that occurs twice is its first lane's.
@@ -130,14 +146,29 @@ __global__ __launch_bounds__(LB_BLOCK) void logprob_grad(const LogprobGrad a, ui
     double gt = 0.0;
     bool first = here;
     for (int i = 0; i < a.T; ++i) {
-        const bool same = __builtin_amdgcn_readlane(tok, i) == tok;
-        const float v = lane_value(g, i);
+        const bool same = (TR < 64 ? __shfl(tok, i, TL) : __builtin_amdgcn_readlane(tok, i)) == tok;
+        const float v = TR < 64 ? __shfl(g, i, TL) : lane_value(g, i);
         gt += same ? (double)v : 0.0;
         first = first && !(same && i < lane);
     }
-    if (!first) return;
-    const double lp = ((double)tx - (double)m) * a.inverse - ln_d, p = exp(lp);
-    double d = gt * -expm1(lp) - p * (G - gt);
+    if (!first || zero || !live) return;
+    // p and 1 - p: next to 1 by the series of e^lp - 1 (the first term left out 2^-26 of it), else
+    // p as precise as the other elements' (the library's binary64 functions, with its logarithm
+    // above: 2000 x 32000 bfloat16, 64 tokens a row, 56 us for 53)
+    const double lp = ((double)tx - (double)m) * a.inverse - ln_d;
+    double p = (double)exp2_hw((float)(lp * 1.4426950408889634074)), q = 1.0 - p;
+    if (lp > -0.5) {
+        q = 1.0 / 40320;
+        q = __builtin_fma(q, lp, 1.0 / 5040);
+        q = __builtin_fma(q, lp, 1.0 / 720);
+        q = __builtin_fma(q, lp, 1.0 / 120);
+        q = __builtin_fma(q, lp, 1.0 / 24);
+        q = __builtin_fma(q, lp, 1.0 / 6);
+        q = __builtin_fma(q, lp, 0.5);
+        q = -lp * __builtin_fma(q, lp, 1.0);
+        p = 1.0 - q;
+    }
+    double d = gt * q - p * (G - gt);
     if (ENT && p > 0.0) d -= (double)h * p * (lp + H);
     store1(dr + tok, (float)(d * a.inverse));
 }
@@ -146,8 +177,8 @@ template <typename T>
 hipError_t launch_logprob_bwd_t(const LogprobGrad& a, hipStream_t st) {
     constexpr int E = Vec<T>::N;
     const int64_t nv = a.V / E;  // at least the whole vectors
-    const bool wave = nv <= 64 * LB_U;
-    const int64_t tr = wave ? 64 : LB_BLOCK;
+    const bool wave = nv <= 64 * LB_U, few = nv <= LB_FEW * LB_U && a.T <= LB_FEW;
+    const int64_t tr = few ? LB_FEW : wave ? 64 : LB_BLOCK;
     int64_t pieces = (nv + tr * LB_U - 1) / (tr * LB_U);
     if (pieces < 1) pieces = 1;
     const int64_t teams = LB_BLOCK / tr;
@@ -165,7 +196,11 @@ hipError_t launch_logprob_bwd_t(const LogprobGrad& a, hipStream_t st) {
         b.dentropy = a.dentropy ? a.dentropy + row0 : nullptr;
         const dim3 grid((unsigned)((b.N * pieces + teams - 1) / teams)), block(LB_BLOCK);
         const uint32_t n = (uint32_t)pieces;
-        if (wave && a.dentropy)
+        if (few && a.dentropy)
+            hipLaunchKernelGGL((logprob_grad<T, LB_FEW, true>), grid, block, 0, st, b, n);
+        else if (few)
+            hipLaunchKernelGGL((logprob_grad<T, LB_FEW, false>), grid, block, 0, st, b, n);
+        else if (wave && a.dentropy)
             hipLaunchKernelGGL((logprob_grad<T, 64, true>), grid, block, 0, st, b, n);
         else if (wave)
             hipLaunchKernelGGL((logprob_grad<T, 64, false>), grid, block, 0, st, b, n);

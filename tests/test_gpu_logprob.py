@@ -354,6 +354,29 @@ def test_gradients_of_batches(N, V, dtype, dev):
     assert torch.equal(dx, osm.logprob_bwd(x, r.stats, tok, dlogp))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 7, 16, 33, 255, 256, 257, 264, 511, 512, 520])
+def test_gradients_of_short_rows(V, dtype, dev):
+    """Several rows a wavefront, with up to sixteen tokens and more, rows without any, without
+    gradients and with no numbers beside others; a batch that does not fill the last wavefront."""
+    for N, T in ((1, 1), (37, 16), (37, 17), (18, 64), (70, 3)):
+        x = logits(N, V, dtype, V + T, dev, V + 3, 1)
+        tok = some_tokens(N, V, T, V, dev)
+        dlogp, dent = torch.randn(N, T, device=dev), torch.randn(N, device=dev)
+        if N > 9:
+            tok[2] = -100
+            dlogp[3], dent[3] = 0.0, 0.0
+            x[4] = -INF
+            x[5, V // 2] = NAN
+            x[6], dlogp[6], dent[6] = NAN, 0.0, 0.0
+            x[7, : V - 1] = -INF
+            x[8, V // 2] += 30.0
+            dlogp[9, 0] = NAN
+            tok[9, 0] = 0
+        for h in (dent, None):
+            check_bwd(x, tok, dlogp, h, 0.9, dtype, what=f"{T} tokens")
+
+
 def test_gradient_against_differences(dev):
     """Of the kernels' own forward pass: a step of 1/8 in binary32, differences of sums of 12
     outputs of order 10 (2^-20 each), and h^2 / 6 times third derivatives below 2."""
