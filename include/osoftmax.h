@@ -429,8 +429,8 @@ typedef struct osm_logprob {
  *                increasing index order), top_logp[i] their log probabilities.
  * A token outside [0, V) is ignored: its logp is 0.  Elements of -inf have no weight,
  * and a log probability of -inf.  A row holding NaN or +inf, or only -inf, gives NaN
- * (0 for ignored tokens) and top_idx -1.  x is read once; sums are binary32, the
- * outputs are formed from them in binary64.
+ * (0 for ignored tokens) and top_idx -1.  x is read once; sums are binary32 (weights
+ * below 2^-126 are 0 in them), the outputs are formed from them in binary64.
  * x: row r starts at x + r * ldx elements, ldx >= V; (max x - min x) / temperature
  * stays below 2.35e38 for finite elements.
  * Errors: OSM_EINVAL for bad sizes, ldx < V, unknown dtype, NULL p, T, K or temperature

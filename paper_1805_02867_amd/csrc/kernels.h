@@ -172,11 +172,13 @@ struct LogprobRows {
 // How a batch is taken: W wavefronts a row (S = 1), or a workgroup of W for each of S chunks a
 // row of `chunk` elements, `rows` rows a launch, with scratch of logprob_scratch_bytes and
 // `rows` zeroed counters, which are left zeroed.  stream: rows or chunks by workgroups of so many
-// wavefronts that stream them (four, where there are alternatives).
+// wavefronts that stream them (four, where there are alternatives).  lanes: short rows by so many
+// lanes each.
 struct LogprobPlan {
     int W, S;
     int64_t chunk, rows;
     int stream;
+    int lanes;
 };
 struct LogprobSplit {
     uint64_t* states;  // two words a chunk

@@ -2,10 +2,10 @@
 // of rows) held in registers or streamed: one read of every element.
 //
 // What bounds them: large batches memory (2048 x 128256 bfloat16 with the entropy 86 us for 525
-// MB, 6.1 TB/s, a plain read of as much 75.5; 300 x 32000 binary32 10.6 us for 38 MB, 8.3), short
-// rows the arithmetic around the elements' own (16385 x 1000 binary32 14.1 us for 66 MB, 12.3; 247
-// vector instructions a row, 70 of them on its elements), and a few rows the chain of a chunk and
-// of the join (1 x 128256 5.1 us, with five alternatives 8.2).
+// MB, 6.1 TB/s, a plain read of as much 75.5; 300 x 32000 binary32 10.6 us for 38 MB, 8.3; 16385 x
+// 1000 13.5 us for 66 MB, 12.3), short rows the arithmetic that is not their elements' (32768 x 32
+// bfloat16 4.8 us), and a few rows the chain of a chunk and of the join (1 x 128256 5.1 us, with
+// five alternatives 8.2).
 //
 // A row's state is (m, s, w) with c = log2(e) / temperature:
 //   m = max x,
@@ -146,29 +146,40 @@ struct LogEnd {
     bool good;
 };
 
-// A row's outputs but for the alternatives, by one wavefront, from its state and lane l's token.
-__device__ __forceinline__ LogEnd log_store(const LogprobRows& a, int64_t row, LogState v,
-                                            LogToken t) {
-    const int lane = threadIdx.x & 63;
-    const bool good = __builtin_fabsf(v.m) < __builtin_inff() && v.s == v.s;
+__device__ __forceinline__ LogEnd log_end_of(const LogState& v) {
+    return {(double)v.m, ln_1p(v.s), __builtin_fabsf(v.m) < __builtin_inff() && v.s == v.s};
+}
+
+// log p of an element.
+__device__ __forceinline__ float log_of(const LogprobRows& a, const LogEnd& v, float x) {
+    const float lp = (float)(((double)x - v.m) * a.inverse - v.ln_d);
+    return v.good ? lp : __builtin_nanf("");
+}
+
+// A row's entropy and state, by lane 0.
+__device__ __forceinline__ void log_store_row(const LogprobRows& a, int64_t row, const LogState& v,
+                                              const LogEnd& end, int lane) {
+    if (lane != 0) return;
     const float nan = __builtin_nanf("");
-    const double ln_d = ln_1p(v.s), m = (double)v.m;
-    if (lane < a.T) {
-        const float lp = (float)(((double)t.x - m) * a.inverse - ln_d);
-        a.logp[row * a.T + lane] = !t.in ? 0.0f : good ? lp : nan;
+    if (a.entropy) {
+        const double d = 1.0 + (double)v.s, q = (double)__builtin_amdgcn_rcpf((float)d);
+        const double h = end.ln_d + 0.69314718055994530942 * (double)v.w * (q * (2.0 - d * q));
+        a.entropy[row] = end.good ? (float)h : nan;
     }
-    if (lane == 0) {
-        if (a.entropy) {
-            const double d = 1.0 + (double)v.s, q = (double)__builtin_amdgcn_rcpf((float)d);
-            const double h = ln_d + 0.69314718055994530942 * (double)v.w * (q * (2.0 - d * q));
-            a.entropy[row] = good ? (float)h : nan;
-        }
-        if (a.stats) {
-            a.stats[row * 2] = good ? v.m : nan;
-            a.stats[row * 2 + 1] = good ? v.s : nan;
-        }
+    if (a.stats) {
+        a.stats[row * 2] = end.good ? v.m : nan;
+        a.stats[row * 2 + 1] = end.good ? v.s : nan;
     }
-    return {m, ln_d, good};
+}
+
+// A row's outputs but for the alternatives, by one wavefront, from its state and lane l's token.
+__device__ __forceinline__ LogEnd log_store(const LogprobRows& a, int64_t row, const LogState& v,
+                                            const LogToken& t) {
+    const int lane = threadIdx.x & 63;
+    const LogEnd end = log_end_of(v);
+    if (lane < a.T) a.logp[row * a.T + lane] = t.in ? log_of(a, end, t.x) : 0.0f;
+    log_store_row(a, row, v, end, lane);
+    return end;
 }
 
 // Lane l has the l-th alternative.
@@ -176,8 +187,7 @@ __device__ __forceinline__ void log_store_top(const LogprobRows& a, int64_t row,
                                               uint64_t key) {
     const int lane = threadIdx.x & 63;
     if (lane >= a.K) return;
-    const float lp = (float)(((double)key_value(key) - v.m) * a.inverse - v.ln_d);
-    a.top_vals[row * a.K + lane] = v.good ? lp : __builtin_nanf("");
+    a.top_vals[row * a.K + lane] = log_of(a, v, key_value(key));
     a.top_idx[row * a.K + lane] = v.good ? key_index(key) : -1;
 }
 
@@ -503,6 +513,96 @@ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (log_waves<T, W, R, SEL, PART>()))
         if (lane == 0) sm.state[wv] = st;
         __syncthreads();
         log_end<T, W, SEL, PART>(a, p, sm, row, in_launch, vr, tok);
+    }
+}
+
+// ------------------------------------------------------------------ short rows
+// Rows of at most TL R whole vectors by TL lanes each, 64 / TL rows a wavefront: what a row costs
+// besides its elements is shared between them.  The element that s leaves out is the first one of
+// the first lane that has the maximum, found as it is added.
+template <typename T, bool ENT, int TL, int R>
+__global__ __launch_bounds__(TK_BLOCK) void logprob_short(const LogprobRows a,
+                                                          const LogprobSplit p) {
+    constexpr int E = Vec<T>::N, ROWS = TK_BLOCK / TL;
+    const int lane = threadIdx.x % TL, at = threadIdx.x & 63;
+    const uint64_t team = ((1ull << TL) - 1) << (at / TL * TL);
+    const float ninf = -__builtin_inff(), c = a.c;
+    // rows behind the last one do that again, and store nothing
+    const int64_t vr = (int64_t)blockIdx.x * ROWS + threadIdx.x / TL;
+    const bool live = vr < p.rows;
+    const int64_t row = p.row0 + (live ? vr : p.rows - 1);
+    const T* xr = static_cast<const T*>(a.x) + row * a.ld;
+    const HeldSpan<T> sp(xr, 0, 0, 0, (int)a.V);
+    const int nvec = sp.nvec;
+    int32_t tok = a.T > 0 ? a.tokens[row * a.T + (lane < a.T ? lane : 0)] : -1;
+    u32x4 buf[R];
+    const uint32_t low = E == 8 ? 0xFF80FF80u : 0xFF800000u;
+#pragma unroll
+    for (int i = 0; i < R; ++i) buf[i] = u32x4{low, low, low, low};
+    if (nvec > 0) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int v = lane + i * TL;
+            buf[i] = __builtin_nontemporal_load(sp.vb + (v < nvec ? v : nvec - 1));
+        }
+    }
+    float ex = lane < sp.ne ? load1(xr + sp.extra(lane)) : ninf;
+    auto inside = [&](int32_t t) { return t >= 0 && (int64_t)t < a.V; };
+    float tx = a.T > 0 ? load1(xr + (inside(tok) ? tok : 0)) : 0.0f;
+    float lm = __builtin_fmaxf(ex, ninf);  // a NaN element gives -inf
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const bool in = lane + i * TL < nvec;
+        buf[i] = u32x4{in ? buf[i].x : low, in ? buf[i].y : low, in ? buf[i].z : low,
+                       in ? buf[i].w : low};
+        opaque(buf[i]);
+        lm = max3_raw(lm, held_vmax<T, TK_VALUES>(buf[i]), ninf);
+    }
+    const float wm = group_max<TL>(lm);
+    const uint64_t who = __builtin_amdgcn_ballot_w64(lm == wm) & team;
+    bool done = at != __builtin_ctzll(who | 1ull << 63) || !(wm > ninf);
+    float m = wm > ninf ? wm : 0.0f;  // (no elements, or only -inf)
+    if (rare(__builtin_amdgcn_ballot_w64(__builtin_fabsf(m * c) >= 0x1p22f) != 0)) {
+        const bool far = __builtin_fabsf(m * c) >= 0x1p22f;
+        const float by = far ? m : 0.0f;
+        ex -= by;
+#pragma unroll
+        for (int i = 0; i < R; ++i) buf[i] = less<T>(buf[i], by);
+        m -= by;
+    }
+    const float S = m * c, delta = __builtin_fmaf(m, c, -S);
+    float s = 0.0f, w = 0.0f;
+    auto add = [&](float x) {
+        const float t = __builtin_fmaf(x, c, -S);
+        const bool is = !done && x == m;
+        done = done || is;
+        const float q = is ? 0.0f : exp2_hw(t);
+        s += q;
+        if constexpr (ENT) w = __builtin_fmaf(q, __builtin_fmaxf(t, kLogFloor), w);
+    };
+    add(ex);
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        opaque(buf[i]);
+        float xv[E];
+        widen<T>(buf[i], xv);
+#pragma unroll
+        for (int e = 0; e < E; ++e) add(xv[e]);
+    }
+    s = group_sum<TL>(s);
+    const float back = exp2_hw(-delta);
+    if constexpr (ENT) w = back * __builtin_fmaf(delta, s, -group_sum<TL>(w));
+    s *= back;
+    LogState st{wm, wm > ninf ? s : s - 1.0f, w};
+    const LogEnd end = log_end_of(st);
+    if (!live) return;
+    log_store_row(a, row, st, end, lane);
+    for (int i = lane; i < a.T; i += TL) {
+        if (i != lane) {
+            tok = a.tokens[row * a.T + i];
+            tx = load1(xr + (inside(tok) ? tok : 0));
+        }
+        a.logp[row * a.T + i] = inside(tok) ? log_of(a, end, tx) : 0.0f;
     }
 }
 
@@ -877,6 +977,27 @@ hipError_t launch_logprob_w(const LogprobRows& a, const LogprobSplit& p, hipStre
     return hipGetLastError();
 }
 
+template <typename T, bool ENT>
+hipError_t launch_logprob_short(const LogprobRows& a, const LogprobSplit& p, int lanes,
+                                hipStream_t st) {
+    const int64_t nv = a.V / Vec<T>::N, per = TK_BLOCK / lanes;
+    const dim3 grid((unsigned)((p.rows + per - 1) / per)), block(TK_BLOCK);
+#define OSM_SHORT(L, R_) \
+    hipLaunchKernelGGL((logprob_short<T, ENT, L, R_>), grid, block, 0, st, a, p)
+    if (lanes == 16) {
+        if (nv <= 16) OSM_SHORT(16, 1);
+        else if (nv <= 32) OSM_SHORT(16, 2);
+        else if (nv <= 64) OSM_SHORT(16, 4);
+        else return hipErrorInvalidValue;
+    } else {
+        if (nv <= 128) OSM_SHORT(32, 4);
+        else if (nv <= 256) OSM_SHORT(32, 8);
+        else return hipErrorInvalidValue;
+    }
+#undef OSM_SHORT
+    return hipGetLastError();
+}
+
 template <typename T, bool SEL, bool ENT>
 hipError_t launch_logprob_t(const LogprobRows& a, const LogprobPlan& plan, void* scratch,
                             uint32_t* ctr, hipStream_t st) {
@@ -904,6 +1025,9 @@ hipError_t launch_logprob_t(const LogprobRows& a, const LogprobPlan& plan, void*
             e = hipGetLastError();
         } else if (plan.S > 1) {
             e = launch_logprob_w<T, 4, SEL, ENT, true>(a, p, st);
+        } else if (plan.lanes) {
+            if constexpr (SEL) e = hipErrorInvalidValue;
+            else e = launch_logprob_short<T, ENT>(a, p, plan.lanes, st);
         } else if (plan.W == 1) {
             e = launch_logprob_w<T, 1, SEL, ENT, false>(a, p, st);
         } else if (plan.W == 4) {

@@ -222,13 +222,15 @@ hipError_t launch_logprob_bwd(const LogprobGrad& a, int dtype, hipStream_t st) {
 // bfloat16 with the entropy; "held w" / "stream w": a workgroup of w wavefronts a row (w = 1: four
 // rows), xS: for each of S chunks.
 //
-// Up to 512 vectors: a wavefront a row where there are rows for all of them (1024 x 1000 f held 1
-// 4.1, held 4 4.7; 8192 x 1000 f 11.4 / 15.3; 8192 x 4000 b 20.4 / 23.6; but 512 x 1000 f 4.0 /
-// 3.8, 256 x 4000 b 5.5 / 4.1).  Up to 2048: held 4 (256 x 8000 f 5.3, stream 4 5.3, held 4 x2
-// 6.6).  Beyond that streams, by eight wavefronts (256 x 16000 f stream 8 6.2, stream 4 6.9, held 8
-// 7.0; 1024 x 128256 f 79.6 / 79.4 / 95; 2048 x 128256 b 84.7 / 90.6 / 105), or by four
-// where rows are not long and there are more of them than CUs (400 x 32000 b stream 4 10.5, 8
-// 10.6; 8192 x 50257 b 139 / 153; 8192 x 16000 b 48.3 / 52.5).
+// Up to 256 vectors, where there is a row for each CU: 16 lanes a row up to 64 vectors, else 32
+// (short, against held 1: 32768 x 32 b 4.8 / 14.8, 100000 x 64 f 11.5 / 33.2, 32768 x 500 b 10.9 /
+// 18.2, 16385 x 1000 b 10.3 / 13.1 and f 13.5 / 14.1; 1000 x 32 f 2.7 / 3.3). Up to 512: a
+// wavefront a row where there are rows for all of them (8192 x 4000 b held 1 20.4, held 4 23.6;
+// but 256 x 4000 b 5.5 / 4.1). Up to 2048: held 4 (256 x 8000 f 5.3, stream 4 5.3, held 4 x2 6.6).
+// Beyond that streams, by eight wavefronts (256 x 16000 f stream 8 6.2, stream 4 6.9, held 8 7.0;
+// 1024 x 128256 f 79.6 / 79.4 / 95; 2048 x 128256 b 84.7 / 90.6 / 105), or by four where rows are
+// not long and there are more of them than CUs (400 x 32000 b stream 4 10.5, 8 10.6; 8192 x 50257
+// b 139 / 153; 8192 x 16000 b 48.3 / 52.5).
 //
 // Few long rows are split into as many chunks as give each CU one, of at least 4096 vectors, or up
 // to four in any case (64 x 128256 f stream 8 x4 10.4, x8 11.2; 16 x 128256 f x8 7.8, x6 8.2; 128
@@ -247,7 +249,7 @@ LogprobPlan logprob_plan(int64_t N, int64_t V, int K, int dtype, int cus) {
     const int64_t E = dtype == 1 ? 8 : 4, c = cus;
     const int64_t nv = (V + E - 1) / E;
     const int64_t hold4 = 256 * 16, hold8 = 512 * 16;  // vectors
-    LogprobPlan p{4, 1, V, N, 0};
+    LogprobPlan p{4, 1, V, N, 0, 0};
     int64_t S = 1;
     if (K > 0 && K <= 32 && ((nv > hold8 && N >= c) || (nv > hold4 && 2 * N >= 3 * c))) {
         p.stream = 4;
@@ -274,6 +276,7 @@ LogprobPlan logprob_plan(int64_t N, int64_t V, int K, int dtype, int cus) {
         p.W = nv <= 512 && N >= 4 * c ? 1
               : nv <= 2048 || (nv <= hold4 && N >= 8 * c) ? 4 : 8;
     }
+    if (K == 0 && nv <= 256 && N >= c) p.lanes = nv <= 64 ? 16 : 32;
     if (S > 1) {
         p.chunk = vecs * E;
         S = (V + p.chunk - 1) / p.chunk;

@@ -169,8 +169,8 @@ __device__ __forceinline__ double order_value64(uint64_t k) {
 
 // ln(1 + s), s >= 0, to 2^-24 of itself and 2^-26: with r, a power of two times a number of 11
 // bits next to 1 / (1 + s), that is -ln r + ln(1 + t) with t = (1 + s) r - 1, exact in binary64 and
-// below 2^-10; where s is small r is 1, and t = s.  (A row of 1000 elements takes logprob_fwd
-// 247 instructions; with the library's binary64 function it took 361.)
+// below 2^-10; where s is small r is 1, and t = s.  (A row of 1000 elements by a
+// wavefront takes 247 instructions with it, 361 with the library's binary64 function.)
 __device__ __forceinline__ double ln_1p(float s) {
     const float d = 1.0f + s;
     const int e = __builtin_amdgcn_frexp_expf(d * 0.70710678f);  // d 2^-e in [1/sqrt 2, sqrt 2]

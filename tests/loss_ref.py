@@ -46,9 +46,12 @@ def logprob(X, tokens, K=0, temperature=1.0):
         live = e > 0
         t = np.where(live, z, 0.0) * LOG2E
         s = e.sum()
-        ds = (e * (power(t) + SUM * U)).sum()
+        # (the hardware's 2^t is 0 where it would be below 2^-126: such a weight is lost as a whole;
+        # twice that bounds where the exponent's own error puts it there)
+        gone = np.where(e < 2.0 ** -125, e, 0.0)
+        ds = (e * (power(t) + SUM * U) + gone).sum()
         w = (e * -t).sum()
-        dw = (e * -t * (power(t) + (SUM + 3) * U)).sum()
+        dw = (e * -t * (power(t) + (SUM + 3) * U) + gone * -t).sum()
         ln_d, dln = np.log1p(s), ds / (1 + s)
 
         def lp(j):

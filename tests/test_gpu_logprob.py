@@ -183,6 +183,54 @@ def test_alternatives_of_long_rows(N, nv, dtype, dev):
 
 @pytest.mark.filterwarnings("ignore:invalid value")     # of the reference, on purpose
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [1, 2, 3, 7, 8, 15, 16, 17, 33, 64, 67, 100, 127, 130, 255, 256, 263,
+                               500, 520, 777, 1000, 1024, 1030, 2047, 2055, 2060])
+def test_short_rows_of_every_kind(V, dtype, dev):
+    """Batches of several rows a wavefront, the last of them not full: masked rows, ties, sure
+    tokens, logits far from 0, rows that are no numbers, beside each other; up to 64 tokens."""
+    print(f"short rows {dtype} {V}", flush=True)
+    M, N = 18, 269
+    x = logits(M, V, "f32", V, dev)
+    g = torch.Generator().manual_seed(V)
+    at = torch.randint(0, V, (M,), generator=g).to(dev)
+    x[0] = -INF
+    x[1] = -INF
+    x[1, at[1]] = -3.0
+    x[2, : at[2]] = -INF
+    x[3] = torch.finfo(DT[dtype]).min / 4
+    x[4] = torch.finfo(DT[dtype]).min / 4
+    x[4, at[4]] = 0.0
+    x[5, at[5]] = NAN
+    x[6, at[6]] = INF
+    x[7] = 1.5
+    x[8, ::3] = 9.0
+    for r, up in ((9, 20.0), (10, 45.0), (11, 70.0)):
+        x[r, at[r]] = x[r].max() + up
+    x[12] += 1e4
+    x[13] = x[13] * 1e5 - 1e7
+    x[14, V - 1] = 12.0
+    x[15, 0] = 12.0
+    x[16] = -x[16].abs() - 50.0
+    rows = torch.arange(N, device=dev) % M
+    each = rows.cpu().numpy()
+    for ld, offset, T, tau in ((V, 0, 3, 1.0), (V + 3, 1, 64, 0.8)):
+        buf = torch.zeros(N * ld + offset, dtype=DT[dtype], device=dev)
+        y = buf[offset:].view(N, ld)[:, :V]
+        y.copy_(x[rows])
+        tok = some_tokens(M, V, T, V, dev)
+        tok[:, 1] = at.int()
+        want = loss_ref.logprob(host(y[:M].contiguous()), tok.cpu().numpy(), 0, tau)
+        got = osm.logprob_fwd(y, tok[rows], entropy=True, stats=True, temperature=tau)
+        for name in ("logp", "entropy", "stats"):
+            loss_ref.check(host(getattr(got, name)), want[name][each], want[name + "_err"][each],
+                           name)
+        only = osm.logprob_fwd(y, tok[rows], stats=True, temperature=tau)
+        loss_ref.check(host(only.logp), want["logp"][each], want["logp_err"][each], "logp alone")
+        assert torch.equal(only.stats.nan_to_num(7.0), got.stats.nan_to_num(7.0))
+
+
+@pytest.mark.filterwarnings("ignore:invalid value")     # of the reference, on purpose
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("N,nv,offset", [(400, 4200, 1), (256, 8300, 0), (270, 16500, 3)])
 def test_alternatives_of_large_batches(N, nv, offset, dtype, dev):
     """Streamed rows and chunks with up to 32 alternatives: rows that rise and fall, of few values,
