@@ -954,8 +954,13 @@ hipError_t launch_logprob_w(const LogprobRows& a, const LogprobSplit& p, hipStre
     const dim3 grid((unsigned)blocks), block(W == 1 ? TK_BLOCK : 64 * W);
 #define OSM_LOG(R_) \
     hipLaunchKernelGGL((logprob_held<T, W, R_, SEL, ENT, PART>), grid, block, 0, st, a, p)
-    if constexpr (W <= 4) {
-        if (r <= 1) OSM_LOG(1);
+    if constexpr (W == 1 && !SEL) {  // (shorter rows: launch_logprob_short)
+        if (r <= 6) OSM_LOG(6);
+        else if (r <= 8) OSM_LOG(8);
+        else return hipErrorInvalidValue;
+    } else if constexpr (W <= 4) {
+        // (chunks have two vectors a lane and more)
+        if (!PART && r <= 1) OSM_LOG((PART ? 2 : 1));
         else if (r <= 2) OSM_LOG(2);
         else if (r <= 4) OSM_LOG(4);
         else if (r <= 6) OSM_LOG(6);
