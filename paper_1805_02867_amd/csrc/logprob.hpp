@@ -368,7 +368,7 @@ __launch_bounds__(W == 1 ? TK_BLOCK : 64 * W, (log_waves<T, W, R, SEL, PART>()))
     float vm[R], lm = __builtin_fmaxf(ex, ninf), wm;  // a NaN element gives -inf
     constexpr bool FAST = E == 8 && !SEL;
     if constexpr (FAST) {
-        int im = ex >= 0.0f ? (int)(__float_as_uint(ex) >> 16) : -1;
+        int im = (int)__float_as_uint(ex) >> 16;  // (negative for -0.0 as well)
 #pragma unroll
         for (int i = 0; i < R; ++i) {
             const int v = tr + i * TR < nvec ? signed_max(buf[i]) : -1;

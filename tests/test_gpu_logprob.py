@@ -334,6 +334,26 @@ def test_ties(V, dtype, dev):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [90, 700, 2500, 4877, 9001, 20005, 70001])
+def test_negative_zeros_beside_the_largest(V, dtype, dev):
+    """-0.0 at the row's ends, which is not above what the same lanes have of its vectors."""
+    for N, ld in ((48, V + 5), (300, V)):
+        x = logits(N, V, dtype, V, dev, ld, 1).round()
+        x[:, :9], x[:, -9:] = -0.0, -0.0
+        g = torch.Generator().manual_seed(V)
+        step = torch.tensor([0, 512, 1024, 2048, 4096])[torch.randint(0, 5, (N,), generator=g)]
+        at = (step + torch.randint(9, 120, (N,), generator=g)) % (V - 18) + 9
+        x[torch.arange(N), at] = 11.0
+        got = osm.logprob_fwd(x, entropy=True, stats=True)
+        assert (got.stats[:, 0] == 11.0).all()
+        only = osm.logprob_fwd(x, stats=True)
+        assert torch.equal(only.stats, got.stats)
+        want = loss_ref.logprob(host(x[:48].contiguous()), None)
+        for name in ("entropy", "stats"):
+            loss_ref.check(host(getattr(got, name)[:48]), want[name], want[name + "_err"], name)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [10, 700, 33333, 140000])
 def test_sure_rows_keep_their_digits(V, dtype, dev):
     """A token with almost all the weight: its log p, and 1 - p in its gradient, are numbers of
