@@ -189,8 +189,9 @@ def balance_bwd(X, idx, counts, rows, dloss, starts=None, score="softmax", scale
         ddot = (q * near * (err + 28 * U)).sum(axis=1, keepdims=True)
         # the shares sum to 1 but for their errors; a slope's error, and five products
         ds = power(np.where(np.isfinite(X[took]), X[took], 0.0) * LOG2E) * (score != "softmax")
+        # (and this form's own: the shares' sum is 1 to 2^-52 an expert, the counts are not centred)
         bound[took] = abs(f) * q * slope * ((err + ds + 8 * U) * np.abs(c - dot) + ddot +
-                                            2 * U * near)
+                                            2 * U * near + 2.0 ** -52 * (E + 2) * c.max())
     bound += HALF[dtype] * np.abs(out) + 2.0 ** (-133 if dtype == "bf16" else -125)
     return out, bound
 
