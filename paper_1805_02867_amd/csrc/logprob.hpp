@@ -674,12 +674,15 @@ struct LogStream {
             S = S2;
             far = far || !(__builtin_fabsf(S2) < 0x1p22f);
         }
+        float ps = 0.0f, pw = 0.0f;  // (a step's apart: the chain of roundings is a tenth as long)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float x[E];
             widen<T>(q[u], x);
-            log_add<ENT, false>(x, 0.0f, c, S, d, w);
+            log_add<ENT, false>(x, 0.0f, c, S, ps, pw);
         }
+        d += ps;
+        if constexpr (ENT) w += pw;
         return v;
     }
     // The wavefront's state.  ex: the lane's head or tail element; the others are its vectors

@@ -98,9 +98,11 @@ def logprob_bwd(X, tokens, dlogp, dentropy=None, temperature=1.0, dtype="f32"):
         dx = -p * G - h * p * (lnp0 + H)
         size = A + abs(h) * (H + np.abs(lnp0))
         t = np.where(e > 0, z, 0.0) * LOG2E
-        # the weight, 1 + s and H as given (u each and of what they stand in), the row's two
-        # constants and three operations; the sum of the tokens' gradients
-        bound = p * (power(t) + 8 * U) * size + p * len(g) * U * A
+        # the weight, 1 + s as logprob_fwd sums it (``logprob``), H as given (u and of what it
+        # stands in), the row's two constants and three operations; the sum of the tokens'
+        # gradients
+        ds = (e * (power(t) + SUM * U)).sum() / d
+        bound = p * (power(t) + 8 * U + ds) * size + p * len(g) * U * A
         for i, j in enumerate(inside):
             dx[tokens[n, j]] += g[i]
         out[n] = dx / tau
