@@ -632,11 +632,13 @@ struct LogStream {
         const uint32_t v = E == 8 ? 0xFF80FF80u : 0xFF800000u;
         return u32x4{v, v, v, v};
     }
-    // The largest element of a step, if that is above the maximum or from `th` on.
+    // The largest element of a step, if that is above the maximum or from `th` on (inf: no such
+    // line).  As integers -0.0 is below all other elements: it is not above a maximum from 0 on, but
+    // it reaches a line at 0.
     template <int U>
     __device__ __forceinline__ float largest(const u32x4 (&q)[U], float th) const {
         if constexpr (E == 8) {
-            if (m >= 0.0f && th >= 0.0f) {
+            if (m >= 0.0f && th > 0.0f) {
                 int v = -1;
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
@@ -910,7 +912,7 @@ __global__ __launch_bounds__(64 * W, 5) void logprob_stream(const LogprobRows a,
             const float v = st.step(q, picks.th);
             picks.step(sp, k, v);
         } else {
-            st.step(q, 0.0f);
+            st.step(q, __builtin_inff());
         }
     };
     LogToken tok;
@@ -923,7 +925,7 @@ __global__ __launch_bounds__(64 * W, 5) void logprob_stream(const LogprobRows a,
     extra.x = E == 8 ? (0xFF800000u | __float_as_uint(ex) >> 16) : __float_as_uint(ex);
     if (sp.ne > 0) {
         u32x4 one[1] = {extra};
-        st.step(one, 0.0f);
+        st.step(one, __builtin_inff());
     }
     if constexpr (SEL) picks.begin(sm.top, notes[wv], wv, a.K, sp, q0, ex);
     for (int k = 0; k < steps; k += 2) {
