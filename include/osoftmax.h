@@ -485,7 +485,7 @@ OSM_API int logprob_bwd(const void* x, int64_t ldx, const int32_t* tokens, const
  * route_fwd gives where it chooses none, are not counted.  So padding is a row of -1, or
  * a row before starts[0] or from starts[S] on.  An index that occurs twice counts twice.  n = 0
  * gives zeros.  A row that takes part and whose shares are no numbers (a NaN, only -inf, for
- * the softmax +inf) makes its sequence's probs and loss NaN.
+ * the softmax +inf) makes its sequence's probs and loss NaN.  Finite logits may have any size.
  * x: N*E logits of dtype.  idx: N*K int32, as route_fwd gave them.  starts: S + 1 int32 that do
  * not decrease, or NULL; numbers outside [0, N] are taken as the nearest inside, results for
  * decreasing ones are unspecified.  loss: S binary32.  counts: S*E int32.  probs: S*E

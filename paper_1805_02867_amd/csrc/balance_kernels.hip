@@ -153,10 +153,22 @@ __device__ __forceinline__ float shares(const float (&x)[R], bool sigmoid, float
         float m = x[0];
 #pragma unroll
         for (int j = 1; j < R; ++j) m = __builtin_elementwise_maximum(m, x[j]);
-        m = team_maximum<LANES>(m) * kLog2e;  // (its rounding is the same in all)
+        // The rounding of m log2(e) is the same in all shares and small below 2^22.  From there on it
+        // would not be, and the product itself may leave binary32: such a row's differences are
+        // taken first (for all rows that is an operation more an element).
+        m = team_maximum<LANES>(m);
+        const float S = m * kLog2e;
+        const bool far = !(__builtin_fabsf(S) < 0x1p22f);
+        if (__builtin_expect(__ballot(far) != 0, 0)) {
+            const float by = far ? m : 0.0f, S1 = far ? 0.0f : S;
+#pragma unroll
+            for (int j = 0; j < R; ++j) q[j] = exp2_hw(__builtin_fmaf(x[j] - by, kLog2e, -S1));
+        } else {
+#pragma unroll
+            for (int j = 0; j < R; ++j) q[j] = exp2_hw(__builtin_fmaf(x[j], kLog2e, -S));
+        }
 #pragma unroll
         for (int j = 0; j < R; ++j) {
-            q[j] = exp2_hw(__builtin_fmaf(x[j], kLog2e, -m));
             if constexpr (SLOPE) slope[j] = 1.0f;
             sum += q[j];
         }
