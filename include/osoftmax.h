@@ -430,9 +430,10 @@ typedef struct osm_logprob {
  * A token outside [0, V) is ignored: its logp is 0.  Elements of -inf have no weight,
  * and a log probability of -inf.  A row holding NaN or +inf, or only -inf, gives NaN
  * (0 for ignored tokens) and top_idx -1.  x is read once; sums are binary32 (weights
- * below 2^-126 are 0 in them), the outputs are formed from them in binary64.
- * x: row r starts at x + r * ldx elements, ldx >= V; (max x - min x) / temperature
- * stays below 2.35e38 for finite elements.
+ * below 2^-126 are 0 in them), the outputs are formed from them in binary64; a log
+ * probability below binary32's lowest value is -inf.  Finite elements may have any size (one
+ * that is more than 3.4e38 below m has no weight, whatever the temperature).
+ * x: row r starts at x + r * ldx elements, ldx >= V.
  * Errors: OSM_EINVAL for bad sizes, ldx < V, unknown dtype, NULL p, T, K or temperature
  * outside of what osm_logprob says, no output, null (with N > 0), misaligned or
  * overlapping buffers (the memory between rows is part of x). */
