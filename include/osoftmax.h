@@ -490,8 +490,10 @@ OSM_API int logprob_bwd(const void* x, int64_t ldx, const int32_t* tokens, const
  * x: N*E logits of dtype.  idx: N*K int32, as route_fwd gave them.  starts: S + 1 int32 that do
  * not decrease, or NULL; numbers outside [0, N] are taken as the nearest inside, results for
  * decreasing ones are unspecified.  loss: S binary32.  counts: S*E int32.  probs: S*E
- * binary32.  rows: S int32.  Shares are binary32, sums over rows binary64 but for
- * 64 rows at a time at most.  N = 0 is no no-op here: the outputs are zeros.
+ * binary32.  rows: S int32.  Shares are binary32; those below 2^-126 (OSM_SCORE_SIGMOID:
+ * 2^-66) may be 0.  Sums over rows are binary64 but for up to 64 rows of a team of lanes and up
+ * to 8 teams, which are added in binary32; of a sequence longer than a workgroup's rows, each
+ * workgroup's sum is rounded to binary32 once.  N = 0 is no no-op here: the outputs are zeros.
  * Errors: OSM_EINVAL for N < 0, E < 1, E > OSM_ROUTE_EMAX, K < 1, K > OSM_TOPK_KMAX, S < 1,
  * N * K, S or S * E above 2^31 - 1, starts NULL with S > 1, unknown dtype or score, null
  * (x and idx only with N > 0), misaligned or overlapping buffers; OSM_ENOMEM if the

@@ -1,9 +1,10 @@
 // The balance loss of a router's experts, with the counts and mean shares that it is made of,
 // and its gradient.
 //
-// A row's shares are q = softmax(x), or the sigmoids over their sum; these are taken relative to
-// the largest, e^{min(x, 0) - z} / (1 + e^-|x|) with z = max min(x, 0), so that they do not
-// underflow together.  For a sequence of n rows (see balance_fwd)
+// A row's shares are q = softmax(x), or the sigmoids 1 / (1 + e^-x) over their sum.  Where that sum
+// is below 2^-60, all x are far below 0 and the sigmoids e^x but for 2^-60 of them: there they
+// are e^{x - max x}, which does not underflow.  In other rows a sigmoid below 2^-126 is 0, a
+// share of less than 2^-66.  For a sequence of n rows (see balance_fwd)
 //   loss = scale E / (K n^2) sum_e c_e sum_r q_re,
 //   d loss / dx_rj = scale E / (K n^2) q_j (c_j - sum_e c_e q_e)      (times 1 - sigma_j).
 // Balanced counts are all about K n / E and cancel in the gradient: they are taken less that
@@ -12,10 +13,13 @@
 // Forward.  Workgroup i takes a span of rows; a row by a team of LANES lanes that hold R experts
 // each, so that a lane sums the shares of its own experts over rows in registers (binary32, of at
 // most 64 rows of a team), and counts go to LDS as integers, whose additions may come in any
-// order.  At the end of each sequence's part of the span the teams' sums are joined in their order,
-// in binary64.  A sequence within the span is finished there: by the workgroup, or one of few rows
-// by a wavefront alone, so that several are worked on at once.  Of others the parts go to scratch,
-// and a second kernel joins them in the order of the spans: the result is the same every time.
+// order.  At the end of each sequence's part of the span the sums of a wavefront's teams, up to
+// eight, are joined in binary32 (three more roundings), then the wavefronts' in their order, in
+// binary64.  A sequence within the span is finished there: by the workgroup, or one of few rows by
+// a wavefront alone, so that several are worked on at once.  Of others the parts go to scratch, in
+// binary32 beside their counts (a rounding of 2^-24 of each part, where 64 additions have made as
+// many), and a second kernel joins them in the order of the spans, in binary64: the result is the
+// same every time.
 //
 // Gradient: a row by a team as well, a lane keeps its experts' counts of the sequence that its row
 // is in.
@@ -23,7 +27,9 @@
 // What bounds them.  65536 x 256 bfloat16 sigmoid in 24 sequences takes 18 us, its 36 MB 5.2 at
 // 6.9 TB/s: the arithmetic (an exponential and a reciprocal an element, about 14 instructions; 7 us
 // of it), the chain ahead of and behind the rows (5 us, a batch of 16 rows) and the join, a launch
-// (5 us).  The gradient of 65536 x 256 binary32 takes 25 us for 134 MB, a large copy's rate.
+// (5 us).  The gradient of 65536 x 256 binary32 takes 26 us for 134 MB, a large copy's rate; of
+// bfloat16 18 with softmax shares and 20 with sigmoids for 67 MB (a copy of as much 13.4): 890 and
+// 1030 vector instructions a wavefront, 13 and 16 us of them on all SIMDs at 2.4 GHz.
 #include <type_traits>
 
 #include "experts.hpp"
@@ -153,9 +159,9 @@ __device__ __forceinline__ float shares(const float (&x)[R], bool sigmoid, float
         float m = x[0];
 #pragma unroll
         for (int j = 1; j < R; ++j) m = __builtin_elementwise_maximum(m, x[j]);
-        // The rounding of m log2(e) is the same in all shares and small below 2^22.  From there on it
-        // would not be, and the product itself may leave binary32: such a row's differences are
-        // taken first (for all rows that is an operation more an element).
+        // The rounding of m log2(e) is the same in all shares and small below 2^22.  From there on
+        // it would not be, and the product itself may leave binary32: such a row's differences
+        // are taken first (for all rows that is an operation more an element).
         m = team_maximum<LANES>(m);
         const float S = m * kLog2e;
         const bool far = !(__builtin_fabsf(S) < 0x1p22f);

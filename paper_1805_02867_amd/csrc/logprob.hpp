@@ -3,7 +3,7 @@
 //
 // What bounds them: large batches memory (2048 x 128256 bfloat16 with the entropy 86 us for 525
 // MB, 6.1 TB/s, a plain read of as much 75.5; 300 x 32000 binary32 10.6 us for 38 MB, 8.3; 16385 x
-// 1000 13.5 us for 66 MB, 12.3), short rows the arithmetic that is not their elements' (32768 x 32
+// 1000 12.7 us for 66 MB, 12.3), short rows the arithmetic that is not their elements' (32768 x 32
 // bfloat16 4.8 us), and a few rows the chain of a chunk and of the join (1 x 128256 5.1 us, with
 // five alternatives 8.2).
 //
@@ -633,8 +633,8 @@ struct LogStream {
         return u32x4{v, v, v, v};
     }
     // The largest element of a step, if that is above the maximum or from `th` on (inf: no such
-    // line).  As integers -0.0 is below all other elements: it is not above a maximum from 0 on, but
-    // it reaches a line at 0.
+    // line).  As integers -0.0 is below all other elements: it is not above a maximum from 0 on,
+    // but it reaches a line at 0.
     template <int U>
     __device__ __forceinline__ float largest(const u32x4 (&q)[U], float th) const {
         if constexpr (E == 8) {

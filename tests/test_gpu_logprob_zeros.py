@@ -60,7 +60,8 @@ def test_zeros_of_either_sign(N, V, dtype, dev):  # noqa: F811
         got = osm.logprob_fwd(y, K=K, stats=True)
         idx = got.top_idx.cpu().numpy()
         bad = np.flatnonzero((idx != want["top_idx"][each, :K]).any(axis=1))
-        assert len(bad) == 0, (K, len(bad), bad[:4], idx[bad[:1]], want["top_idx"][each[bad[:1]], :K])
+        assert len(bad) == 0, (K, len(bad), bad[:4], idx[bad[:1]],
+                               want["top_idx"][each[bad[:1]], :K])
         loss_ref.check(host(got.top_vals), want["top_vals"][each, :K],
                        want["top_vals_err"][each, :K], f"top K={K}")
         loss_ref.check(host(got.stats), want["stats"][each], want["stats_err"][each], "stats")
