@@ -431,8 +431,9 @@ typedef struct osm_logprob {
  * and a log probability of -inf.  A row holding NaN or +inf, or only -inf, gives NaN
  * (0 for ignored tokens) and top_idx -1.  x is read once; sums are binary32 (weights
  * below 2^-126 are 0 in them), the outputs are formed from them in binary64; a log
- * probability below binary32's lowest value is -inf.  Finite elements may have any size (one
- * that is more than 3.4e38 below m has no weight, whatever the temperature).
+ * probability below binary32's lowest value is -inf.  Finite elements may have any size (the
+ * weight of one that is more than 3.4e38 below m may count as 0, which it is but at temperatures
+ * above 1e36).
  * x: row r starts at x + r * ldx elements, ldx >= V.
  * Errors: OSM_EINVAL for bad sizes, ldx < V, unknown dtype, NULL p, T, K or temperature
  * outside of what osm_logprob says, no output, null (with N > 0), misaligned or
